@@ -457,6 +457,70 @@ int sar_linear_bwd_rows(const void* X, const void* E, const int32_t* E_rank, int
 
 int sar_linear_workspace_bytes(int64_t n, int K, int F, size_t* bytes);
 
+/* ------------------------------------------------ node-wise rows in 8 bits
+ * A layer's input is kept from its forward to its backward pass for sums over many rows (dW, the
+ * parameters of a norm).  Kept in 8 bits it takes a quarter of fp32 rows' memory:
+ *   q  int8  [n, round_up(K, 16)]  whole numbers -127..127, zeros behind a row's K values (16-byte aligned)
+ *   e  uint8 [n, ceil(K / 32)]     one step 2^(e - 127) for every 32 values of a row
+ * value = q 2^(e - 127), the step being the smallest power of two (2^-126 at least, 2^121 at most) that leaves no q beyond 127
+ * and q the nearest whole number, ties to even: the error is at most half a step, 2^-7 of the block's largest size.  (Sizes
+ * beyond 127.5 2^121, within 2^-7 of the largest fp32 number, are kept as 127 2^121.)  A block with an infinity or a
+ * NaN in it has e = 255, q = 0 and stands for NaN.
+ */
+
+/* X [n,K] of `dtype` -> q, e. */
+int sar_pack(const void* X, int dtype, int64_t n, int K, int8_t* q, uint8_t* e, void* stream);
+
+/* q, e -> the values they stand for, X [n,K] of `dtype` (exact in either type). */
+int sar_unpack(const int8_t* q, const uint8_t* e, int dtype, int64_t n, int K, void* X, void* stream);
+
+/* ------------------------------------------------------------- layer norm */
+
+/* Y[i] = (X[i] - mu_i) r_i gamma + beta with mu_i = mean(X[i]), r_i = 1 / sqrt(mean((X[i] - mu_i)^2) + eps).
+ * X, Y [n,D] of `dtype` (Y may alias X), D <= 8192; gamma, beta fp32 [D], either NULL for 1 / 0; stats fp32 [n,2]
+ * = (mu_i, r_i), what the backward pass reads, or NULL.
+ * Xq,Xe and Yq,Ye: NULL, or where the input and the output (as stored) go in 8 bits as well, in the same pass: what
+ * the backward passes of the norm and of the transform behind it need. */
+int sar_layernorm_fwd(const void* X, const float* gamma, const float* beta, float eps, void* Y, float* stats, int dtype,
+                      int64_t n, int D, int8_t* Xq, uint8_t* Xe, int8_t* Yq, uint8_t* Ye, void* stream);
+
+/* With xh = (X - mu) r and d = dY gamma:  dX = r (d - mean(d) - xh mean(d xh)) (OVERWRITTEN, `dtype`, may be NULL,
+ * may alias dY or X), dgamma = sum_i dY xh, dbeta = sum_i dY (fp32 [D], either may be NULL; added to what is there
+ * where accumulate != 0, else overwritten; summed in a fixed order).  The input is X [n,D] of `dtype`, or, with X
+ * NULL, its packed form Xq, Xe.  work: scratch of at least sar_layernorm_workspace_bytes, 16-byte aligned. */
+int sar_layernorm_bwd(const void* dY, const void* X, const int8_t* Xq, const uint8_t* Xe, const float* stats,
+                      const float* gamma, int accumulate, void* dX, float* dgamma, float* dbeta, int dtype, int64_t n,
+                      int D, void* work, size_t work_bytes, void* stream);
+
+int sar_layernorm_workspace_bytes(int64_t n, int D, size_t* bytes);
+
+/* -------------------------------------- transforms with a weight per node type
+ * Rows sorted by type: those of type t are [type_ptr[t], type_ptr[t+1]), type_ptr device int32 [T+1], ascending, with
+ * values of 0..n (what lies outside is cut off; rows that no type has are neither read nor written).  T <= 65535; a
+ * type may have no row.  n < 2^31 - 256; K, F <= 65536.  fp32 results are sums of products that are exact for operands of at
+ * least 2^-110 in size (smaller ones count to within 2^-126); bf16 rows meet weights taken to 16 bits, and are rounded when stored.
+ * work: scratch of at least sar_linear_typed_workspace_bytes, 16-byte aligned.
+ */
+
+/* Z[i] = X[i] W[t(i)]: X [n,K], Z [n,F] of `dtype` (no alias), W fp32 [T,K,F]. */
+int sar_linear_typed_fwd(const void* X, const float* W, const int32_t* type_ptr, int T, void* Z, int dtype, int64_t n,
+                         int K, int F, void* work, size_t work_bytes, void* stream);
+
+/* dW[t] = X_t^T dZ_t (fp32 [T,K,F]; added to what is there where accumulate != 0, else overwritten, zeros for a type
+ * without rows; summed in a fixed order; may be NULL) and dX[i] = dZ[i] W[t(i)]^T (OVERWRITTEN, `dtype`, may be NULL, must
+ * not alias dZ).  The input is X [n,K] of `dtype`, or, with X NULL, its packed form Xq, Xe (sar_pack); without dW
+ * none is needed. */
+int sar_linear_typed_bwd(const void* X, const int8_t* Xq, const uint8_t* Xe, const void* dZ, const float* W,
+                         const int32_t* type_ptr, int T, int accumulate, float* dW, void* dX, int dtype, int64_t n, int K,
+                         int F, void* work, size_t work_bytes, void* stream);
+
+int sar_linear_typed_workspace_bytes(int64_t n, int K, int F, int T, size_t* bytes);
+
+/* sar_linear_bwd from rows kept in 8 bits: what sar_linear_typed_bwd does of one type that has all rows (W, dW fp32
+ * [K,F]).  work: sar_linear_typed_workspace_bytes with T = 1. */
+int sar_linear_bwd_packed(const int8_t* Xq, const uint8_t* Xe, const void* dZ, const float* W, int accumulate, float* dW,
+                          void* dX, int dtype, int64_t n, int K, int F, void* work, size_t work_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

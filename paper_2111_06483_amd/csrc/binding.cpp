@@ -12,6 +12,7 @@
 
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 #include <string>
 #include <vector>
 
@@ -594,12 +595,205 @@ SAR_CALL(linear_bwd_rows, 14)
     });
 SAR_CALL_END
 
+// ---- the node-wise operators.  Every tensor has the shape and type that the call states, and lies on the current device, whose
+// stream the work is sent to.
+
+const at::Tensor& given(PyObject* o, const char* what, at::ScalarType dtype, std::initializer_list<int64_t> shape)
+{
+    const at::Tensor& t = tensor(o);
+    if (t.scalar_type() != dtype) refuse("%s is %s, the call needs %s", what, type_name(t.scalar_type()).c_str(), type_name(dtype).c_str());
+    if (t.sizes() != at::IntArrayRef(shape)) {
+        std::string s;
+        for (int64_t d : shape) s += (s.empty() ? "" : ", ") + std::to_string(d);
+        refuse("%s has shape %s, the call needs (%s)", what, shape_text(t).c_str(), s.c_str());
+    }
+    if (!t.is_contiguous()) refuse("%s must be contiguous", what);
+    return t;
+}
+
+template <typename T = void>
+T* at_of(PyObject* o, const char* what, at::ScalarType dtype, std::initializer_list<int64_t> shape)
+{
+    return static_cast<T*>(given(o, what, dtype, shape).data_ptr());
+}
+
+template <typename T = void>
+T* at_if(PyObject* o, const char* what, at::ScalarType dtype, std::initializer_list<int64_t> shape)
+{
+    return o == Py_None ? nullptr : at_of<T>(o, what, dtype, shape);
+}
+
+// The first of a call's tensors, which says how many rows and columns there are, and of which type.
+struct Rows {
+    at::ScalarType dtype;
+    int code;
+    int64_t n, width;
+    void* p;
+};
+Rows rows_of(PyObject* o, const char* what)
+{
+    const at::Tensor& t = tensor(o);
+    const int code = dtype_code(t.scalar_type());
+    int64_t s[2];
+    unpack_sizes(t, s);
+    return {t.scalar_type(), code, s[0], s[1], at_of(o, what, t.scalar_type(), {s[0], s[1]})};
+}
+
+// Rows in 8 bits: a pair (q, e), or None.
+struct Packed {
+    int8_t* q = nullptr;
+    uint8_t* e = nullptr;
+};
+bool is_pair(PyObject* o) { return PyTuple_Check(o) || PyList_Check(o); }
+Packed packed(PyObject* o, const char* what, int64_t n, int64_t K)
+{
+    if (o == Py_None) return {};
+    if (!is_pair(o) || PySequence_Fast_GET_SIZE(o) != 2) refuse("%s: packed rows are a pair (q, e)", what);
+    PyObject* const* const items = PySequence_Fast_ITEMS(o);
+    return {at_of<int8_t>(items[0], what, at::kChar, {n, (K + 15) / 16 * 16}), at_of<uint8_t>(items[1], what, at::kByte, {n, (K + 31) / 32})};
+}
+
+// Scratch: any type, any shape, or None.
+void* scratch(PyObject* o)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor(o);
+    if (!t.is_contiguous()) refuse("work must be contiguous");
+    return t.data_ptr();
+}
+
+// The last check: whatever tensors a call's arguments are or hold lie on the current device.
+void all_here(PyObject* const* a, int n)
+{
+    for (int k = 0; k < n; ++k) {
+        if (is_pair(a[k])) {
+            all_here(PySequence_Fast_ITEMS(a[k]), (int)PySequence_Fast_GET_SIZE(a[k]));
+        } else if (THPVariable_Check(a[k])) {
+            const at::Tensor& t = THPVariable_Unpack(a[k]);
+            if (!t.is_cuda()) refuse("the call takes device tensors, and one of shape %s is in host memory", shape_text(t).c_str());
+            if (t.get_device() != c10::hip::current_device())
+                refuse("a tensor of shape %s is on device %d, the current one is %d", shape_text(t).c_str(), (int)t.get_device(),
+                       (int)c10::hip::current_device());
+        }
+    }
+}
+
+// X, (q, e)
+SAR_CALL(pack, 2)
+    const Rows X = rows_of(a[0], "X");
+    if (a[1] == Py_None) refuse("packed rows are a pair (q, e)");
+    const Packed p = packed(a[1], "packed rows", X.n, X.width);
+    void* const st = stream();
+    all_here(a, 2);
+    call([&] { return sar_pack(X.p, X.code, X.n, (int)X.width, p.q, p.e, st); });
+SAR_CALL_END
+
+// (q, e), X
+SAR_CALL(unpack, 2)
+    const Rows X = rows_of(a[1], "X");
+    if (a[0] == Py_None) refuse("packed rows are a pair (q, e)");
+    const Packed p = packed(a[0], "packed rows", X.n, X.width);
+    void* const st = stream();
+    all_here(a, 2);
+    call([&] { return sar_unpack(p.q, p.e, X.code, X.n, (int)X.width, X.p, st); });
+SAR_CALL_END
+
+// X, gamma, beta, eps, Y, stats, X's (q, e), Y's (q, e)
+SAR_CALL(layernorm_fwd, 8)
+    const Rows X = rows_of(a[0], "X");
+    const int64_t D = X.width;
+    float *const gamma = at_if<float>(a[1], "gamma", at::kFloat, {D}), *const beta = at_if<float>(a[2], "beta", at::kFloat, {D});
+    const float eps = real(a[3]);
+    void* const Y = at_of(a[4], "Y", X.dtype, {X.n, D});
+    float* const stats = at_if<float>(a[5], "stats", at::kFloat, {X.n, 2});
+    const Packed xp = packed(a[6], "Xp", X.n, D), yp = packed(a[7], "Yp", X.n, D);
+    void* const st = stream();
+    all_here(a, 8);
+    call([&] { return sar_layernorm_fwd(X.p, gamma, beta, eps, Y, stats, X.code, X.n, (int)D, xp.q, xp.e, yp.q, yp.e, st); });
+SAR_CALL_END
+
+// dY, X or its (q, e), stats, gamma, accumulate, dX, dgamma, dbeta, work
+SAR_CALL(layernorm_bwd, 9)
+    const Rows dY = rows_of(a[0], "dY");
+    const int64_t n = dY.n, D = dY.width;
+    const bool p = is_pair(a[1]);
+    void* const X = p ? nullptr : at_of(a[1], "X", dY.dtype, {n, D});
+    const Packed xp = p ? packed(a[1], "X", n, D) : Packed{};
+    float *const stats = at_of<float>(a[2], "stats", at::kFloat, {n, 2}), *const gamma = at_if<float>(a[3], "gamma", at::kFloat, {D});
+    const int acc = truth(a[4]);
+    void *const dX = at_if(a[5], "dX", dY.dtype, {n, D}), *const work = scratch(a[8]), *const st = stream();
+    float *const dg = at_if<float>(a[6], "dgamma", at::kFloat, {D}), *const db = at_if<float>(a[7], "dbeta", at::kFloat, {D});
+    const size_t wb = bytes_if(a[8]);
+    all_here(a, 9);
+    call([&] { return sar_layernorm_bwd(dY.p, X, xp.q, xp.e, stats, gamma, acc, dX, dg, db, dY.code, n, (int)D, work, wb, st); });
+SAR_CALL_END
+
+// The weights of T types, and where each type's rows begin.
+struct TypedW {
+    int64_t T, K, F;
+    float* W;
+    int32_t* ptr;
+};
+TypedW typed_w(PyObject* W, PyObject* ptr, int64_t K, int64_t F)
+{
+    int64_t s[3];
+    unpack_sizes(tensor(W), s);
+    if (K < 0) K = s[1];
+    if (F < 0) F = s[2];
+    return {s[0], K, F, at_of<float>(W, "W", at::kFloat, {s[0], K, F}), at_of<int32_t>(ptr, "type_ptr", at::kInt, {s[0] + 1})};
+}
+
+// X, W, type_ptr, Z, work
+SAR_CALL(linear_typed_fwd, 5)
+    const Rows X = rows_of(a[0], "X");
+    const TypedW w = typed_w(a[1], a[2], X.width, -1);
+    void *const Z = at_of(a[3], "Z", X.dtype, {X.n, w.F}), *const work = scratch(a[4]), *const st = stream();
+    const size_t wb = bytes_if(a[4]);
+    all_here(a, 5);
+    call([&] { return sar_linear_typed_fwd(X.p, w.W, w.ptr, (int)w.T, Z, X.code, X.n, (int)w.K, (int)w.F, work, wb, st); });
+SAR_CALL_END
+
+// X or its (q, e) or None, dZ, W, type_ptr, accumulate, dW, dX, work
+SAR_CALL(linear_typed_bwd, 8)
+    const Rows dZ = rows_of(a[1], "dZ");
+    const TypedW w = typed_w(a[2], a[3], -1, dZ.width);
+    const bool p = is_pair(a[0]);
+    void* const X = p ? nullptr : at_if(a[0], "X", dZ.dtype, {dZ.n, w.K});
+    const Packed xp = p ? packed(a[0], "X", dZ.n, w.K) : Packed{};
+    const int acc = truth(a[4]);
+    float* const dW = at_if<float>(a[5], "dW", at::kFloat, {w.T, w.K, w.F});
+    void *const dX = at_if(a[6], "dX", dZ.dtype, {dZ.n, w.K}), *const work = scratch(a[7]), *const st = stream();
+    const size_t wb = bytes_if(a[7]);
+    all_here(a, 8);
+    call([&] {
+        return sar_linear_typed_bwd(X, xp.q, xp.e, dZ.p, w.W, w.ptr, (int)w.T, acc, dW, dX, dZ.code, dZ.n, (int)w.K, (int)w.F, work, wb, st);
+    });
+SAR_CALL_END
+
+// (q, e) or None, dZ, W, accumulate, dW, dX, work
+SAR_CALL(linear_bwd_packed, 7)
+    const Rows dZ = rows_of(a[1], "dZ");
+    int64_t kf[2];
+    unpack_sizes(tensor(a[2]), kf);
+    const int64_t K = kf[0], F = dZ.width;
+    float* const W = at_of<float>(a[2], "W", at::kFloat, {K, F});
+    const Packed xp = packed(a[0], "X", dZ.n, K);
+    const int acc = truth(a[3]);
+    float* const dW = at_if<float>(a[4], "dW", at::kFloat, {K, F});
+    void *const dX = at_if(a[5], "dX", dZ.dtype, {dZ.n, K}), *const work = scratch(a[6]), *const st = stream();
+    const size_t wb = bytes_if(a[6]);
+    all_here(a, 7);
+    call([&] { return sar_linear_bwd_packed(xp.q, xp.e, dZ.p, W, acc, dW, dX, dZ.code, dZ.n, (int)K, (int)F, work, wb, st); });
+SAR_CALL_END
+
 #define SAR_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     SAR_METHOD(spmm_all), SAR_METHOD(act_bwd), SAR_METHOD(spmm_bwd_all), SAR_METHOD(error_add), SAR_METHOD(gat_scores),
     SAR_METHOD(gat_fwd_begin), SAR_METHOD(gat_fwd_block), SAR_METHOD(gat_fwd_end), SAR_METHOD(gat_fwd_all),
     SAR_METHOD(gat_bwd_begin), SAR_METHOD(gat_bwd_block), SAR_METHOD(gat_bwd_all), SAR_METHOD(gat_bwd_end),
-    SAR_METHOD(linear_fwd), SAR_METHOD(linear_bwd), SAR_METHOD(linear_bwd_rows), {nullptr, nullptr, 0, nullptr}};
+    SAR_METHOD(linear_fwd), SAR_METHOD(linear_bwd), SAR_METHOD(linear_bwd_rows), SAR_METHOD(pack), SAR_METHOD(unpack),
+    SAR_METHOD(layernorm_fwd), SAR_METHOD(layernorm_bwd), SAR_METHOD(linear_typed_fwd), SAR_METHOD(linear_typed_bwd),
+    SAR_METHOD(linear_bwd_packed), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

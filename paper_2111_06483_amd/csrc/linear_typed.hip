@@ -1,0 +1,436 @@
+// Products of rows with the weight of their type: Z = X W_t and dX = dZ W_t^T for rows sorted by type, of any numbers.
+//
+// Both are rows (contraction index contiguous) times a small operand B [C, N] per type, and bound by memory at these widths (256 x 256: 64
+// multiply-adds a byte of fp32 rows) as long as the matrix cores are fed without a pause:
+//   - A first launch lays B out in pieces of bf16, in the order in which a wavefront's lanes want them: fp32 rows three pieces a weight (exact
+//     products, linear_pieces.h), bf16 rows two (the weight to 16 bits).  T K F values, against n (K + F) in the main launch.
+//   - A workgroup of 8 wavefronts takes 256 rows of one type and up to 256 columns; a wavefront 32 rows, whose values go from memory to registers
+//     (a lane holds 64 bytes of a row's 128: whole lines), one chunk ahead; B's chunks go to LDS by asynchronous copies that take no
+//     registers, one chunk ahead as well, with one barrier a chunk.
+//   - Columns are dealt to the column tiles by turns (`column_of`), so that a lane ends up with four neighbours of a row and writes them at once:
+//     a wavefront's store covers whole lines, with no turn through LDS.
+// fp32 sums: the matrix unit cuts (does not round) when it adds, so a chunk's 32 products are summed from zero there and added to the
+// running sum by vector instructions, which round to nearest; and every other chunk is multiplied by -B and subtracted, so that what is
+// cut leans to neither side.  A result that is not finite (infinities and NaN have no such pieces, and the largest numbers round to infinity) sends the
+// wavefront's tile back to the fp32 matrix instruction, from the operands themselves.  Operands below 2^-110 in size are taken to within 2^-126.
+#include <algorithm>
+
+#include "linear_pieces.h"
+#include "linear_typed.h"
+
+namespace sar {
+
+namespace {
+
+template <typename T>
+struct Mode;
+template <>
+struct Mode<float> {
+    static constexpr int kPieces = 3, kSteps = 2;      // pieces of a weight; products of 16 a chunk
+};
+template <>
+struct Mode<bf16_t> {
+    static constexpr int kPieces = 2, kSteps = 4;
+};
+// Contraction values of a chunk: 128 bytes of a row.  Lanes 0..31 (half 0) hold the first 64 bytes of their rows, lanes 32..63 the others; in step s a
+// lane contributes the eight values from 8 s on.
+template <typename T>
+constexpr int kChunk = 16 * Mode<T>::kSteps;
+
+// Column c (0..31) of column tile i of NT: tiles in groups of four (or two) take columns by turns.
+template <int NT>
+__host__ __device__ constexpr int column_of(int i, int c)
+{
+    constexpr int IL = NT < 4 ? NT : 4;
+    return i / IL * (32 * IL) + c * IL + i % IL;
+}
+
+// ---- the small operand's pieces
+//
+// out [T, column blocks, chunks, steps, pieces, NT, 64 lanes] of 16 bytes: eight consecutive contraction values of a column.
+struct LayArgs {
+    const float* W;        // [T, K, F]
+    uint4* out;
+    int T, K, F, C, N, chunks, blocks;
+};
+
+template <typename T, int NT, bool TRANS>
+__global__ __launch_bounds__(256) void k_typed_lay(LayArgs a)
+{
+    constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps;
+    const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int lane = unit & 63, tile = (unit >> 6) % NT;
+    int64_t rest = unit / (64 * NT);
+    const int s = rest % S;
+    rest /= S;
+    const int chunk = (int)(rest % a.chunks);
+    rest /= a.chunks;
+    const int block = (int)(rest % a.blocks);
+    const int t = (int)(rest / a.blocks);
+    if (t >= a.T) return;
+    const int n = block * (32 * NT) + column_of<NT>(tile, lane & 31);
+    const int c = chunk * kChunk<T> + (lane >> 5) * (kChunk<T> / 2) + s * 8;
+    const float* W = a.W + (int64_t)t * a.K * a.F;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        v[j] = 0.f;
+        if (n < a.N && c + j < a.C) v[j] = TRANS ? W[(int64_t)n * a.F + c + j] : W[(int64_t)(c + j) * a.F + n];
+        if (P == 3 && (chunk & 1)) v[j] = -v[j];
+    }
+    uint4* out = a.out + (((int64_t)(t * a.blocks + block) * a.chunks + chunk) * S + s) * (P * NT * 64) + tile * 64 + lane;
+    if constexpr (P == 3) {
+        uint4 p[3];
+        split8(v, p);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) out[k * NT * 64] = p[k];
+    } else {
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            hi[j] = pack2_bf16(v[2 * j], v[2 * j + 1]);
+            lo[j] = pack2_bf16(v[2 * j] - __uint_as_float(hi[j] << 16), v[2 * j + 1] - __uint_as_float(hi[j] & 0xffff0000u));
+        }
+        out[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        out[NT * 64] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+}
+
+// ---- rows times pieces
+
+struct RowsArgs {
+    const void* A;         // [n, C]
+    const uint4* B;        // as k_typed_lay leaves it
+    const float* W;        // [T, K, F]
+    void* out;             // [n, N]
+    Types types;
+    int C, N, chunks, blocks;
+    int K, F;
+};
+
+// The wavefront's tiles once more by the fp32 matrix instruction.
+template <typename T, int NT, bool TRANS>
+__device__ inline void exact_tiles(const RowsArgs& a, int t, const T* row, int n0, float16_t (&acc)[NT])
+{
+    const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
+    const float* W = a.W + (int64_t)t * a.K * a.F;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) acc[i] = float16_t{};
+    for (int k = 0; k < a.C; k += 2) {
+        const bool in = k + h < a.C;
+        float x = 0.f;
+        if (in) {
+            if constexpr (sizeof(T) == 4) x = row[k + h];
+            else x = bf16_to_f32(row[k + h]);
+        }
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int n = n0 + column_of<NT>(i, c);
+            float w = 0.f;
+            if (in && n < a.N) w = TRANS ? W[(int64_t)n * a.F + k + h] : W[(int64_t)(k + h) * a.F + n];
+            acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w, acc[i], 0, 0, 0);
+        }
+    }
+}
+
+using LdsPtr = __attribute__((address_space(3))) void;
+using GlobalSrc = const __attribute__((address_space(1))) void;
+
+template <typename T, int NT, int WAVES, bool TRANS>
+__global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
+{
+    constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps, CH = kChunk<T>, N = Cols<T>::N;
+    constexpr int kRaw = 64 / 16;                        // 16-byte pieces of a row that a lane holds of a chunk
+    constexpr int kFrags = S * P * NT;                   // KiB of B a chunk
+    extern __shared__ __attribute__((aligned(16))) uint4 lds[];      // [2][kFrags][64]
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+
+    // which rows: blocks of WAVES * 32 of a type, type after type
+    int t = -1;
+    int64_t first = 0, end = 0;
+    {
+        int64_t left = blockIdx.x;
+        for (int base = 0; base < a.types.T; base += 64) {
+            int64_t lo = 0, hi = 0;
+            if (base + lane < a.types.T) a.types.span(base + lane, lo, hi);
+            const int mine = (int)((hi - lo + WAVES * 32 - 1) / (WAVES * 32));
+            int upto = mine;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int v = __shfl_up(upto, o);
+                if (lane >= o) upto += v;
+            }
+            const uint64_t here = __ballot(left < upto);
+            if (here) {
+                const int l = __builtin_ctzll(here);
+                t = base + l;
+                const int64_t f = lo + (left - (upto - mine)) * (WAVES * 32);
+                first = (int64_t)__shfl((int)f, l);      // (rows are fewer than 2^31)
+                end = (int64_t)__shfl((int)hi, l);
+                break;
+            }
+            left -= __shfl(upto, 63);
+        }
+    }
+    if (t < 0) return;
+    t = __builtin_amdgcn_readfirstlane(t);
+    first = __builtin_amdgcn_readfirstlane((int)first);
+    end = __builtin_amdgcn_readfirstlane((int)end);
+
+    const int64_t r0 = first + wave * 32;
+    const T* row = static_cast<const T*>(a.A) + min(r0 + (lane & 31), end - 1) * a.C;
+    const uint4* B = a.B + ((int64_t)(t * a.blocks + blockIdx.y) * a.chunks) * (kFrags * 64);
+    const bool works = r0 < end;
+
+    auto fetch_b = [&](int chunk, int buffer) SAR_INLINE {
+        for (int f = wave; f < kFrags; f += WAVES)
+            __builtin_amdgcn_global_load_lds((GlobalSrc*)(B + ((int64_t)chunk * kFrags + f) * 64 + lane),
+                                             (LdsPtr*)(lds + (buffer * kFrags + f) * 64), 16, 0, 0);
+    };
+    auto fetch_a = [&](int chunk, uint4 (&x)[kRaw]) SAR_INLINE {
+#pragma unroll
+        for (int p = 0; p < kRaw; ++p) x[p] = Cols<T>::load(row, chunk * CH + h * (CH / 2) + p * N, a.C);
+    };
+    auto settle_a = [&](int chunk, uint4 (&x)[kRaw]) SAR_INLINE {
+        if ((chunk + 1) * CH <= a.C) return;
+#pragma unroll
+        for (int p = 0; p < kRaw; ++p) {
+            const int c = chunk * CH + h * (CH / 2) + p * N;
+            if (c + N <= a.C) continue;
+            if (c >= a.C) x[p] = make_uint4(0u, 0u, 0u, 0u);
+            else if (a.C >= N) x[p] = front_of_piece<T>(x[p], a.C - c);
+        }
+    };
+
+    float16_t acc[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) acc[i] = float16_t{};
+    uint4 x[kRaw], next[kRaw];
+    fetch_b(0, 0);
+    fetch_a(0, x);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    float sign = 1.f;
+    for (int chunk = 0; chunk < a.chunks; ++chunk) {
+        const int buffer = chunk & 1;
+        if (chunk + 1 < a.chunks) {
+            fetch_b(chunk + 1, buffer ^ 1);
+            fetch_a(chunk + 1, next);
+        }
+        if (works) {
+            settle_a(chunk, x);
+            const uint4* b = lds + buffer * kFrags * 64 + lane;
+            if constexpr (P == 3) {
+                uint4 p[S][3];
+#pragma unroll
+                for (int s = 0; s < S; ++s) {
+                    const float v[8] = {__uint_as_float(x[2 * s].x), __uint_as_float(x[2 * s].y), __uint_as_float(x[2 * s].z),
+                                        __uint_as_float(x[2 * s].w), __uint_as_float(x[2 * s + 1].x), __uint_as_float(x[2 * s + 1].y),
+                                        __uint_as_float(x[2 * s + 1].z), __uint_as_float(x[2 * s + 1].w)};
+                    split8(v, p[s]);
+                }
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    float16_t sum = {};
+#pragma unroll
+                    for (int s = 0; s < S; ++s) {
+                        uint4 w[3];
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) w[k] = b[((s * P + k) * NT + i) * 64];
+#pragma unroll
+                        for (int k = 0; k < 6; ++k)
+                            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[s][kTerm[k][0]]),
+                                                                          __builtin_bit_cast(bf16x8_t, w[kTerm[k][1]]), sum, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[i][r] = fmaf(sum[r], sign, acc[i][r]);
+                }
+                sign = -sign;
+            } else {
+#pragma unroll
+                for (int s = 0; s < S; ++s)
+#pragma unroll
+                    for (int i = 0; i < NT; ++i)
+#pragma unroll
+                        for (int k = P - 1; k >= 0; --k)
+                            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x[s]),
+                                                                             __builtin_bit_cast(bf16x8_t, b[((s * P + k) * NT + i) * 64]),
+                                                                             acc[i], 0, 0, 0);
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+#pragma unroll
+        for (int p = 0; p < kRaw; ++p) x[p] = next[p];
+    }
+    if (!works) return;
+
+    const int n0 = blockIdx.y * (32 * NT);
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) odd |= not_finite(acc[i]);
+    if (__any(odd)) exact_tiles<T, NT, TRANS>(a, t, row, n0, acc);
+
+    // lane holds columns of its place; register r holds row 8*(r/4) + 4*h + r%4
+    constexpr int IL = NT < 4 ? NT : 4;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int64_t i = r0 + 8 * (r / 4) + 4 * h + r % 4;
+        if (i >= end) continue;
+        T* out = static_cast<T*>(a.out) + i * a.N;
+#pragma unroll
+        for (int g = 0; g < NT / IL; ++g) {
+            const int n = n0 + column_of<NT>(g * IL, lane & 31);
+            if (n + IL <= a.N) {
+                if constexpr (sizeof(T) == 4) {
+                    struct __attribute__((packed, aligned(4))) V { float v[IL]; } v;
+#pragma unroll
+                    for (int j = 0; j < IL; ++j) v.v[j] = acc[g * IL + j][r];
+                    *reinterpret_cast<V*>(out + n) = v;
+                } else {
+                    struct __attribute__((packed, aligned(2))) V { uint32_t v[IL / 2]; } v;
+#pragma unroll
+                    for (int j = 0; j < IL / 2; ++j) v.v[j] = pack2_bf16(acc[g * IL + 2 * j][r], acc[g * IL + 2 * j + 1][r]);
+                    *reinterpret_cast<V*>(out + n) = v;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < IL; ++j)
+                    if (n + j < a.N) out[n + j] = from_f32<T>(acc[g * IL + j][r]);
+            }
+        }
+    }
+}
+
+// Column tiles a wavefront forms at once.
+int tiles_of(int64_t n, int N)
+{
+    // with few rows, more workgroups of fewer columns: 256 rows a workgroup leave most of the chip idle
+    if (N <= 64 || n * N <= (int64_t)256 * 256 * 128) return 2;
+    return 8;
+}
+
+template <typename T, int NT, bool TRANS>
+int run_rows(const RowsArgs& a, LayArgs l, hipStream_t st)
+{
+    constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps, kWaves = 8;
+    const int64_t units = (int64_t)l.T * l.blocks * l.chunks * S * NT * 64;
+    const int64_t lay = (units + 255) / 256, groups = a.types.n / (kWaves * 32) + a.types.T;
+    if (lay > 0x7fffffff || groups > 0x7fffffff || l.blocks > 65535)
+        return fail(SAR_ERR_UNSUPPORTED, "typed products: %lld rows, %d x %d weights of %d types are too many for one launch",
+                    (long long)a.types.n, a.K, a.F, l.T);
+    k_typed_lay<T, NT, TRANS><<<(unsigned)lay, 256, 0, st>>>(l);
+    SAR_LAUNCH_CHECK();
+    constexpr size_t shared = (size_t)2 * S * P * NT * 1024;
+    auto* fn = k_typed_rows<T, NT, kWaves, TRANS>;
+    if (shared > 65536) SAR_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)shared));
+    fn<<<dim3((unsigned)groups, l.blocks), kWaves * 64, shared, st>>>(a);
+    SAR_LAUNCH_CHECK();
+    return SAR_OK;
+}
+
+// Bytes of B's pieces for contraction C and N columns (either type, either number of tiles).
+size_t lay_bytes(int C, int N, int T)
+{
+    const size_t f32 = (size_t)((C + 31) / 32) * 2 * 3, b16 = (size_t)((C + 63) / 64) * 4 * 2;
+    return (size_t)T * ((N + 255) / 256 * 8) * std::max(f32, b16) * 1024;
+}
+
+// out [n, N] = A [n, C] B; TRANS: B = W^T.
+template <typename T, bool TRANS>
+int rows_product(const void* A, const float* W, const Types& types, void* out, int K, int F, void* work, hipStream_t st)
+{
+    const int C = TRANS ? F : K, N = TRANS ? K : F, NT = tiles_of(types.n, N);
+    const int chunks = (C + kChunk<T> - 1) / kChunk<T>, blocks = (N + 32 * NT - 1) / (32 * NT);
+    const RowsArgs a{A, static_cast<const uint4*>(work), W, out, types, C, N, chunks, blocks, K, F};
+    const LayArgs l{W, static_cast<uint4*>(work), types.T, K, F, C, N, chunks, blocks};
+    return NT == 2 ? run_rows<T, 2, TRANS>(a, l, st) : run_rows<T, 8, TRANS>(a, l, st);
+}
+
+size_t round256(size_t b) { return (b + 255) / 256 * 256; }
+
+int check_shape(int64_t n, int K, int F, int T)
+{
+    SAR_CHECK_ARG(n >= 0 && K >= 1 && F >= 1, "typed products: n = %lld rows, K = %d, F = %d", (long long)n, K, F);
+    SAR_CHECK_ARG(T >= 1, "typed products: T = %d types", T);
+    if (n > 0x7fffffff - 256 || K > 65536 || F > 65536 || T > 65535)
+        return fail(SAR_ERR_UNSUPPORTED, "typed products: n = %lld rows (below 2^31 - 256), K = %d, F = %d (at most 65536), T = %d types (at most 65535)",
+                    (long long)n, K, F, T);
+    return SAR_OK;
+}
+
+size_t work_bytes_of(int64_t n, int K, int F, int T)
+{
+    return round256(std::max(std::max(lay_bytes(K, F, T), lay_bytes(F, K, T)), typed_dw_bytes(n, K, F, T)));
+}
+
+int check_call(int dtype, int64_t n, int K, int F, int T, const void* ptr, const void* work, size_t work_bytes)
+{
+    if (dtype != SAR_F32 && dtype != SAR_BF16) return fail(SAR_ERR_UNSUPPORTED, "dtype %d is neither SAR_F32 nor SAR_BF16", dtype);
+    SAR_TRY(check_shape(n, K, F, T));
+    SAR_CHECK_ARG(ptr || T == 1, "typed products: type_ptr is null with T = %d types", T);
+    const size_t need = work_bytes_of(n, K, F, T);
+    SAR_CHECK_ARG(work && work_bytes >= need, "typed products: work has %zu bytes, needs %zu", work ? work_bytes : 0, need);
+    SAR_CHECK_ARG((reinterpret_cast<uintptr_t>(work) & 15) == 0, "typed products: work must be 16-byte aligned");
+    return SAR_OK;
+}
+
+// The backward pass of both entry points (ptr null: one type).
+int typed_bwd(const void* X, const int8_t* Xq, const uint8_t* Xe, const void* dZ, const float* W, const int32_t* ptr, int T, int accumulate,
+              float* dW, void* dX, int dtype, int64_t n, int K, int F, void* work, hipStream_t st)
+{
+    SAR_TRY(check_packed("Xq", Xq, Xe));
+    SAR_CHECK_ARG(!(X && Xq), "typed products: X and Xq are both given");
+    if (n > 0) {
+        SAR_CHECK_ARG(dZ || (!dW && !dX), "null pointer (dZ)");
+        SAR_CHECK_ARG(!dW || X || Xq, "null pointer (X or Xq)");
+        SAR_CHECK_ARG(!dX || W, "null pointer (W)");
+        SAR_CHECK_ARG(!dX || dX != dZ, "typed products: dX must not alias dZ");
+    }
+    const Types types{ptr, T, n};
+    if (dW) SAR_TRY(sar::typed_dw(dtype, {X, Xq, Xe, dZ, dW, types, K, F, accumulate, static_cast<float*>(work)}, st));
+    if (dX && n > 0)
+        return dtype == SAR_F32 ? rows_product<float, true>(dZ, W, types, dX, K, F, work, st)
+                                : rows_product<bf16_t, true>(dZ, W, types, dX, K, F, work, st);
+    return SAR_OK;
+}
+
+}  // namespace
+}  // namespace sar
+
+using namespace sar;
+
+extern "C" int sar_linear_typed_workspace_bytes(int64_t n, int K, int F, int T, size_t* bytes)
+{
+    SAR_CHECK_ARG(bytes, "bytes is null");
+    SAR_TRY(check_shape(n, K, F, T));
+    *bytes = work_bytes_of(n, K, F, T);
+    return SAR_OK;
+}
+
+extern "C" int sar_linear_typed_fwd(const void* X, const float* W, const int32_t* type_ptr, int T, void* Z, int dtype, int64_t n, int K, int F,
+                                    void* work, size_t work_bytes, void* stream)
+{
+    SAR_TRY(check_call(dtype, n, K, F, T, type_ptr, work, work_bytes));
+    if (n == 0) return SAR_OK;
+    SAR_CHECK_ARG(X && W && Z, "null pointer (X, W, Z)");
+    SAR_CHECK_ARG(X != Z, "typed products: Z must not alias X");
+    const Types types{type_ptr, T, n};
+    return dtype == SAR_F32 ? rows_product<float, false>(X, W, types, Z, K, F, work, as_stream(stream))
+                            : rows_product<bf16_t, false>(X, W, types, Z, K, F, work, as_stream(stream));
+}
+
+extern "C" int sar_linear_typed_bwd(const void* X, const int8_t* Xq, const uint8_t* Xe, const void* dZ, const float* W,
+                                    const int32_t* type_ptr, int T, int accumulate, float* dW, void* dX, int dtype, int64_t n, int K, int F,
+                                    void* work, size_t work_bytes, void* stream)
+{
+    SAR_TRY(check_call(dtype, n, K, F, T, type_ptr, work, work_bytes));
+    return typed_bwd(X, Xq, Xe, dZ, W, type_ptr, T, accumulate, dW, dX, dtype, n, K, F, work, as_stream(stream));
+}
+
+extern "C" int sar_linear_bwd_packed(const int8_t* Xq, const uint8_t* Xe, const void* dZ, const float* W, int accumulate, float* dW, void* dX,
+                                     int dtype, int64_t n, int K, int F, void* work, size_t work_bytes, void* stream)
+{
+    SAR_TRY(check_call(dtype, n, K, F, 1, nullptr, work, work_bytes));
+    return typed_bwd(nullptr, Xq, Xe, dZ, W, nullptr, 1, accumulate, dW, dX, dtype, n, K, F, work, as_stream(stream));
+}

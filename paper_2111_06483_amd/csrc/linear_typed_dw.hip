@@ -1,0 +1,472 @@
+// Weight gradients by type: dW[t] (+)= X_t^T dZ_t over the rows of every type, X as fp32 or bf16 rows or in 8 bits (packed.h).
+//
+// The contraction runs along the rows, which both operands have as their slow dimension.  A workgroup of 8 wavefronts holds a whole tile of up
+// to 256 x 256 sums in registers, so that at the usual widths every value is read once; its rows come in chunks:
+//   - A thread reads eight rows of two columns (four of packed rows) into registers, one chunk ahead, turns them into bf16 pieces along the rows
+//     (fp32: three, exact; bf16 rows and packed ones, whose values are bf16 values: one) and puts them to LDS as whole fragments: 16 bytes are eight
+//     rows of a column, conflict-free to read.  Two buffers, one barrier a chunk.
+//   - fp32 x fp32 takes six products of pieces (linear_pieces.h), packed x fp32 three, packed or bf16 x bf16 one.
+//   - Sums: from zero in the matrix unit over kSteps x 16 rows, then added by vector instructions, every other chunk with the other sign of X: the
+//     matrix unit cuts where it adds, and over a million rows that would lean to one side.
+// Rows are dealt evenly to the workgroups, whatever the types' sizes: a workgroup that meets the end of a type writes its sums and starts
+// anew, so no workgroup has more rows than another.  Workgroup w writes its sums of type t to place w + t (every step along the rows goes to the
+// next workgroup or the next type, so no two have the same place), and a second launch adds a type's places up in order: the result is the
+// same in every run.
+// Sums that are not finite are taken again there, from the operands.
+#include <algorithm>
+
+#include "linear_pieces.h"
+#include "linear_typed.h"
+
+namespace sar {
+
+namespace {
+
+constexpr int kThreads = 512;
+
+// What rows an operand has: pieces of a value, values a thread takes of a row, and their bytes.
+struct F32Rows {
+    using T = float;
+    static constexpr int kPieces = 3, kCols = 2;
+};
+struct Bf16Rows {
+    using T = bf16_t;
+    static constexpr int kPieces = 1, kCols = 2;
+};
+struct PackedRows {
+    static constexpr int kPieces = 1, kCols = 4;
+};
+
+struct DwArgs {
+    const void* X;
+    const int8_t* Xq;
+    const uint8_t* Xe;
+    const void* dZ;
+    float* partial;        // [workgroups + T, K, F]
+    Types types;
+    int K, F;
+    int64_t share;         // rows of a workgroup
+};
+
+// Where column c of a tile's columns lies in LDS: of 64 columns the even ones first, so that the two that a thread writes go to runs of
+// their own, and a lane of two neighbouring column tiles holds two neighbouring columns.
+__device__ inline int place_of(int c) { return (c & ~63) | (c & 1) << 5 | (c >> 1 & 31); }
+__device__ inline int column_at(int p) { return (p & ~63) | (p & 31) << 1 | (p >> 5 & 1); }
+
+// Eight rows of kCols columns of a tile on their way from memory to LDS.  `base` is the chunk's first row, the same for all lanes; a chunk
+// that is not full reads its last row again in place of those that are not there, and counts them as zeros.
+template <typename R>
+struct Unit {
+    using T = typename R::T;
+    static constexpr int kRegs = 8 * (int)sizeof(T) * 2 / 4;
+    // c: column of the tensor (its rows are `width` values wide)
+    static __device__ inline void load(uint32_t* w, const T* base, int group, int rows, bool full, int c, int width)
+    {
+        const uint32_t bytes = (uint32_t)width * sizeof(T), at = (uint32_t)min(c, max(width - 2, 0)) * sizeof(T);
+        auto one = [&](int k, const char* p) SAR_INLINE {
+            if constexpr (sizeof(T) == 4) {
+                struct __attribute__((packed, aligned(4))) V { uint32_t x, y; };
+                if (width >= 2) {
+                    const V v = *reinterpret_cast<const V*>(p);
+                    w[2 * k] = v.x, w[2 * k + 1] = v.y;
+                } else {
+                    w[2 * k] = w[2 * k + 1] = *reinterpret_cast<const uint32_t*>(p);
+                }
+            } else {
+                struct __attribute__((packed, aligned(2))) V { uint32_t x; };
+                w[k] = width >= 2 ? reinterpret_cast<const V*>(p)->x : *reinterpret_cast<const uint16_t*>(p) * 0x10001u;
+            }
+        };
+        const char* p = reinterpret_cast<const char*>(base);
+        if (full) {
+            const uint32_t off = at + (uint32_t)group * 8 * bytes;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) one(k, p + (size_t)k * bytes + off);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) one(k, p + (at + (uint32_t)min(8 * group + k, rows - 1) * bytes));
+        }
+    }
+    // ... and into out[piece * stride], out[piece * stride + 32], the two columns' fragments
+    static __device__ inline void put(uint32_t* w, uint4* out, int stride, int group, int rows, bool full, int c, int width, bool negate)
+    {
+        if (!full) {
+#pragma unroll
+            for (int k = 0; k < kRegs; ++k)
+                if (8 * group + k * 8 / kRegs >= rows) w[k] = 0u;
+        }
+        if (c == width - 1) {          // the two values end with the row's last
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if constexpr (sizeof(T) == 4) w[2 * k] = w[2 * k + 1];
+                else w[k] >>= 16;
+            }
+        }
+        if constexpr (sizeof(T) == 4) {
+            const uint32_t flip = negate ? 0x80000000u : 0u;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float v[8];
+                uint4 p[3];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(w[2 * k + j] ^ flip);
+                split8(v, p);
+#pragma unroll
+                for (int t = 0; t < 3; ++t) out[t * stride + 32 * j] = p[t];
+            }
+        } else {
+            const uint32_t flip = negate ? 0x80008000u : 0u;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                uint32_t p[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) p[k] = __builtin_amdgcn_perm(w[2 * k + 1], w[2 * k], j ? 0x07060302u : 0x05040100u) ^ flip;
+                out[32 * j] = make_uint4(p[0], p[1], p[2], p[3]);
+            }
+        }
+    }
+};
+struct PackedUnit {
+    static constexpr int kRegs = 16;           // eight rows' numbers, eight steps
+    static __device__ inline void load(uint32_t* w, const int8_t* q, const uint8_t* e, int group, int rows, bool full, int c, int K)
+    {
+        const uint32_t stride = packed_stride(K), steps = packed_steps(K), at = (uint32_t)min(c, (int)stride - 4);
+        if (full) {
+            const uint32_t off = at + (uint32_t)group * 8 * stride, eoff = at / kPackBlock + (uint32_t)group * 8 * steps;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                w[k] = *reinterpret_cast<const uint32_t*>(q + (size_t)k * stride + off);
+                w[8 + k] = (e + (size_t)k * steps)[eoff];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t r = (uint32_t)min(8 * group + k, rows - 1);
+                w[k] = *reinterpret_cast<const uint32_t*>(q + (at + r * stride));
+                w[8 + k] = e[at / kPackBlock + r * steps];
+            }
+        }
+    }
+    static __device__ inline void put(uint32_t* w, uint4* out, int group, int rows, bool full, bool negate)
+    {
+        if (!full) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (8 * group + k >= rows) w[k] = 0u, w[8 + k] = 1u;
+        }
+        uint32_t p[4][4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float a[4], b[4];
+            const float sa = step_of(w[8 + 2 * k]), sb = step_of(w[8 + 2 * k + 1]);
+            unpack4(w[2 * k], negate ? -sa : sa, a);
+            unpack4(w[2 * k + 1], negate ? -sb : sb, b);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) p[j][k] = pack2_bf16(a[j], b[j]);        // (bf16 values: not rounded)
+        }
+        // columns c, c + 1, c + 2, c + 3: two even ones and two odd ones
+        out[0] = make_uint4(p[0][0], p[0][1], p[0][2], p[0][3]);
+        out[1] = make_uint4(p[2][0], p[2][1], p[2][2], p[2][3]);
+        out[32] = make_uint4(p[1][0], p[1][1], p[1][2], p[1][3]);
+        out[33] = make_uint4(p[3][0], p[3][1], p[3][2], p[3][3]);
+    }
+};
+template <typename XR>
+constexpr int kXRegs = Unit<XR>::kRegs;
+template <>
+constexpr int kXRegs<PackedRows> = PackedUnit::kRegs;
+
+// A value of X as fp32.
+template <typename XR>
+__device__ inline float x_value(const DwArgs& a, int64_t row, int c)
+{
+    if constexpr (XR::kCols == 4) {
+        return (float)a.Xq[row * packed_stride(a.K) + c] * step_of(a.Xe[row * packed_steps(a.K) + c / kPackBlock]);
+    } else if constexpr (sizeof(typename XR::T) == 4) {
+        return static_cast<const float*>(a.X)[row * a.K + c];
+    } else {
+        return bf16_to_f32(static_cast<const bf16_t*>(a.X)[row * a.K + c]);
+    }
+}
+template <typename ZR>
+__device__ inline float z_value(const DwArgs& a, int64_t row, int c)
+{
+    if constexpr (sizeof(typename ZR::T) == 4) return static_cast<const float*>(a.dZ)[row * a.F + c];
+    else return bf16_to_f32(static_cast<const bf16_t*>(a.dZ)[row * a.F + c]);
+}
+
+// WM x WN wavefronts of MT x NT tiles of 32 x 32; S products of 16 rows a chunk.
+template <typename XR, typename ZR, int MT, int NT, int WM, int WN, int S>
+__global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
+{
+    constexpr int TK = WM * MT * 32, TF = WN * NT * 32, PX = XR::kPieces, PZ = ZR::kPieces;
+    static_assert(WM * WN * 64 == kThreads, "eight wavefronts");
+    constexpr int kGroups = 2 * S;                                  // eight rows each
+    constexpr int kXUnits = kGroups * TK / XR::kCols, kZUnits = kGroups * TF / ZR::kCols;
+    constexpr int kSlots = (kXUnits + kZUnits + kThreads - 1) / kThreads;
+    constexpr int kXSize = PX * kGroups * TK, kSize = kXSize + PZ * kGroups * TF;      // fragments a buffer
+    extern __shared__ __attribute__((aligned(16))) uint4 lds[];                         // [2][kSize]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const int wm = wave % WM, wn = wave / WM;
+    const int k0 = blockIdx.y * TK, f0 = blockIdx.z * TF;
+
+    // the units of a chunk, X's before dZ's, columns fastest: thread by thread, so that a wavefront's are all of one operand
+    uint32_t raw[kSlots][kXRegs<XR> > Unit<ZR>::kRegs ? kXRegs<XR> : Unit<ZR>::kRegs];
+    auto fetch = [&](int64_t r0, int64_t end) SAR_INLINE {
+        const int rows = (int)min(end - r0, (int64_t)(16 * S));
+        const bool full = rows == 16 * S;
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u) {
+            const int first = wave * 64 + u * kThreads;
+            if (first < kXUnits) {
+                const int id = first + lane, g = id / (TK / XR::kCols), c = k0 + id % (TK / XR::kCols) * XR::kCols;
+                if constexpr (XR::kCols == 4)
+                    PackedUnit::load(raw[u], a.Xq + r0 * packed_stride(a.K), a.Xe + r0 * packed_steps(a.K), g, rows, full, c, a.K);
+                else
+                    Unit<XR>::load(raw[u], static_cast<const typename XR::T*>(a.X) + r0 * a.K, g, rows, full, c, a.K);
+            } else if (first < kXUnits + kZUnits) {
+                const int id = first + lane - kXUnits, g = id / (TF / 2), c = f0 + id % (TF / 2) * 2;
+                Unit<ZR>::load(raw[u], static_cast<const typename ZR::T*>(a.dZ) + r0 * a.F, g, rows, full, c, a.F);
+            }
+        }
+    };
+    auto put = [&](int64_t r0, int64_t end, uint4* buf, bool negate) SAR_INLINE {
+        const int rows = (int)min(end - r0, (int64_t)(16 * S));
+        const bool full = rows == 16 * S;
+#pragma unroll
+        for (int u = 0; u < kSlots; ++u) {
+            const int first = wave * 64 + u * kThreads;
+            if (first < kXUnits) {
+                const int id = first + lane, g = id / (TK / XR::kCols), c = id % (TK / XR::kCols) * XR::kCols;
+                if constexpr (XR::kCols == 4) PackedUnit::put(raw[u], buf + g * TK + place_of(c), g, rows, full, negate);
+                else Unit<XR>::put(raw[u], buf + g * TK + place_of(c), kGroups * TK, g, rows, full, k0 + c, a.K, negate);
+            } else if (first < kXUnits + kZUnits) {
+                const int id = first + lane - kXUnits, g = id / (TF / 2), c = id % (TF / 2) * 2;
+                Unit<ZR>::put(raw[u], buf + kXSize + g * TF + place_of(c), kGroups * TF, g, rows, full, f0 + c, a.F, false);
+            }
+        }
+    };
+
+    const int64_t from = blockIdx.x * a.share, to = min(from + a.share, a.types.n);
+    for (int base = 0; base < a.types.T; base += 64) {
+        // the types that have rows among mine
+        int64_t lo = 0, hi = 0;
+        if (base + lane < a.types.T) a.types.span(base + lane, lo, hi);
+        lo = max(lo, from), hi = min(hi, to);
+        uint64_t mine = __ballot(lo < hi);
+        while (mine) {
+            const int l = __builtin_ctzll(mine);
+            mine &= mine - 1;
+            const int t = base + l;
+            const int64_t first = __builtin_amdgcn_readfirstlane(__shfl((int)lo, l));
+            const int64_t end = __builtin_amdgcn_readfirstlane(__shfl((int)hi, l));
+
+            float16_t acc[MT][NT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[m][n] = float16_t{};
+            fetch(first, end);
+            put(first, end, lds, false);
+            __syncthreads();
+            int buffer = 0;
+            float sign = 1.f;
+            for (int64_t r0 = first; r0 < end; r0 += 16 * S) {
+                const bool more = r0 + 16 * S < end;
+                if (more) fetch(r0 + 16 * S, end);
+                const uint4* xb = lds + buffer * kSize + wm * MT * 32 + (lane & 31);
+                const uint4* zb = lds + buffer * kSize + kXSize + wn * NT * 32 + (lane & 31);
+                if constexpr (PZ == 1) {
+                    uint4 x[S][MT];
+#pragma unroll
+                    for (int s = 0; s < S; ++s)
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) x[s][m] = xb[(2 * s + h) * TK + m * 32];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        uint4 z[S];
+#pragma unroll
+                        for (int s = 0; s < S; ++s) z[s] = zb[(2 * s + h) * TF + n * 32];
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) {
+                            float16_t sum = {};
+#pragma unroll
+                            for (int s = 0; s < S; ++s)
+                                sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x[s][m]),
+                                                                              __builtin_bit_cast(bf16x8_t, z[s]), sum, 0, 0, 0);
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) acc[m][n][r] = fmaf(sum[r], sign, acc[m][n][r]);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int s = 0; s < S; ++s) {
+                        uint4 x[MT][PX];
+#pragma unroll
+                        for (int m = 0; m < MT; ++m)
+#pragma unroll
+                            for (int p = 0; p < PX; ++p) x[m][p] = xb[p * kGroups * TK + (2 * s + h) * TK + m * 32];
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            uint4 z[PZ];
+#pragma unroll
+                            for (int p = 0; p < PZ; ++p) z[p] = zb[p * kGroups * TF + (2 * s + h) * TF + n * 32];
+#pragma unroll
+                            for (int m = 0; m < MT; ++m) {
+                                float16_t sum = {};
+#pragma unroll
+                                for (int k = 0; k < 6; ++k)
+                                    if (kTerm[k][0] < PX)
+                                        sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x[m][kTerm[k][0] < PX ? kTerm[k][0] : 0]),
+                                                                                      __builtin_bit_cast(bf16x8_t, z[kTerm[k][1]]), sum, 0, 0, 0);
+#pragma unroll
+                                for (int r = 0; r < 16; ++r) acc[m][n][r] = fmaf(sum[r], sign, acc[m][n][r]);
+                            }
+                        }
+                    }
+                }
+                sign = -sign;
+                buffer ^= 1;
+                if (more) put(r0 + 16 * S, end, lds + buffer * kSize, sign < 0.f);
+                __syncthreads();
+            }
+
+            float* out = a.partial + ((int64_t)blockIdx.x + t) * a.K * a.F;
+            // lane holds column f; register r holds the weight's row at place 8*(r/4) + 4*h + r%4.  (The places are worked out here: carried
+            // through the loops they are registers that the sums need.)
+            int own = lane;
+            asm volatile("" : "+v"(own));
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int k = k0 + column_at((wm * MT + m) * 32 + 8 * (r / 4) + 4 * (own >> 5) + r % 4);
+                    if (k >= a.K) continue;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const int f = f0 + column_at((wn * NT + n) * 32 + (own & 31));
+                        if (f < a.F) out[(int64_t)k * a.F + f] = acc[m][n][r];
+                    }
+                }
+        }
+    }
+}
+
+// What a workgroup's place w + t should hold where it holds no finite number: three pieces of bf16 are no infinity, no NaN and none of the
+// largest numbers, whose rounding up is an infinity.  Summed again from the operands, by multiply-adds.
+template <typename XR, typename ZR>
+__device__ float sum_again(const DwArgs& a, int64_t w, int64_t lo, int64_t hi, int64_t element)
+{
+    const int k = (int)(element / a.F), f = (int)(element % a.F);
+    float v = 0.f;
+    for (int64_t r = max(lo, w * a.share); r < min(hi, (w + 1) * a.share); ++r) v = fmaf(x_value<XR>(a, r, k), z_value<ZR>(a, r, f), v);
+    return v;
+}
+
+// dW[t] (+)= the places of the workgroups that have rows of type t, in order.  32 consecutive values a workgroup of 256 threads, which take
+// every eighth place, eight at a time.
+template <typename XR, typename ZR>
+__global__ __launch_bounds__(256) void k_typed_sum(DwArgs a, int accumulate, float* dW)
+{
+    __shared__ float part[8][32];
+    const int e = threadIdx.x & 31, z = threadIdx.x >> 5, t = blockIdx.y;
+    const int64_t count = (int64_t)a.K * a.F;
+    int64_t lo, hi;
+    a.types.span(t, lo, hi);
+    const int64_t w0 = lo / a.share, w1 = hi > lo ? (hi - 1) / a.share + 1 : w0;
+    for (int64_t k0 = (int64_t)blockIdx.x * 32; k0 < count; k0 += (int64_t)gridDim.x * 32) {
+        const int64_t k = k0 + e;
+        float v = 0.f;
+        if (k < count) {
+            const float* p = a.partial + t * count + k;
+            for (int64_t w = w0 + z; w < w1; w += 8 * 8) {
+                float x[8], zero = 0.f;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) x[u] = w + u * 8 < w1 ? p[(w + u * 8) * count] : 0.f;
+                if constexpr (ZR::kPieces == 3) {
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) zero = fmaf(x[u], 0.f, zero);
+                    if (zero != 0.f) {         // (NaN)
+                        for (int u = 0; u < 8; ++u)
+                            if (w + u * 8 < w1 && !(fabsf(p[(w + u * 8) * count]) < __builtin_inff())) x[u] = sum_again<XR, ZR>(a, w + u * 8, lo, hi, k);
+                    }
+                }
+                v += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+            }
+        }
+        part[z][e] = v;
+        __syncthreads();
+        if (z == 0 && k < count) {
+            float total = 0.f;
+#pragma unroll
+            for (int s = 0; s < 8; ++s) total += part[s][e];
+            float* out = dW + t * count + k;
+            *out = accumulate ? *out + total : total;
+        }
+        __syncthreads();
+    }
+}
+
+struct Shape {
+    int tk, tf, tiles;
+    int64_t share, groups;
+};
+Shape shape_of(int64_t n, int K, int F)
+{
+    auto tile = [](int w) { return (w + 127) / 128 % 2 == 0 || w > 512 ? 256 : 128; };
+    Shape s;
+    s.tk = tile(K), s.tf = tile(F);
+    s.tiles = ((K + s.tk - 1) / s.tk) * ((F + s.tf - 1) / s.tf);
+    // a workgroup per compute unit (its registers and LDS leave no room for a second), none with fewer than 64 rows
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((n + 63) / 64, std::max(1, 256 / s.tiles)));
+    s.share = std::max<int64_t>(64, ((n + want - 1) / want + 63) / 64 * 64);
+    s.groups = std::max<int64_t>(1, (n + s.share - 1) / s.share);
+    return s;
+}
+
+template <typename XR, typename ZR, int MT, int NT, int WM, int WN, int S>
+int run(const DwArgs& a, const Shape& s, hipStream_t st)
+{
+    constexpr int TK = WM * MT * 32, TF = WN * NT * 32;
+    constexpr size_t shared = (size_t)2 * (XR::kPieces * TK + ZR::kPieces * TF) * 2 * S * sizeof(uint4);
+    auto* fn = k_typed_dw<XR, ZR, MT, NT, WM, WN, S>;
+    if (shared > 65536) SAR_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)shared));
+    fn<<<dim3((unsigned)s.groups, (a.K + TK - 1) / TK, (a.F + TF - 1) / TF), kThreads, shared, st>>>(a);
+    SAR_LAUNCH_CHECK();
+    return SAR_OK;
+}
+
+// S2: products of 16 rows a chunk where a wavefront holds eight tiles, S1: fewer.  (A chunk under way is what a thread holds
+// in registers beside its sums.)
+template <typename XR, typename ZR, int S1, int S2>
+int run_all(const DwArgs& a, const Shape& s, int accumulate, float* dW, hipStream_t st)
+{
+    if (a.types.n > 0) {
+        if (s.tk == 256 && s.tf == 256) SAR_TRY((run<XR, ZR, 2, 4, 4, 2, S2>(a, s, st)));
+        else if (s.tk == 256) SAR_TRY((run<XR, ZR, 2, 2, 4, 2, S1>(a, s, st)));
+        else if (s.tf == 256) SAR_TRY((run<XR, ZR, 2, 2, 2, 4, S1>(a, s, st)));
+        else SAR_TRY((run<XR, ZR, 1, 2, 4, 2, S1>(a, s, st)));
+    }
+    const int64_t count = (int64_t)a.K * a.F, blocks = std::min<int64_t>((count + 31) / 32, 1 << 20);
+    k_typed_sum<XR, ZR><<<dim3((unsigned)blocks, a.types.T), 256, 0, st>>>(a, accumulate, dW);
+    SAR_LAUNCH_CHECK();
+    return SAR_OK;
+}
+
+}  // namespace
+
+size_t typed_dw_bytes(int64_t n, int K, int F, int T)
+{
+    return (size_t)(shape_of(n, K, F).groups + T) * K * F * sizeof(float);
+}
+
+int typed_dw(int dtype, const TypedDw& g, hipStream_t st)
+{
+    const Shape s = shape_of(g.types.n, g.K, g.F);
+    const DwArgs a{g.X, g.Xq, g.Xe, g.dZ, g.partial, g.types, g.K, g.F, s.share};
+    if (dtype == SAR_F32)
+        return g.Xq ? run_all<PackedRows, F32Rows, 1, 1>(a, s, g.accumulate, g.dW, st) : run_all<F32Rows, F32Rows, 1, 1>(a, s, g.accumulate, g.dW, st);
+    return g.Xq ? run_all<PackedRows, Bf16Rows, 4, 2>(a, s, g.accumulate, g.dW, st) : run_all<Bf16Rows, Bf16Rows, 4, 2>(a, s, g.accumulate, g.dW, st);
+}
+
+}  // namespace sar

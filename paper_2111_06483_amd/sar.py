@@ -111,6 +111,10 @@ _SIGNATURES = {
     "sar_gat_bwd_end_noalloc": "pppppppiliip",
     "sar_linear_fwd": "pppiliiiippppp", "sar_linear_bwd": "pppppiliipzp", "sar_linear_bwd_rows": "ppplppiipppilippzp",
     "sar_linear_workspace_bytes": "liip",
+    "sar_pack": "pilippp", "sar_unpack": "ppilipp", "sar_layernorm_fwd": "pppfppilippppp",
+    "sar_layernorm_bwd": "ppppppipppilipzp", "sar_layernorm_workspace_bytes": "lip",
+    "sar_linear_typed_fwd": "pppipiliipzp", "sar_linear_typed_bwd": "ppppppiippiliipzp", "sar_linear_typed_workspace_bytes": "liiip",
+    "sar_linear_bwd_packed": "ppppippiliipzp",
 }
 _CTYPES = {"p": _vp, "i": _c_int, "l": _c_i64, "z": ctypes.c_size_t, "f": ctypes.c_float}
 EXPORTS = list(_SIGNATURES)
@@ -473,3 +477,64 @@ def sar_linear_bwd_rows(X: Optional[torch.Tensor], E: Optional[torch.Tensor], E_
                         rows: Optional[torch.Tensor] = None) -> None:
     """E_rank: device address of a t_rank array (BlockView.t_rank) when E is compact."""
     native().linear_bwd_rows(X, E, E_rank, ds, a_r, H, D, W, dW, dX, n, dtype_code(dtype), work, rows)
+
+
+# ------------------------------------------------------ node-wise rows in 8 bits, layer norm
+
+def packed_empty(n: int, K: int, device="cuda"):
+    """Room for n rows of K values in 8 bits: the pair (q, e) of sar_pack."""
+    return (torch.empty((n, -(-K // 16) * 16), dtype=torch.int8, device=device),
+            torch.empty((n, -(-K // 32)), dtype=torch.uint8, device=device))
+
+
+def sar_pack(X: torch.Tensor, packed) -> None:
+    """packed: a pair (q, e) as packed_empty makes it."""
+    native().pack(X, packed)
+
+
+def sar_unpack(packed, X: torch.Tensor) -> None:
+    native().unpack(packed, X)
+
+
+def sar_layernorm_fwd(X: torch.Tensor, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float, Y: torch.Tensor,
+                      stats: Optional[torch.Tensor] = None, Xp=None, Yp=None) -> None:
+    """Xp, Yp: pairs (q, e) that receive X and Y in 8 bits."""
+    native().layernorm_fwd(X, gamma, beta, eps, Y, stats, Xp, Yp)
+
+
+def sar_layernorm_bwd(dY: torch.Tensor, X, stats: torch.Tensor, gamma: Optional[torch.Tensor], accumulate: bool,
+                      dX: Optional[torch.Tensor], dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor],
+                      work: Optional[torch.Tensor]) -> None:
+    """X: the input, or the pair (q, e) it was packed into."""
+    native().layernorm_bwd(dY, X, stats, gamma, accumulate, dX, dgamma, dbeta, work)
+
+
+def sar_layernorm_workspace_bytes(n: int, D: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().sar_layernorm_workspace_bytes(n, D, ctypes.byref(out)))
+    return out.value
+
+
+# ------------------------------------------------------ transforms with a weight per node type
+
+def sar_linear_typed_fwd(X: torch.Tensor, W: torch.Tensor, type_ptr: torch.Tensor, Z: torch.Tensor, work: torch.Tensor) -> None:
+    """W [T, K, F]; type_ptr int32 [T + 1]: the rows of type t are type_ptr[t] to type_ptr[t + 1]."""
+    native().linear_typed_fwd(X, W, type_ptr, Z, work)
+
+
+def sar_linear_typed_bwd(X, dZ: torch.Tensor, W: torch.Tensor, type_ptr: torch.Tensor, accumulate: bool,
+                         dW: Optional[torch.Tensor], dX: Optional[torch.Tensor], work: torch.Tensor) -> None:
+    """X: the input, the pair (q, e) it was packed into, or None without dW."""
+    native().linear_typed_bwd(X, dZ, W, type_ptr, accumulate, dW, dX, work)
+
+
+def sar_linear_typed_workspace_bytes(n: int, K: int, F: int, T: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().sar_linear_typed_workspace_bytes(n, K, F, T, ctypes.byref(out)))
+    return out.value
+
+
+def sar_linear_bwd_packed(packed, dZ: torch.Tensor, W: torch.Tensor, accumulate: bool, dW: Optional[torch.Tensor],
+                          dX: Optional[torch.Tensor], work: torch.Tensor) -> None:
+    """packed: the pair (q, e) of the input, or None without dW."""
+    native().linear_bwd_packed(packed, dZ, W, accumulate, dW, dX, work)

@@ -1,0 +1,264 @@
+"""Transforms with a weight per node type, and weight gradients from rows in 8 bits, against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2111_06483_amd import sar
+from tests import nodewise as nw
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+DTYPES = [F32, BF16]
+KINDS = [(F32, False), (F32, True), (BF16, False), (BF16, True)]       # rows' type; X in 8 bits
+
+
+def inputs(n, K, F, T, dtype, seed=0):
+    g = torch.Generator().manual_seed(seed * 104729 + n * 131 + K * 17 + F)
+    X = torch.randn(n, K, generator=g).to(dtype).cuda()
+    dZ = torch.randn(n, F, generator=g).to(dtype).cuda()
+    W = (torch.randn(T, K, F, generator=g) / K ** 0.5).cuda()
+    return X, dZ, W
+
+
+def ptr_of(ends):
+    return torch.tensor(ends, dtype=torch.int32, device="cuda")
+
+
+def work_for(n, K, F, T):
+    return torch.empty(sar.sar_linear_typed_workspace_bytes(n, K, F, T), dtype=torch.uint8, device="cuda")
+
+
+def packed_of(X):
+    p = sar.packed_empty(*X.shape)
+    sar.sar_pack(X, p)
+    return p, nw.unpack(p[0].cpu().numpy(), p[1].cpu().numpy(), X.shape[1])
+
+
+def rows_off(size, C, dtype):
+    """How far a product of C terms may be off, `size` = sum |a||b|: fp32 sums of 32 exact products cut at up to 24 places (a unit
+    each) and added, the weights' 16 bits and a unit for each of the C/8 additions where rows are bf16; the rounding of the result."""
+    if dtype == F32:
+        return (32 + C / 32) * 2 * nw.U * size
+    return (2.0 ** -16 + C / 8 * 2 * nw.U) * size
+
+
+def dw_off(size, rows):
+    """Sums of up to 64 products from zero, cut; a workgroup's sums one after the other, then the workgroups'."""
+    return (64 + rows / 32) * 2 * nw.U * size
+
+
+def check_rows(A, W, Z, spans, dtype, trans):
+    """Z = A W_t (trans: A W_t^T) on the types' rows."""
+    a, w, z = nw.f64(A), nw.f64(W), nw.f64(Z)
+    for t, lo, hi in spans:
+        m = w[t].T if trans else w[t]
+        want, size = a[lo:hi] @ m, np.abs(a[lo:hi]) @ np.abs(m)
+        off = rows_off(size, m.shape[0], dtype)
+        tol = off + (nw.half_step(dtype)(np.abs(want) + off) if dtype == BF16 else 0)
+        assert (np.abs(z[lo:hi] - want) <= tol).all(), (t, lo, hi)
+
+
+def check_dw(x, dZ, dW, spans, before=None):
+    d, got = nw.f64(dZ), nw.f64(dW)
+    for t, lo, hi in spans:
+        want, size = x[lo:hi].T @ d[lo:hi], np.abs(x[lo:hi]).T @ np.abs(d[lo:hi])
+        if before is not None:
+            want, size = want + before[t], size + np.abs(before[t])
+        assert (np.abs(got[t] - want) <= dw_off(size, hi - lo)).all(), (t, lo, hi)
+
+
+def check_all(n, K, F, ends, dtype, packed, accumulate=False):
+    T = len(ends) - 1
+    X, dZ, W = inputs(n, K, F, T, dtype)
+    ptr, work, spans = ptr_of(ends), work_for(n, K, F, T), nw.spans(ends, n)
+    outside = np.ones(n, bool)
+    for _, lo, hi in spans:
+        outside[lo:hi] = False
+    Z = torch.full((n, F), 3.0, dtype=dtype, device="cuda")
+    sar.sar_linear_typed_fwd(X, W, ptr, Z, work)
+    check_rows(X, W, Z, spans, dtype, False)
+    dX = torch.full((n, K), 3.0, dtype=dtype, device="cuda")
+    p, x = packed_of(X) if packed else (X, nw.f64(X))
+    first = torch.randn(T, K, F, generator=torch.Generator().manual_seed(9)).cuda()
+    dW = first.clone()
+    sar.sar_linear_typed_bwd(p, dZ, W, ptr, accumulate, dW, dX, work)
+    check_rows(dZ, W, dX, spans, dtype, True)
+    check_dw(x, dZ, dW, spans, nw.f64(first) if accumulate else None)
+    assert (nw.f64(Z)[outside] == 3).all() and (nw.f64(dX)[outside] == 3).all()
+    return Z, dW, dX
+
+
+# widths at which tiles, pieces and chunks end, whole and ragged
+SHAPES = [(1, 1), (1, 40), (3, 2), (4, 4), (7, 9), (8, 8), (16, 47), (31, 33), (32, 64), (47, 65), (63, 100), (64, 129), (100, 256), (128, 128), (129, 31),
+          (200, 47), (255, 257), (256, 256), (300, 200), (400, 130), (513, 20), (520, 520)]
+
+
+@pytest.mark.parametrize("dtype,packed", KINDS)
+@pytest.mark.parametrize("K,F", SHAPES)
+def test_shapes(K, F, dtype, packed):
+    check_all(331, K, F, [0, 100, 101, 101, 330], dtype, packed)
+
+
+@pytest.mark.parametrize("dtype,packed", KINDS)
+@pytest.mark.parametrize("K,F", [(100, 256), (256, 256), (72, 60)])
+def test_many_rows(K, F, dtype, packed):
+    """Enough rows for the wide tiles, several chunks a workgroup, types that end anywhere in a workgroup's rows."""
+    n = 140_003
+    check_all(n, K, F, [0, 5, 5, 40_000, 40_001, 90_017, n - 7], dtype, packed)
+
+
+@pytest.mark.parametrize("dtype,packed", KINDS)
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 63, 64, 65, 255, 256, 257, 1000])
+def test_every_number_of_rows(n, dtype, packed):
+    check_all(n, 40, 24, [0, n], dtype, packed)
+    check_all(n, 40, 24, [0, n // 3, n // 3, n], dtype, packed, accumulate=True)
+
+
+@pytest.mark.parametrize("dtype,packed", KINDS)
+def test_types_without_rows_and_rows_without_a_type(dtype, packed):
+    check_all(90, 33, 20, [0, 0, 0, 0], dtype, packed)
+    check_all(90, 33, 20, [0, 0, 50, 50, 50, 80], dtype, packed)
+    check_all(90, 33, 20, [10, 30, 80], dtype, packed, accumulate=True)
+    check_all(90, 33, 20, [90, 90], dtype, packed)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_more_types_than_a_wavefront_has_lanes(dtype):
+    rng = np.random.default_rng(1)
+    sizes = rng.integers(0, 40, 150)
+    sizes[60:70] = 0
+    ends = np.concatenate([[0], np.cumsum(sizes)])
+    check_all(int(ends[-1]) + 3, 24, 40, ends.tolist(), dtype, False)
+    check_all(int(ends[-1]), 24, 40, ends.tolist(), dtype, True)
+
+
+def test_bounds_that_leave_the_rows_are_cut():
+    check_all(50, 20, 20, [-5, 10, 70, 2_000_000_000], F32, False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_no_rows(dtype):
+    X, dZ, W = inputs(0, 12, 20, 2, dtype)
+    ptr, work = ptr_of([0, 0, 0]), work_for(0, 12, 20, 2)
+    sar.sar_linear_typed_fwd(X, W, ptr, torch.empty(0, 20, dtype=dtype, device="cuda"), work)
+    dW = torch.ones_like(W)
+    sar.sar_linear_typed_bwd(X, dZ, W, ptr, True, dW, torch.empty_like(X), work)
+    assert bool((dW == 1).all())
+    sar.sar_linear_typed_bwd(X, dZ, W, ptr, False, dW, torch.empty_like(X), work)
+    assert bool((dW == 0).all())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,K,F", [(1, 5, 7), (700, 100, 256), (50_001, 47, 130)])
+def test_plain_transform_from_packed_rows(n, K, F, dtype):
+    X, dZ, W = inputs(n, K, F, 1, dtype)
+    p, x = packed_of(X)
+    work = work_for(n, K, F, 1)
+    dW, dX = torch.empty(K, F, device="cuda"), torch.empty_like(X)
+    sar.sar_linear_bwd_packed(p, dZ, W[0], False, dW, dX, work)
+    check_dw(x, dZ, dW[None], [(0, 0, n)])
+    check_rows(dZ, W, dX, [(0, 0, n)], dtype, True)
+    once = dW.clone()
+    sar.sar_linear_bwd_packed(p, dZ, W[0], True, dW, None, work)         # added: the same sums once more
+    assert torch.equal(dW, once + once)
+    only = torch.empty_like(dX)
+    sar.sar_linear_bwd_packed(None, dZ, W[0], False, None, only, work)
+    assert torch.equal(only, dX)
+
+
+def test_packed_rows_are_bf16_rows():
+    """A packed row's values are bf16 values: dW from them is that from bf16 rows, bit for bit."""
+    X, dZ, W = inputs(3001, 90, 70, 1, BF16)
+    p, _ = packed_of(X)
+    same = torch.empty_like(X)
+    sar.sar_unpack(p, same)
+    ptr, work = ptr_of([0, 3001]), work_for(3001, 90, 70, 1)
+    a, b = torch.empty_like(W), torch.empty_like(W)
+    sar.sar_linear_typed_bwd(p, dZ, W, ptr, False, a, None, work)
+    sar.sar_linear_typed_bwd(same, dZ, W, ptr, False, b, None, work)
+    assert torch.equal(a, b)
+
+
+def test_sums_lean_to_no_side():
+    """Sums of 400 thousand products of one sign's mean error: cut sums would all be too small."""
+    n, K, F = 400_000, 40, 40
+    for dtype, packed in KINDS:
+        X, dZ, W = inputs(n, K, F, 1, dtype)
+        p, x = packed_of(X) if packed else (X, nw.f64(X))
+        dW = torch.empty_like(W)
+        sar.sar_linear_typed_bwd(p, dZ, W, ptr_of([0, n]), False, dW, None, work_for(n, K, F, 1))
+        d = nw.f64(dZ)
+        off = nw.f64(dW)[0] - x.T @ d
+        # 1600 sums of n terms: their errors' mean is zero within 4 of its deviations, and each is some roundings of the sum's size
+        assert abs(off.mean()) <= 4 * off.std() / 40 + 1e-12
+        assert off.std() <= 1e-6 * np.sqrt(n)
+
+
+@pytest.mark.parametrize("dtype,packed", [(F32, False), (BF16, False)])
+def test_infinities_and_nan_stay_where_they_belong(dtype, packed):
+    n, K, F = 300, 40, 50
+    X, dZ, W = inputs(n, K, F, 2, dtype)
+    X[7, 3] = float("inf")
+    X[200, 5] = float("nan")
+    dZ[9, 4] = -float("inf")
+    W = W.clone()
+    W[1, 6, 8] = float("inf")
+    ends = [0, 150, n]
+    ptr, work = ptr_of(ends), work_for(n, K, F, 2)
+    Z, dX, dW = torch.empty(n, F, dtype=dtype, device="cuda"), torch.empty_like(X), torch.empty_like(W)
+    sar.sar_linear_typed_fwd(X, W, ptr, Z, work)
+    sar.sar_linear_typed_bwd(X, dZ, W, ptr, False, dW, dX, work)
+    x, d, w = nw.f64(X), nw.f64(dZ), nw.f64(W)
+    with np.errstate(invalid="ignore"):
+        for t, lo, hi in nw.spans(ends, n):
+            for got, a, b in ((nw.f64(Z)[lo:hi], x[lo:hi], w[t]), (nw.f64(dX)[lo:hi], d[lo:hi], w[t].T), (nw.f64(dW)[t], x[lo:hi].T, d[lo:hi])):
+                want = (a[:, :, None] * b[None, :, :]).sum(1)            # (term by term: a library product may differ here)
+                fine = np.isfinite(want)
+                assert np.array_equal(got[~fine], want[~fine], equal_nan=True)
+                size = (np.abs(np.where(np.isfinite(a), a, 0)) @ np.abs(np.where(np.isfinite(b), b, 0)))
+                tol = (80 + a.shape[1] / 32) * 2 * nw.U * size + (0 if dtype == F32 else 2.0 ** -16 * size + 2.0 ** -8 * (np.abs(np.where(fine, want, 0)) + size * 2.0 ** -8))
+                assert (np.abs(got - want)[fine] <= tol[fine]).all()
+
+
+def test_the_largest_and_the_smallest_numbers():
+    """fp32 values whose pieces round up to infinity, and values near 2^-110."""
+    n, K, F = 70, 40, 36
+    X, dZ, W = inputs(n, K, F, 1, F32)
+    X, dZ = torch.zeros_like(X), torch.zeros_like(dZ)
+    X[3, 2] = torch.finfo(F32).max
+    X[4, 5] = 2.0 ** -100 * 1.7
+    dZ[3, 1] = 0.25
+    dZ[4, 6] = 1.3
+    W = torch.zeros_like(W)
+    W[0, 2, 3] = 0.5
+    W[0, 5, 7] = 1.9
+    ptr, work = ptr_of([0, n]), work_for(n, K, F, 1)
+    Z, dW = torch.empty(n, F, device="cuda"), torch.empty_like(W)
+    sar.sar_linear_typed_fwd(X, W, ptr, Z, work)
+    sar.sar_linear_typed_bwd(X, dZ, W, ptr, False, dW, None, work)
+    for got, want in ((nw.f64(Z), nw.f64(X) @ nw.f64(W)[0]), (nw.f64(dW)[0], nw.f64(X).T @ nw.f64(dZ))):
+        assert (np.abs(got - want) <= 2 * nw.U * 2 * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_tensors_that_begin_anywhere_and_neighbours(dtype):
+    n, K, F, ends = 77, 37, 29, [0, 30, 70]
+    X, dZ, W = inputs(n, K, F, 2, dtype)
+    odd = lambda t, dt: torch.full((t.numel() + 5,), 6.0, dtype=dt, device="cuda")
+    place = lambda buf, t: buf[1:1 + t.numel()].view(t.shape)
+    room = {k: odd(t, t.dtype) for k, t in (("x", X), ("dz", dZ), ("w", W), ("dx", X), ("z", dZ), ("dw", W))}
+    v = {k: place(room[k], t) for k, t in (("x", X), ("dz", dZ), ("w", W), ("dx", X), ("z", dZ), ("dw", W))}
+    v["x"].copy_(X), v["dz"].copy_(dZ), v["w"].copy_(W)
+    ptr, work, spans = ptr_of(ends), work_for(n, K, F, 2), nw.spans(ends, n)
+    sar.sar_linear_typed_fwd(v["x"], v["w"], ptr, v["z"], work)
+    sar.sar_linear_typed_bwd(v["x"], v["dz"], v["w"], ptr, False, v["dw"], v["dx"], work)
+    check_rows(X, W, v["z"], spans, dtype, False)
+    check_rows(dZ, W, v["dx"], spans, dtype, True)
+    check_dw(nw.f64(X), dZ, v["dw"], spans)
+    assert all(float(r[0]) == 6 and bool((r[-4:] == 6).all()) for r in room.values())
+
+
+def test_the_same_in_every_run():
+    n = 20_011
+    got = [check_all(n, 100, 64, [0, 7000, 7001, n], F32, True) for _ in range(2)]
+    assert all(torch.equal(a, b) for a, b in zip(*got))
