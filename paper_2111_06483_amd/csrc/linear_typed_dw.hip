@@ -62,29 +62,36 @@ struct Unit {
     // c: column of the tensor (its rows are `width` values wide)
     static __device__ inline void load(uint32_t* w, const T* base, int group, int rows, bool full, int c, int width)
     {
-        const uint32_t bytes = (uint32_t)width * sizeof(T), at = (uint32_t)min(c, max(width - 2, 0)) * sizeof(T);
-        auto one = [&](int k, const char* p) SAR_INLINE {
-            if constexpr (sizeof(T) == 4) {
-                struct __attribute__((packed, aligned(4))) V { uint32_t x, y; };
-                if (width >= 2) {
-                    const V v = *reinterpret_cast<const V*>(p);
+        const uint32_t bytes = (uint32_t)width * sizeof(T);
+        const char* p = reinterpret_cast<const char*>(base);
+        if (full && width >= 2) {
+            const uint32_t at = (uint32_t)min(c, width - 2) * sizeof(T) + (uint32_t)group * 8 * bytes;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if constexpr (sizeof(T) == 4) {
+                    struct __attribute__((packed, aligned(4))) V { uint32_t x, y; };
+                    const V v = *reinterpret_cast<const V*>(p + (size_t)k * bytes + at);
                     w[2 * k] = v.x, w[2 * k + 1] = v.y;
                 } else {
-                    w[2 * k] = w[2 * k + 1] = *reinterpret_cast<const uint32_t*>(p);
+                    struct __attribute__((packed, aligned(2))) V { uint32_t x; };
+                    w[k] = reinterpret_cast<const V*>(p + (size_t)k * bytes + at)->x;
                 }
-            } else {
-                struct __attribute__((packed, aligned(2))) V { uint32_t x; };
-                w[k] = width >= 2 ? reinterpret_cast<const V*>(p)->x : *reinterpret_cast<const uint16_t*>(p) * 0x10001u;
             }
-        };
-        const char* p = reinterpret_cast<const char*>(base);
-        if (full) {
-            const uint32_t off = at + (uint32_t)group * 8 * bytes;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) one(k, p + (size_t)k * bytes + off);
         } else {
+            // value by value (a type's or a workgroup's last rows; rows of one value); addresses worked out here, not kept through the loop
+            asm volatile("" : "+v"(c), "+v"(group));
+            const uint32_t first = (uint32_t)min(c, max(width - 2, 0)) * sizeof(T), second = min(first + (uint32_t)sizeof(T), bytes - (uint32_t)sizeof(T));
 #pragma unroll
-            for (int k = 0; k < 8; ++k) one(k, p + (at + (uint32_t)min(8 * group + k, rows - 1) * bytes));
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t row = (uint32_t)min(8 * group + k, rows - 1) * bytes;
+                if constexpr (sizeof(T) == 4) {
+                    w[2 * k] = *reinterpret_cast<const uint32_t*>(p + (row + first));
+                    w[2 * k + 1] = *reinterpret_cast<const uint32_t*>(p + (row + second));
+                } else {
+                    const uint32_t lo = *reinterpret_cast<const uint16_t*>(p + (row + first)), hi = *reinterpret_cast<const uint16_t*>(p + (row + second));
+                    w[k] = lo | hi << 16;
+                }
+            }
         }
     }
     // ... and into out[piece * stride], out[piece * stride + 32], the two columns' fragments
@@ -139,6 +146,7 @@ struct PackedUnit {
                 w[8 + k] = (e + (size_t)k * steps)[eoff];
             }
         } else {
+            asm volatile("" : "+v"(group));
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const uint32_t r = (uint32_t)min(8 * group + k, rows - 1);
@@ -276,53 +284,61 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
                 if (more) fetch(r0 + 16 * S, end);
                 const uint4* xb = lds + buffer * kSize + wm * MT * 32 + (lane & 31);
                 const uint4* zb = lds + buffer * kSize + kXSize + wn * NT * 32 + (lane & 31);
+                // one tile's products run while the sums of the one before are added; no more than these two are kept at once
+                auto add = [&](int i, const float16_t& sum) SAR_INLINE {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[i % MT][i / MT][r] = fmaf(sum[r], sign, acc[i % MT][i / MT][r]);
+                    // (here, not where the compiler would have them: behind the next chunk's way to LDS, with all tiles' sums kept until then)
+                    asm volatile("" : "+v"(acc[i % MT][i / MT]));
+                };
+                float16_t last;
                 if constexpr (PZ == 1) {
-                    uint4 x[S][MT];
+                    uint4 x[S][MT], z[S];
 #pragma unroll
                     for (int s = 0; s < S; ++s)
 #pragma unroll
                         for (int m = 0; m < MT; ++m) x[s][m] = xb[(2 * s + h) * TK + m * 32];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        uint4 z[S];
+                    for (int i = 0; i < MT * NT; ++i) {
+                        if (i % MT == 0) {
 #pragma unroll
-                        for (int s = 0; s < S; ++s) z[s] = zb[(2 * s + h) * TF + n * 32];
-#pragma unroll
-                        for (int m = 0; m < MT; ++m) {
-                            float16_t sum = {};
-#pragma unroll
-                            for (int s = 0; s < S; ++s)
-                                sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x[s][m]),
-                                                                              __builtin_bit_cast(bf16x8_t, z[s]), sum, 0, 0, 0);
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) acc[m][n][r] = fmaf(sum[r], sign, acc[m][n][r]);
+                            for (int s = 0; s < S; ++s) z[s] = zb[(2 * s + h) * TF + i / MT * 32];
                         }
+                        float16_t sum = {};
+#pragma unroll
+                        for (int s = 0; s < S; ++s)
+                            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x[s][i % MT]),
+                                                                          __builtin_bit_cast(bf16x8_t, z[s]), sum, 0, 0, 0);
+                        if (i > 0) add(i - 1, last);
+                        last = sum;
+                        __builtin_amdgcn_sched_barrier(0);
                     }
+                    add(MT * NT - 1, last);
                 } else {
 #pragma unroll
                     for (int s = 0; s < S; ++s) {
-                        uint4 x[MT][PX];
+                        uint4 x[MT][PX], z[PZ];
 #pragma unroll
                         for (int m = 0; m < MT; ++m)
 #pragma unroll
                             for (int p = 0; p < PX; ++p) x[m][p] = xb[p * kGroups * TK + (2 * s + h) * TK + m * 32];
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            uint4 z[PZ];
+                        for (int i = 0; i < MT * NT; ++i) {
+                            if (i % MT == 0) {
 #pragma unroll
-                            for (int p = 0; p < PZ; ++p) z[p] = zb[p * kGroups * TF + (2 * s + h) * TF + n * 32];
-#pragma unroll
-                            for (int m = 0; m < MT; ++m) {
-                                float16_t sum = {};
-#pragma unroll
-                                for (int k = 0; k < 6; ++k)
-                                    if (kTerm[k][0] < PX)
-                                        sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x[m][kTerm[k][0] < PX ? kTerm[k][0] : 0]),
-                                                                                      __builtin_bit_cast(bf16x8_t, z[kTerm[k][1]]), sum, 0, 0, 0);
-#pragma unroll
-                                for (int r = 0; r < 16; ++r) acc[m][n][r] = fmaf(sum[r], sign, acc[m][n][r]);
+                                for (int p = 0; p < PZ; ++p) z[p] = zb[p * kGroups * TF + (2 * s + h) * TF + i / MT * 32];
                             }
+                            float16_t sum = {};
+#pragma unroll
+                            for (int k = 0; k < 6; ++k)
+                                if (kTerm[k][0] < PX)
+                                    sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x[i % MT][kTerm[k][0] < PX ? kTerm[k][0] : 0]),
+                                                                                  __builtin_bit_cast(bf16x8_t, z[kTerm[k][1]]), sum, 0, 0, 0);
+                            if (i > 0) add(i - 1, last);
+                            last = sum;
+                            __builtin_amdgcn_sched_barrier(0);
                         }
+                        add(MT * NT - 1, last);
                     }
                 }
                 sign = -sign;
