@@ -26,11 +26,11 @@ template <typename T>
 struct Mode;
 template <>
 struct Mode<float> {
-    static constexpr int kPieces = 3, kSteps = 2;      // pieces of a weight; products of 16 a chunk
+    static constexpr int kPieces = 3, kSteps = 2, kStage = 1;      // pieces of a weight; products of 16 a chunk; of those, how many a stage
 };
 template <>
 struct Mode<bf16_t> {
-    static constexpr int kPieces = 2, kSteps = 4;
+    static constexpr int kPieces = 2, kSteps = 4, kStage = 2;
 };
 // Contraction values of a chunk: 128 bytes of a row.  Lanes 0..31 (half 0) hold the first 64 bytes of their rows, lanes 32..63 the others; in step s a
 // lane contributes the eight values from 8 s on.
@@ -141,8 +141,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
 {
     constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps, CH = kChunk<T>, N = Cols<T>::N;
     constexpr int kRaw = 64 / 16;                        // 16-byte pieces of a row that a lane holds of a chunk
-    constexpr int kFrags = S * P * NT;                   // KiB of B a chunk
-    extern __shared__ __attribute__((aligned(16))) uint4 lds[];      // [2][kFrags][64]
+    constexpr int SB = Mode<T>::kStage, kFrags = SB * P * NT;        // KiB of B a stage
+    extern __shared__ __attribute__((aligned(16))) uint4 lds[];      // [2][kFrags][64] of B, [WAVES][32][8] of rows
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
 
     // which rows: blocks of WAVES * 32 of a type, type after type
@@ -178,50 +178,64 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
     end = __builtin_amdgcn_readfirstlane((int)end);
 
     const int64_t r0 = first + wave * 32;
-    const T* row = static_cast<const T*>(a.A) + min(r0 + (lane & 31), end - 1) * a.C;
-    const uint4* B = a.B + ((int64_t)(t * a.blocks + blockIdx.y) * a.chunks) * (kFrags * 64);
+    const uint4* B = a.B + ((int64_t)(t * a.blocks + blockIdx.y) * a.chunks) * (S * P * NT * 64);
     const bool works = r0 < end;
 
-    auto fetch_b = [&](int chunk, int buffer) SAR_INLINE {
+    auto fetch_b = [&](int stage, int buffer) SAR_INLINE {
         for (int f = wave; f < kFrags; f += WAVES)
-            __builtin_amdgcn_global_load_lds((GlobalSrc*)(B + ((int64_t)chunk * kFrags + f) * 64 + lane),
+            __builtin_amdgcn_global_load_lds((GlobalSrc*)(B + ((int64_t)stage * kFrags + f) * 64 + lane),
                                              (LdsPtr*)(lds + (buffer * kFrags + f) * 64), 16, 0, 0);
     };
-    auto fetch_a = [&](int chunk, uint4 (&x)[kRaw]) SAR_INLINE {
+    // Rows come by whole lines: eight lanes a row, eight rows a load.  (By the lanes that multiply them, 16 bytes of 64 rows a load, every
+    // line was fetched anew for each of its pieces: 256 rows' lines are what a first-level cache holds.)  They are handed to those lanes through
+    // 4 KiB of LDS that are the wavefront's own, pieces turned by the row so that neither side meets a bank twice.
+    const T* tile = static_cast<const T*>(a.A) + r0 * a.C;
+    const uint32_t most = works ? (uint32_t)min(end - 1 - r0, (int64_t)31) : 0u;
+    uint32_t from[kRaw];
 #pragma unroll
-        for (int p = 0; p < kRaw; ++p) x[p] = Cols<T>::load(row, chunk * CH + h * (CH / 2) + p * N, a.C);
+    for (int p = 0; p < kRaw; ++p) from[p] = min((uint32_t)(8 * p + (lane >> 3)), most) * (uint32_t)a.C;
+    auto fetch_a = [&](int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
+#pragma unroll
+        for (int p = 0; p < kRaw; ++p) v[p] = Cols<T>::load(tile + from[p], chunk * CH + (lane & 7) * N, a.C);
     };
-    auto settle_a = [&](int chunk, uint4 (&x)[kRaw]) SAR_INLINE {
-        if ((chunk + 1) * CH <= a.C) return;
+    uint4* const mine = lds + 2 * kFrags * 64 + wave * 256;
+    auto hand_over = [&](int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
+        const int c = chunk * CH + (lane & 7) * N;
+        if ((chunk + 1) * CH > a.C && c + N > a.C) {
 #pragma unroll
-        for (int p = 0; p < kRaw; ++p) {
-            const int c = chunk * CH + h * (CH / 2) + p * N;
-            if (c + N <= a.C) continue;
-            if (c >= a.C) x[p] = make_uint4(0u, 0u, 0u, 0u);
-            else if (a.C >= N) x[p] = front_of_piece<T>(x[p], a.C - c);
+            for (int p = 0; p < kRaw; ++p) {
+                if (c >= a.C) v[p] = make_uint4(0u, 0u, 0u, 0u);
+                else if (a.C >= N) v[p] = front_of_piece<T>(v[p], a.C - c);
+            }
         }
+#pragma unroll
+        for (int p = 0; p < kRaw; ++p) mine[(8 * p + (lane >> 3)) * 8 + ((lane & 7) ^ (lane >> 3))] = v[p];
+    };
+    auto take = [&](uint4 (&v)[kRaw]) SAR_INLINE {
+#pragma unroll
+        for (int p = 0; p < kRaw; ++p) v[p] = mine[(lane & 31) * 8 + ((h * kRaw + p) ^ (lane & 7))];
     };
 
     float16_t acc[NT];
 #pragma unroll
     for (int i = 0; i < NT; ++i) acc[i] = float16_t{};
-    uint4 x[kRaw], next[kRaw];
+    uint4 raw[kRaw];
     fetch_b(0, 0);
-    fetch_a(0, x);
+    if (works) {
+        fetch_a(0, raw);
+        hand_over(0, raw);
+    }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     float sign = 1.f;
+    const int stages = a.chunks * (S / SB);
     for (int chunk = 0; chunk < a.chunks; ++chunk) {
-        const int buffer = chunk & 1;
-        if (chunk + 1 < a.chunks) {
-            fetch_b(chunk + 1, buffer ^ 1);
-            fetch_a(chunk + 1, next);
-        }
+        const bool more = chunk + 1 < a.chunks;
+        uint4 p[S][P == 3 ? 3 : 1];
         if (works) {
-            settle_a(chunk, x);
-            const uint4* b = lds + buffer * kFrags * 64 + lane;
+            uint4 x[kRaw];
+            take(x);
             if constexpr (P == 3) {
-                uint4 p[S][3];
 #pragma unroll
                 for (int s = 0; s < S; ++s) {
                     const float v[8] = {__uint_as_float(x[2 * s].x), __uint_as_float(x[2 * s].y), __uint_as_float(x[2 * s].z),
@@ -229,39 +243,70 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
                                         __uint_as_float(x[2 * s + 1].z), __uint_as_float(x[2 * s + 1].w)};
                     split8(v, p[s]);
                 }
-#pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    float16_t sum = {};
-#pragma unroll
-                    for (int s = 0; s < S; ++s) {
-                        uint4 w[3];
-#pragma unroll
-                        for (int k = 0; k < 3; ++k) w[k] = b[((s * P + k) * NT + i) * 64];
-#pragma unroll
-                        for (int k = 0; k < 6; ++k)
-                            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[s][kTerm[k][0]]),
-                                                                          __builtin_bit_cast(bf16x8_t, w[kTerm[k][1]]), sum, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[i][r] = fmaf(sum[r], sign, acc[i][r]);
-                }
-                sign = -sign;
             } else {
 #pragma unroll
-                for (int s = 0; s < S; ++s)
-#pragma unroll
-                    for (int i = 0; i < NT; ++i)
-#pragma unroll
-                        for (int k = P - 1; k >= 0; --k)
-                            acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x[s]),
-                                                                             __builtin_bit_cast(bf16x8_t, b[((s * P + k) * NT + i) * 64]),
-                                                                             acc[i], 0, 0, 0);
+                for (int s = 0; s < S; ++s) p[s][0] = x[s];
             }
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
 #pragma unroll
-        for (int p = 0; p < kRaw; ++p) x[p] = next[p];
+        for (int part = 0; part < S / SB; ++part) {
+            const int stage = chunk * (S / SB) + part, buffer = stage & 1;
+            const uint4* b = lds + buffer * kFrags * 64 + lane;
+            if (stage + 1 < stages) fetch_b(stage + 1, buffer ^ 1);
+            if (works) {
+                if (part == 0 && more) fetch_a(chunk + 1, raw);
+                if constexpr (P == 3) {
+                    // a tile's products run while the sums of the tile before are added and the pieces of the next one are read
+                    uint4 w[2][3];
+                    float16_t sum, last;
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) w[0][k] = b[k * NT * 64];
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        sum = float16_t{};
+                        if (i + 1 < NT) {
+#pragma unroll
+                            for (int k = 0; k < 3; ++k) w[(i + 1) & 1][k] = b[(k * NT + i + 1) * 64];
+                        }
+#pragma unroll
+                        for (int k = 0; k < 6; ++k)
+                            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[part][kTerm[k][0]]),
+                                                                          __builtin_bit_cast(bf16x8_t, w[i & 1][kTerm[k][1]]), sum, 0, 0, 0);
+                        if (i > 0) {
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) acc[i - 1][r] = fmaf(last[r], sign, acc[i - 1][r]);
+                            asm volatile("" : "+v"(acc[i - 1]));
+                        }
+                        last = sum;
+#pragma unroll
+                        for (int k = 0; k < 6; ++k) {
+                            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                        // a product
+                            if (k % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);       // a read
+                            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);                        // additions
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) acc[NT - 1][r] = fmaf(last[r], sign, acc[NT - 1][r]);
+                    asm volatile("" : "+v"(acc[NT - 1]));
+                } else {
+#pragma unroll
+                    for (int s = 0; s < SB; ++s)
+#pragma unroll
+                        for (int i = 0; i < NT; ++i)
+#pragma unroll
+                            for (int k = P - 1; k >= 0; --k)
+                                acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[part * SB + s][0]),
+                                                                                 __builtin_bit_cast(bf16x8_t, b[((s * P + k) * NT + i) * 64]),
+                                                                                 acc[i], 0, 0, 0);
+                }
+                if (part == S / SB - 1 && more) hand_over(chunk + 1, raw);
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+        }
+        sign = -sign;
     }
     if (!works) return;
 
@@ -269,7 +314,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < NT; ++i) odd |= not_finite(acc[i]);
-    if (__any(odd)) exact_tiles<T, NT, TRANS>(a, t, row, n0, acc);
+    if (__any(odd)) exact_tiles<T, NT, TRANS>(a, t, static_cast<const T*>(a.A) + min(r0 + (lane & 31), end - 1) * a.C, n0, acc);
 
     // lane holds columns of its place; register r holds row 8*(r/4) + 4*h + r%4
     constexpr int IL = NT < 4 ? NT : 4;
@@ -307,13 +352,13 @@ int tiles_of(int64_t n, int N)
 {
     // with few rows, more workgroups of fewer columns: 256 rows a workgroup leave most of the chip idle
     if (N <= 64 || n * N <= (int64_t)256 * 256 * 128) return 2;
-    return 8;
+    return (N + 127) / 128 % 2 ? 4 : 8;
 }
 
 template <typename T, int NT, bool TRANS>
 int run_rows(const RowsArgs& a, LayArgs l, hipStream_t st)
 {
-    constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps, kWaves = 8;
+    constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps, kWaves = 4;
     const int64_t units = (int64_t)l.T * l.blocks * l.chunks * S * NT * 64;
     const int64_t lay = (units + 255) / 256, groups = a.types.n / (kWaves * 32) + a.types.T;
     if (lay > 0x7fffffff || groups > 0x7fffffff || l.blocks > 65535)
@@ -321,7 +366,7 @@ int run_rows(const RowsArgs& a, LayArgs l, hipStream_t st)
                     (long long)a.types.n, a.K, a.F, l.T);
     k_typed_lay<T, NT, TRANS><<<(unsigned)lay, 256, 0, st>>>(l);
     SAR_LAUNCH_CHECK();
-    constexpr size_t shared = (size_t)2 * S * P * NT * 1024;
+    constexpr size_t shared = (size_t)(2 * Mode<T>::kStage * P * NT + 4 * kWaves) * 1024;
     auto* fn = k_typed_rows<T, NT, kWaves, TRANS>;
     if (shared > 65536) SAR_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)shared));
     fn<<<dim3((unsigned)groups, l.blocks), kWaves * 64, shared, st>>>(a);
@@ -344,7 +389,7 @@ int rows_product(const void* A, const float* W, const Types& types, void* out, i
     const int chunks = (C + kChunk<T> - 1) / kChunk<T>, blocks = (N + 32 * NT - 1) / (32 * NT);
     const RowsArgs a{A, static_cast<const uint4*>(work), W, out, types, C, N, chunks, blocks, K, F};
     const LayArgs l{W, static_cast<uint4*>(work), types.T, K, F, C, N, chunks, blocks};
-    return NT == 2 ? run_rows<T, 2, TRANS>(a, l, st) : run_rows<T, 8, TRANS>(a, l, st);
+    return NT == 2 ? run_rows<T, 2, TRANS>(a, l, st) : NT == 4 ? run_rows<T, 4, TRANS>(a, l, st) : run_rows<T, 8, TRANS>(a, l, st);
 }
 
 size_t round256(size_t b) { return (b + 255) / 256 * 256; }
