@@ -22,7 +22,7 @@ namespace sar {
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
 
 // What rows an operand has: pieces of a value, values a thread takes of a row, and their bytes.
 struct F32Rows {
@@ -60,7 +60,7 @@ struct Unit {
     using T = typename R::T;
     static constexpr int kRegs = 8 * (int)sizeof(T) * 2 / 4;
     // c: column of the tensor (its rows are `width` values wide)
-    static __device__ inline void load(uint32_t* w, const T* base, int group, int rows, bool full, int c, int width)
+    static __device__ SAR_INLINE inline void load(uint32_t* w, const T* base, int group, int rows, bool full, int c, int width)
     {
         const uint32_t bytes = (uint32_t)width * sizeof(T);
         const char* p = reinterpret_cast<const char*>(base);
@@ -70,11 +70,11 @@ struct Unit {
             for (int k = 0; k < 8; ++k) {
                 if constexpr (sizeof(T) == 4) {
                     struct __attribute__((packed, aligned(4))) V { uint32_t x, y; };
-                    const V v = *reinterpret_cast<const V*>(p + (size_t)k * bytes + at);
+                    const V v = *reinterpret_cast<const V*>(p + (at + (uint32_t)k * bytes));
                     w[2 * k] = v.x, w[2 * k + 1] = v.y;
                 } else {
                     struct __attribute__((packed, aligned(2))) V { uint32_t x; };
-                    w[k] = reinterpret_cast<const V*>(p + (size_t)k * bytes + at)->x;
+                    w[k] = reinterpret_cast<const V*>(p + (at + (uint32_t)k * bytes))->x;
                 }
             }
         } else {
@@ -95,7 +95,7 @@ struct Unit {
         }
     }
     // ... and into out[piece * stride], out[piece * stride + 32], the two columns' fragments
-    static __device__ inline void put(uint32_t* w, uint4* out, int stride, int group, int rows, bool full, int c, int width, bool negate)
+    static __device__ SAR_INLINE inline void put(uint32_t* w, uint4* out, int stride, int group, int rows, bool full, int c, int width, bool negate)
     {
         if (!full) {
 #pragma unroll
@@ -135,15 +135,15 @@ struct Unit {
 };
 struct PackedUnit {
     static constexpr int kRegs = 16;           // eight rows' numbers, eight steps
-    static __device__ inline void load(uint32_t* w, const int8_t* q, const uint8_t* e, int group, int rows, bool full, int c, int K)
+    static __device__ SAR_INLINE inline void load(uint32_t* w, const int8_t* q, const uint8_t* e, int group, int rows, bool full, int c, int K)
     {
         const uint32_t stride = packed_stride(K), steps = packed_steps(K), at = (uint32_t)min(c, (int)stride - 4);
         if (full) {
             const uint32_t off = at + (uint32_t)group * 8 * stride, eoff = at / kPackBlock + (uint32_t)group * 8 * steps;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                w[k] = *reinterpret_cast<const uint32_t*>(q + (size_t)k * stride + off);
-                w[8 + k] = (e + (size_t)k * steps)[eoff];
+                w[k] = *reinterpret_cast<const uint32_t*>(q + (off + (uint32_t)k * stride));
+                w[8 + k] = e[eoff + (uint32_t)k * steps];
             }
         } else {
             asm volatile("" : "+v"(group));
@@ -155,7 +155,7 @@ struct PackedUnit {
             }
         }
     }
-    static __device__ inline void put(uint32_t* w, uint4* out, int group, int rows, bool full, bool negate)
+    static __device__ SAR_INLINE inline void put(uint32_t* w, uint4* out, int group, int rows, bool full, bool negate)
     {
         if (!full) {
 #pragma unroll
@@ -204,54 +204,71 @@ __device__ inline float z_value(const DwArgs& a, int64_t row, int c)
 }
 
 // WM x WN wavefronts of MT x NT tiles of 32 x 32; S products of 16 rows a chunk.
-template <typename XR, typename ZR, int MT, int NT, int WM, int WN, int S>
+template <typename XR, typename ZR, int MT, int NT, int WM, int WN, int S, int AHEAD>
 __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
 {
     constexpr int TK = WM * MT * 32, TF = WN * NT * 32, PX = XR::kPieces, PZ = ZR::kPieces;
-    static_assert(WM * WN * 64 == kThreads, "eight wavefronts");
+    static_assert(WM * WN * 64 == kThreads, "four wavefronts");
     constexpr int kGroups = 2 * S;                                  // eight rows each
     constexpr int kXUnits = kGroups * TK / XR::kCols, kZUnits = kGroups * TF / ZR::kCols;
-    constexpr int kSlots = (kXUnits + kZUnits + kThreads - 1) / kThreads;
+    constexpr int kXSlots = (kXUnits + kThreads - 1) / kThreads, kZSlots = (kZUnits + kThreads - 1) / kThreads;
     constexpr int kXSize = PX * kGroups * TK, kSize = kXSize + PZ * kGroups * TF;      // fragments a buffer
     extern __shared__ __attribute__((aligned(16))) uint4 lds[];                         // [2][kSize]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int wm = wave % WM, wn = wave / WM;
     const int k0 = blockIdx.y * TK, f0 = blockIdx.z * TF;
 
-    // the units of a chunk, X's before dZ's, columns fastest: thread by thread, so that a wavefront's are all of one operand
-    uint32_t raw[kSlots][kXRegs<XR> > Unit<ZR>::kRegs ? kXRegs<XR> : Unit<ZR>::kRegs];
-    auto fetch = [&](int64_t r0, int64_t end) SAR_INLINE {
+    // A chunk's units, columns fastest, wavefront by wavefront; X's are dealt from the last wavefront on and dZ's from the first, so that
+    // few units are spread over all of them.
+    struct Chunk {
+        uint32_t x[kXSlots][kXRegs<XR>], z[kZSlots][Unit<ZR>::kRegs];
+    };
+    Chunk raw[AHEAD];
+    // (a thread's places are worked out anew for every chunk: carried through the loop, their addresses are dozens of registers)
+    auto anew = [](int v) SAR_INLINE {
+        asm volatile("" : "+v"(v));
+        return v;
+    };
+    auto fetch = [&](Chunk& raw, int64_t r0, int64_t end) SAR_INLINE {
         const int rows = (int)min(end - r0, (int64_t)(16 * S));
         const bool full = rows == 16 * S;
+        const int lane = anew(threadIdx.x & 63);
 #pragma unroll
-        for (int u = 0; u < kSlots; ++u) {
-            const int first = wave * 64 + u * kThreads;
-            if (first < kXUnits) {
-                const int id = first + lane, g = id / (TK / XR::kCols), c = k0 + id % (TK / XR::kCols) * XR::kCols;
-                if constexpr (XR::kCols == 4)
-                    PackedUnit::load(raw[u], a.Xq + r0 * packed_stride(a.K), a.Xe + r0 * packed_steps(a.K), g, rows, full, c, a.K);
-                else
-                    Unit<XR>::load(raw[u], static_cast<const typename XR::T*>(a.X) + r0 * a.K, g, rows, full, c, a.K);
-            } else if (first < kXUnits + kZUnits) {
-                const int id = first + lane - kXUnits, g = id / (TF / 2), c = f0 + id % (TF / 2) * 2;
-                Unit<ZR>::load(raw[u], static_cast<const typename ZR::T*>(a.dZ) + r0 * a.F, g, rows, full, c, a.F);
-            }
+        for (int u = 0; u < kXSlots; ++u) {
+            const int first = (kWaves - 1 - wave) * 64 + u * kThreads, id = first + lane;
+            if (first >= kXUnits || (kXUnits % 64 && id >= kXUnits)) continue;
+            const int g = id / (TK / XR::kCols), c = k0 + id % (TK / XR::kCols) * XR::kCols;
+            if constexpr (XR::kCols == 4)
+                PackedUnit::load(raw.x[u], a.Xq + r0 * packed_stride(a.K), a.Xe + r0 * packed_steps(a.K), g, rows, full, c, a.K);
+            else
+                Unit<XR>::load(raw.x[u], static_cast<const typename XR::T*>(a.X) + r0 * a.K, g, rows, full, c, a.K);
+        }
+#pragma unroll
+        for (int u = 0; u < kZSlots; ++u) {
+            const int first = wave * 64 + u * kThreads, id = first + lane;
+            if (first >= kZUnits || (kZUnits % 64 && id >= kZUnits)) continue;
+            const int g = id / (TF / 2), c = f0 + id % (TF / 2) * 2;
+            Unit<ZR>::load(raw.z[u], static_cast<const typename ZR::T*>(a.dZ) + r0 * a.F, g, rows, full, c, a.F);
         }
     };
-    auto put = [&](int64_t r0, int64_t end, uint4* buf, bool negate) SAR_INLINE {
+    auto put = [&](Chunk& raw, int64_t r0, int64_t end, uint4* buf, bool negate) SAR_INLINE {
         const int rows = (int)min(end - r0, (int64_t)(16 * S));
         const bool full = rows == 16 * S;
+        const int lane = anew(threadIdx.x & 63);
 #pragma unroll
-        for (int u = 0; u < kSlots; ++u) {
-            const int first = wave * 64 + u * kThreads;
-            if (first < kXUnits) {
-                const int id = first + lane, g = id / (TK / XR::kCols), c = id % (TK / XR::kCols) * XR::kCols;
-                if constexpr (XR::kCols == 4) PackedUnit::put(raw[u], buf + g * TK + place_of(c), g, rows, full, negate);
-                else Unit<XR>::put(raw[u], buf + g * TK + place_of(c), kGroups * TK, g, rows, full, k0 + c, a.K, negate);
-            } else if (first < kXUnits + kZUnits) {
-                const int id = first + lane - kXUnits, g = id / (TF / 2), c = id % (TF / 2) * 2;
-                Unit<ZR>::put(raw[u], buf + kXSize + g * TF + place_of(c), kGroups * TF, g, rows, full, f0 + c, a.F, false);
-            }
+        for (int u = 0; u < kXSlots; ++u) {
+            const int first = (kWaves - 1 - wave) * 64 + u * kThreads, id = first + lane;
+            if (first >= kXUnits || (kXUnits % 64 && id >= kXUnits)) continue;
+            const int g = id / (TK / XR::kCols), c = id % (TK / XR::kCols) * XR::kCols;
+            if constexpr (XR::kCols == 4) PackedUnit::put(raw.x[u], buf + g * TK + place_of(c), g, rows, full, negate);
+            else Unit<XR>::put(raw.x[u], buf + g * TK + place_of(c), kGroups * TK, g, rows, full, k0 + c, a.K, negate);
+        }
+#pragma unroll
+        for (int u = 0; u < kZSlots; ++u) {
+            const int first = wave * 64 + u * kThreads, id = first + lane;
+            if (first >= kZUnits || (kZUnits % 64 && id >= kZUnits)) continue;
+            const int g = id / (TF / 2), c = id % (TF / 2) * 2;
+            Unit<ZR>::put(raw.z[u], buf + kXSize + g * TF + place_of(c), kGroups * TF, g, rows, full, f0 + c, a.F, false);
         }
     };
 
@@ -274,47 +291,43 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) acc[m][n] = float16_t{};
-            fetch(first, end);
-            put(first, end, lds, false);
-            __syncthreads();
-            int buffer = 0;
-            float sign = 1.f;
-            for (int64_t r0 = first; r0 < end; r0 += 16 * S) {
-                const bool more = r0 + 16 * S < end;
-                if (more) fetch(r0 + 16 * S, end);
-                const uint4* xb = lds + buffer * kSize + wm * MT * 32 + (lane & 31);
-                const uint4* zb = lds + buffer * kSize + kXSize + wn * NT * 32 + (lane & 31);
-                // one tile's products run while the sums of the one before are added; no more than these two are kept at once
-                auto add = [&](int i, const float16_t& sum) SAR_INLINE {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[i % MT][i / MT][r] = fmaf(sum[r], sign, acc[i % MT][i / MT][r]);
-                    // (here, not where the compiler would have them: behind the next chunk's way to LDS, with all tiles' sums kept until then)
-                    asm volatile("" : "+v"(acc[i % MT][i / MT]));
-                };
-                float16_t last;
+            // Which sign X has in chunk i, so that what the matrix unit cuts leans to neither side.  Bf16 products, which are added to the sums
+            // there: the other sign every four chunks and in every other workgroup, with the sums turned round where it changes.
+            auto minus = [&](int i) SAR_INLINE { return PZ == 1 ? (((i >> 2) + (int)blockIdx.x) & 1) != 0 : (i & 1) != 0; };
+            auto step = [&](int i, int64_t r0, Chunk& later, Chunk& next) SAR_INLINE {
+                constexpr int kRows = 16 * S;
+                if (r0 + AHEAD * kRows < end) fetch(later, r0 + AHEAD * kRows, end);
+                const uint4* xb = lds + (i & 1) * kSize + wm * MT * 32 + (lane & 31);
+                const uint4* zb = lds + (i & 1) * kSize + kXSize + wn * NT * 32 + (lane & 31);
                 if constexpr (PZ == 1) {
-                    uint4 x[S][MT], z[S];
+                    if (i > 0 && minus(i) != minus(i - 1)) {
 #pragma unroll
-                    for (int s = 0; s < S; ++s)
-#pragma unroll
-                        for (int m = 0; m < MT; ++m) x[s][m] = xb[(2 * s + h) * TK + m * 32];
-#pragma unroll
-                    for (int i = 0; i < MT * NT; ++i) {
-                        if (i % MT == 0) {
-#pragma unroll
-                            for (int s = 0; s < S; ++s) z[s] = zb[(2 * s + h) * TF + i / MT * 32];
-                        }
-                        float16_t sum = {};
-#pragma unroll
-                        for (int s = 0; s < S; ++s)
-                            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x[s][i % MT]),
-                                                                          __builtin_bit_cast(bf16x8_t, z[s]), sum, 0, 0, 0);
-                        if (i > 0) add(i - 1, last);
-                        last = sum;
-                        __builtin_amdgcn_sched_barrier(0);
+                        for (int n = 0; n < MT * NT; ++n) acc[n % MT][n / MT] = -acc[n % MT][n / MT];
                     }
-                    add(MT * NT - 1, last);
+#pragma unroll
+                    for (int s = 0; s < S; ++s) {
+                        uint4 x[MT];
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) x[m] = xb[(2 * s + h) * TK + m * 32];
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const uint4 z = zb[(2 * s + h) * TF + n * 32];
+#pragma unroll
+                            for (int m = 0; m < MT; ++m)
+                                acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, x[m]),
+                                                                                    __builtin_bit_cast(bf16x8_t, z), acc[m][n], 0, 0, 0);
+                        }
+                    }
                 } else {
+                    const float sign = minus(i) ? -1.f : 1.f;
+                    // one tile's products run while the sums of the one before are added; no more than these two are kept at once
+                    auto add = [&](int i, const float16_t& sum) SAR_INLINE {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[i % MT][i / MT][r] = fmaf(sum[r], sign, acc[i % MT][i / MT][r]);
+                        // (here, not where the compiler would have them: behind the next chunk's way to LDS, with all tiles' sums kept until then)
+                        asm volatile("" : "+v"(acc[i % MT][i / MT]));
+                    };
+                    float16_t last;
 #pragma unroll
                     for (int s = 0; s < S; ++s) {
                         uint4 x[MT][PX], z[PZ];
@@ -341,10 +354,24 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
                         add(MT * NT - 1, last);
                     }
                 }
-                sign = -sign;
-                buffer ^= 1;
-                if (more) put(r0 + 16 * S, end, lds + buffer * kSize, sign < 0.f);
+                if (r0 + kRows < end) put(next, r0 + kRows, end, lds + ((i & 1) ^ 1) * kSize, minus(i + 1));
                 __syncthreads();
+            };
+            fetch(raw[0], first, end);
+            if (AHEAD == 2 && first + 16 * S < end) fetch(raw[1 % AHEAD], first + 16 * S, end);
+            put(raw[0], first, end, lds, minus(0));
+            __syncthreads();
+            int chunks = 0;
+            for (int64_t r0 = first; r0 < end;) {
+                step(chunks, r0, raw[0], raw[1 % AHEAD]);
+                ++chunks, r0 += 16 * S;
+                if (AHEAD == 1 || r0 >= end) continue;
+                step(chunks, r0, raw[1 % AHEAD], raw[0]);
+                ++chunks, r0 += 16 * S;
+            }
+            if (PZ == 1 && minus(chunks - 1)) {
+#pragma unroll
+                for (int n = 0; n < MT * NT; ++n) acc[n % MT][n / MT] = -acc[n % MT][n / MT];
             }
 
             float* out = a.partial + ((int64_t)blockIdx.x + t) * a.K * a.F;
@@ -423,45 +450,50 @@ __global__ __launch_bounds__(256) void k_typed_sum(DwArgs a, int accumulate, flo
     }
 }
 
+// The tile of sums of a workgroup, its rows, and how many workgroups of the kernel a compute unit holds.
 struct Shape {
     int tk, tf, tiles;
     int64_t share, groups;
 };
 Shape shape_of(int64_t n, int K, int F)
 {
-    auto tile = [](int w) { return (w + 127) / 128 % 2 == 0 || w > 512 ? 256 : 128; };
+    // 128 x 256 sums a workgroup, 256 x 128 where only K is that wide, 128 x 128 where neither is; 64 columns or rows where that is all
     Shape s;
-    s.tk = tile(K), s.tf = tile(F);
+    s.tk = s.tf = 128;
+    if (F <= 64) s.tf = 64;
+    else if (K <= 64) s.tk = 64;
+    else if ((F + 127) / 128 % 2 == 0) s.tf = 256;
+    else if ((K + 127) / 128 % 2 == 0) s.tk = 256;
     s.tiles = ((K + s.tk - 1) / s.tk) * ((F + s.tf - 1) / s.tf);
-    // a workgroup per compute unit (its registers and LDS leave no room for a second), none with fewer than 64 rows
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((n + 63) / 64, std::max(1, 256 / s.tiles)));
-    s.share = std::max<int64_t>(64, ((n + want - 1) / want + 63) / 64 * 64);
+    const int resident = s.tk * s.tf > 128 * 128 ? 2 : s.tk * s.tf == 128 * 128 ? 3 : 4;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((n + 63) / 64, std::max(1, 256 * resident / s.tiles)));
+    s.share = std::max<int64_t>(64, ((n + want - 1) / want + 31) / 32 * 32);
     s.groups = std::max<int64_t>(1, (n + s.share - 1) / s.share);
     return s;
 }
 
-template <typename XR, typename ZR, int MT, int NT, int WM, int WN, int S>
+template <typename XR, typename ZR, int MT, int NT, int WM, int WN, int S, int AHEAD>
 int run(const DwArgs& a, const Shape& s, hipStream_t st)
 {
     constexpr int TK = WM * MT * 32, TF = WN * NT * 32;
     constexpr size_t shared = (size_t)2 * (XR::kPieces * TK + ZR::kPieces * TF) * 2 * S * sizeof(uint4);
-    auto* fn = k_typed_dw<XR, ZR, MT, NT, WM, WN, S>;
+    auto* fn = k_typed_dw<XR, ZR, MT, NT, WM, WN, S, AHEAD>;
     if (shared > 65536) SAR_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)shared));
     fn<<<dim3((unsigned)s.groups, (a.K + TK - 1) / TK, (a.F + TF - 1) / TF), kThreads, shared, st>>>(a);
     SAR_LAUNCH_CHECK();
     return SAR_OK;
 }
 
-// S2: products of 16 rows a chunk where a wavefront holds eight tiles, S1: fewer.  (A chunk under way is what a thread holds
-// in registers beside its sums.)
-template <typename XR, typename ZR, int S1, int S2>
+// S: products of 16 rows a chunk; W: chunks under way in the wide tiles, whose sums leave fewer registers.
+template <typename XR, typename ZR, int S, int W>
 int run_all(const DwArgs& a, const Shape& s, int accumulate, float* dW, hipStream_t st)
 {
     if (a.types.n > 0) {
-        if (s.tk == 256 && s.tf == 256) SAR_TRY((run<XR, ZR, 2, 4, 4, 2, S2>(a, s, st)));
-        else if (s.tk == 256) SAR_TRY((run<XR, ZR, 2, 2, 4, 2, S1>(a, s, st)));
-        else if (s.tf == 256) SAR_TRY((run<XR, ZR, 2, 2, 2, 4, S1>(a, s, st)));
-        else SAR_TRY((run<XR, ZR, 1, 2, 4, 2, S1>(a, s, st)));
+        if (s.tk == 256) SAR_TRY((run<XR, ZR, 4, 2, 2, 2, S, W>(a, s, st)));
+        else if (s.tf == 256) SAR_TRY((run<XR, ZR, 2, 4, 2, 2, S, W>(a, s, st)));
+        else if (s.tf == 64) SAR_TRY((run<XR, ZR, 2, 1, 2, 2, S, 2>(a, s, st)));
+        else if (s.tk == 64) SAR_TRY((run<XR, ZR, 1, 2, 2, 2, S, 2>(a, s, st)));
+        else SAR_TRY((run<XR, ZR, 2, 2, 2, 2, S, 2>(a, s, st)));
     }
     const int64_t count = (int64_t)a.K * a.F, blocks = std::min<int64_t>((count + 31) / 32, 1 << 20);
     k_typed_sum<XR, ZR><<<dim3((unsigned)blocks, a.types.T), 256, 0, st>>>(a, accumulate, dW);
@@ -481,8 +513,8 @@ int typed_dw(int dtype, const TypedDw& g, hipStream_t st)
     const Shape s = shape_of(g.types.n, g.K, g.F);
     const DwArgs a{g.X, g.Xq, g.Xe, g.dZ, g.partial, g.types, g.K, g.F, s.share};
     if (dtype == SAR_F32)
-        return g.Xq ? run_all<PackedRows, F32Rows, 1, 1>(a, s, g.accumulate, g.dW, st) : run_all<F32Rows, F32Rows, 1, 1>(a, s, g.accumulate, g.dW, st);
-    return g.Xq ? run_all<PackedRows, Bf16Rows, 4, 2>(a, s, g.accumulate, g.dW, st) : run_all<Bf16Rows, Bf16Rows, 4, 2>(a, s, g.accumulate, g.dW, st);
+        return g.Xq ? run_all<PackedRows, F32Rows, 1, 2>(a, s, g.accumulate, g.dW, st) : run_all<F32Rows, F32Rows, 1, 1>(a, s, g.accumulate, g.dW, st);
+    return g.Xq ? run_all<PackedRows, Bf16Rows, 2, 2>(a, s, g.accumulate, g.dW, st) : run_all<Bf16Rows, Bf16Rows, 2, 2>(a, s, g.accumulate, g.dW, st);
 }
 
 }  // namespace sar
