@@ -52,12 +52,43 @@ struct LayArgs {
     const float* W;        // [T, K, F]
     uint4* out;
     int T, K, F, C, N, chunks, blocks;
+    Types types;
+    int4* list;            // the launch's list of row blocks: how many, then (type, first row, the row behind the last)
+    int64_t most;          // places in it
+    unsigned lay;          // workgroups that lay out weights; one for each type's rows behind them
 };
+
+// The blocks of kTileRows rows of type t, behind those of the types before it.
+constexpr int kTileRows = 128;
+__device__ inline void list_rows(const LayArgs& a, int t)
+{
+    __shared__ int64_t sums[4];
+    auto blocks_of = [&](int u) {
+        int64_t lo, hi;
+        a.types.span(u, lo, hi);
+        return (hi - lo + kTileRows - 1) / kTileRows;
+    };
+    int64_t before = 0;
+    for (int u = threadIdx.x; u < t; u += 256) before += blocks_of(u);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) before += (int64_t)__shfl_xor((long long)before, o);
+    if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = before;
+    __syncthreads();
+    before = sums[0] + sums[1] + sums[2] + sums[3];
+    int64_t lo, hi;
+    a.types.span(t, lo, hi);
+    const int64_t mine = (hi - lo + kTileRows - 1) / kTileRows;
+    // (bounds that do not ascend can ask for more blocks than there is room for: those are left out)
+    for (int64_t k = threadIdx.x; k < mine && before + k < a.most; k += 256)
+        a.list[1 + before + k] = make_int4(t, (int)(lo + k * kTileRows), (int)hi, 0);
+    if (t == a.T - 1 && threadIdx.x == 0) a.list[0] = make_int4((int)min(before + mine, a.most), 0, 0, 0);
+}
 
 template <typename T, int NT, bool TRANS>
 __global__ __launch_bounds__(256) void k_typed_lay(LayArgs a)
 {
     constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps;
+    if (blockIdx.x >= a.lay) return list_rows(a, (int)(blockIdx.x - a.lay));
     const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const int lane = unit & 63, tile = (unit >> 6) % NT;
     int64_t rest = unit / (64 * NT);
@@ -103,7 +134,7 @@ struct RowsArgs {
     const uint4* B;        // as k_typed_lay leaves it
     const float* W;        // [T, K, F]
     void* out;             // [n, N]
-    Types types;
+    const int4* list;      // row blocks, as k_typed_lay leaves them
     int C, N, chunks, blocks;
     int K, F;
 };
@@ -136,6 +167,71 @@ __device__ inline void exact_tiles(const RowsArgs& a, int t, const T* row, int n
 using LdsPtr = __attribute__((address_space(3))) void;
 using GlobalSrc = const __attribute__((address_space(1))) void;
 
+// A stage's products from its pieces of B at `b`, while the next stage's pieces go to `to`.  (A function of its own for its arguments' sake: it
+// is by them that the compiler knows the two apart.  Otherwise every first read of a stage waits for the copy that was just begun:
+// bf16 rows 256 -> 256 took 1.3 times as long.)
+template <typename T, int NT, int WAVES, int SP, typename Fetch>
+__device__ SAR_INLINE inline void stage_products(uint4* __restrict__ to, const uint4* from, const uint4* __restrict__ b, const uint4 (&p)[Mode<T>::kStage][SP],
+                                                 float sign, bool works, float16_t (&acc)[NT], Fetch&& fetch_rows)
+{
+    constexpr int P = Mode<T>::kPieces, SB = Mode<T>::kStage, kFrags = SB * P * NT;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (from) {
+#pragma unroll
+        for (int f = 0; f < (kFrags + WAVES - 1) / WAVES; ++f)
+            if (kFrags % WAVES == 0 || wave + f * WAVES < kFrags)
+                __builtin_amdgcn_global_load_lds((GlobalSrc*)(from + (wave + f * WAVES) * 64 + lane), (LdsPtr*)(to + (wave + f * WAVES) * 64), 16, 0, 0);
+    }
+    fetch_rows();
+    if (!works) return;
+                    if constexpr (P == 3) {
+                        // a tile's products run while the sums of the tile before are added and the pieces of the next one are read
+                        uint4 w[2][3];
+                        float16_t sum, last;
+#pragma unroll
+                        for (int k = 0; k < 3; ++k) w[0][k] = b[k * NT * 64];
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int i = 0; i < NT; ++i) {
+                            sum = float16_t{};
+                            if (i + 1 < NT) {
+#pragma unroll
+                                for (int k = 0; k < 3; ++k) w[(i + 1) & 1][k] = b[(k * NT + i + 1) * 64];
+                            }
+#pragma unroll
+                            for (int k = 0; k < 6; ++k)
+                                sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[0][kTerm[k][0]]),
+                                                                              __builtin_bit_cast(bf16x8_t, w[i & 1][kTerm[k][1]]), sum, 0, 0, 0);
+                            if (i > 0) {
+#pragma unroll
+                                for (int r = 0; r < 16; ++r) acc[i - 1][r] = fmaf(last[r], sign, acc[i - 1][r]);
+                                asm volatile("" : "+v"(acc[i - 1]));
+                            }
+                            last = sum;
+#pragma unroll
+                            for (int k = 0; k < 6; ++k) {
+                                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                        // a product
+                                if (k % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);       // a read
+                                __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);                        // additions
+                            }
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[NT - 1][r] = fmaf(last[r], sign, acc[NT - 1][r]);
+                        asm volatile("" : "+v"(acc[NT - 1]));
+                    } else {
+#pragma unroll
+                        for (int s = 0; s < SB; ++s)
+#pragma unroll
+                            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                                for (int k = P - 1; k >= 0; --k)
+                                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[s][0]),
+                                                                                     __builtin_bit_cast(bf16x8_t, b[((s * P + k) * NT + i) * 64]),
+                                                                                     acc[i], 0, 0, 0);
+                    }
+}
+
 template <typename T, int NT, int WAVES, bool TRANS>
 __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
 {
@@ -145,58 +241,38 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
     extern __shared__ __attribute__((aligned(16))) uint4 lds[];      // [2][kFrags][64] of B, [WAVES][32][8] of rows
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
 
-    // which rows: blocks of WAVES * 32 of a type, type after type
-    int t = -1;
-    int64_t first = 0, end = 0;
-    {
-        int64_t left = blockIdx.x;
-        for (int base = 0; base < a.types.T; base += 64) {
-            int64_t lo = 0, hi = 0;
-            if (base + lane < a.types.T) a.types.span(base + lane, lo, hi);
-            const int mine = (int)((hi - lo + WAVES * 32 - 1) / (WAVES * 32));
-            int upto = mine;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int v = __shfl_up(upto, o);
-                if (lane >= o) upto += v;
-            }
-            const uint64_t here = __ballot(left < upto);
-            if (here) {
-                const int l = __builtin_ctzll(here);
-                t = base + l;
-                const int64_t f = lo + (left - (upto - mine)) * (WAVES * 32);
-                first = (int64_t)__shfl((int)f, l);      // (rows are fewer than 2^31)
-                end = (int64_t)__shfl((int)hi, l);
-                break;
-            }
-            left -= __shfl(upto, 63);
-        }
-    }
-    if (t < 0) return;
-    t = __builtin_amdgcn_readfirstlane(t);
-    first = __builtin_amdgcn_readfirstlane((int)first);
-    end = __builtin_amdgcn_readfirstlane((int)end);
+    // a workgroup takes every gridDim.x-th of the listed row blocks; what it multiplies first of the next one travels while it
+    // finishes and stores this one
+    const int total = a.list[0].x;
+    struct Tile {
+        int t, first, end;
+    };
+    auto tile_at = [&](int i) SAR_INLINE {
+        const int4 v = a.list[1 + min(i, total - 1)];
+        return Tile{__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y), __builtin_amdgcn_readfirstlane(v.z)};
+    };
+    if ((int)blockIdx.x >= total) return;
+    static_assert(WAVES * 32 == kTileRows, "a workgroup's rows");
 
-    const int64_t r0 = first + wave * 32;
-    const uint4* B = a.B + ((int64_t)(t * a.blocks + blockIdx.y) * a.chunks) * (S * P * NT * 64);
-    const bool works = r0 < end;
-
-    auto fetch_b = [&](int stage, int buffer) SAR_INLINE {
-        for (int f = wave; f < kFrags; f += WAVES)
-            __builtin_amdgcn_global_load_lds((GlobalSrc*)(B + ((int64_t)stage * kFrags + f) * 64 + lane),
-                                             (LdsPtr*)(lds + (buffer * kFrags + f) * 64), 16, 0, 0);
+    auto pieces_of = [&](const Tile& w, int stage) SAR_INLINE {
+        return a.B + (((int64_t)(w.t * a.blocks + blockIdx.y) * a.chunks) * (S / SB) + stage) * (kFrags * 64);
     };
     // Rows come by whole lines: eight lanes a row, eight rows a load.  (By the lanes that multiply them, 16 bytes of 64 rows a load, every
     // line was fetched anew for each of its pieces: 256 rows' lines are what a first-level cache holds.)  They are handed to those lanes through
     // 4 KiB of LDS that are the wavefront's own, pieces turned by the row so that neither side meets a bank twice.
-    const T* tile = static_cast<const T*>(a.A) + r0 * a.C;
-    const uint32_t most = works ? (uint32_t)min(end - 1 - r0, (int64_t)31) : 0u;
-    uint32_t from[kRaw];
+    auto fetch_a = [&](const Tile& w, int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
+        const int64_t r0 = w.first + wave * 32;
+        const T* tile = static_cast<const T*>(a.A) + r0 * a.C;
+        const uint32_t most = (uint32_t)min((int64_t)w.end - 1 - r0, (int64_t)31);
+        const int c = chunk * CH + (lane & 7) * N;
+        if (a.C >= N) {
+            const uint32_t at = (uint32_t)min(c, a.C - N);
 #pragma unroll
-    for (int p = 0; p < kRaw; ++p) from[p] = min((uint32_t)(8 * p + (lane >> 3)), most) * (uint32_t)a.C;
-    auto fetch_a = [&](int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
+            for (int p = 0; p < kRaw; ++p) v[p] = load16(tile + (min((uint32_t)(8 * p + (lane >> 3)), most) * (uint32_t)a.C + at));
+        } else {
 #pragma unroll
-        for (int p = 0; p < kRaw; ++p) v[p] = Cols<T>::load(tile + from[p], chunk * CH + (lane & 7) * N, a.C);
+            for (int p = 0; p < kRaw; ++p) v[p] = Cols<T>::load(tile + min((uint32_t)(8 * p + (lane >> 3)), most) * (uint32_t)a.C, c, a.C);
+        }
     };
     uint4* const mine = lds + 2 * kFrags * 64 + wave * 256;
     auto hand_over = [&](int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
@@ -216,19 +292,27 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
         for (int p = 0; p < kRaw; ++p) v[p] = mine[(lane & 31) * 8 + ((h * kRaw + p) ^ (lane & 7))];
     };
 
-    float16_t acc[NT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) acc[i] = float16_t{};
     uint4 raw[kRaw];
-    fetch_b(0, 0);
-    if (works) {
-        fetch_a(0, raw);
+    Tile tile = tile_at(blockIdx.x);
+    auto has_rows = [&](const Tile& w) SAR_INLINE { return w.first + wave * 32 < w.end; };
+    for (int f = wave; f < kFrags; f += WAVES)
+        __builtin_amdgcn_global_load_lds((GlobalSrc*)(pieces_of(tile, 0) + f * 64 + lane), (LdsPtr*)(lds + f * 64), 16, 0, 0);
+    if (has_rows(tile)) {
+        fetch_a(tile, 0, raw);
         hand_over(0, raw);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    float sign = 1.f;
     const int stages = a.chunks * (S / SB);
+    int buffer = 0;
+    for (int index = blockIdx.x; index < total; index += gridDim.x) {
+    const bool another = index + (int)gridDim.x < total;
+    const Tile after = tile_at(index + gridDim.x);
+    const bool works = has_rows(tile), works_after = another && has_rows(after);
+    float16_t acc[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) acc[i] = float16_t{};
+    float sign = 1.f;
     for (int chunk = 0; chunk < a.chunks; ++chunk) {
         const bool more = chunk + 1 < a.chunks;
         uint4 p[S][P == 3 ? 3 : 1];
@@ -250,71 +334,37 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
         }
 #pragma unroll
         for (int part = 0; part < S / SB; ++part) {
-            const int stage = chunk * (S / SB) + part, buffer = stage & 1;
-            const uint4* b = lds + buffer * kFrags * 64 + lane;
-            if (stage + 1 < stages) fetch_b(stage + 1, buffer ^ 1);
-            if (works) {
-                if (part == 0 && more) fetch_a(chunk + 1, raw);
-                if constexpr (P == 3) {
-                    // a tile's products run while the sums of the tile before are added and the pieces of the next one are read
-                    uint4 w[2][3];
-                    float16_t sum, last;
+            const int stage = chunk * (S / SB) + part;
+            const uint4* from = stage + 1 < stages ? pieces_of(tile, stage + 1) : another ? pieces_of(after, 0) : nullptr;
+            uint4 now[SB][P == 3 ? 3 : 1];
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) w[0][k] = b[k * NT * 64];
-                    __builtin_amdgcn_sched_barrier(0);
+            for (int s = 0; s < SB; ++s)
 #pragma unroll
-                    for (int i = 0; i < NT; ++i) {
-                        sum = float16_t{};
-                        if (i + 1 < NT) {
-#pragma unroll
-                            for (int k = 0; k < 3; ++k) w[(i + 1) & 1][k] = b[(k * NT + i + 1) * 64];
-                        }
-#pragma unroll
-                        for (int k = 0; k < 6; ++k)
-                            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[part][kTerm[k][0]]),
-                                                                          __builtin_bit_cast(bf16x8_t, w[i & 1][kTerm[k][1]]), sum, 0, 0, 0);
-                        if (i > 0) {
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) acc[i - 1][r] = fmaf(last[r], sign, acc[i - 1][r]);
-                            asm volatile("" : "+v"(acc[i - 1]));
-                        }
-                        last = sum;
-#pragma unroll
-                        for (int k = 0; k < 6; ++k) {
-                            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                        // a product
-                            if (k % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);       // a read
-                            __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);                        // additions
-                        }
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[NT - 1][r] = fmaf(last[r], sign, acc[NT - 1][r]);
-                    asm volatile("" : "+v"(acc[NT - 1]));
-                } else {
-#pragma unroll
-                    for (int s = 0; s < SB; ++s)
-#pragma unroll
-                        for (int i = 0; i < NT; ++i)
-#pragma unroll
-                            for (int k = P - 1; k >= 0; --k)
-                                acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[part * SB + s][0]),
-                                                                                 __builtin_bit_cast(bf16x8_t, b[((s * P + k) * NT + i) * 64]),
-                                                                                 acc[i], 0, 0, 0);
+                for (int k = 0; k < (P == 3 ? 3 : 1); ++k) now[s][k] = p[part * SB + s][k];
+            stage_products<T, NT, WAVES>(lds + (buffer ^ 1) * kFrags * 64, from, lds + buffer * kFrags * 64 + lane, now, sign, works, acc, [&]() SAR_INLINE {
+                if (part == 0) {
+                    if (more ? works : works_after) fetch_a(more ? tile : after, more ? chunk + 1 : 0, raw);
                 }
-                if (part == S / SB - 1 && more) hand_over(chunk + 1, raw);
+            });
+            if (part == S / SB - 1) {
+                if (more ? works : works_after) hand_over(more ? chunk + 1 : 0, raw);
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
+            buffer ^= 1;
         }
         sign = -sign;
     }
-    if (!works) return;
+    const Tile done = tile;
+    tile = after;
+    if (!works) continue;
 
+    const int64_t r0 = done.first + wave * 32, end = done.end;
     const int n0 = blockIdx.y * (32 * NT);
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < NT; ++i) odd |= not_finite(acc[i]);
-    if (__any(odd)) exact_tiles<T, NT, TRANS>(a, t, static_cast<const T*>(a.A) + min(r0 + (lane & 31), end - 1) * a.C, n0, acc);
+    if (__any(odd)) exact_tiles<T, NT, TRANS>(a, done.t, static_cast<const T*>(a.A) + min(r0 + (lane & 31), end - 1) * a.C, n0, acc);
 
     // lane holds columns of its place; register r holds row 8*(r/4) + 4*h + r%4
     constexpr int IL = NT < 4 ? NT : 4;
@@ -345,6 +395,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
             }
         }
     }
+    }
 }
 
 // Column tiles a wavefront forms at once.
@@ -358,17 +409,18 @@ int tiles_of(int64_t n, int N)
 template <typename T, int NT, bool TRANS>
 int run_rows(const RowsArgs& a, LayArgs l, hipStream_t st)
 {
-    constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps, kWaves = 4;
-    const int64_t units = (int64_t)l.T * l.blocks * l.chunks * S * NT * 64;
-    const int64_t lay = (units + 255) / 256, groups = a.types.n / (kWaves * 32) + a.types.T;
-    if (lay > 0x7fffffff || groups > 0x7fffffff || l.blocks > 65535)
-        return fail(SAR_ERR_UNSUPPORTED, "typed products: %lld rows, %d x %d weights of %d types are too many for one launch",
-                    (long long)a.types.n, a.K, a.F, l.T);
-    k_typed_lay<T, NT, TRANS><<<(unsigned)lay, 256, 0, st>>>(l);
+    constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps, kWaves = kTileRows / 32;
+    const int64_t units = (int64_t)l.T * l.blocks * l.chunks * S * NT * 64, lay = (units + 255) / 256;
+    if (lay > 0x7fffffff - 65536 || l.blocks > 65535)
+        return fail(SAR_ERR_UNSUPPORTED, "typed products: %d x %d weights of %d types are too many for one launch", a.K, a.F, l.T);
+    l.lay = (unsigned)lay;
+    k_typed_lay<T, NT, TRANS><<<(unsigned)lay + l.T, 256, 0, st>>>(l);
     SAR_LAUNCH_CHECK();
     constexpr size_t shared = (size_t)(2 * Mode<T>::kStage * P * NT + 4 * kWaves) * 1024;
     auto* fn = k_typed_rows<T, NT, kWaves, TRANS>;
     if (shared > 65536) SAR_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)shared));
+    // as many workgroups as are resident at once: two per compute unit, of the narrow ones three
+    const int64_t groups = std::min<int64_t>(l.most, std::max(1, 256 * (NT == 2 ? 3 : 2) / l.blocks));
     fn<<<dim3((unsigned)groups, l.blocks), kWaves * 64, shared, st>>>(a);
     SAR_LAUNCH_CHECK();
     return SAR_OK;
@@ -380,6 +432,8 @@ size_t lay_bytes(int C, int N, int T)
     const size_t f32 = (size_t)((C + 31) / 32) * 2 * 3, b16 = (size_t)((C + 63) / 64) * 4 * 2;
     return (size_t)T * ((N + 255) / 256 * 8) * std::max(f32, b16) * 1024;
 }
+int64_t most_tiles(int64_t n, int T) { return n / kTileRows + T; }
+size_t list_bytes(int64_t n, int T) { return (size_t)(most_tiles(n, T) + 1) * sizeof(int4); }
 
 // out [n, N] = A [n, C] B; TRANS: B = W^T.
 template <typename T, bool TRANS>
@@ -387,8 +441,11 @@ int rows_product(const void* A, const float* W, const Types& types, void* out, i
 {
     const int C = TRANS ? F : K, N = TRANS ? K : F, NT = tiles_of(types.n, N);
     const int chunks = (C + kChunk<T> - 1) / kChunk<T>, blocks = (N + 32 * NT - 1) / (32 * NT);
-    const RowsArgs a{A, static_cast<const uint4*>(work), W, out, types, C, N, chunks, blocks, K, F};
-    const LayArgs l{W, static_cast<uint4*>(work), types.T, K, F, C, N, chunks, blocks};
+    const int64_t most = most_tiles(types.n, types.T);
+    int4* const list = static_cast<int4*>(work);
+    uint4* const pieces = static_cast<uint4*>(work) + (most + 1);
+    const RowsArgs a{A, pieces, W, out, list, C, N, chunks, blocks, K, F};
+    const LayArgs l{W, pieces, types.T, K, F, C, N, chunks, blocks, types, list, most, 0};
     return NT == 2 ? run_rows<T, 2, TRANS>(a, l, st) : NT == 4 ? run_rows<T, 4, TRANS>(a, l, st) : run_rows<T, 8, TRANS>(a, l, st);
 }
 
@@ -406,7 +463,7 @@ int check_shape(int64_t n, int K, int F, int T)
 
 size_t work_bytes_of(int64_t n, int K, int F, int T)
 {
-    return round256(std::max(std::max(lay_bytes(K, F, T), lay_bytes(F, K, T)), typed_dw_bytes(n, K, F, T)));
+    return round256(std::max(std::max(lay_bytes(K, F, T), lay_bytes(F, K, T)) + list_bytes(n, T), typed_dw_bytes(n, K, F, T)));
 }
 
 int check_call(int dtype, int64_t n, int K, int F, int T, const void* ptr, const void* work, size_t work_bytes)
