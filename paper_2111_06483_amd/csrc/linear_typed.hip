@@ -37,13 +37,17 @@ struct Mode<bf16_t> {
 template <typename T>
 constexpr int kChunk = 16 * Mode<T>::kSteps;
 
-// Column c (0..31) of column tile i of NT: tiles in groups of four (or two) take columns by turns.
-template <int NT>
-__host__ __device__ constexpr int column_of(int i, int c)
-{
-    constexpr int IL = NT < 4 ? NT : 4;
-    return i / IL * (32 * IL) + c * IL + i % IL;
-}
+// How the four wavefronts share 128 rows and NT column tiles.  fp32: 32 rows and all columns each, so that a row's values are cut into pieces by
+// one of them; bf16, where there is nothing to cut and reading B from LDS takes as long as multiplying (32 rows each: 64 KiB of LDS a
+// chunk and wavefront for 64 products): 64 rows and half of the columns, a fragment of B for two products.
+template <typename T, int NT>
+struct Share {
+    static constexpr int MR = sizeof(T) == 2 && NT >= 4 ? 2 : 1;       // row tiles a wavefront
+    static constexpr int WC = MR, WR = 4 / WC, NW = NT / WC;           // wavefronts beside and below each other; column tiles a wavefront
+    static constexpr int IL = NW < 4 ? NW : 4;
+    // Column c (0..31) of column tile i: tiles in groups of four (or two) take columns by turns.
+    static __host__ __device__ constexpr int column_of(int i, int c) { return i / IL * (32 * IL) + c * IL + i % IL; }
+};
 
 // ---- the small operand's pieces
 //
@@ -99,7 +103,7 @@ __global__ __launch_bounds__(256) void k_typed_lay(LayArgs a)
     const int block = (int)(rest % a.blocks);
     const int t = (int)(rest / a.blocks);
     if (t >= a.T) return;
-    const int n = block * (32 * NT) + column_of<NT>(tile, lane & 31);
+    const int n = block * (32 * NT) + Share<T, NT>::column_of(tile, lane & 31);
     const int c = chunk * kChunk<T> + (lane >> 5) * (kChunk<T> / 2) + s * 8;
     const float* W = a.W + (int64_t)t * a.K * a.F;
     float v[8];
@@ -139,14 +143,15 @@ struct RowsArgs {
     int K, F;
 };
 
-// The wavefront's tiles once more by the fp32 matrix instruction.
+// A wavefront's tiles of 32 rows once more by the fp32 matrix instruction; column tiles from `first` on of the block that begins at n0.
 template <typename T, int NT, bool TRANS>
-__device__ inline void exact_tiles(const RowsArgs& a, int t, const T* row, int n0, float16_t (&acc)[NT])
+__device__ inline void exact_tiles(const RowsArgs& a, int t, const T* row, int n0, int first, float16_t (&acc)[Share<T, NT>::NW])
 {
+    constexpr int NW = Share<T, NT>::NW;
     const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
     const float* W = a.W + (int64_t)t * a.K * a.F;
 #pragma unroll
-    for (int i = 0; i < NT; ++i) acc[i] = float16_t{};
+    for (int i = 0; i < NW; ++i) acc[i] = float16_t{};
     for (int k = 0; k < a.C; k += 2) {
         const bool in = k + h < a.C;
         float x = 0.f;
@@ -155,8 +160,8 @@ __device__ inline void exact_tiles(const RowsArgs& a, int t, const T* row, int n
             else x = bf16_to_f32(row[k + h]);
         }
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            const int n = n0 + column_of<NT>(i, c);
+        for (int i = 0; i < NW; ++i) {
+            const int n = n0 + Share<T, NT>::column_of(first + i, c);
             float w = 0.f;
             if (in && n < a.N) w = TRANS ? W[(int64_t)n * a.F + k + h] : W[(int64_t)(k + h) * a.F + n];
             acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w, acc[i], 0, 0, 0);
@@ -166,80 +171,99 @@ __device__ inline void exact_tiles(const RowsArgs& a, int t, const T* row, int n
 
 using LdsPtr = __attribute__((address_space(3))) void;
 using GlobalSrc = const __attribute__((address_space(1))) void;
+constexpr int kTileWaves = kTileRows / 32;
 
-// A stage's products from its pieces of B at `b`, while the next stage's pieces go to `to`.  (A function of its own for its arguments' sake: it
-// is by them that the compiler knows the two apart.  Otherwise every first read of a stage waits for the copy that was just begun:
-// bf16 rows 256 -> 256 took 1.3 times as long.)
-template <typename T, int NT, int WAVES, int SP, typename Fetch>
-__device__ SAR_INLINE inline void stage_products(uint4* __restrict__ to, const uint4* from, const uint4* __restrict__ b, const uint4 (&p)[Mode<T>::kStage][SP],
-                                                 float sign, bool works, float16_t (&acc)[NT], Fetch&& fetch_rows)
+// KiB of B a stage.
+template <typename T, int NT>
+constexpr int kStageFrags = Mode<T>::kStage * Mode<T>::kPieces * NT;
+
+template <typename T, int NT>
+__device__ SAR_INLINE inline void copy_stage(uint4* to, const uint4* from)
 {
-    constexpr int P = Mode<T>::kPieces, SB = Mode<T>::kStage, kFrags = SB * P * NT;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (from) {
 #pragma unroll
-        for (int f = 0; f < (kFrags + WAVES - 1) / WAVES; ++f)
-            if (kFrags % WAVES == 0 || wave + f * WAVES < kFrags)
-                __builtin_amdgcn_global_load_lds((GlobalSrc*)(from + (wave + f * WAVES) * 64 + lane), (LdsPtr*)(to + (wave + f * WAVES) * 64), 16, 0, 0);
+    for (int f = 0; f < (kStageFrags<T, NT> + kTileWaves - 1) / kTileWaves; ++f) {
+        if (kStageFrags<T, NT> % kTileWaves && wave + f * kTileWaves >= kStageFrags<T, NT>) continue;
+        __builtin_amdgcn_global_load_lds((GlobalSrc*)(from + (wave + f * kTileWaves) * 64 + lane), (LdsPtr*)(to + (wave + f * kTileWaves) * 64), 16, 0, 0);
     }
-    fetch_rows();
-    if (!works) return;
-                    if constexpr (P == 3) {
-                        // a tile's products run while the sums of the tile before are added and the pieces of the next one are read
-                        uint4 w[2][3];
-                        float16_t sum, last;
-#pragma unroll
-                        for (int k = 0; k < 3; ++k) w[0][k] = b[k * NT * 64];
-                        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                        for (int i = 0; i < NT; ++i) {
-                            sum = float16_t{};
-                            if (i + 1 < NT) {
-#pragma unroll
-                                for (int k = 0; k < 3; ++k) w[(i + 1) & 1][k] = b[(k * NT + i + 1) * 64];
-                            }
-#pragma unroll
-                            for (int k = 0; k < 6; ++k)
-                                sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[0][kTerm[k][0]]),
-                                                                              __builtin_bit_cast(bf16x8_t, w[i & 1][kTerm[k][1]]), sum, 0, 0, 0);
-                            if (i > 0) {
-#pragma unroll
-                                for (int r = 0; r < 16; ++r) acc[i - 1][r] = fmaf(last[r], sign, acc[i - 1][r]);
-                                asm volatile("" : "+v"(acc[i - 1]));
-                            }
-                            last = sum;
-#pragma unroll
-                            for (int k = 0; k < 6; ++k) {
-                                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                        // a product
-                                if (k % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);       // a read
-                                __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);                        // additions
-                            }
-                            __builtin_amdgcn_sched_barrier(0);
-                        }
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) acc[NT - 1][r] = fmaf(last[r], sign, acc[NT - 1][r]);
-                        asm volatile("" : "+v"(acc[NT - 1]));
-                    } else {
-#pragma unroll
-                        for (int s = 0; s < SB; ++s)
-#pragma unroll
-                            for (int i = 0; i < NT; ++i)
-#pragma unroll
-                                for (int k = P - 1; k >= 0; --k)
-                                    acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[s][0]),
-                                                                                     __builtin_bit_cast(bf16x8_t, b[((s * P + k) * NT + i) * 64]),
-                                                                                     acc[i], 0, 0, 0);
-                    }
 }
 
-template <typename T, int NT, int WAVES, bool TRANS>
-__global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
+// A stage's products of the rows' fragments p with the pieces of B at `b`, while the next stage's pieces (`from`, null where there is none) go to
+// `to`.  (A function of its own for its arguments' sake: it is by them that the compiler knows the two apart.  Otherwise every
+// first read of a stage waits for the copy that was just begun: 237500 x 256 -> 256, fp32, 226 us for 195.)
+template <typename T, int NT, int SP, typename Fetch>
+__device__ SAR_INLINE inline void stage_products(uint4* __restrict__ to, const uint4* from, const uint4* __restrict__ b,
+                                                 const uint4 (&p)[Share<T, NT>::MR][Mode<T>::kStage][SP], float sign, bool works,
+                                                 float16_t (&acc)[Share<T, NT>::MR][Share<T, NT>::NW], Fetch&& fetch_rows)
 {
-    constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps, CH = kChunk<T>, N = Cols<T>::N;
+    constexpr int P = Mode<T>::kPieces, SB = Mode<T>::kStage, MR = Share<T, NT>::MR, NW = Share<T, NT>::NW;
+    if (from) copy_stage<T, NT>(to, from);
+    fetch_rows();
+    if (!works) return;
+    if constexpr (P == 3) {
+        // a tile's products run while the sums of the tile before are added and the pieces of the next one are read
+        static_assert(MR == 1 && SB == 1, "one product of 16 a stage and row tile");
+        uint4 w[2][3];
+        float16_t sum, last;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) w[0][k] = b[k * NT * 64];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            sum = float16_t{};
+            if (i + 1 < NW) {
+#pragma unroll
+                for (int k = 0; k < 3; ++k) w[(i + 1) & 1][k] = b[(k * NT + i + 1) * 64];
+            }
+#pragma unroll
+            for (int k = 0; k < 6; ++k)
+                sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[0][0][kTerm[k][0]]),
+                                                              __builtin_bit_cast(bf16x8_t, w[i & 1][kTerm[k][1]]), sum, 0, 0, 0);
+            if (i > 0) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[0][i - 1][r] = fmaf(last[r], sign, acc[0][i - 1][r]);
+                // (here, not where the compiler would have them: behind the stage, with all tiles' products kept until then)
+                asm volatile("" : "+v"(acc[0][i - 1]));
+            }
+            last = sum;
+#pragma unroll
+            for (int k = 0; k < 6; ++k) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);                        // a product
+                if (k % 2 == 0) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);       // a read
+                __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);                        // additions
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[0][NW - 1][r] = fmaf(last[r], sign, acc[0][NW - 1][r]);
+        asm volatile("" : "+v"(acc[0][NW - 1]));
+    } else {
+#pragma unroll
+        for (int s = 0; s < SB; ++s)
+#pragma unroll
+            for (int i = 0; i < NW; ++i)
+#pragma unroll
+                for (int k = P - 1; k >= 0; --k) {
+                    const uint4 w = b[((s * P + k) * NT + i) * 64];
+#pragma unroll
+                    for (int m = 0; m < MR; ++m)
+                        acc[m][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[m][s][0]),
+                                                                            __builtin_bit_cast(bf16x8_t, w), acc[m][i], 0, 0, 0);
+                }
+    }
+}
+
+template <typename T, int NT, bool TRANS>
+__global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs a)
+{
+    constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps, CH = kChunk<T>, N = Cols<T>::N, SB = Mode<T>::kStage;
+    using Sh = Share<T, NT>;
+    constexpr int MR = Sh::MR, NW = Sh::NW, IL = Sh::IL;
     constexpr int kRaw = 64 / 16;                        // 16-byte pieces of a row that a lane holds of a chunk
-    constexpr int SB = Mode<T>::kStage, kFrags = SB * P * NT;        // KiB of B a stage
-    extern __shared__ __attribute__((aligned(16))) uint4 lds[];      // [2][kFrags][64] of B, [WAVES][32][8] of rows
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    constexpr int kFrags = kStageFrags<T, NT>, kSP = P == 3 ? 3 : 1;
+    static_assert(S / SB == 2, "a barrier between taking a chunk's rows and handing over the next one's");
+    extern __shared__ __attribute__((aligned(16))) uint4 lds[];      // [2][kFrags][64] of B, [4][32][8] of rows
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, wr = wave / Sh::WC, wc = wave % Sh::WC;
 
     // a workgroup takes every gridDim.x-th of the listed row blocks; what it multiplies first of the next one travels while it
     // finishes and stores this one
@@ -252,14 +276,14 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
         return Tile{__builtin_amdgcn_readfirstlane(v.x), __builtin_amdgcn_readfirstlane(v.y), __builtin_amdgcn_readfirstlane(v.z)};
     };
     if ((int)blockIdx.x >= total) return;
-    static_assert(WAVES * 32 == kTileRows, "a workgroup's rows");
 
     auto pieces_of = [&](const Tile& w, int stage) SAR_INLINE {
         return a.B + (((int64_t)(w.t * a.blocks + blockIdx.y) * a.chunks) * (S / SB) + stage) * (kFrags * 64);
     };
-    // Rows come by whole lines: eight lanes a row, eight rows a load.  (By the lanes that multiply them, 16 bytes of 64 rows a load, every
-    // line was fetched anew for each of its pieces: 256 rows' lines are what a first-level cache holds.)  They are handed to those lanes through
-    // 4 KiB of LDS that are the wavefront's own, pieces turned by the row so that neither side meets a bank twice.
+    // Rows come by whole lines: eight lanes a row, eight rows a load, 32 rows a wavefront.  (By the lanes that multiply them, 16 bytes of
+    // 64 rows a load, every line was asked for once for each of its pieces.)  They are handed to those lanes through LDS, pieces turned by the row
+    // so that neither side meets a bank twice.
+    auto brings = [&](const Tile& w) SAR_INLINE { return w.first + wave * 32 < w.end; };
     auto fetch_a = [&](const Tile& w, int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
         const int64_t r0 = w.first + wave * 32;
         const T* tile = static_cast<const T*>(a.A) + r0 * a.C;
@@ -274,7 +298,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
             for (int p = 0; p < kRaw; ++p) v[p] = Cols<T>::load(tile + min((uint32_t)(8 * p + (lane >> 3)), most) * (uint32_t)a.C, c, a.C);
         }
     };
-    uint4* const mine = lds + 2 * kFrags * 64 + wave * 256;
+    uint4* const rows = lds + 2 * kFrags * 64;
     auto hand_over = [&](int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
         const int c = chunk * CH + (lane & 7) * N;
         if ((chunk + 1) * CH > a.C && c + N > a.C) {
@@ -285,19 +309,17 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
             }
         }
 #pragma unroll
-        for (int p = 0; p < kRaw; ++p) mine[(8 * p + (lane >> 3)) * 8 + ((lane & 7) ^ (lane >> 3))] = v[p];
+        for (int p = 0; p < kRaw; ++p) rows[wave * 256 + (8 * p + (lane >> 3)) * 8 + ((lane & 7) ^ (lane >> 3))] = v[p];
     };
-    auto take = [&](uint4 (&v)[kRaw]) SAR_INLINE {
+    auto take = [&](int m, uint4 (&v)[kRaw]) SAR_INLINE {
 #pragma unroll
-        for (int p = 0; p < kRaw; ++p) v[p] = mine[(lane & 31) * 8 + ((h * kRaw + p) ^ (lane & 7))];
+        for (int p = 0; p < kRaw; ++p) v[p] = rows[(wr * MR + m) * 256 + (lane & 31) * 8 + ((h * kRaw + p) ^ (lane & 7))];
     };
 
     uint4 raw[kRaw];
     Tile tile = tile_at(blockIdx.x);
-    auto has_rows = [&](const Tile& w) SAR_INLINE { return w.first + wave * 32 < w.end; };
-    for (int f = wave; f < kFrags; f += WAVES)
-        __builtin_amdgcn_global_load_lds((GlobalSrc*)(pieces_of(tile, 0) + f * 64 + lane), (LdsPtr*)(lds + f * 64), 16, 0, 0);
-    if (has_rows(tile)) {
+    copy_stage<T, NT>(lds, pieces_of(tile, 0));
+    if (brings(tile)) {
         fetch_a(tile, 0, raw);
         hand_over(0, raw);
     }
@@ -306,95 +328,94 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_rows(RowsArgs a)
     const int stages = a.chunks * (S / SB);
     int buffer = 0;
     for (int index = blockIdx.x; index < total; index += gridDim.x) {
-    const bool another = index + (int)gridDim.x < total;
-    const Tile after = tile_at(index + gridDim.x);
-    const bool works = has_rows(tile), works_after = another && has_rows(after);
-    float16_t acc[NT];
+        const bool another = index + (int)gridDim.x < total;
+        const Tile after = tile_at(index + gridDim.x);
+        const bool works = tile.first + wr * MR * 32 < tile.end, here = brings(tile), there = another && brings(after);
+        float16_t acc[MR][NW];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) acc[i] = float16_t{};
-    float sign = 1.f;
-    for (int chunk = 0; chunk < a.chunks; ++chunk) {
-        const bool more = chunk + 1 < a.chunks;
-        uint4 p[S][P == 3 ? 3 : 1];
-        if (works) {
-            uint4 x[kRaw];
-            take(x);
-            if constexpr (P == 3) {
+        for (int m = 0; m < MR; ++m)
 #pragma unroll
-                for (int s = 0; s < S; ++s) {
-                    const float v[8] = {__uint_as_float(x[2 * s].x), __uint_as_float(x[2 * s].y), __uint_as_float(x[2 * s].z),
-                                        __uint_as_float(x[2 * s].w), __uint_as_float(x[2 * s + 1].x), __uint_as_float(x[2 * s + 1].y),
-                                        __uint_as_float(x[2 * s + 1].z), __uint_as_float(x[2 * s + 1].w)};
-                    split8(v, p[s]);
+            for (int i = 0; i < NW; ++i) acc[m][i] = float16_t{};
+        float sign = 1.f;
+        for (int chunk = 0; chunk < a.chunks; ++chunk) {
+            const bool more = chunk + 1 < a.chunks, coming = more ? here : there;
+            uint4 p[S / SB][MR][SB][kSP];
+            if (works) {
+#pragma unroll
+                for (int m = 0; m < MR; ++m) {
+                    uint4 x[kRaw];
+                    take(m, x);
+#pragma unroll
+                    for (int s = 0; s < S; ++s) {
+                        if constexpr (P == 3) {
+                            const float v[8] = {__uint_as_float(x[2 * s].x), __uint_as_float(x[2 * s].y), __uint_as_float(x[2 * s].z),
+                                                __uint_as_float(x[2 * s].w), __uint_as_float(x[2 * s + 1].x), __uint_as_float(x[2 * s + 1].y),
+                                                __uint_as_float(x[2 * s + 1].z), __uint_as_float(x[2 * s + 1].w)};
+                            split8(v, p[s / SB][m][s % SB]);
+                        } else {
+                            p[s / SB][m][s % SB][0] = x[s];
+                        }
+                    }
                 }
-            } else {
-#pragma unroll
-                for (int s = 0; s < S; ++s) p[s][0] = x[s];
             }
-        }
 #pragma unroll
-        for (int part = 0; part < S / SB; ++part) {
-            const int stage = chunk * (S / SB) + part;
-            const uint4* from = stage + 1 < stages ? pieces_of(tile, stage + 1) : another ? pieces_of(after, 0) : nullptr;
-            uint4 now[SB][P == 3 ? 3 : 1];
-#pragma unroll
-            for (int s = 0; s < SB; ++s)
-#pragma unroll
-                for (int k = 0; k < (P == 3 ? 3 : 1); ++k) now[s][k] = p[part * SB + s][k];
-            stage_products<T, NT, WAVES>(lds + (buffer ^ 1) * kFrags * 64, from, lds + buffer * kFrags * 64 + lane, now, sign, works, acc, [&]() SAR_INLINE {
-                if (part == 0) {
-                    if (more ? works : works_after) fetch_a(more ? tile : after, more ? chunk + 1 : 0, raw);
-                }
-            });
-            if (part == S / SB - 1) {
-                if (more ? works : works_after) hand_over(more ? chunk + 1 : 0, raw);
+            for (int part = 0; part < S / SB; ++part) {
+                const int stage = chunk * (S / SB) + part;
+                const uint4* from = stage + 1 < stages ? pieces_of(tile, stage + 1) : another ? pieces_of(after, 0) : nullptr;
+                stage_products<T, NT>(lds + (buffer ^ 1) * kFrags * 64, from, lds + (buffer * kFrags + wc * NW) * 64 + lane, p[part], sign, works,
+                                      acc, [&]() SAR_INLINE {
+                                          if (part == 0 && coming) fetch_a(more ? tile : after, more ? chunk + 1 : 0, raw);
+                                      });
+                if (part == S / SB - 1 && coming) hand_over(more ? chunk + 1 : 0, raw);
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+                buffer ^= 1;
             }
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-            buffer ^= 1;
+            sign = -sign;
         }
-        sign = -sign;
-    }
-    const Tile done = tile;
-    tile = after;
-    if (!works) continue;
+        const Tile done = tile;
+        tile = after;
+        const int n0 = blockIdx.y * (32 * NT);
+#pragma unroll
+        for (int m = 0; m < MR; ++m) {
+            const int64_t r0 = done.first + (wr * MR + m) * 32, end = done.end;
+            if (r0 >= end) continue;
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < NW; ++i) odd |= not_finite(acc[m][i]);
+            if (__any(odd))
+                exact_tiles<T, NT, TRANS>(a, done.t, static_cast<const T*>(a.A) + min(r0 + (lane & 31), end - 1) * a.C, n0, wc * NW, acc[m]);
 
-    const int64_t r0 = done.first + wave * 32, end = done.end;
-    const int n0 = blockIdx.y * (32 * NT);
-    bool odd = false;
+            // lane holds columns of its place; register r holds row 8*(r/4) + 4*h + r%4
 #pragma unroll
-    for (int i = 0; i < NT; ++i) odd |= not_finite(acc[i]);
-    if (__any(odd)) exact_tiles<T, NT, TRANS>(a, done.t, static_cast<const T*>(a.A) + min(r0 + (lane & 31), end - 1) * a.C, n0, acc);
-
-    // lane holds columns of its place; register r holds row 8*(r/4) + 4*h + r%4
-    constexpr int IL = NT < 4 ? NT : 4;
+            for (int r = 0; r < 16; ++r) {
+                const int64_t i = r0 + 8 * (r / 4) + 4 * h + r % 4;
+                if (i >= end) continue;
+                T* out = static_cast<T*>(a.out) + i * a.N;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const int64_t i = r0 + 8 * (r / 4) + 4 * h + r % 4;
-        if (i >= end) continue;
-        T* out = static_cast<T*>(a.out) + i * a.N;
+                for (int g = 0; g < NW / IL; ++g) {
+                    const int n = n0 + Sh::column_of(wc * NW + g * IL, lane & 31);
+                    const float16_t* v = &acc[m][g * IL];
+                    if (n + IL <= a.N) {
+                        if constexpr (sizeof(T) == 4) {
+                            struct __attribute__((packed, aligned(4))) V { float x[IL]; } w;
 #pragma unroll
-        for (int g = 0; g < NT / IL; ++g) {
-            const int n = n0 + column_of<NT>(g * IL, lane & 31);
-            if (n + IL <= a.N) {
-                if constexpr (sizeof(T) == 4) {
-                    struct __attribute__((packed, aligned(4))) V { float v[IL]; } v;
+                            for (int j = 0; j < IL; ++j) w.x[j] = v[j][r];
+                            *reinterpret_cast<V*>(out + n) = w;
+                        } else {
+                            struct __attribute__((packed, aligned(2))) V { uint32_t x[IL / 2]; } w;
 #pragma unroll
-                    for (int j = 0; j < IL; ++j) v.v[j] = acc[g * IL + j][r];
-                    *reinterpret_cast<V*>(out + n) = v;
-                } else {
-                    struct __attribute__((packed, aligned(2))) V { uint32_t v[IL / 2]; } v;
+                            for (int j = 0; j < IL / 2; ++j) w.x[j] = pack2_bf16(v[2 * j][r], v[2 * j + 1][r]);
+                            *reinterpret_cast<V*>(out + n) = w;
+                        }
+                    } else {
 #pragma unroll
-                    for (int j = 0; j < IL / 2; ++j) v.v[j] = pack2_bf16(acc[g * IL + 2 * j][r], acc[g * IL + 2 * j + 1][r]);
-                    *reinterpret_cast<V*>(out + n) = v;
+                        for (int j = 0; j < IL; ++j)
+                            if (n + j < a.N) out[n + j] = from_f32<T>(v[j][r]);
+                    }
                 }
-            } else {
-#pragma unroll
-                for (int j = 0; j < IL; ++j)
-                    if (n + j < a.N) out[n + j] = from_f32<T>(acc[g * IL + j][r]);
             }
         }
-    }
     }
 }
 
@@ -409,19 +430,19 @@ int tiles_of(int64_t n, int N)
 template <typename T, int NT, bool TRANS>
 int run_rows(const RowsArgs& a, LayArgs l, hipStream_t st)
 {
-    constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps, kWaves = kTileRows / 32;
+    constexpr int S = Mode<T>::kSteps;
     const int64_t units = (int64_t)l.T * l.blocks * l.chunks * S * NT * 64, lay = (units + 255) / 256;
     if (lay > 0x7fffffff - 65536 || l.blocks > 65535)
         return fail(SAR_ERR_UNSUPPORTED, "typed products: %d x %d weights of %d types are too many for one launch", a.K, a.F, l.T);
     l.lay = (unsigned)lay;
     k_typed_lay<T, NT, TRANS><<<(unsigned)lay + l.T, 256, 0, st>>>(l);
     SAR_LAUNCH_CHECK();
-    constexpr size_t shared = (size_t)(2 * Mode<T>::kStage * P * NT + 4 * kWaves) * 1024;
-    auto* fn = k_typed_rows<T, NT, kWaves, TRANS>;
+    constexpr size_t shared = (size_t)(2 * kStageFrags<T, NT> + 4 * kTileWaves) * 1024;
+    auto* fn = k_typed_rows<T, NT, TRANS>;
     if (shared > 65536) SAR_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)shared));
     // as many workgroups as are resident at once: two per compute unit, of the narrow ones three
     const int64_t groups = std::min<int64_t>(l.most, std::max(1, 256 * (NT == 2 ? 3 : 2) / l.blocks));
-    fn<<<dim3((unsigned)groups, l.blocks), kWaves * 64, shared, st>>>(a);
+    fn<<<dim3((unsigned)groups, l.blocks), kTileWaves * 64, shared, st>>>(a);
     SAR_LAUNCH_CHECK();
     return SAR_OK;
 }
