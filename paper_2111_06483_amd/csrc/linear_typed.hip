@@ -295,7 +295,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs a)
             for (int p = 0; p < kRaw; ++p) v[p] = load16(tile + (min((uint32_t)(8 * p + (lane >> 3)), most) * (uint32_t)a.C + at));
         } else {
 #pragma unroll
-            for (int p = 0; p < kRaw; ++p) v[p] = Cols<T>::load(tile + min((uint32_t)(8 * p + (lane >> 3)), most) * (uint32_t)a.C, c, a.C);
+            for (int p = 0; p < kRaw; ++p) v[p] = Cols<T>::load(tile + min((uint32_t)(8 * p + (lane >> 3)), most) * (uint32_t)a.C, c, a.C, a.C);
         }
     };
     uint4* const rows = lds + 2 * kFrags * 64;

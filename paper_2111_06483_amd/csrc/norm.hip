@@ -98,7 +98,10 @@ __global__ __launch_bounds__(kThreads) void k_norm_fwd(FwdArgs a)
     for (int i = 0; i < NR; ++i)
 #pragma unroll
         for (int r = 0; r < R; ++r)        // (rows behind the last one are read as the last one)
-            raw[i][r] = Cols<T>::load(static_cast<const T*>(a.X) + min(row0 + i * kRows, a.n - 1) * D, (t + r * TPR) * N, D);
+        {
+            const int64_t row = min(row0 + i * kRows, a.n - 1);
+            raw[i][r] = Cols<T>::load(static_cast<const T*>(a.X) + row * D, (t + r * TPR) * N, D, (a.n - row) * D);
+        }
     float g[R][N], b[R][N];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -183,9 +186,11 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(BwdArgs a)
     const int t = threadIdx.x % TPR, D = a.D;
     const float over = 1.f / (float)D;
     float g[R][N], dg[R][N], db[R][N];
+    uint4 within[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         load_params<N>(a.gamma, (t + r * TPR) * N, D, 1.f, g[r]);
+        within[r] = Cols<T>::within((t + r * TPR) * N, D);
 #pragma unroll
         for (int j = 0; j < N; ++j) dg[r][j] = db[r][j] = 0.f;
     }
@@ -204,8 +209,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(BwdArgs a)
                 if constexpr (PACKED)
                     xp[i][r] = PackedCols<N>::load(a.Xq + row * packed_stride(D), a.Xe + row * packed_steps(D), c, packed_stride(D));
                 else
-                    xr[i][r] = Cols<T>::load(static_cast<const T*>(a.X) + row * D, c, D);
-                dr[i][r] = Cols<T>::load(static_cast<const T*>(a.dY) + row * D, c, D);
+                    xr[i][r] = Cols<T>::load(static_cast<const T*>(a.X) + row * D, c, D, (a.n - row) * D);
+                dr[i][r] = Cols<T>::load(static_cast<const T*>(a.dY) + row * D, c, D, (a.n - row) * D);
             }
         }
 #pragma unroll
@@ -216,8 +221,8 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(BwdArgs a)
             for (int r = 0; r < R; ++r) {
                 const int c = (t + r * TPR) * N;
                 if constexpr (PACKED) PackedCols<N>::values(xp[i][r], c, packed_stride(D), x[i][r]);
-                else Cols<T>::values(xr[i][r], c, D, x[i][r]);
-                Cols<T>::values(dr[i][r], c, D, dy[i][r]);
+                else Cols<T>::values(xr[i][r], within[r], x[i][r]);
+                Cols<T>::values(dr[i][r], within[r], dy[i][r]);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
                     // (dy is zero behind a row's end; x is not looked at there, nor in a row that is not there)

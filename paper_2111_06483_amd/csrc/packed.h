@@ -59,8 +59,9 @@ __device__ inline uint32_t lanes_max(uint32_t v)
     return v;
 }
 
-// A piece of 16 bytes of a row of D values, from column c on, as fp32; zeros behind the row's end.  The last piece of a row that is no
-// whole number of pieces is read where the row ends and moved to its front; rows of less than a piece are read value by value.
+// A piece of 16 bytes of a row of D values, from column c on, as fp32; zeros behind the row's end.  A row's last piece may end in the next
+// row; where there is none (`left`: values from the row's beginning to the tensor's end), it is read where the row ends and moved to its front, or,
+// of rows of less than a piece, value by value.
 template <typename T>
 struct Cols {
     static constexpr int N = 16 / (int)sizeof(T);
@@ -72,23 +73,37 @@ struct Cols {
             Vec<bf16_t>::unpack(r, v);
         }
     }
-    // (the load and what is done with it apart, so that a thread can have several under way)
-    static __device__ inline uint4 load(const T* row, int c, int D)
+    // (the load and what is done with it apart, so that a thread can have several under way; lanes behind the row read its first piece)
+    static __device__ inline uint4 load(const T* row, int c, int D, int64_t left)
     {
-        if (D >= N) return load16(row + min(c, D - N));
+        if (c >= D) c = 0;
+        if (c + N <= left) return load16(row + c);
+        if (D >= N) return front_of_piece<T>(load16(row + D - N), D - c);
         T one[N] = {};
 #pragma unroll
         for (int j = 0; j < N; ++j)
             if (c + j < D) one[j] = row[c + j];
         return __builtin_bit_cast(uint4, one);
     }
-    static __device__ inline void values(uint4 r, int c, int D, float (&v)[N])
+    // What a piece's words have within the row.
+    static __device__ inline uint4 within(int c, int D)
     {
-        if (c + N > D) {
-            if (c >= D) r = make_uint4(0u, 0u, 0u, 0u);
-            else if (D >= N) r = front_of_piece<T>(r, D - c);
+        uint32_t m[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (N == 4) m[k] = c + k < D ? 0xffffffffu : 0u;
+            else m[k] = c + 2 * k + 1 < D ? 0xffffffffu : c + 2 * k < D ? 0xffffu : 0u;
         }
-        unpack(r, v);
+        return make_uint4(m[0], m[1], m[2], m[3]);
+    }
+    static __device__ inline void values(const uint4& r, const uint4& m, float (&v)[N])
+    {
+        unpack(make_uint4(r.x & m.x, r.y & m.y, r.z & m.z, r.w & m.w), v);
+    }
+    static __device__ inline void values(const uint4& r, int c, int D, float (&v)[N])
+    {
+        if (c + N <= D) unpack(r, v);
+        else values(r, within(c, D), v);
     }
     static __device__ inline uint4 round(const float (&v)[N])
     {
@@ -99,12 +114,28 @@ struct Cols {
     }
     static __device__ inline void store(T* row, int c, int D, const float (&v)[N])
     {
+        const uint4 r = round(v);
         if (c + N <= D) {
-            store16(row + c, round(v));
-        } else {
-#pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (c + j < D) row[c + j] = from_f32<T>(v[j]);
+            store16(row + c, r);
+        } else if (c < D) {
+            // the rest of a row, the same for all rows: 8, 4 and 2 bytes
+            struct __attribute__((packed, aligned(2))) U2 { uint32_t x, y; };
+            struct __attribute__((packed, aligned(2))) U1 { uint32_t x; };
+            uint32_t w[4] = {r.x, r.y, r.z, r.w};
+            const int rest = D % N;
+            constexpr int kPer = 4 / (int)sizeof(T);
+            T* p = row + c;
+            if (rest & (2 * kPer)) {
+                *reinterpret_cast<U2*>(p) = U2{w[0], w[1]};
+                p += 2 * kPer, w[0] = w[2], w[1] = w[3];
+            }
+            if (rest & kPer) {
+                reinterpret_cast<U1*>(p)->x = w[0];
+                p += kPer, w[0] = w[1];
+            }
+            if constexpr (kPer == 2) {
+                if (rest & 1) *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+            }
         }
     }
 };

@@ -43,7 +43,7 @@ __global__ __launch_bounds__(kThreads) void k_packed(T* X, int8_t* q, uint8_t* e
         c[u] = (int)(at - r * per_row) * N;
         // (rows behind the last one are read as the last one: the lanes of a block stay together)
         const int64_t i = min(row[u], n - 1);
-        if constexpr (PACK) x[u] = Cols<T>::load(X + i * K, c[u], K);
+        if constexpr (PACK) x[u] = Cols<T>::load(X + i * K, c[u], K, (n - i) * K);
         else y[u] = PackedCols<N>::load(q + i * stride, e + i * steps, c[u], stride);
     }
 #pragma unroll
