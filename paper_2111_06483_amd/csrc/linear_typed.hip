@@ -561,6 +561,174 @@ __global__ __launch_bounds__(512, 2) void k_typed_tall(RowsArgs a)
     }
 }
 
+// ---- few rows
+//
+// Here a call is latency: one launch, a wavefront for every 32 x 32 outputs, operands from memory to registers in chunks of 64 contraction
+// values, a chunk ahead, weights cut into pieces where they are multiplied.  (2000 x 128 -> 128, bf16, 4 types: 10 us by two launches as above.)
+// (Forward, 256 -> 256, 8 thousand rows, 2032 blocks: fp32 21.6 us here and 23.4 by two launches, bf16 12.1 and 15.0; 16 thousand rows 37.6 and 26.9,
+// 21.3 and 17.1.)
+constexpr int kFewBlocks = 2560;
+struct FewArgs {
+    const void* A;         // [n, C]
+    const float* W;        // [T, K, F]
+    void* out;             // [n, N]
+    Types types;
+    int C, N, K, F;
+};
+
+// Which rows: block `index` of 32 of a type, type after type; false behind the last one.
+__device__ inline bool few_rows_of(const Types& types, int64_t index, int& t, int64_t& first, int64_t& end)
+{
+    const int lane = threadIdx.x & 63;
+    for (int base = 0; base < types.T; base += 64) {
+        int64_t lo = 0, hi = 0;
+        if (base + lane < types.T) types.span(base + lane, lo, hi);
+        const int mine = (int)((hi - lo + 31) / 32);
+        int upto = mine;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(upto, o);
+            if (lane >= o) upto += v;
+        }
+        const uint64_t here = __ballot(index < upto);
+        if (here) {
+            const int l = __builtin_ctzll(here);
+            t = __builtin_amdgcn_readfirstlane(base + l);
+            first = __builtin_amdgcn_readfirstlane(__shfl((int)(lo + (index - (upto - mine)) * 32), l));      // (rows are fewer than 2^31)
+            end = __builtin_amdgcn_readfirstlane(__shfl((int)hi, l));
+            return true;
+        }
+        index -= __shfl(upto, 63);
+    }
+    return false;
+}
+
+template <typename T, bool TRANS>
+__global__ __launch_bounds__(256, 2) void k_typed_few(FewArgs a)
+{
+    constexpr int N = Cols<T>::N, kRaw = 8 / N, U = 4;                // 16-byte pieces of a row a product of 16; products a chunk
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const int n0 = (blockIdx.y * 4 + (threadIdx.x >> 6)) * 32, n = n0 + (lane & 31);
+    int t;
+    int64_t first, end;
+    if (n0 >= a.N || !few_rows_of(a.types, blockIdx.x, t, first, end)) return;
+    const int64_t i = min(first + (lane & 31), end - 1);
+    const T* row = static_cast<const T*>(a.A) + i * a.C;
+    const int64_t left = (a.types.n - i) * a.C;
+    const float* W = a.W + (int64_t)t * a.K * a.F;
+    const int nc = min(n, a.N - 1);
+    struct Chunk {
+        uint4 x[U][kRaw];
+        float w[U][8];
+    };
+    auto load = [&](Chunk& g, int k0) SAR_INLINE {
+        const float* w = TRANS ? W + (int64_t)nc * a.F : W + nc;
+        if (k0 + 16 * U <= a.C) {          // the same for all lanes: one run of loads
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int c = k0 + u * 16 + h * 8;
+#pragma unroll
+                for (int p = 0; p < kRaw; ++p) g.x[u][p] = load16(row + c + p * N);
+                if constexpr (TRANS) {
+#pragma unroll
+                    for (int j = 0; j < 8; j += 4) {
+                        const uint4 v = load16(w + c + j);
+                        g.w[u][j] = __uint_as_float(v.x), g.w[u][j + 1] = __uint_as_float(v.y);
+                        g.w[u][j + 2] = __uint_as_float(v.z), g.w[u][j + 3] = __uint_as_float(v.w);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) g.w[u][j] = w[(int64_t)(c + j) * a.F];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int c = k0 + u * 16 + h * 8;
+#pragma unroll
+                for (int p = 0; p < kRaw; ++p) g.x[u][p] = Cols<T>::load(row, c + p * N, a.C, left);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) g.w[u][j] = w[(int64_t)min(c + j, a.C - 1) * (TRANS ? 1 : a.F)];
+            }
+        }
+    };
+    float16_t acc[1] = {};
+    auto multiply = [&](const Chunk& g, int k0) SAR_INLINE {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = k0 + u * 16 + h * 8;
+            if (k0 + u * 16 >= a.C) break;
+            float w[8], x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = c + j < a.C ? g.w[u][j] : 0.f;
+            if constexpr (sizeof(T) == 4) {
+                float lo[4], hi[4];
+                Cols<T>::values(g.x[u][0], c, a.C, lo);
+                Cols<T>::values(g.x[u][1 % kRaw], c + 4, a.C, hi);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = lo[j], x[4 + j] = hi[j];
+                uint4 p[3], q[3];
+                split8(x, p);
+                split8(w, q);
+                float16_t sum;
+                multiply_split(p, q, sum);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[0][r] += sum[r];
+            } else {
+                const uint4 m = Cols<T>::within(c, a.C), v = g.x[u][0];
+                const uint4 p = make_uint4(v.x & m.x, v.y & m.y, v.z & m.z, v.w & m.w);
+                uint32_t big[4], small[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    big[j] = pack2_bf16(w[2 * j], w[2 * j + 1]);
+                    small[j] = pack2_bf16(w[2 * j] - __uint_as_float(big[j] << 16), w[2 * j + 1] - __uint_as_float(big[j] & 0xffff0000u));
+                }
+                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p), __builtin_bit_cast(bf16x8_t, make_uint4(small[0], small[1], small[2], small[3])), acc[0], 0, 0, 0);
+                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p), __builtin_bit_cast(bf16x8_t, make_uint4(big[0], big[1], big[2], big[3])), acc[0], 0, 0, 0);
+            }
+        }
+    };
+    Chunk g[2];
+    load(g[0], 0);
+    for (int k0 = 0; k0 < a.C; k0 += 32 * U) {
+        if (k0 + 16 * U < a.C) load(g[1], k0 + 16 * U);
+        multiply(g[0], k0);
+        if (k0 + 16 * U >= a.C) break;
+        if (k0 + 32 * U < a.C) load(g[0], k0 + 32 * U);
+        multiply(g[1], k0 + 16 * U);
+    }
+    if (__any(not_finite(acc[0]))) {
+        acc[0] = float16_t{};
+        for (int k = 0; k < a.C; k += 2) {
+            const bool in = k + h < a.C;
+            float x = 0.f, w = 0.f;
+            if (in) {
+                if constexpr (sizeof(T) == 4) x = row[k + h];
+                else x = bf16_to_f32(row[k + h]);
+                w = TRANS ? W[(int64_t)nc * a.F + k + h] : W[(int64_t)(k + h) * a.F + nc];
+            }
+            acc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w, acc[0], 0, 0, 0);
+        }
+    }
+    if (n >= a.N) return;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int64_t o = first + 8 * (r / 4) + 4 * h + r % 4;
+        if (o < end) static_cast<T*>(a.out)[o * a.N + n] = from_f32<T>(acc[0][r]);
+    }
+}
+
+template <typename T, bool TRANS>
+int few_product(const FewArgs& a, hipStream_t st)
+{
+    const int64_t groups = a.types.n / 32 + a.types.T;
+    k_typed_few<T, TRANS><<<dim3((unsigned)groups, (a.N + 127) / 128), 256, 0, st>>>(a);
+    SAR_LAUNCH_CHECK();
+    return SAR_OK;
+}
+// Whether a product's blocks of 32 x 32 outputs, whose wavefronts read all the weights they need anew, are few.
+bool few_blocks(const Types& types, int N) { return (types.n / 32 + types.T) * ((N + 31) / 32) <= kFewBlocks; }
+
 // Column tiles a wavefront forms at once.
 int tiles_of(int64_t n, int N)
 {
@@ -607,6 +775,7 @@ template <typename T, bool TRANS>
 int rows_product(const void* A, const float* W, const Types& types, void* out, int K, int F, void* work, hipStream_t st)
 {
     const int C = TRANS ? F : K, N = TRANS ? K : F, NT = tiles_of(types.n, N);
+    if (few_blocks(types, N)) return few_product<T, TRANS>({A, W, out, types, C, N, K, F}, st);
     const int chunks = (C + kChunk<T> - 1) / kChunk<T>, blocks = (N + 32 * NT - 1) / (32 * NT);
     const int64_t most = most_tiles(types.n, types.T);
     int4* const list = static_cast<int4*>(work);

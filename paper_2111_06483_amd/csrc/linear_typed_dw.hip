@@ -375,20 +375,26 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
             }
 
             float* out = a.partial + ((int64_t)blockIdx.x + t) * a.K * a.F;
-            // lane holds column f; register r holds the weight's row at place 8*(r/4) + 4*h + r%4.  (The places are worked out here: carried
-            // through the loops they are registers that the sums need.)
+            // lane holds column f (of two neighbouring tiles: f and f + 1); register r holds the weight's row at place 8*(r/4) + 4*h + r%4.  (The
+            // places are worked out here: carried through the loops they are registers that the sums need.)
             int own = lane;
             asm volatile("" : "+v"(own));
+            struct __attribute__((packed, aligned(4))) Two { float x, y; };
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int k = k0 + column_at((wm * MT + m) * 32 + 8 * (r / 4) + 4 * (own >> 5) + r % 4);
                     if (k >= a.K) continue;
+                    float* to = out + (int64_t)k * a.F;
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         const int f = f0 + column_at((wn * NT + n) * 32 + (own & 31));
-                        if (f < a.F) out[(int64_t)k * a.F + f] = acc[m][n][r];
+                        if (NT > 1 && n % 2 == 0 && f + 1 < a.F) {
+                            *reinterpret_cast<Two*>(to + f) = Two{acc[m][n][r], acc[m][NT > 1 ? n + 1 : n][r]};
+                        } else if ((NT == 1 || n % 2 == 0) && f < a.F) {
+                            to[f] = acc[m][n][r];
+                        }
                     }
                 }
         }
@@ -461,6 +467,103 @@ __global__ __launch_bounds__(256) void k_typed_sum(DwArgs a, int accumulate, flo
     }
 }
 
+// ---- few rows
+//
+// One launch: a workgroup for 32 x 32 weights of a type, whose four wavefronts take every fourth 16 of the type's rows straight from memory
+// (lanes are columns: whole lines), add up their sums in LDS and write dW.
+constexpr int64_t kFewRows = 2048, kFewColumns = 1 << 18;
+template <typename XR, typename ZR>
+__global__ __launch_bounds__(256, 2) void k_typed_dw_few(DwArgs a, int accumulate, float* dW)
+{
+    constexpr int PX = XR::kPieces, PZ = ZR::kPieces, U = 2;          // products of 16 rows a step
+    __shared__ float part[4][16][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const int k0 = blockIdx.x * 32, f0 = blockIdx.y * 32, t = blockIdx.z;
+    const int k = min(k0 + (lane & 31), a.K - 1), f = min(f0 + (lane & 31), a.F - 1);
+    int64_t lo, hi;
+    a.types.span(t, lo, hi);
+    float16_t acc = {};
+    struct Step {
+        float x[U][8], z[U][8];
+    };
+    auto load = [&](Step& s, int64_t r0) SAR_INLINE {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int64_t r = min(r0 + u * 64 + h * 8 + j, hi - 1);
+                s.x[u][j] = x_value<XR>(a, r, k);
+                s.z[u][j] = z_value<ZR>(a, r, f);
+            }
+    };
+    auto multiply = [&](Step& s, int64_t r0) SAR_INLINE {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (r0 + u * 64 >= hi) break;
+            float x[8], z[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool in = r0 + u * 64 + h * 8 + j < hi;
+                x[j] = in ? s.x[u][j] : 0.f, z[j] = in ? s.z[u][j] : 0.f;
+            }
+            uint4 p[3], q[3];
+            auto whole = [](const float (&v)[8]) SAR_INLINE {        // (bf16 values: not rounded)
+                return make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
+            };
+            if constexpr (PX == 3) split8(x, p);
+            else p[0] = whole(x);
+            if constexpr (PZ == 3) split8(z, q);
+            else q[0] = whole(z);
+            float16_t sum = {};
+#pragma unroll
+            for (int i = 0; i < 6; ++i)
+                if (kTerm[i][0] < PX && kTerm[i][1] < PZ)
+                    sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[kTerm[i][0] < PX ? kTerm[i][0] : 0]),
+                                                                  __builtin_bit_cast(bf16x8_t, q[kTerm[i][1] < PZ ? kTerm[i][1] : 0]), sum, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[r] += sum[r];
+        }
+    };
+    const int64_t from = lo + wave * 16;
+    constexpr int kNext = U * 64;
+    if (from < hi) {
+        Step s[2];
+        load(s[0], from);
+        for (int64_t r0 = from; r0 < hi; r0 += 2 * kNext) {
+            if (r0 + kNext < hi) load(s[1], r0 + kNext);
+            multiply(s[0], r0);
+            if (r0 + kNext >= hi) break;
+            if (r0 + 2 * kNext < hi) load(s[0], r0 + 2 * kNext);
+            multiply(s[1], r0 + kNext);
+        }
+        if (PZ == 3 && __any(not_finite(acc))) {
+            acc = float16_t{};
+            for (int64_t r0 = from; r0 < hi; r0 += 64)
+                for (int64_t r = r0; r < min(r0 + 16, hi); r += 2) {
+                    const bool in = r + h < hi;
+                    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(in ? x_value<XR>(a, r + h, k) : 0.f, in ? z_value<ZR>(a, r + h, f) : 0.f, acc, 0, 0, 0);
+                }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) part[wave][r][lane] = acc[r];
+    __syncthreads();
+    // lane holds column f; register r holds weight row 8*(r/4) + 4*h + r%4: four registers a wavefront
+    if (f0 + (lane & 31) >= a.F) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = wave * 4 + j, row = k0 + 8 * (r / 4) + 4 * h + r % 4;
+        if (row >= a.K) continue;
+        const float v = (part[0][r][lane] + part[1][r][lane]) + (part[2][r][lane] + part[3][r][lane]);
+        float* out = dW + ((int64_t)t * a.K + row) * a.F + f;
+        *out = accumulate ? *out + v : v;
+    }
+}
+
+// Whether it takes a call: all of the rows may be of one type, whose workgroups then read 64 of them in a step of theirs, and every 32 x 32 weights
+// read their columns anew.
+bool few_rows_dw(int64_t n, int K, int F) { return n <= kFewRows && n * ((K + 31) / 32) * ((F + 31) / 32) <= kFewColumns; }
+
 // The tile of sums of a workgroup, its rows, and how many workgroups of the kernel a compute unit holds.
 struct Shape {
     int tk, tf, tiles;
@@ -499,6 +602,11 @@ int run(const DwArgs& a, const Shape& s, hipStream_t st)
 template <typename XR, typename ZR, int S, int W>
 int run_all(const DwArgs& a, const Shape& s, int accumulate, float* dW, hipStream_t st)
 {
+    if (few_rows_dw(a.types.n, a.K, a.F)) {
+        k_typed_dw_few<XR, ZR><<<dim3((a.K + 31) / 32, (a.F + 31) / 32, a.types.T), 256, 0, st>>>(a, accumulate, dW);
+        SAR_LAUNCH_CHECK();
+        return SAR_OK;
+    }
     if (a.types.n > 0) {
         if (s.tk == 256) SAR_TRY((run<XR, ZR, 4, 2, 2, 2, S, W>(a, s, st)));
         else if (s.tf == 256) SAR_TRY((run<XR, ZR, 2, 4, 2, 2, S, W>(a, s, st)));
