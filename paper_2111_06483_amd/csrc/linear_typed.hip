@@ -567,7 +567,7 @@ __global__ __launch_bounds__(512, 2) void k_typed_tall(RowsArgs a)
 // values, a chunk ahead, weights cut into pieces where they are multiplied.  (2000 x 128 -> 128, bf16, 4 types: 10 us by two launches as above.)
 // (Forward, 256 -> 256, 8 thousand rows, 2032 blocks: fp32 21.6 us here and 23.4 by two launches, bf16 12.1 and 15.0; 16 thousand rows 37.6 and 26.9,
 // 21.3 and 17.1.)
-constexpr int kFewBlocks = 2560;
+constexpr int kFewBlocks = 2560, kFewShared = 1024;
 struct FewArgs {
     const void* A;         // [n, C]
     const float* W;        // [T, K, F]
@@ -603,12 +603,16 @@ __device__ inline bool few_rows_of(const Types& types, int64_t index, int& t, in
     return false;
 }
 
-template <typename T, bool TRANS>
+// PARTS: wavefronts that share one block's contraction, chunk by chunk, and add up in LDS (4), or one a block (1).
+template <typename T, bool TRANS, int PARTS>
 __global__ __launch_bounds__(256, 2) void k_typed_few(FewArgs a)
 {
     constexpr int N = Cols<T>::N, kRaw = 8 / N, U = 4;                // 16-byte pieces of a row a product of 16; products a chunk
-    const int lane = threadIdx.x & 63, h = lane >> 5;
-    const int n0 = (blockIdx.y * 4 + (threadIdx.x >> 6)) * 32, n = n0 + (lane & 31);
+    __shared__ float part[PARTS == 4 ? 4 : 1][16][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const int n0 = (PARTS == 4 ? blockIdx.y : blockIdx.y * 4 + wave) * 32, n = n0 + (lane & 31);
+    const int k_from = PARTS == 4 ? wave * 16 * U : 0;
+    constexpr int kTurn = PARTS * 16 * U;
     int t;
     int64_t first, end;
     if (n0 >= a.N || !few_rows_of(a.types, blockIdx.x, t, first, end)) return;
@@ -688,33 +692,47 @@ __global__ __launch_bounds__(256, 2) void k_typed_few(FewArgs a)
             }
         }
     };
-    Chunk g[2];
-    load(g[0], 0);
-    for (int k0 = 0; k0 < a.C; k0 += 32 * U) {
-        if (k0 + 16 * U < a.C) load(g[1], k0 + 16 * U);
-        multiply(g[0], k0);
-        if (k0 + 16 * U >= a.C) break;
-        if (k0 + 32 * U < a.C) load(g[0], k0 + 32 * U);
-        multiply(g[1], k0 + 16 * U);
-    }
-    if (__any(not_finite(acc[0]))) {
-        acc[0] = float16_t{};
-        for (int k = 0; k < a.C; k += 2) {
-            const bool in = k + h < a.C;
-            float x = 0.f, w = 0.f;
-            if (in) {
-                if constexpr (sizeof(T) == 4) x = row[k + h];
-                else x = bf16_to_f32(row[k + h]);
-                w = TRANS ? W[(int64_t)nc * a.F + k + h] : W[(int64_t)(k + h) * a.F + nc];
-            }
-            acc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w, acc[0], 0, 0, 0);
+    if (k_from < a.C) {
+        Chunk g[2];
+        load(g[0], k_from);
+        for (int k0 = k_from; k0 < a.C; k0 += 2 * kTurn) {
+            if (k0 + kTurn < a.C) load(g[1], k0 + kTurn);
+            multiply(g[0], k0);
+            if (k0 + kTurn >= a.C) break;
+            if (k0 + 2 * kTurn < a.C) load(g[0], k0 + 2 * kTurn);
+            multiply(g[1], k0 + kTurn);
+        }
+        if (__any(not_finite(acc[0]))) {
+            acc[0] = float16_t{};
+            for (int k0 = k_from; k0 < a.C; k0 += kTurn)
+                for (int k = k0; k < min(k0 + 16 * U, a.C); k += 2) {
+                    const bool in = k + h < a.C;
+                    float x = 0.f, w = 0.f;
+                    if (in) {
+                        if constexpr (sizeof(T) == 4) x = row[k + h];
+                        else x = bf16_to_f32(row[k + h]);
+                        w = TRANS ? W[(int64_t)nc * a.F + k + h] : W[(int64_t)(k + h) * a.F + nc];
+                    }
+                    acc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w, acc[0], 0, 0, 0);
+                }
         }
     }
-    if (n >= a.N) return;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
+    auto store = [&](int r, float v) SAR_INLINE {
         const int64_t o = first + 8 * (r / 4) + 4 * h + r % 4;
-        if (o < end) static_cast<T*>(a.out)[o * a.N + n] = from_f32<T>(acc[0][r]);
+        if (n < a.N && o < end) static_cast<T*>(a.out)[o * a.N + n] = from_f32<T>(v);
+    };
+    if constexpr (PARTS == 4) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) part[wave][r][lane] = acc[0][r];
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int r = wave * 4 + j;
+            store(r, (part[0][r][lane] + part[1][r][lane]) + (part[2][r][lane] + part[3][r][lane]));
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) store(r, acc[0][r]);
     }
 }
 
@@ -722,7 +740,12 @@ template <typename T, bool TRANS>
 int few_product(const FewArgs& a, hipStream_t st)
 {
     const int64_t groups = a.types.n / 32 + a.types.T;
-    k_typed_few<T, TRANS><<<dim3((unsigned)groups, (a.N + 127) / 128), 256, 0, st>>>(a);
+    // (four wavefronts a block where that is no more than four a SIMD: 2000 rows 256 -> 256, fp32, 544 blocks 9.2 us, one a block 13.0; 8000 rows 25.2 and
+    // 21.4)
+    if (a.C > 64 && groups * ((a.N + 31) / 32) <= kFewShared)
+        k_typed_few<T, TRANS, 4><<<dim3((unsigned)groups, (a.N + 31) / 32), 256, 0, st>>>(a);
+    else
+        k_typed_few<T, TRANS, 1><<<dim3((unsigned)groups, (a.N + 127) / 128), 256, 0, st>>>(a);
     SAR_LAUNCH_CHECK();
     return SAR_OK;
 }
