@@ -100,7 +100,14 @@ def test_shapes(K, F, dtype, packed):
 
 
 @pytest.mark.parametrize("dtype,packed", KINDS)
-@pytest.mark.parametrize("K,F", [(100, 256), (256, 256), (72, 60)])
+@pytest.mark.parametrize("K,F", [(1, 1), (1, 40), (3, 2), (7, 9), (16, 47), (31, 33), (47, 65), (63, 100), (64, 129), (129, 31)])
+def test_shapes_by_the_kernels_of_many_rows(K, F, dtype, packed):
+    """Ragged widths where the calls of few rows are not taken: both products of rows, and the weights' gradients in shares."""
+    check_all(85_003, K, F, [0, 100, 101, 101, 40_000, 85_000], dtype, packed)
+
+
+@pytest.mark.parametrize("dtype,packed", KINDS)
+@pytest.mark.parametrize("K,F", [(100, 256), (256, 256), (72, 60), (4, 264), (520, 100), (8, 1000), (300, 130), (99, 256), (250, 88)])
 def test_many_rows(K, F, dtype, packed):
     """Enough rows for the wide tiles, several chunks a workgroup, types that end anywhere in a workgroup's rows."""
     n = 140_003
@@ -194,30 +201,48 @@ def test_sums_lean_to_no_side():
         assert off.std() <= 1e-6 * np.sqrt(n)
 
 
-@pytest.mark.parametrize("dtype,packed", [(F32, False), (BF16, False)])
-def test_infinities_and_nan_stay_where_they_belong(dtype, packed):
-    n, K, F = 300, 40, 50
+def with_specials(a, b):
+    """a b where both have infinities and NaN: the finite part by a product, every special number's terms one by one."""
+    fa, fb = np.where(np.isfinite(a), a, 0.0), np.where(np.isfinite(b), b, 0.0)
+    want, size = fa @ fb, np.abs(fa) @ np.abs(fb)
+    with np.errstate(invalid="ignore"):
+        for i, k in np.argwhere(~np.isfinite(a)):
+            want[i] += a[i, k] * b[k]
+        for k, j in np.argwhere(~np.isfinite(b)):
+            rest = np.isfinite(a[:, k])
+            want[rest, j] += a[rest, k] * b[k, j]
+    return want, size
+
+
+# (rows, widths): calls of few rows, of many in blocks of 128 (a width that is no whole piece) and of 256
+@pytest.mark.parametrize("n,K,F", [(300, 40, 50), (2000, 256, 130), (70_000, 101, 256), (70_000, 256, 128)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_infinities_and_nan_stay_where_they_belong(n, K, F, dtype):
     X, dZ, W = inputs(n, K, F, 2, dtype)
     X[7, 3] = float("inf")
-    X[200, 5] = float("nan")
+    X[n - 100, 5] = float("nan")
     dZ[9, 4] = -float("inf")
+    dZ[n // 2, 0] = float("inf")
     W = W.clone()
     W[1, 6, 8] = float("inf")
-    ends = [0, 150, n]
+    ends = [0, n // 2, n]
     ptr, work = ptr_of(ends), work_for(n, K, F, 2)
     Z, dX, dW = torch.empty(n, F, dtype=dtype, device="cuda"), torch.empty_like(X), torch.empty_like(W)
     sar.sar_linear_typed_fwd(X, W, ptr, Z, work)
     sar.sar_linear_typed_bwd(X, dZ, W, ptr, False, dW, dX, work)
     x, d, w = nw.f64(X), nw.f64(dZ), nw.f64(W)
-    with np.errstate(invalid="ignore"):
-        for t, lo, hi in nw.spans(ends, n):
-            for got, a, b in ((nw.f64(Z)[lo:hi], x[lo:hi], w[t]), (nw.f64(dX)[lo:hi], d[lo:hi], w[t].T), (nw.f64(dW)[t], x[lo:hi].T, d[lo:hi])):
-                want = (a[:, :, None] * b[None, :, :]).sum(1)            # (term by term: a library product may differ here)
-                fine = np.isfinite(want)
-                assert np.array_equal(got[~fine], want[~fine], equal_nan=True)
-                size = (np.abs(np.where(np.isfinite(a), a, 0)) @ np.abs(np.where(np.isfinite(b), b, 0)))
-                tol = (80 + a.shape[1] / 32) * 2 * nw.U * size + (0 if dtype == F32 else 2.0 ** -16 * size + 2.0 ** -8 * (np.abs(np.where(fine, want, 0)) + size * 2.0 ** -8))
-                assert (np.abs(got - want)[fine] <= tol[fine]).all()
+    for t, lo, hi in nw.spans(ends, n):
+        for got, a, b, rounded in ((nw.f64(Z)[lo:hi], x[lo:hi], w[t], True), (nw.f64(dX)[lo:hi], d[lo:hi], w[t].T, True),
+                                   (nw.f64(dW)[t], x[lo:hi].T, d[lo:hi], False)):
+            want, size = with_specials(a, b)
+            fine = np.isfinite(want)
+            assert np.array_equal(got[~fine], want[~fine], equal_nan=True)
+            off = rows_off(size, a.shape[1], dtype) if rounded else dw_off(size, a.shape[1])
+            # (a tile that is taken again adds its products one by one)
+            off = off + a.shape[1] * nw.U * size
+            if rounded and dtype == BF16:
+                off = off + nw.half_step(dtype)(np.abs(np.where(fine, want, 0)) + off)
+            assert (np.abs(got - want)[fine] <= off[fine]).all()
 
 
 def test_the_largest_and_the_smallest_numbers():
@@ -256,6 +281,37 @@ def test_tensors_that_begin_anywhere_and_neighbours(dtype):
     check_rows(dZ, W, v["dx"], spans, dtype, True)
     check_dw(nw.f64(X), dZ, v["dw"], spans)
     assert all(float(r[0]) == 6 and bool((r[-4:] == 6).all()) for r in room.values())
+
+
+# Which kernels take a call: few rows; blocks of 128 rows where a row is no whole number of 16-byte pieces or begins anywhere; blocks of 256.
+@pytest.mark.parametrize("n,K,F,dtype,fwd,dw", [
+    (2000, 128, 128, BF16, "k_typed_few", "k_typed_dw_few"), (2048, 64, 64, F32, "k_typed_few", "k_typed_dw_few"),
+    (2049, 64, 64, F32, "k_typed_few", "k_typed_dw<"), (1500, 512, 512, F32, "k_typed_few", "k_typed_dw<"), (40_000, 64, 64, F32, "k_typed_few", "k_typed_dw<"),
+    (41_000, 64, 64, F32, "k_typed_rows", "k_typed_dw<"), (70_000, 100, 256, F32, "k_typed_tall", "k_typed_dw<"), (70_000, 102, 256, F32, "k_typed_rows", "k_typed_dw<"),
+    (70_000, 100, 256, BF16, "k_typed_rows", "k_typed_dw<"), (70_000, 104, 256, BF16, "k_typed_tall", "k_typed_dw<"), (66_000, 256, 100, F32, "k_typed_rows", "k_typed_dw<")])
+def test_which_kernels_run(n, K, F, dtype, fwd, dw):
+    from tests import gpu_util as gu
+    X, dZ, W = inputs(n, K, F, 1, dtype)
+    ptr, work, Z, dW = ptr_of([0, n]), work_for(n, K, F, 1), torch.empty(n, F, dtype=dtype, device="cuda"), torch.empty_like(W)
+    names = gu.kernels_of(lambda: sar.sar_linear_typed_fwd(X, W, ptr, Z, work))
+    assert fwd in names and sum(k in names for k in ("k_typed_few", "k_typed_rows", "k_typed_tall")) == 1, names
+    names = gu.kernels_of(lambda: sar.sar_linear_typed_bwd(X, dZ, W, ptr, False, dW, None, work))
+    assert dw in names, names
+    check_rows(X, W, Z, [(0, 0, n)], dtype, False)
+    check_dw(nw.f64(X), dZ, dW, [(0, 0, n)])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_many_rows_that_begin_anywhere(dtype):
+    """As blocks of 256 rows would be taken, were the first value on a 16-byte boundary."""
+    n, K, F = 70_000, 128, 256
+    X, dZ, W = inputs(n, K, F, 1, dtype)
+    room = torch.empty(n * K + 1, dtype=dtype, device="cuda")
+    x = room[1:].view(n, K)
+    x.copy_(X)
+    ptr, work, Z = ptr_of([0, n]), work_for(n, K, F, 1), torch.empty(n, F, dtype=dtype, device="cuda")
+    sar.sar_linear_typed_fwd(x, W, ptr, Z, work)
+    check_rows(X, W, Z, [(0, 0, n)], dtype, False)
 
 
 def test_the_same_in_every_run():

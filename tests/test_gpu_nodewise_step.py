@@ -85,9 +85,10 @@ def test_a_layer(n, K, F, ends, dtype):
         assert norm(nw.f64(got) - want) <= (2.0 ** -6 + 2 * nw.HALF[dtype]) * norm(want)
 
 
-def test_a_replayed_graph_and_an_eager_layer_beside_it():
+@pytest.mark.parametrize("n,K,F", [(500, 96, 64), (5000, 200, 70), (70_000, 128, 256)])
+def test_a_replayed_graph_and_an_eager_layer_beside_it(n, K, F):
     """Two layers recorded into one graph share their scratch, one after the other; between the replays the same calls run eagerly."""
-    a, b = (Layer(5000, 96, 64, [0, 2000, 2000, 4990], dt, seed=k) for k, dt in enumerate([torch.float32, torch.bfloat16]))
+    a, b = (Layer(n, K, F, [0, n // 3, n // 3, n - 10], dt, seed=k) for k, dt in enumerate([torch.float32, torch.bfloat16]))
     size = max(a.lwork.numel(), b.lwork.numel())
     a.lwork = b.lwork = torch.empty(size, dtype=torch.uint8, device="cuda")
     a.step(), b.step()                                           # (a first call of each kernel outside the recording)
