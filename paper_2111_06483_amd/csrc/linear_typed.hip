@@ -1,18 +1,20 @@
 // Products of rows with the weight of their type: Z = X W_t and dX = dZ W_t^T for rows sorted by type, of any numbers.
 //
-// Both are rows (contraction index contiguous) times a small operand B [C, N] per type, and bound by memory at these widths (256 x 256: 64
-// multiply-adds a byte of fp32 rows) as long as the matrix cores are fed without a pause:
-//   - A first launch lays B out in pieces of bf16, in the order in which a wavefront's lanes want them: fp32 rows three pieces a weight (exact
-//     products, linear_pieces.h), bf16 rows two (the weight to 16 bits).  T K F values, against n (K + F) in the main launch.
-//   - A workgroup of 8 wavefronts takes 256 rows of one type and up to 256 columns; a wavefront 32 rows, whose values go from memory to registers
-//     (a lane holds 64 bytes of a row's 128: whole lines), one chunk ahead; B's chunks go to LDS by asynchronous copies that take no
-//     registers, one chunk ahead as well, with one barrier a chunk.
+// Both are rows (contraction index contiguous) times a small operand B [C, N] per type.  Three kernels:
+//   - Few rows (k_typed_few): latency.  One launch, a wavefront or four for every 32 x 32 results.
+//   - Otherwise a first launch (k_typed_lay) lays B out in pieces of bf16, in the order in which a wavefront's lanes want them: fp32 rows three pieces a
+//     weight (exact products, linear_pieces.h), bf16 rows two (the weight to 16 bits), T K F values; and lists the row blocks of every type, as many
+//     as its rows need, which the persistent workgroups of the main launch share.  That is k_typed_rows (blocks of 128 rows, four wavefronts, rows through
+//     registers) or, where rows are whole 16-byte pieces and many, k_typed_tall (256 rows, eight wavefronts, both operands by asynchronous copies).
 //   - Columns are dealt to the column tiles by turns (`column_of`), so that a lane ends up with four neighbours of a row and writes them at once:
 //     a wavefront's store covers whole lines, with no turn through LDS.
-// fp32 sums: the matrix unit cuts (does not round) when it adds, so a chunk's 32 products are summed from zero there and added to the
+// fp32 sums: the matrix unit cuts (does not round) when it adds, so a chunk's 16 products are summed from zero there and added to the
 // running sum by vector instructions, which round to nearest; and every other chunk is multiplied by -B and subtracted, so that what is
-// cut leans to neither side.  A result that is not finite (infinities and NaN have no such pieces, and the largest numbers round to infinity) sends the
-// wavefront's tile back to the fp32 matrix instruction, from the operands themselves.  Operands below 2^-110 in size are taken to within 2^-126.
+// cut leans to neither side.  bf16 products of at most a few hundred terms, whose sums are rounded to 8 bits, are added there.  A result that is not finite
+// (infinities and NaN have no such pieces, and the largest numbers round to infinity) sends the wavefront's tile back to the fp32 matrix instruction, from
+// the operands themselves.  Operands below 2^-110 in size are taken to within 2^-126.
+// What bounds them (256 -> 256, four types): fp32, 237500 rows, 195 us = 160 TFLOP/s: the six products, 958 TFLOP/s of bf16 (a large library product in
+// bf16 reaches 1095, one in fp32 154); bf16, 867187 rows, 278 us: its two products 816 TFLOP/s, its 888 MB 3.2 TB/s, neither alone (207 and 187 us).
 #include <algorithm>
 
 #include "linear_pieces.h"
@@ -564,9 +566,9 @@ __global__ __launch_bounds__(512, 2) void k_typed_tall(RowsArgs a)
 // ---- few rows
 //
 // Here a call is latency: one launch, a wavefront for every 32 x 32 outputs, operands from memory to registers in chunks of 64 contraction
-// values, a chunk ahead, weights cut into pieces where they are multiplied.  (2000 x 128 -> 128, bf16, 4 types: 10 us by two launches as above.)
-// (Forward, 256 -> 256, 8 thousand rows, 2032 blocks: fp32 21.6 us here and 23.4 by two launches, bf16 12.1 and 15.0; 16 thousand rows 37.6 and 26.9,
-// 21.3 and 17.1.)
+// values, a chunk ahead, weights cut into pieces where they are multiplied.  (2000 x 128 -> 128, bf16, 4 types: 4.3 us, 10 by two launches as above.)
+// The line: 256 -> 256, 8 thousand rows, 2032 blocks, fp32 21.1 us here and 23.9 by two launches, bf16 12.4 and 15.1; 16 thousand rows 36.0 and 27.3,
+// 20.8 and 17.0.
 constexpr int kFewBlocks = 2560, kFewShared = 1024;
 struct FewArgs {
     const void* A;         // [n, C]
@@ -752,12 +754,14 @@ int few_product(const FewArgs& a, hipStream_t st)
 // Whether a product's blocks of 32 x 32 outputs, whose wavefronts read all the weights they need anew, are few.
 bool few_blocks(const Types& types, int N) { return (types.n / 32 + types.T) * ((N + 31) / 32) <= kFewBlocks; }
 
-// Column tiles a wavefront forms at once.
+// Column tiles a workgroup forms at once: as few as let all workgroups run at the same time (three a compute unit of two tiles, two of more).
+// 256 -> 256, fp32, by two / four / eight: 16 thousand rows 27.3 / 28.6 / 31.6 us, 32 thousand 42.8 / 34.0 / 34.0, 48 thousand 52.1 / 53.3 / 48.2; bf16
+// 17.0 / 16.9 / 19.7, 22.9 / 20.7 / 20.6, 26.4 / 29.1 / 26.0.  Beyond that eight, so that rows are read once, unless half of them would lie behind the last column.
 int tiles_of(int64_t n, int N)
 {
-    // with few rows, more workgroups of fewer columns: 256 rows a workgroup leave most of the chip idle
-    if (N <= 64 || n * N <= (int64_t)256 * 256 * 128) return 2;
-    return (N + 127) / 128 % 2 ? 4 : 8;
+    auto groups = [&](int tiles) { return (n + kTileRows - 1) / kTileRows * ((N + 32 * tiles - 1) / (32 * tiles)); };
+    if (N <= 64 || groups(2) <= 256 * 3) return 2;
+    return groups(4) <= 256 * 2 || (N + 127) / 128 % 2 ? 4 : 8;
 }
 
 template <typename T, int NT, bool TRANS>
@@ -805,7 +809,8 @@ int rows_product(const void* A, const float* W, const Types& types, void* out, i
     uint4* const pieces = static_cast<uint4*>(work) + (most + 1);
     const RowsArgs a{A, pieces, W, out, list, C, N, chunks, blocks, K, F};
     const LayArgs l{W, pieces, types.T, K, F, C, N, chunks, blocks, types, list, most, 0, 0};
-    // whole 16-byte pieces everywhere, and a block for every compute unit
+    // whole 16-byte pieces everywhere, and a block for every compute unit (256 -> 256: 64 thousand rows, fp32 57.5 us by blocks of 256 and 54.3 of 128, bf16 26.8 and
+    // 28.2; 100 thousand rows 92.0 and 94.2, 41.6 and 43.3)
     const bool tall = NT > 2 && C % Cols<T>::N == 0 && (reinterpret_cast<uintptr_t>(A) & 15) == 0 && types.n >= (int64_t)kTallRows * 256 / blocks;
     return NT == 2 ? run_rows<T, 2, TRANS>(a, l, tall, st) : NT == 4 ? run_rows<T, 4, TRANS>(a, l, tall, st) : run_rows<T, 8, TRANS>(a, l, tall, st);
 }

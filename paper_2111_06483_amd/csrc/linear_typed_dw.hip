@@ -1,18 +1,21 @@
 // Weight gradients by type: dW[t] (+)= X_t^T dZ_t over the rows of every type, X as fp32 or bf16 rows or in 8 bits (packed.h).
 //
-// The contraction runs along the rows, which both operands have as their slow dimension.  A workgroup of 8 wavefronts holds a whole tile of up
-// to 256 x 256 sums in registers, so that at the usual widths every value is read once; its rows come in chunks:
-//   - A thread reads eight rows of two columns (four of packed rows) into registers, one chunk ahead, turns them into bf16 pieces along the rows
-//     (fp32: three, exact; bf16 rows and packed ones, whose values are bf16 values: one) and puts them to LDS as whole fragments: 16 bytes are eight
-//     rows of a column, conflict-free to read.  Two buffers, one barrier a chunk.
+// The contraction runs along the rows, which both operands have as their slow dimension.  A workgroup of four wavefronts holds a tile of 128 x 256
+// (256 x 128, 128 x 128, 128 x 64, 64 x 128) sums in registers, two or three of them a compute unit; its rows come in chunks of 16 (bf16: 32):
+//   - A thread reads eight rows of two columns (four of packed rows) into registers, two chunks ahead (fp32 x fp32 in the wide tiles: one), turns them
+//     into bf16 pieces along the rows (fp32: three, exact; bf16 rows and packed ones, whose values are bf16 values: one) and puts them to LDS as whole
+//     fragments: 16 bytes are eight rows of a column, conflict-free to read.  Two buffers, one barrier a chunk.
 //   - fp32 x fp32 takes six products of pieces (linear_pieces.h), packed x fp32 three, packed or bf16 x bf16 one.
-//   - Sums: from zero in the matrix unit over kSteps x 16 rows, then added by vector instructions, every other chunk with the other sign of X: the
-//     matrix unit cuts where it adds, and over a million rows that would lean to one side.
+//   - Sums: fp32 products are summed from zero in the matrix unit over 16 rows, then added by vector instructions, every other chunk with the other
+//     sign of X: the matrix unit cuts where it adds, and over a million rows that would lean to one side.  Bf16 products, as many times fewer, are
+//     added to the sums there, X's sign turning every four chunks and with the workgroup.
 // Rows are dealt evenly to the workgroups, whatever the types' sizes: a workgroup that meets the end of a type writes its sums and starts
 // anew, so no workgroup has more rows than another.  Workgroup w writes its sums of type t to place w + t (every step along the rows goes to the
 // next workgroup or the next type, so no two have the same place), and a second launch adds a type's places up in order: the result is the
-// same in every run.
-// Sums that are not finite are taken again there, from the operands.
+// same in every run.  Sums that are not finite are taken again there, from the operands.
+// What bounds it: 237500 x 256 x 256, fp32, 226 us = 138 TFLOP/s (the six products' 829 TFLOP/s of bf16, of 1095 that a large library product reaches); bf16 from
+// 8 bits, 867187 rows, 240 us: 680 MB once would be 143, its products 104; every chunk's way from memory through registers to LDS takes as many issue
+// slots as the products leave.
 #include <algorithm>
 
 #include "linear_pieces.h"
@@ -23,6 +26,7 @@ namespace sar {
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kChunk32 = 16, kChunk16 = 32;          // rows of a chunk: fp32, bf16
 
 // What rows an operand has: pieces of a value, values a thread takes of a row, and their bytes.
 struct F32Rows {
@@ -561,31 +565,46 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void k_typed_dw_few(DwArgs a, in
     }
 }
 
-// Whether it takes a call: all of the rows may be of one type, whose workgroups take 128 of them at a time, and every 32 x 32 weights
-// read their columns anew.
-constexpr int64_t kFewRows = 2048, kFewColumns = 1 << 18;
-bool few_rows_dw(int64_t n, int K, int F) { return n <= kFewRows && n * ((K + 31) / 32) * ((F + 31) / 32) <= kFewColumns; }
+// Whether it takes a call.  Every 32 x 32 weights read their columns anew, and of one type a wavefront takes every eighth 16 rows (256 x 256, fp32: 500
+// rows 6.5 us and 10.6 in shares as above, 1000 rows 10.6 and 11.6, 2000 rows 19.1 and 13.9); of several, whose shares are seldom even, twice as many rows (2000
+// rows of four even types 6.9 and 16.1, 4000 rows 12.1 and 20.5; were they all of one type, 35.0 and 16.4).
+constexpr int64_t kFewRows = 1024, kFewColumns = 1 << 18;
+bool few_rows_dw(int64_t n, int T, int K, int F)
+{
+    return n <= (T > 1 ? 2 * kFewRows : kFewRows) && n * ((K + 31) / 32) * ((F + 31) / 32) <= kFewColumns;
+}
 
-// The tile of sums of a workgroup, its rows, and how many workgroups of the kernel a compute unit holds.
+// The tile of sums of a workgroup, its rows, and how many workgroups share them.
 struct Shape {
-    int tk, tf, tiles;
+    int tk, tf;
     int64_t share, groups;
 };
-Shape shape_of(int64_t n, int K, int F)
+// Wide tiles read the rows fewer times, narrow ones are more workgroups for as many shares of the rows, and every share is a set of sums to write and read
+// again: the widest tile whose workgroups have chunks enough.  256 x 256 by tiles of 128 x 256 / 128 x 128 / 128 x 64, us:
+//   fp32, from 8 bits:  10 thousand rows 27.3 / 22.3 / 20.5, 40 thousand 43.3 / 39.3 / 40.7, 160 thousand 107 / 111 / 122
+//   bf16, from 8 bits:  10 thousand rows 24.3 / 22.9 / 18.0, 80 thousand 41.5 / 37.8 / 40.7, 160 thousand 56.8 / 58.0 / 67.9
+// A compute unit holds two workgroups of 128 x 128 with fp32 rows (three asked for: 160 thousand rows 128 x 128, 60.1 us, two 50.8) and three with bf16 ones
+// (256 x 256: 58.0, two 66.1), three of 64 columns or rows (256 x 47, fp32: four 61.8, three 56.3).  Four chunks are a share's least (100 x 47, fp32: two, four, eight chunks, 4
+// thousand rows 10.5, 10.6, 13.6 us, 16 thousand 20.5, 15.5, 15.9).
+Shape shape_of(int64_t n, int K, int F, int chunk)
 {
-    // 128 x 256 sums a workgroup, 256 x 128 where only K is that wide, 128 x 128 where neither is; 64 columns or rows where that is all
-    Shape s;
-    s.tk = s.tf = 128;
-    if (F <= 64) s.tf = 64;
-    else if (K <= 64) s.tk = 64;
-    else if ((F + 127) / 128 % 2 == 0) s.tf = 256;
-    else if ((K + 127) / 128 % 2 == 0) s.tk = 256;
-    s.tiles = ((K + s.tk - 1) / s.tk) * ((F + s.tf - 1) / s.tf);
-    const int resident = s.tk * s.tf > 128 * 128 ? 2 : s.tk * s.tf == 128 * 128 ? 3 : 4;
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((n + 63) / 64, std::max(1, 256 * resident / s.tiles)));
-    s.share = std::max<int64_t>(64, ((n + want - 1) / want + 31) / 32 * 32);
-    s.groups = std::max<int64_t>(1, (n + s.share - 1) / s.share);
-    return s;
+    auto shape = [&](int tk, int tf, int resident) {
+        const int tiles = ((K + tk - 1) / tk) * ((F + tf - 1) / tf);
+        const int64_t least = 4 * chunk;
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>((n + least - 1) / least, std::max(1, 256 * resident / tiles)));
+        Shape s{tk, tf, std::max<int64_t>(least, ((n + want - 1) / want + 31) / 32 * 32), 0};
+        s.groups = std::max<int64_t>(1, (n + s.share - 1) / s.share);
+        return s;
+    };
+    if (F > 64 && K > 64) {
+        Shape s{};
+        if ((F + 127) / 128 % 2 == 0) s = shape(128, 256, 2);
+        else if ((K + 127) / 128 % 2 == 0) s = shape(256, 128, 2);
+        if (s.share >= 16 * chunk) return s;
+        s = shape(128, 128, chunk == kChunk32 ? 2 : 3);
+        if (s.share >= 8 * chunk) return s;
+    }
+    return K <= 64 && F > 64 ? shape(64, 128, 3) : shape(128, 64, 3);
 }
 
 template <typename XR, typename ZR, int MT, int NT, int WM, int WN, int S, int AHEAD>
@@ -604,7 +623,7 @@ int run(const DwArgs& a, const Shape& s, hipStream_t st)
 template <typename XR, typename ZR, int S, int W>
 int run_all(const DwArgs& a, const Shape& s, int accumulate, float* dW, hipStream_t st)
 {
-    if (few_rows_dw(a.types.n, a.K, a.F)) {
+    if (few_rows_dw(a.types.n, a.types.T, a.K, a.F)) {
         // (eight wavefronts where types have rows for them: 2000 rows of 4 types, 256 x 256 from 8 bits, 17.0 us, by four 21.9; 300 rows of 20 types,
         // 400 x 512, 30.7 and 15.7)
         const dim3 grid((a.K + 31) / 32, (a.F + 31) / 32, a.types.T);
@@ -635,16 +654,18 @@ int run_all(const DwArgs& a, const Shape& s, int accumulate, float* dW, hipStrea
 
 size_t typed_dw_bytes(int64_t n, int K, int F, int T)
 {
-    return (size_t)(shape_of(n, K, F).groups + T) * K * F * sizeof(float);
+    return (size_t)(std::max(shape_of(n, K, F, kChunk32).groups, shape_of(n, K, F, kChunk16).groups) + T) * K * F * sizeof(float);
 }
 
 int typed_dw(int dtype, const TypedDw& g, hipStream_t st)
 {
-    const Shape s = shape_of(g.types.n, g.K, g.F);
+    const Shape s = shape_of(g.types.n, g.K, g.F, dtype == SAR_F32 ? kChunk32 : kChunk16);
     const DwArgs a{g.X, g.Xq, g.Xe, g.dZ, g.partial, g.types, g.K, g.F, s.share};
     if (dtype == SAR_F32)
-        return g.Xq ? run_all<PackedRows, F32Rows, 1, 2>(a, s, g.accumulate, g.dW, st) : run_all<F32Rows, F32Rows, 1, 1>(a, s, g.accumulate, g.dW, st);
-    return g.Xq ? run_all<PackedRows, Bf16Rows, 2, 2>(a, s, g.accumulate, g.dW, st) : run_all<Bf16Rows, Bf16Rows, 2, 2>(a, s, g.accumulate, g.dW, st);
+        return g.Xq ? run_all<PackedRows, F32Rows, kChunk32 / 16, 2>(a, s, g.accumulate, g.dW, st)
+                    : run_all<F32Rows, F32Rows, kChunk32 / 16, 1>(a, s, g.accumulate, g.dW, st);
+    return g.Xq ? run_all<PackedRows, Bf16Rows, kChunk16 / 16, 2>(a, s, g.accumulate, g.dW, st)
+                : run_all<Bf16Rows, Bf16Rows, kChunk16 / 16, 2>(a, s, g.accumulate, g.dW, st);
 }
 
 }  // namespace sar
