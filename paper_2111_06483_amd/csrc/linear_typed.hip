@@ -4,8 +4,9 @@
 //   - Few rows (k_typed_few): latency.  One launch, a wavefront or four for every 32 x 32 results.
 //   - Otherwise a first launch (k_typed_lay) lays B out in pieces of bf16, in the order in which a wavefront's lanes want them: fp32 rows three pieces a
 //     weight (exact products, linear_pieces.h), bf16 rows two (the weight to 16 bits), T K F values; and lists the row blocks of every type, as many
-//     as its rows need, which the persistent workgroups of the main launch share.  That is k_typed_rows (blocks of 128 rows, four wavefronts, rows through
-//     registers) or, where rows are whole 16-byte pieces and many, k_typed_tall (256 rows, eight wavefronts, both operands by asynchronous copies).
+//     as its rows need, which the workgroups of the main launch (k_typed_rows) share: 128 rows and up to 256 columns at a time, four wavefronts, the
+//     pieces by asynchronous copies to LDS, two buffers, a barrier a stage.  (Tried, with no gain beyond a twentieth either way: 256 rows by eight
+//     wavefronts, rows by asynchronous copies as well, both two stages ahead.)
 //   - Columns are dealt to the column tiles by turns (`column_of`), so that a lane ends up with four neighbours of a row and writes them at once:
 //     a wavefront's store covers whole lines, with no turn through LDS.
 // fp32 sums: the matrix unit cuts (does not round) when it adds, so a chunk's 16 products are summed from zero there and added to the
@@ -13,8 +14,8 @@
 // cut leans to neither side.  bf16 products of at most a few hundred terms, whose sums are rounded to 8 bits, are added there.  A result that is not finite
 // (infinities and NaN have no such pieces, and the largest numbers round to infinity) sends the wavefront's tile back to the fp32 matrix instruction, from
 // the operands themselves.  Operands below 2^-110 in size are taken to within 2^-126.
-// What bounds them (256 -> 256, four types): fp32, 237500 rows, 195 us = 160 TFLOP/s: the six products, 958 TFLOP/s of bf16 (a large library product in
-// bf16 reaches 1095, one in fp32 154); bf16, 867187 rows, 278 us: its two products 816 TFLOP/s, its 888 MB 3.2 TB/s, neither alone (207 and 187 us).
+// What bounds them (256 -> 256, four types): fp32, 237500 rows, 191 us = 163 TFLOP/s: the six products, 978 TFLOP/s of bf16 (a large library product in
+// bf16 reaches 1170, one in fp32 154); bf16, 867187 rows, 276 us: its two products 823 TFLOP/s, its 888 MB 3.2 TB/s, neither alone (195 and 185 us).
 #include <algorithm>
 
 #include "linear_pieces.h"
@@ -61,19 +62,18 @@ struct LayArgs {
     Types types;
     int4* list;            // the launch's list of row blocks: how many, then (type, first row, the row behind the last)
     int64_t most;          // places in it
-    int rows;              // of a block
     unsigned lay;          // workgroups that lay out weights; one for each type's rows behind them
 };
 
-// The blocks of a.rows rows of type t, behind those of the types before it.
-constexpr int kTileRows = 128, kTallRows = 256;
+// The blocks of kTileRows rows of type t, behind those of the types before it.
+constexpr int kTileRows = 128;
 __device__ inline void list_rows(const LayArgs& a, int t)
 {
     __shared__ int64_t sums[4];
     auto blocks_of = [&](int u) {
         int64_t lo, hi;
         a.types.span(u, lo, hi);
-        return (hi - lo + a.rows - 1) / a.rows;
+        return (hi - lo + kTileRows - 1) / kTileRows;
     };
     int64_t before = 0;
     for (int u = threadIdx.x; u < t; u += 256) before += blocks_of(u);
@@ -84,10 +84,10 @@ __device__ inline void list_rows(const LayArgs& a, int t)
     before = sums[0] + sums[1] + sums[2] + sums[3];
     int64_t lo, hi;
     a.types.span(t, lo, hi);
-    const int64_t mine = (hi - lo + a.rows - 1) / a.rows;
+    const int64_t mine = (hi - lo + kTileRows - 1) / kTileRows;
     // (bounds that do not ascend can ask for more blocks than there is room for: those are left out)
     for (int64_t k = threadIdx.x; k < mine && before + k < a.most; k += 256)
-        a.list[1 + before + k] = make_int4(t, (int)(lo + k * a.rows), (int)hi, 0);
+        a.list[1 + before + k] = make_int4(t, (int)(lo + k * kTileRows), (int)hi, 0);
     if (t == a.T - 1 && threadIdx.x == 0) a.list[0] = make_int4((int)min(before + mine, a.most), 0, 0, 0);
 }
 
@@ -435,134 +435,6 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs a)
     }
 }
 
-// ---- the same for many rows of whole 16-byte pieces
-//
-// 256 rows a workgroup of eight wavefronts, one workgroup a compute unit.  Rows go to LDS by asynchronous copies as well, which leaves the
-// registers that they travel in above to nobody and lets both operands be two stages under way: a stage waits for the copies of the one
-// behind it only, and B is read half as often.
-template <typename T, int NT>
-struct Tall {
-    static constexpr int MR = sizeof(T) == 2 ? 2 : 1, WC = MR, WR = 8 / WC, NW = NT / WC, IL = NW < 4 ? NW : 4;
-    static constexpr int kWaves = 8, kFrags = kStageFrags<T, NT>, kCopies = kFrags / kWaves;       // (at least; of B, a wavefront and stage)
-    static constexpr int kRowsAt = 3 * kFrags * 64, kShared = (3 * kFrags + 2 * 4 * kWaves) * 1024;
-};
-
-// One stage: products of the rows at `rows` (the chunk's stage `part`) with the pieces at `b`; on their way: the next chunk's rows to `rows_to` (from
-// null: not now) and B's pieces of the stage after the next one to `b_to`.  (Its arguments tell the compiler what does not overlap, as above: this is
-// the only place that reads LDS, and no read waits for a copy.)
-template <typename T, int NT, typename From>
-__device__ SAR_INLINE inline void tall_stage(const uint4* __restrict__ rows, const uint4* __restrict__ b, uint4* __restrict__ rows_to, uint4* __restrict__ b_to,
-                                             const uint4* b_from, bool bring, From&& row_piece, int part, float sign,
-                                             float16_t (&acc)[Tall<T, NT>::MR][Tall<T, NT>::NW])
-{
-    using Sh = Tall<T, NT>;
-    constexpr int P = Mode<T>::kPieces, SB = Mode<T>::kStage, MR = Sh::MR, NW = Sh::NW;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    if (bring) {
-        // (addresses worked out here: carried through the loop they are registers that the sums need)
-        int own = lane;
-        asm volatile("" : "+v"(own));
-#pragma unroll
-        for (int p = 0; p < 4; ++p) __builtin_amdgcn_global_load_lds((GlobalSrc*)row_piece(own, p), (LdsPtr*)(rows_to + (wave * 4 + p) * 64), 16, 0, 0);
-    }
-    if (b_from) {
-#pragma unroll
-        for (int f = 0; f < (Sh::kFrags + Sh::kWaves - 1) / Sh::kWaves; ++f) {
-            if (Sh::kFrags % Sh::kWaves && wave + f * Sh::kWaves >= Sh::kFrags) continue;
-            __builtin_amdgcn_global_load_lds((GlobalSrc*)(b_from + (wave + f * Sh::kWaves) * 64 + lane), (LdsPtr*)(b_to + (wave + f * Sh::kWaves) * 64), 16, 0, 0);
-        }
-    }
-    uint4 p[MR][SB][P == 3 ? 3 : 1];
-#pragma unroll
-    for (int m = 0; m < MR; ++m) {
-        const uint4* mine = rows + ((wave / Sh::WC) * MR + m) * 256 + (lane & 31) * 8;
-        if constexpr (P == 3) {
-            const uint4 x = mine[(h * 4 + 2 * part) ^ (lane & 7)], y = mine[(h * 4 + 2 * part + 1) ^ (lane & 7)];
-            const float v[8] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w),
-                                __uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z), __uint_as_float(y.w)};
-            split8(v, p[m][0]);
-        } else {
-#pragma unroll
-            for (int s = 0; s < SB; ++s) p[m][s][0] = mine[(h * 4 + part * SB + s) ^ (lane & 7)];
-        }
-    }
-    multiply_stage<T, NT, MR, NW>(b + (wave % Sh::WC) * NW * 64 + lane, p, sign, acc);
-}
-
-template <typename T, int NT, bool TRANS>
-__global__ __launch_bounds__(512, 2) void k_typed_tall(RowsArgs a)
-{
-    constexpr int CH = kChunk<T>, N = Cols<T>::N;
-    using Sh = Tall<T, NT>;
-    constexpr int MR = Sh::MR, NW = Sh::NW;
-    extern __shared__ __attribute__((aligned(16))) uint4 lds[];      // [3][kFrags][64] of B, [2][8][32][8] of rows
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wr = wave / Sh::WC, wc = wave % Sh::WC;
-    const auto* const list = (const __attribute__((address_space(4))) int*)a.list;       // (read by scalar loads)
-    const int total = list[0];
-    if ((int)blockIdx.x >= total) return;
-    struct Tile {
-        int t, first, end;
-    };
-    auto tile_at = [&](int i) SAR_INLINE {
-        const auto* v = list + 4 * (1 + min(i, total - 1));
-        return Tile{v[0], v[1], v[2]};
-    };
-    auto pieces_of = [&](const Tile& w, int stage) SAR_INLINE {
-        return a.B + (((int64_t)(w.t * a.blocks + blockIdx.y) * a.chunks) * 2 + stage) * (Sh::kFrags * 64);
-    };
-    // The 16 bytes of load p that go to this lane's place: row 8 p + lane / 8 of the wavefront's 32, pieces turned by the row.  Rows behind
-    // the block's last one are read as that, pieces behind a row's last one as that (B is zero there).
-    auto row_piece = [&](const Tile& w, int chunk, int lane, int p) SAR_INLINE {
-        const uint32_t row = (uint32_t)min(wave * 32 + 8 * p + (lane >> 3), w.end - 1 - w.first);
-        const uint32_t c = (uint32_t)min(chunk * CH + ((lane & 7) ^ (lane >> 3)) * N, a.C - N);
-        return static_cast<const T*>(a.A) + (int64_t)w.first * a.C + (row * (uint32_t)a.C + c);
-    };
-
-    Tile tile = tile_at(blockIdx.x), after = tile_at(blockIdx.x + gridDim.x);
-#pragma unroll
-    for (int p = 0; p < 4; ++p)
-        __builtin_amdgcn_global_load_lds((GlobalSrc*)row_piece(tile, 0, lane, p), (LdsPtr*)(lds + Sh::kRowsAt + (wave * 4 + p) * 64), 16, 0, 0);
-    for (int f = wave; f < 2 * Sh::kFrags; f += Sh::kWaves)
-        __builtin_amdgcn_global_load_lds((GlobalSrc*)(pieces_of(tile, 0) + f * 64 + lane), (LdsPtr*)(lds + f * 64), 16, 0, 0);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-
-    int slot = 0, half = 0;                                          // of B's three and the rows' two
-    for (int index = blockIdx.x; index < total; index += gridDim.x) {
-        const bool another = index + (int)gridDim.x < total;
-        float16_t acc[MR][NW];
-#pragma unroll
-        for (int m = 0; m < MR; ++m)
-#pragma unroll
-            for (int i = 0; i < NW; ++i) acc[m][i] = float16_t{};
-        for (int stage = 0; stage < 2 * a.chunks; ++stage) {
-            const int chunk = stage >> 1, part = stage & 1;
-            const bool more = chunk + 1 < a.chunks, coming = more || another;
-            const Tile& w = more ? tile : after;
-            const int next = more ? chunk + 1 : 0;
-            const int to = slot == 0 ? 2 : slot - 1;
-            tall_stage<T, NT>(lds + Sh::kRowsAt + half * (Sh::kWaves * 256), lds + slot * Sh::kFrags * 64, lds + Sh::kRowsAt + (half ^ 1) * (Sh::kWaves * 256),
-                              lds + to * Sh::kFrags * 64, coming ? pieces_of(w, 2 * next + part) : nullptr, coming && part == 0,
-                              [&](int lane, int p) SAR_INLINE { return row_piece(w, next, lane, p); }, part, chunk & 1 ? -1.f : 1.f, acc);
-            // the copies that the next stage reads have arrived: those of this one may be under way (of part 0 the rows' four too, which the
-            // stage after the next one reads)
-            if (!coming) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            else if (part == 0) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(4 + Sh::kCopies) : "memory");
-            else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(Sh::kCopies) : "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            slot = slot == 2 ? 0 : slot + 1;
-            half ^= part;
-        }
-        const Tile done = tile;
-        tile = after;
-        after = tile_at(index + 2 * gridDim.x);
-#pragma unroll
-        for (int m = 0; m < MR; ++m)
-            store_tiles<T, NT, TRANS>(a, done.t, done.first + (wr * MR + m) * 32, done.end, wc * NW, acc[m]);
-    }
-}
-
 // ---- few rows
 //
 // Here a call is latency: one launch, a wavefront for every 32 x 32 outputs, operands from memory to registers in chunks of 64 contraction
@@ -765,27 +637,24 @@ int tiles_of(int64_t n, int N)
 }
 
 template <typename T, int NT, bool TRANS>
-int run_rows(const RowsArgs& a, LayArgs l, bool tall, hipStream_t st)
+int run_rows(const RowsArgs& a, LayArgs l, hipStream_t st)
 {
     const int64_t units = (int64_t)l.T * l.blocks * l.chunks * Mode<T>::kSteps * NT * 64, lay = (units + 255) / 256;
     if (lay > 0x7fffffff - 65536 || l.blocks > 65535)
         return fail(SAR_ERR_UNSUPPORTED, "typed products: %d x %d weights of %d types are too many for one launch", a.K, a.F, l.T);
     l.lay = (unsigned)lay;
-    l.rows = tall ? kTallRows : kTileRows;
     k_typed_lay<T, NT, TRANS><<<(unsigned)lay + l.T, 256, 0, st>>>(l);
     SAR_LAUNCH_CHECK();
-    // as many workgroups as are resident at once
-    auto launch = [&](auto* fn, int threads, size_t shared, int resident) {
-        if (shared > 65536) SAR_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)shared));
-        const int64_t groups = std::min<int64_t>(l.types.n / l.rows + l.T, std::max(1, 256 * resident / l.blocks));
-        fn<<<dim3((unsigned)groups, l.blocks), threads, shared, st>>>(a);
-        SAR_LAUNCH_CHECK();
-        return (int)SAR_OK;
-    };
-    if constexpr (NT > 2) {
-        if (tall) return launch(k_typed_tall<T, NT, TRANS>, 512, Tall<T, NT>::kShared, 1);
-    }
-    return launch(k_typed_rows<T, NT, TRANS>, kTileWaves * 64, (size_t)(2 * kStageFrags<T, NT> + 4 * kTileWaves) * 1024, NT == 2 ? 3 : 2);
+    // as many workgroups as a compute unit holds (three of two column tiles, two of more), each with every so-manyth block; of eight, two turns of
+    // them, so that no unit waits long for the last (100000 x 512 -> 512, fp32, 332 us by one turn, 302 by two, 301 by four; 237500 x 256 -> 256 197, 191, 193)
+    constexpr int kGroups = NT == 2 ? 3 : NT == 4 ? 2 : 4;
+    constexpr size_t shared = (size_t)(2 * kStageFrags<T, NT> + 4 * kTileWaves) * 1024;
+    auto* fn = k_typed_rows<T, NT, TRANS>;
+    if (shared > 65536) SAR_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)shared));
+    const int64_t groups = std::min<int64_t>(l.types.n / kTileRows + l.T, std::max(1, 256 * kGroups / l.blocks));
+    fn<<<dim3((unsigned)groups, l.blocks), kTileWaves * 64, shared, st>>>(a);
+    SAR_LAUNCH_CHECK();
+    return SAR_OK;
 }
 
 // Bytes of B's pieces for contraction C and N columns (either type, either number of tiles).
@@ -808,11 +677,8 @@ int rows_product(const void* A, const float* W, const Types& types, void* out, i
     int4* const list = static_cast<int4*>(work);
     uint4* const pieces = static_cast<uint4*>(work) + (most + 1);
     const RowsArgs a{A, pieces, W, out, list, C, N, chunks, blocks, K, F};
-    const LayArgs l{W, pieces, types.T, K, F, C, N, chunks, blocks, types, list, most, 0, 0};
-    // whole 16-byte pieces everywhere, and a block for every compute unit (256 -> 256: 64 thousand rows, fp32 57.5 us by blocks of 256 and 54.3 of 128, bf16 26.8 and
-    // 28.2; 100 thousand rows 92.0 and 94.2, 41.6 and 43.3)
-    const bool tall = NT > 2 && C % Cols<T>::N == 0 && (reinterpret_cast<uintptr_t>(A) & 15) == 0 && types.n >= (int64_t)kTallRows * 256 / blocks;
-    return NT == 2 ? run_rows<T, 2, TRANS>(a, l, tall, st) : NT == 4 ? run_rows<T, 4, TRANS>(a, l, tall, st) : run_rows<T, 8, TRANS>(a, l, tall, st);
+    const LayArgs l{W, pieces, types.T, K, F, C, N, chunks, blocks, types, list, most, 0};
+    return NT == 2 ? run_rows<T, 2, TRANS>(a, l, st) : NT == 4 ? run_rows<T, 4, TRANS>(a, l, st) : run_rows<T, 8, TRANS>(a, l, st);
 }
 
 size_t round256(size_t b) { return (b + 255) / 256 * 256; }

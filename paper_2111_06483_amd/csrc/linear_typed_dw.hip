@@ -13,8 +13,8 @@
 // anew, so no workgroup has more rows than another.  Workgroup w writes its sums of type t to place w + t (every step along the rows goes to the
 // next workgroup or the next type, so no two have the same place), and a second launch adds a type's places up in order: the result is the
 // same in every run.  Sums that are not finite are taken again there, from the operands.
-// What bounds it: 237500 x 256 x 256, fp32, 226 us = 138 TFLOP/s (the six products' 829 TFLOP/s of bf16, of 1095 that a large library product reaches); bf16 from
-// 8 bits, 867187 rows, 240 us: 680 MB once would be 143, its products 104; every chunk's way from memory through registers to LDS takes as many issue
+// What bounds it: 237500 x 256 x 256, fp32, 218 us = 143 TFLOP/s (the six products' 857 TFLOP/s of bf16, of 1170 that a large library product reaches); bf16 from
+// 8 bits, 867187 rows, 231 us: 680 MB once would be 141, its products 97; every chunk's way from memory through registers to LDS takes as many issue
 // slots as the products leave.
 #include <algorithm>
 

@@ -214,7 +214,7 @@ def with_specials(a, b):
     return want, size
 
 
-# (rows, widths): calls of few rows, of many in blocks of 128 (a width that is no whole piece) and of 256
+# (rows, widths): calls of few rows, and of many
 @pytest.mark.parametrize("n,K,F", [(300, 40, 50), (2000, 256, 130), (70_000, 101, 256), (70_000, 256, 128)])
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_infinities_and_nan_stay_where_they_belong(n, K, F, dtype):
@@ -283,18 +283,19 @@ def test_tensors_that_begin_anywhere_and_neighbours(dtype):
     assert all(float(r[0]) == 6 and bool((r[-4:] == 6).all()) for r in room.values())
 
 
-# Which kernels take a call: few rows; blocks of 128 rows where a row is no whole number of 16-byte pieces or begins anywhere; blocks of 256.
+# Which kernels take a call, on both sides of the lines.
 @pytest.mark.parametrize("n,K,F,dtype,fwd,dw", [
     (1000, 128, 128, BF16, "k_typed_few", "k_typed_dw_few"), (1024, 64, 64, F32, "k_typed_few", "k_typed_dw_few"),
     (1025, 64, 64, F32, "k_typed_few", "k_typed_dw<"), (1500, 512, 512, F32, "k_typed_few", "k_typed_dw<"), (40_000, 64, 64, F32, "k_typed_few", "k_typed_dw<"),
-    (41_000, 64, 64, F32, "k_typed_rows", "k_typed_dw<"), (70_000, 100, 256, F32, "k_typed_tall", "k_typed_dw<"), (70_000, 102, 256, F32, "k_typed_rows", "k_typed_dw<"),
-    (70_000, 100, 256, BF16, "k_typed_rows", "k_typed_dw<"), (70_000, 104, 256, BF16, "k_typed_tall", "k_typed_dw<"), (48_000, 256, 100, F32, "k_typed_rows", "k_typed_dw<")])
+    (41_000, 64, 64, F32, "k_typed_rows<float, 2,", "k_typed_dw<"), (24_500, 100, 256, F32, "k_typed_rows<float, 2,", "k_typed_dw<"),
+    (24_600, 100, 256, BF16, "k_typed_rows<sar::bf16_t, 4,", "k_typed_dw<"), (33_000, 102, 256, F32, "k_typed_rows<float, 8,", "k_typed_dw<"),
+    (70_000, 104, 256, BF16, "k_typed_rows<sar::bf16_t, 8,", "k_typed_dw<"), (66_000, 256, 100, F32, "k_typed_rows<float, 4,", "k_typed_dw<")])
 def test_which_kernels_run(n, K, F, dtype, fwd, dw):
     from tests import gpu_util as gu
     X, dZ, W = inputs(n, K, F, 1, dtype)
     ptr, work, Z, dW = ptr_of([0, n]), work_for(n, K, F, 1), torch.empty(n, F, dtype=dtype, device="cuda"), torch.empty_like(W)
     names = gu.kernels_of(lambda: sar.sar_linear_typed_fwd(X, W, ptr, Z, work))
-    assert fwd in names and sum(k in names for k in ("k_typed_few", "k_typed_rows", "k_typed_tall")) == 1, names
+    assert fwd in names and ("k_typed_few" in names) != ("k_typed_rows" in names), names
     names = gu.kernels_of(lambda: sar.sar_linear_typed_bwd(X, dZ, W, ptr, False, dW, None, work))
     assert dw in names, names
     check_rows(X, W, Z, [(0, 0, n)], dtype, False)
@@ -303,7 +304,7 @@ def test_which_kernels_run(n, K, F, dtype, fwd, dw):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_many_rows_that_begin_anywhere(dtype):
-    """As blocks of 256 rows would be taken, were the first value on a 16-byte boundary."""
+    """The first value off a 16-byte boundary."""
     n, K, F = 70_000, 128, 256
     X, dZ, W = inputs(n, K, F, 1, dtype)
     room = torch.empty(n * K + 1, dtype=dtype, device="cuda")
