@@ -516,8 +516,8 @@ int sar_linear_typed_bwd(const void* X, const int8_t* Xq, const uint8_t* Xe, con
 
 int sar_linear_typed_workspace_bytes(int64_t n, int K, int F, int T, size_t* bytes);
 
-/* sar_linear_bwd from rows kept in 8 bits: what sar_linear_typed_bwd does of one type that has all rows (W, dW fp32
- * [K,F]).  work: sar_linear_typed_workspace_bytes with T = 1. */
+/* sar_linear_bwd from rows kept in 8 bits: dW (fp32 [K,F]) as sar_linear_typed_bwd forms it of one type that has all
+ * rows, dX as sar_linear_bwd does (must not alias dZ).  work: sar_linear_typed_workspace_bytes with T = 1. */
 int sar_linear_bwd_packed(const int8_t* Xq, const uint8_t* Xe, const void* dZ, const float* W, int accumulate, float* dW,
                           void* dX, int dtype, int64_t n, int K, int F, void* work, size_t work_bytes, void* stream);
 

@@ -37,4 +37,62 @@ struct TypedDw {
 size_t typed_dw_bytes(int64_t n, int K, int F, int T);
 int typed_dw(int dtype, const TypedDw& g, hipStream_t st);
 
+// Calls of few rows (linear_typed_few.hip): whether they are, and one launch each, or one for both of a backward pass.
+bool few_blocks(const Types& types, int N);
+bool few_rows_dw(int64_t n, int T, int K, int F);
+struct FewArgs {
+    const void* A;         // [n, C]
+    const float* W;        // [T, K, F]
+    void* out;             // [n, N]
+    Types types;
+    int C, N, K, F;
+};
+int few_product(int dtype, bool trans, const FewArgs& a, hipStream_t st);
+int few_dw(int dtype, const TypedDw& g, hipStream_t st);
+int few_dw_and_dx(int dtype, const TypedDw& g, const FewArgs& a, hipStream_t st);
+
+// What rows an operand has: pieces of a value, values a thread takes of a row, and their bytes.
+struct F32Rows {
+    using T = float;
+    static constexpr int kPieces = 3, kCols = 2;
+};
+struct Bf16Rows {
+    using T = bf16_t;
+    static constexpr int kPieces = 1, kCols = 2;
+};
+struct PackedRows {
+    static constexpr int kPieces = 1, kCols = 4;
+};
+
+struct DwArgs {
+    const void* X;
+    const int8_t* Xq;
+    const uint8_t* Xe;
+    const void* dZ;
+    float* partial;        // [workgroups + T, K, F]
+    Types types;
+    int K, F;
+    int64_t share;         // rows of a workgroup
+};
+
+// A value of X as fp32.
+template <typename XR>
+__device__ inline float x_value(const DwArgs& a, int64_t row, int c)
+{
+    if constexpr (XR::kCols == 4) {
+        return (float)a.Xq[row * packed_stride(a.K) + c] * step_of(a.Xe[row * packed_steps(a.K) + c / kPackBlock]);
+    } else if constexpr (sizeof(typename XR::T) == 4) {
+        return static_cast<const float*>(a.X)[row * a.K + c];
+    } else {
+        return bf16_to_f32(static_cast<const bf16_t*>(a.X)[row * a.K + c]);
+    }
+}
+template <typename ZR>
+__device__ inline float z_value(const DwArgs& a, int64_t row, int c)
+{
+    if constexpr (sizeof(typename ZR::T) == 4) return static_cast<const float*>(a.dZ)[row * a.F + c];
+    else return bf16_to_f32(static_cast<const bf16_t*>(a.dZ)[row * a.F + c]);
+}
+
+
 }  // namespace sar

@@ -1,7 +1,7 @@
 // Products of rows with the weight of their type: Z = X W_t and dX = dZ W_t^T for rows sorted by type, of any numbers.
 //
-// Both are rows (contraction index contiguous) times a small operand B [C, N] per type.  Three kernels:
-//   - Few rows (k_typed_few): latency.  One launch, a wavefront or four for every 32 x 32 results.
+// Both are rows (contraction index contiguous) times a small operand B [C, N] per type.
+//   - Few rows (linear_typed_few.hip): latency.  One launch.
 //   - Otherwise a first launch (k_typed_lay) lays B out in pieces of bf16, in the order in which a wavefront's lanes want them: fp32 rows three pieces a
 //     weight (exact products, linear_pieces.h), bf16 rows two (the weight to 16 bits), T K F values; and lists the row blocks of every type, as many
 //     as its rows need, which the workgroups of the main launch (k_typed_rows) share: 128 rows and up to 256 columns at a time, four wavefronts, the
@@ -435,197 +435,6 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs a)
     }
 }
 
-// ---- few rows
-//
-// Here a call is latency: one launch, a wavefront for every 32 x 32 outputs, operands from memory to registers in chunks of 64 contraction
-// values, a chunk ahead, weights cut into pieces where they are multiplied.  (2000 x 128 -> 128, bf16, 4 types: 4.3 us, 10 by two launches as above.)
-// The line: 256 -> 256, 8 thousand rows, 2032 blocks, fp32 21.1 us here and 23.9 by two launches, bf16 12.4 and 15.1; 16 thousand rows 36.0 and 27.3,
-// 20.8 and 17.0.
-constexpr int kFewBlocks = 2560, kFewShared = 1024;
-struct FewArgs {
-    const void* A;         // [n, C]
-    const float* W;        // [T, K, F]
-    void* out;             // [n, N]
-    Types types;
-    int C, N, K, F;
-};
-
-// Which rows: block `index` of 32 of a type, type after type; false behind the last one.
-__device__ inline bool few_rows_of(const Types& types, int64_t index, int& t, int64_t& first, int64_t& end)
-{
-    const int lane = threadIdx.x & 63;
-    for (int base = 0; base < types.T; base += 64) {
-        int64_t lo = 0, hi = 0;
-        if (base + lane < types.T) types.span(base + lane, lo, hi);
-        const int mine = (int)((hi - lo + 31) / 32);
-        int upto = mine;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int v = __shfl_up(upto, o);
-            if (lane >= o) upto += v;
-        }
-        const uint64_t here = __ballot(index < upto);
-        if (here) {
-            const int l = __builtin_ctzll(here);
-            t = __builtin_amdgcn_readfirstlane(base + l);
-            first = __builtin_amdgcn_readfirstlane(__shfl((int)(lo + (index - (upto - mine)) * 32), l));      // (rows are fewer than 2^31)
-            end = __builtin_amdgcn_readfirstlane(__shfl((int)hi, l));
-            return true;
-        }
-        index -= __shfl(upto, 63);
-    }
-    return false;
-}
-
-// PARTS: wavefronts that share one block's contraction, chunk by chunk, and add up in LDS (4), or one a block (1).
-template <typename T, bool TRANS, int PARTS>
-__global__ __launch_bounds__(256, 2) void k_typed_few(FewArgs a)
-{
-    constexpr int N = Cols<T>::N, kRaw = 8 / N, U = 4;                // 16-byte pieces of a row a product of 16; products a chunk
-    __shared__ float part[PARTS == 4 ? 4 : 1][16][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const int n0 = (PARTS == 4 ? blockIdx.y : blockIdx.y * 4 + wave) * 32, n = n0 + (lane & 31);
-    const int k_from = PARTS == 4 ? wave * 16 * U : 0;
-    constexpr int kTurn = PARTS * 16 * U;
-    int t;
-    int64_t first, end;
-    if (n0 >= a.N || !few_rows_of(a.types, blockIdx.x, t, first, end)) return;
-    const int64_t i = min(first + (lane & 31), end - 1);
-    const T* row = static_cast<const T*>(a.A) + i * a.C;
-    const int64_t left = (a.types.n - i) * a.C;
-    const float* W = a.W + (int64_t)t * a.K * a.F;
-    const int nc = min(n, a.N - 1);
-    struct Chunk {
-        uint4 x[U][kRaw];
-        float w[U][8];
-    };
-    auto load = [&](Chunk& g, int k0) SAR_INLINE {
-        const float* w = TRANS ? W + (int64_t)nc * a.F : W + nc;
-        if (k0 + 16 * U <= a.C) {          // the same for all lanes: one run of loads
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int c = k0 + u * 16 + h * 8;
-#pragma unroll
-                for (int p = 0; p < kRaw; ++p) g.x[u][p] = load16(row + c + p * N);
-                if constexpr (TRANS) {
-#pragma unroll
-                    for (int j = 0; j < 8; j += 4) {
-                        const uint4 v = load16(w + c + j);
-                        g.w[u][j] = __uint_as_float(v.x), g.w[u][j + 1] = __uint_as_float(v.y);
-                        g.w[u][j + 2] = __uint_as_float(v.z), g.w[u][j + 3] = __uint_as_float(v.w);
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) g.w[u][j] = w[(int64_t)(c + j) * a.F];
-                }
-            }
-        } else {
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int c = k0 + u * 16 + h * 8;
-#pragma unroll
-                for (int p = 0; p < kRaw; ++p) g.x[u][p] = Cols<T>::load(row, c + p * N, a.C, left);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) g.w[u][j] = w[(int64_t)min(c + j, a.C - 1) * (TRANS ? 1 : a.F)];
-            }
-        }
-    };
-    float16_t acc[1] = {};
-    auto multiply = [&](const Chunk& g, int k0) SAR_INLINE {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int c = k0 + u * 16 + h * 8;
-            if (k0 + u * 16 >= a.C) break;
-            float w[8], x[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = c + j < a.C ? g.w[u][j] : 0.f;
-            if constexpr (sizeof(T) == 4) {
-                float lo[4], hi[4];
-                Cols<T>::values(g.x[u][0], c, a.C, lo);
-                Cols<T>::values(g.x[u][1 % kRaw], c + 4, a.C, hi);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = lo[j], x[4 + j] = hi[j];
-                uint4 p[3], q[3];
-                split8(x, p);
-                split8(w, q);
-                float16_t sum;
-                multiply_split(p, q, sum);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[0][r] += sum[r];
-            } else {
-                const uint4 m = Cols<T>::within(c, a.C), v = g.x[u][0];
-                const uint4 p = make_uint4(v.x & m.x, v.y & m.y, v.z & m.z, v.w & m.w);
-                uint32_t big[4], small[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    big[j] = pack2_bf16(w[2 * j], w[2 * j + 1]);
-                    small[j] = pack2_bf16(w[2 * j] - __uint_as_float(big[j] << 16), w[2 * j + 1] - __uint_as_float(big[j] & 0xffff0000u));
-                }
-                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p), __builtin_bit_cast(bf16x8_t, make_uint4(small[0], small[1], small[2], small[3])), acc[0], 0, 0, 0);
-                acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p), __builtin_bit_cast(bf16x8_t, make_uint4(big[0], big[1], big[2], big[3])), acc[0], 0, 0, 0);
-            }
-        }
-    };
-    if (k_from < a.C) {
-        Chunk g[2];
-        load(g[0], k_from);
-        for (int k0 = k_from; k0 < a.C; k0 += 2 * kTurn) {
-            if (k0 + kTurn < a.C) load(g[1], k0 + kTurn);
-            multiply(g[0], k0);
-            if (k0 + kTurn >= a.C) break;
-            if (k0 + 2 * kTurn < a.C) load(g[0], k0 + 2 * kTurn);
-            multiply(g[1], k0 + kTurn);
-        }
-        if (__any(not_finite(acc[0]))) {
-            acc[0] = float16_t{};
-            for (int k0 = k_from; k0 < a.C; k0 += kTurn)
-                for (int k = k0; k < min(k0 + 16 * U, a.C); k += 2) {
-                    const bool in = k + h < a.C;
-                    float x = 0.f, w = 0.f;
-                    if (in) {
-                        if constexpr (sizeof(T) == 4) x = row[k + h];
-                        else x = bf16_to_f32(row[k + h]);
-                        w = TRANS ? W[(int64_t)nc * a.F + k + h] : W[(int64_t)(k + h) * a.F + nc];
-                    }
-                    acc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w, acc[0], 0, 0, 0);
-                }
-        }
-    }
-    auto store = [&](int r, float v) SAR_INLINE {
-        const int64_t o = first + 8 * (r / 4) + 4 * h + r % 4;
-        if (n < a.N && o < end) static_cast<T*>(a.out)[o * a.N + n] = from_f32<T>(v);
-    };
-    if constexpr (PARTS == 4) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) part[wave][r][lane] = acc[0][r];
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r = wave * 4 + j;
-            store(r, (part[0][r][lane] + part[1][r][lane]) + (part[2][r][lane] + part[3][r][lane]));
-        }
-    } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) store(r, acc[0][r]);
-    }
-}
-
-template <typename T, bool TRANS>
-int few_product(const FewArgs& a, hipStream_t st)
-{
-    const int64_t groups = a.types.n / 32 + a.types.T;
-    // (four wavefronts a block where that is no more than four a SIMD: 2000 rows 256 -> 256, fp32, 544 blocks 9.2 us, one a block 13.0; 8000 rows 25.2 and
-    // 21.4)
-    if (a.C > 64 && groups * ((a.N + 31) / 32) <= kFewShared)
-        k_typed_few<T, TRANS, 4><<<dim3((unsigned)groups, (a.N + 31) / 32), 256, 0, st>>>(a);
-    else
-        k_typed_few<T, TRANS, 1><<<dim3((unsigned)groups, (a.N + 127) / 128), 256, 0, st>>>(a);
-    SAR_LAUNCH_CHECK();
-    return SAR_OK;
-}
-// Whether a product's blocks of 32 x 32 outputs, whose wavefronts read all the weights they need anew, are few.
-bool few_blocks(const Types& types, int N) { return (types.n / 32 + types.T) * ((N + 31) / 32) <= kFewBlocks; }
-
 // Column tiles a workgroup forms at once: as few as let all workgroups run at the same time (three a compute unit of two tiles, two of more).
 // 256 -> 256, fp32, by two / four / eight: 16 thousand rows 27.3 / 28.6 / 31.6 us, 32 thousand 42.8 / 34.0 / 34.0, 48 thousand 52.1 / 53.3 / 48.2; bf16
 // 17.0 / 16.9 / 19.7, 22.9 / 20.7 / 20.6, 26.4 / 29.1 / 26.0.  Beyond that eight, so that rows are read once, unless half of them would lie behind the last column.
@@ -671,7 +480,7 @@ template <typename T, bool TRANS>
 int rows_product(const void* A, const float* W, const Types& types, void* out, int K, int F, void* work, hipStream_t st)
 {
     const int C = TRANS ? F : K, N = TRANS ? K : F, NT = tiles_of(types.n, N);
-    if (few_blocks(types, N)) return few_product<T, TRANS>({A, W, out, types, C, N, K, F}, st);
+    if (few_blocks(types, N)) return few_product(sizeof(T) == 4 ? SAR_F32 : SAR_BF16, TRANS, {A, W, out, types, C, N, K, F}, st);
     const int chunks = (C + kChunk<T> - 1) / kChunk<T>, blocks = (N + 32 * NT - 1) / (32 * NT);
     const int64_t most = most_tiles(types.n, types.T);
     int4* const list = static_cast<int4*>(work);
@@ -709,9 +518,16 @@ int check_call(int dtype, int64_t n, int K, int F, int T, const void* ptr, const
     return SAR_OK;
 }
 
-// The backward pass of both entry points (ptr null: one type).
+bool few_bwd(const Types& types, int K, int F) { return few_rows_dw(types.n, types.T, K, F) && few_blocks(types, K); }
+bool apart(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return !b || x + a_bytes <= y || y + b_bytes <= x;
+}
+
+// The backward pass of both entry points (ptr null: one type); with rows, dX too.
 int typed_bwd(const void* X, const int8_t* Xq, const uint8_t* Xe, const void* dZ, const float* W, const int32_t* ptr, int T, int accumulate,
-              float* dW, void* dX, int dtype, int64_t n, int K, int F, void* work, hipStream_t st)
+              float* dW, void* dX, bool rows, int dtype, int64_t n, int K, int F, void* work, hipStream_t st)
 {
     SAR_TRY(check_packed("Xq", Xq, Xe));
     SAR_CHECK_ARG(!(X && Xq), "typed products: X and Xq are both given");
@@ -720,10 +536,16 @@ int typed_bwd(const void* X, const int8_t* Xq, const uint8_t* Xe, const void* dZ
         SAR_CHECK_ARG(!dW || X || Xq, "null pointer (X or Xq)");
         SAR_CHECK_ARG(!dX || W, "null pointer (W)");
         SAR_CHECK_ARG(!dX || dX != dZ, "typed products: dX must not alias dZ");
+        SAR_CHECK_ARG(!dX || !dW || dW != W, "typed products: dW must not alias W");
     }
     const Types types{ptr, T, n};
-    if (dW) SAR_TRY(sar::typed_dw(dtype, {X, Xq, Xe, dZ, dW, types, K, F, accumulate, static_cast<float*>(work)}, st));
-    if (dX && n > 0)
+    const TypedDw g{X, Xq, Xe, dZ, dW, types, K, F, accumulate, static_cast<float*>(work)};
+    const size_t size = (size_t)n * K * (dtype == SAR_F32 ? 4 : 2);
+    if (dW && dX && n > 0 && few_bwd(types, K, F) && apart(dX, size, X, size) && apart(dX, size, Xq, (size_t)n * packed_stride(K)) &&
+        apart(dX, size, Xe, (size_t)n * packed_steps(K)))
+        return few_dw_and_dx(dtype, g, {dZ, W, dX, types, F, K, K, F}, st);
+    if (dW) SAR_TRY(typed_dw(dtype, g, st));
+    if (rows && dX && n > 0)
         return dtype == SAR_F32 ? rows_product<float, true>(dZ, W, types, dX, K, F, work, st)
                                 : rows_product<bf16_t, true>(dZ, W, types, dX, K, F, work, st);
     return SAR_OK;
@@ -759,12 +581,15 @@ extern "C" int sar_linear_typed_bwd(const void* X, const int8_t* Xq, const uint8
                                     void* work, size_t work_bytes, void* stream)
 {
     SAR_TRY(check_call(dtype, n, K, F, T, type_ptr, work, work_bytes));
-    return typed_bwd(X, Xq, Xe, dZ, W, type_ptr, T, accumulate, dW, dX, dtype, n, K, F, work, as_stream(stream));
+    return typed_bwd(X, Xq, Xe, dZ, W, type_ptr, T, accumulate, dW, dX, true, dtype, n, K, F, work, as_stream(stream));
 }
 
 extern "C" int sar_linear_bwd_packed(const int8_t* Xq, const uint8_t* Xe, const void* dZ, const float* W, int accumulate, float* dW, void* dX,
                                      int dtype, int64_t n, int K, int F, void* work, size_t work_bytes, void* stream)
 {
     SAR_TRY(check_call(dtype, n, K, F, 1, nullptr, work, work_bytes));
-    return typed_bwd(nullptr, Xq, Xe, dZ, W, nullptr, 1, accumulate, dW, dX, dtype, n, K, F, work, as_stream(stream));
+    // of more than a few rows the product that sar_linear_bwd has: the errors of the rows do not depend on the form of the input
+    const bool few = few_bwd({nullptr, 1, n}, K, F);
+    SAR_TRY(typed_bwd(nullptr, Xq, Xe, dZ, W, nullptr, 1, accumulate, dW, dX, few, dtype, n, K, F, work, as_stream(stream)));
+    return dX && !few ? sar_linear_bwd(nullptr, dZ, W, nullptr, dX, dtype, n, K, F, nullptr, 0, stream) : SAR_OK;
 }

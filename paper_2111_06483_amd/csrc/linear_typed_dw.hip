@@ -28,30 +28,6 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kChunk32 = 16, kChunk16 = 32;          // rows of a chunk: fp32, bf16
 
-// What rows an operand has: pieces of a value, values a thread takes of a row, and their bytes.
-struct F32Rows {
-    using T = float;
-    static constexpr int kPieces = 3, kCols = 2;
-};
-struct Bf16Rows {
-    using T = bf16_t;
-    static constexpr int kPieces = 1, kCols = 2;
-};
-struct PackedRows {
-    static constexpr int kPieces = 1, kCols = 4;
-};
-
-struct DwArgs {
-    const void* X;
-    const int8_t* Xq;
-    const uint8_t* Xe;
-    const void* dZ;
-    float* partial;        // [workgroups + T, K, F]
-    Types types;
-    int K, F;
-    int64_t share;         // rows of a workgroup
-};
-
 // Where column c of a tile's columns lies in LDS: of 64 columns the even ones first, so that the two that a thread writes go to runs of
 // their own, and a lane of two neighbouring column tiles holds two neighbouring columns.
 __device__ inline int place_of(int c) { return (c & ~63) | (c & 1) << 5 | (c >> 1 & 31); }
@@ -187,25 +163,6 @@ template <typename XR>
 constexpr int kXRegs = Unit<XR>::kRegs;
 template <>
 constexpr int kXRegs<PackedRows> = PackedUnit::kRegs;
-
-// A value of X as fp32.
-template <typename XR>
-__device__ inline float x_value(const DwArgs& a, int64_t row, int c)
-{
-    if constexpr (XR::kCols == 4) {
-        return (float)a.Xq[row * packed_stride(a.K) + c] * step_of(a.Xe[row * packed_steps(a.K) + c / kPackBlock]);
-    } else if constexpr (sizeof(typename XR::T) == 4) {
-        return static_cast<const float*>(a.X)[row * a.K + c];
-    } else {
-        return bf16_to_f32(static_cast<const bf16_t*>(a.X)[row * a.K + c]);
-    }
-}
-template <typename ZR>
-__device__ inline float z_value(const DwArgs& a, int64_t row, int c)
-{
-    if constexpr (sizeof(typename ZR::T) == 4) return static_cast<const float*>(a.dZ)[row * a.F + c];
-    else return bf16_to_f32(static_cast<const bf16_t*>(a.dZ)[row * a.F + c]);
-}
 
 // WM x WN wavefronts of MT x NT tiles of 32 x 32; S products of 16 rows a chunk.
 template <typename XR, typename ZR, int MT, int NT, int WM, int WN, int S, int AHEAD>
@@ -471,109 +428,6 @@ __global__ __launch_bounds__(256) void k_typed_sum(DwArgs a, int accumulate, flo
     }
 }
 
-// ---- few rows
-//
-// One launch: a workgroup for 32 x 32 weights of a type, whose wavefronts take every fourth or eighth 16 of the type's rows straight from memory
-// (lanes are columns: whole lines), add up their sums in LDS and write dW.
-template <typename XR, typename ZR, int kFewWaves>
-__global__ __launch_bounds__(kFewWaves * 64, 2) void k_typed_dw_few(DwArgs a, int accumulate, float* dW)
-{
-    constexpr int PX = XR::kPieces, PZ = ZR::kPieces, U = 2, kTurn = kFewWaves * 16;          // products of 16 rows a step
-    __shared__ float part[kFewWaves][16][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const int k0 = blockIdx.x * 32, f0 = blockIdx.y * 32, t = blockIdx.z;
-    const int k = min(k0 + (lane & 31), a.K - 1), f = min(f0 + (lane & 31), a.F - 1);
-    int64_t lo, hi;
-    a.types.span(t, lo, hi);
-    float16_t acc = {};
-    struct Step {
-        float x[U][8], z[U][8];
-    };
-    auto load = [&](Step& s, int64_t r0) SAR_INLINE {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int64_t r = min(r0 + u * kTurn + h * 8 + j, hi - 1);
-                s.x[u][j] = x_value<XR>(a, r, k);
-                s.z[u][j] = z_value<ZR>(a, r, f);
-            }
-    };
-    auto multiply = [&](Step& s, int64_t r0) SAR_INLINE {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (r0 + u * kTurn >= hi) break;
-            float x[8], z[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool in = r0 + u * kTurn + h * 8 + j < hi;
-                x[j] = in ? s.x[u][j] : 0.f, z[j] = in ? s.z[u][j] : 0.f;
-            }
-            uint4 p[3], q[3];
-            auto whole = [](const float (&v)[8]) SAR_INLINE {        // (bf16 values: not rounded)
-                return make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
-            };
-            if constexpr (PX == 3) split8(x, p);
-            else p[0] = whole(x);
-            if constexpr (PZ == 3) split8(z, q);
-            else q[0] = whole(z);
-            float16_t sum = {};
-#pragma unroll
-            for (int i = 0; i < 6; ++i)
-                if (kTerm[i][0] < PX && kTerm[i][1] < PZ)
-                    sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[kTerm[i][0] < PX ? kTerm[i][0] : 0]),
-                                                                  __builtin_bit_cast(bf16x8_t, q[kTerm[i][1] < PZ ? kTerm[i][1] : 0]), sum, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[r] += sum[r];
-        }
-    };
-    const int64_t from = lo + wave * 16;
-    constexpr int kNext = U * kTurn;
-    if (from < hi) {
-        Step s[2];
-        load(s[0], from);
-        for (int64_t r0 = from; r0 < hi; r0 += 2 * kNext) {
-            if (r0 + kNext < hi) load(s[1], r0 + kNext);
-            multiply(s[0], r0);
-            if (r0 + kNext >= hi) break;
-            if (r0 + 2 * kNext < hi) load(s[0], r0 + 2 * kNext);
-            multiply(s[1], r0 + kNext);
-        }
-        if (PZ == 3 && __any(not_finite(acc))) {
-            acc = float16_t{};
-            for (int64_t r0 = from; r0 < hi; r0 += kTurn)
-                for (int64_t r = r0; r < min(r0 + 16, hi); r += 2) {
-                    const bool in = r + h < hi;
-                    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(in ? x_value<XR>(a, r + h, k) : 0.f, in ? z_value<ZR>(a, r + h, f) : 0.f, acc, 0, 0, 0);
-                }
-        }
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r) part[wave][r][lane] = acc[r];
-    __syncthreads();
-    // lane holds column f; register r holds weight row 8*(r/4) + 4*h + r%4: two registers a wavefront
-    if (f0 + (lane & 31) >= a.F) return;
-#pragma unroll
-    for (int j = 0; j < 16 / kFewWaves; ++j) {
-        const int r = wave * (16 / kFewWaves) + j, row = k0 + 8 * (r / 4) + 4 * h + r % 4;
-        if (row >= a.K) continue;
-        float v = 0.f;
-#pragma unroll
-        for (int w = 0; w < kFewWaves; ++w) v += part[w][r][lane];
-        float* out = dW + ((int64_t)t * a.K + row) * a.F + f;
-        *out = accumulate ? *out + v : v;
-    }
-}
-
-// Whether it takes a call.  Every 32 x 32 weights read their columns anew, and of one type a wavefront takes every eighth 16 rows (256 x 256, fp32: 500
-// rows 6.5 us and 10.6 in shares as above, 1000 rows 10.6 and 11.6, 2000 rows 19.1 and 13.9); of several, whose shares are seldom even, twice as many rows (2000
-// rows of four even types 6.9 and 16.1, 4000 rows 12.1 and 20.5; were they all of one type, 35.0 and 16.4).
-constexpr int64_t kFewRows = 1024, kFewColumns = 1 << 18;
-bool few_rows_dw(int64_t n, int T, int K, int F)
-{
-    return n <= (T > 1 ? 2 * kFewRows : kFewRows) && n * ((K + 31) / 32) * ((F + 31) / 32) <= kFewColumns;
-}
-
 // The tile of sums of a workgroup, its rows, and how many workgroups share them.
 struct Shape {
     int tk, tf;
@@ -623,15 +477,6 @@ int run(const DwArgs& a, const Shape& s, hipStream_t st)
 template <typename XR, typename ZR, int S, int W>
 int run_all(const DwArgs& a, const Shape& s, int accumulate, float* dW, hipStream_t st)
 {
-    if (few_rows_dw(a.types.n, a.types.T, a.K, a.F)) {
-        // (eight wavefronts where types have rows for them: 2000 rows of 4 types, 256 x 256 from 8 bits, 17.0 us, by four 21.9; 300 rows of 20 types,
-        // 400 x 512, 30.7 and 15.7)
-        const dim3 grid((a.K + 31) / 32, (a.F + 31) / 32, a.types.T);
-        if (a.types.n > 64 * (int64_t)a.types.T) k_typed_dw_few<XR, ZR, 8><<<grid, 512, 0, st>>>(a, accumulate, dW);
-        else k_typed_dw_few<XR, ZR, 4><<<grid, 256, 0, st>>>(a, accumulate, dW);
-        SAR_LAUNCH_CHECK();
-        return SAR_OK;
-    }
     if (a.types.n > 0) {
         if (s.tk == 256) SAR_TRY((run<XR, ZR, 4, 2, 2, 2, S, W>(a, s, st)));
         else if (s.tf == 256) SAR_TRY((run<XR, ZR, 2, 4, 2, 2, S, W>(a, s, st)));
@@ -659,6 +504,7 @@ size_t typed_dw_bytes(int64_t n, int K, int F, int T)
 
 int typed_dw(int dtype, const TypedDw& g, hipStream_t st)
 {
+    if (few_rows_dw(g.types.n, g.types.T, g.K, g.F)) return few_dw(dtype, g, st);
     const Shape s = shape_of(g.types.n, g.K, g.F, dtype == SAR_F32 ? kChunk32 : kChunk16);
     const DwArgs a{g.X, g.Xq, g.Xe, g.dZ, g.partial, g.types, g.K, g.F, s.share};
     if (dtype == SAR_F32)

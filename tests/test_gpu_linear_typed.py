@@ -315,6 +315,30 @@ def test_many_rows_that_begin_anywhere(dtype):
     check_rows(X, W, Z, [(0, 0, n)], dtype, False)
 
 
+@pytest.mark.parametrize("n,K,F,ends", [(1, 40, 30, [0, 1]), (90, 200, 140, [0, 30, 30, 80]), (600, 100, 300, [0, 600]), (2000, 400, 64, [0, 900, 2000]),
+                                        (900, 256, 256, [0, 20, 900]), (5000, 64, 64, [0, 2500, 5000])])
+@pytest.mark.parametrize("dtype,packed", KINDS)
+def test_one_call_for_both_products_and_one_for_each(n, K, F, ends, dtype, packed):
+    """The same bits, whichever launch they come from; also with dX in the place of X, which dW still has to read."""
+    T = len(ends) - 1
+    X, dZ, W = inputs(n, K, F, T, dtype)
+    ptr, work, p = ptr_of(ends), work_for(n, K, F, T), packed_of(X)[0] if packed else X
+    dW, dX = torch.empty_like(W), torch.zeros_like(X)
+    sar.sar_linear_typed_bwd(p, dZ, W, ptr, False, dW, dX, work)
+    dW1, dX1 = torch.empty_like(W), torch.zeros_like(X)
+    sar.sar_linear_typed_bwd(p, dZ, W, ptr, False, dW1, None, work)
+    sar.sar_linear_typed_bwd(None, dZ, W, ptr, False, None, dX1, work)
+    assert torch.equal(dW, dW1) and torch.equal(dX, dX1)
+    if not packed:
+        X[ends[-1]:] = 0
+        sar.sar_linear_typed_bwd(X, dZ, W, ptr, False, dW1, X, work)
+        assert torch.equal(dW, dW1) and torch.equal(dX, X)
+    if packed and T == 1:
+        dW2, dX2 = torch.empty_like(W[0]), torch.empty_like(X)
+        sar.sar_linear_bwd_packed(p, dZ, W[0], False, dW2, dX2, work)
+        assert torch.equal(dW2, dW[0])
+
+
 def test_the_same_in_every_run():
     n = 20_011
     got = [check_all(n, 100, 64, [0, 7000, 7001, n], F32, True) for _ in range(2)]

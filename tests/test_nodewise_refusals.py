@@ -162,6 +162,7 @@ def test_errors_of_the_library():
     assert bwd(xq=at, xe=at) == bad and "both given" in err()
     assert bwd(X=none, xq=at) == bad and bwd(X=none, xq=at + 8, xe=at) == bad
     assert bwd(dX=at) == bad and "alias" in err()
+    assert bwd() == bad and "dW must not alias W" in err()
     assert bwd(wb=0) == bad
     assert bwd(dW=none, dX=none) == 0
     assert lib.sar_linear_bwd_packed(none, none, at, at, 0, at, none, 0, 1000, 8, 6, at, 1 << 40, none) == bad
