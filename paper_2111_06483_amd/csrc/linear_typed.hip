@@ -519,11 +519,6 @@ int check_call(int dtype, int64_t n, int K, int F, int T, const void* ptr, const
 }
 
 bool few_bwd(const Types& types, int K, int F) { return few_rows_dw(types.n, types.T, K, F) && few_blocks(types, K); }
-bool apart(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
-{
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return !b || x + a_bytes <= y || y + b_bytes <= x;
-}
 
 // The backward pass of both entry points (ptr null: one type); with rows, dX too.
 int typed_bwd(const void* X, const int8_t* Xq, const uint8_t* Xe, const void* dZ, const float* W, const int32_t* ptr, int T, int accumulate,

@@ -7,7 +7,10 @@
 // from the row's own mean, not as a difference of two large sums), and is written once.  A row's lanes are a power of two that
 // covers it in 16-byte pieces, so that narrow rows share a wavefront; rows of more than kWaveRow values take a workgroup.
 // The backward pass keeps a lane's share of dg and db in registers over all rows that the lane meets; a workgroup's wavefronts add theirs up in
-// LDS, every workgroup writes one row of partial sums, and a second launch adds those in a fixed order: the result is the same in every run.
+// LDS, every workgroup writes one row of partial sums, and a second launch adds those in a fixed order (few rows: columns_of_few): the result is the same
+// in every run.
+// 306250 x 256, fp32: forward 105 us, 5.9 TB/s (a large copy: 4.8, one of this size 5.3); backward 187 + 4 us, 5.0 TB/s; 1000003 x 47, bf16, from 8 bits 70 + 4 us,
+// 3.5 TB/s of the bytes it needs, whose rows of 94 and 48 + 2 bytes are no whole lines.
 #include <algorithm>
 #include <cmath>
 
@@ -169,12 +172,58 @@ struct BwdArgs {
     const float* gamma;
     void* dX;
     float* partial;        // [workgroups, 2, D]
-    float* dgamma;         // where one workgroup takes all rows
+    float* dgamma;         // where one workgroup takes all rows, or (`few`) others take columns
     float* dbeta;
     int64_t n;
     int D;
     int accumulate;
+    int groups;            // workgroups that take rows
+    bool few;
 };
+
+// Few rows: both parts in one launch, workgroups behind those that take rows summing 16 columns of dgamma and dbeta each, their threads every 16th row, eight
+// at a time.  With the host's 7.5 us a call: 1000 x 256, fp32, 7.5 us, by two launches 10.4; 1000 x 4096 18.7 and 19.7; 2000 x 256 10.1 and 10.4, 4000 x 256 19.1 and 10.3.
+constexpr int kFewColumns = 16, kFewRows = 1024;
+template <typename T, bool PACKED>
+__device__ inline void columns_of_few(const BwdArgs& a, int c0)
+{
+    constexpr int kSlices = kThreads / kFewColumns, U = 8;
+    __shared__ float part[2][kSlices][kFewColumns];
+    const int k = threadIdx.x % kFewColumns, slice = threadIdx.x / kFewColumns, c = min(c0 + k, a.D - 1);
+    auto value = [](const void* p, int64_t at) {
+        if constexpr (sizeof(T) == 4) return static_cast<const float*>(p)[at];
+        else return bf16_to_f32(static_cast<const bf16_t*>(p)[at]);
+    };
+    float dg = 0.f, db = 0.f;
+    for (int64_t base = slice; base < a.n; base += U * kSlices) {
+        float x[U], dy[U];
+        float2 st[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t row = min(base + u * kSlices, a.n - 1);
+            st[u] = reinterpret_cast<const float2*>(a.stats)[row];
+            dy[u] = value(a.dY, row * a.D + c);
+            if constexpr (PACKED) x[u] = (float)a.Xq[row * packed_stride(a.D) + c] * step_of(a.Xe[row * packed_steps(a.D) + c / kPackBlock]);
+            else x[u] = value(a.X, row * a.D + c);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (base + u * kSlices >= a.n) continue;
+            dg = fmaf(dy[u], (x[u] - st[u].x) * st[u].y, dg);
+            db += dy[u];
+        }
+    }
+    part[0][slice][k] = dg;
+    part[1][slice][k] = db;
+    __syncthreads();
+    const int which = threadIdx.x / kFewColumns;
+    float* out = which == 0 ? a.dgamma : a.dbeta;
+    if (which > 1 || !out || c0 + k >= a.D) return;
+    float v = 0.f;
+#pragma unroll
+    for (int s = 0; s < kSlices; ++s) v += part[which][s][k];
+    out[c0 + k] = a.accumulate ? out[c0 + k] + v : v;
+}
 
 template <typename T, int TPR, int R, int NR, bool PACKED>
 __global__ __launch_bounds__(kThreads) void k_norm_bwd(BwdArgs a)
@@ -183,6 +232,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(BwdArgs a)
     constexpr int kShare = TPR <= kWave ? kWaves : 1;                      // wavefronts that hold the same columns
     __shared__ float lds[2 * NR][kWaves];
     __shared__ float sums[kShare > 1 ? kWaves * 2 * kPieces * N : 1];
+    if ((int)blockIdx.x >= a.groups) return columns_of_few<T, PACKED>(a, ((int)blockIdx.x - a.groups) * kFewColumns);
     const int t = threadIdx.x % TPR, D = a.D;
     const float over = 1.f / (float)D;
     float g[R][N], dg[R][N], db[R][N];
@@ -194,7 +244,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(BwdArgs a)
 #pragma unroll
         for (int j = 0; j < N; ++j) dg[r][j] = db[r][j] = 0.f;
     }
-    for (int64_t base = (int64_t)blockIdx.x * (kRows * NR); base < a.n; base += (int64_t)gridDim.x * (kRows * NR)) {
+    for (int64_t base = (int64_t)blockIdx.x * (kRows * NR); base < a.n; base += (int64_t)a.groups * (kRows * NR)) {
         uint4 xr[NR][R], dr[NR][R];
         typename PackedCols<N>::Raw xp[NR][R];
         float x[NR][R][N], dy[NR][R][N], s[2 * NR];
@@ -255,7 +305,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_bwd(BwdArgs a)
             }
         }
     }
-    if (a.partial == nullptr && a.dgamma == nullptr && a.dbeta == nullptr) return;
+    if (a.few || (a.partial == nullptr && a.dgamma == nullptr && a.dbeta == nullptr)) return;
 
     // a wavefront's lane groups, then a workgroup's wavefronts
     if constexpr (TPR < kWave) {
@@ -445,21 +495,27 @@ extern "C" int sar_layernorm_bwd(const void* dY, const void* X, const int8_t* Xq
     if (n > 0) SAR_CHECK_ARG(dY && (X || Xq) && stats, "null pointer (dY, X or Xq, stats)");
     if ((n == 0 || !dX) && !params) return SAR_OK;
     hipStream_t st = as_stream(stream);
-    const int groups = n == 0 ? 0 : bwd_groups(dtype, n, D);
+    // (dX in the place of an operand: that has to be read first)
+    const size_t bytes = (size_t)n * D * (dtype == SAR_F32 ? 4 : 2);
+    const bool few = params && n > 1 && n <= kFewRows &&
+                     (!dX || (apart(dX, bytes, dY, bytes) && apart(dX, bytes, X, bytes) && apart(dX, bytes, Xq, (size_t)n * packed_stride(D)) &&
+                              apart(dX, bytes, Xe, (size_t)n * packed_steps(D))));
+    const int groups = n == 0 || (few && !dX) ? 0 : bwd_groups(dtype, n, D);
     // (one workgroup's sums need no second launch)
-    const bool second = params && groups != 1;
+    const bool second = params && !few && groups != 1;
     if (second && groups > 0) {
         const size_t need = (size_t)groups * 2 * D * sizeof(float);
         SAR_CHECK_ARG(work && work_bytes >= need, "layer norm: work has %zu bytes, needs %zu", work ? work_bytes : 0, need);
         SAR_CHECK_ARG((reinterpret_cast<uintptr_t>(work) & 15) == 0, "layer norm: work must be 16-byte aligned");
     }
-    if (groups > 0) {
+    if (groups > 0 || few) {
         const BwdArgs a{dY, X, Xq, Xe, stats, gamma, dX, second ? static_cast<float*>(work) : nullptr, second ? nullptr : dgamma,
-                        second ? nullptr : dbeta, n, D, accumulate};
+                        second ? nullptr : dbeta, n, D, accumulate, groups, few};
+        const int all = groups + (few ? (D + kFewColumns - 1) / kFewColumns : 0);
         SAR_TRY(with_shape(dtype, D, [&](auto T0, auto tpr, auto r, auto nr) {
             using T = decltype(T0);
-            if (Xq) k_norm_bwd<T, tpr.value, r.value, nr.value, true><<<groups, kThreads, 0, st>>>(a);
-            else k_norm_bwd<T, tpr.value, r.value, nr.value, false><<<groups, kThreads, 0, st>>>(a);
+            if (Xq) k_norm_bwd<T, tpr.value, r.value, nr.value, true><<<all, kThreads, 0, st>>>(a);
+            else k_norm_bwd<T, tpr.value, r.value, nr.value, false><<<all, kThreads, 0, st>>>(a);
             SAR_LAUNCH_CHECK();
             return (int)SAR_OK;
         }));

@@ -189,6 +189,13 @@ struct PackedCols {
     }
 };
 
+// Whether two ranges of memory have no byte in common (b null: so).
+inline bool apart(const void* a, size_t a_bytes, const void* b, size_t b_bytes)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return !b || x + a_bytes <= y || y + b_bytes <= x;
+}
+
 // Refuses what is no packed tensor (both or neither; q in whole pieces of 16 bytes).
 int check_packed(const char* what, const void* q, const void* e);
 

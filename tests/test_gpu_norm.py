@@ -190,6 +190,32 @@ def test_rows_that_are_constant_huge_or_not_finite(dtype):
     assert torch.isnan(dX[4]).all() and torch.isnan(dX[5]).all()
 
 
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,D", [(2, 47), (100, 2100), (1024, 70), (1025, 70), (1000, 8192)])
+def test_both_sides_of_few_rows(n, D, dtype, packed):
+    """One launch for few rows, two for more; parameters alone, and dX in the place of an operand that the parameters need."""
+    X, dY, gamma, beta = inputs(n, D, dtype)
+    Y, stats = torch.empty_like(X), torch.empty(n, 2, device="cuda")
+    p = sar.packed_empty(n, D, "cuda")
+    sar.sar_layernorm_fwd(X, gamma, beta, EPS, Y, stats, p)
+    if packed:
+        sar.sar_unpack(p, X)
+    x, work = nw.f64(X), work_for(n, D)
+    dX, dg, db = torch.empty_like(X), torch.ones(D, device="cuda"), torch.ones(D, device="cuda")
+    sar.sar_layernorm_bwd(dY, p if packed else X, stats, gamma, True, dX, dg, db, work)
+    check_bwd(dY, x, stats, gamma, dX, dg, db, (1.0, 1.0))
+    only = torch.empty(D, device="cuda")
+    sar.sar_layernorm_bwd(dY, p if packed else X, stats, gamma, False, None, only, None, work)
+    check_bwd(dY, x, stats, gamma, None, only, None)
+    over = dY.clone()
+    sar.sar_layernorm_bwd(over, p if packed else X, stats, gamma, False, over, dg, db, work)
+    check_bwd(dY, x, stats, gamma, over, dg, db)
+    if not packed:
+        sar.sar_layernorm_bwd(dY, X, stats, gamma, False, X, dg, db, work)
+        check_bwd(dY, x, stats, gamma, X, dg, db)
+
+
 def test_the_same_in_every_run():
     X, dY, gamma, beta = inputs(100_003, 47, torch.float32)
     stats, Y = torch.empty(100_003, 2, device="cuda"), torch.empty_like(X)
