@@ -4,8 +4,8 @@
 // a call, the backward pass's two products in the same one, operands straight from memory, the contraction shared by a workgroup's wavefronts,
 // which add up in LDS.  The numbers are formed as there (linear_pieces.h: fp32 as three bf16 pieces, six products, from zero, added by vector
 // instructions; sums that are not finite once more by the fp32 matrix instruction).
-// 2000 x 128 -> 128, bf16, 4 types: 4.3 us, 10 with pieces and lists laid out first; 300 x 256 -> 256, fp32, 5 types: forward 5.1, backward, both products, 7.2, by a launch
-// each 10.9.
+// 2000 x 128 -> 128, bf16, 4 types: 4.3 us, 10 with pieces and lists laid out first; 300 x 256 -> 256, fp32, 5 types: forward 5.1, backward, both products, 7.3, by a launch
+// each 11.2.
 #include <algorithm>
 
 #include "linear_pieces.h"
@@ -289,18 +289,18 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_dw_few(DwArgs a, int ac
     few_weights<XR, ZR, WAVES>(a, accumulate, dW, blockIdx.x * 32, blockIdx.y * 32, blockIdx.z, sums);
 }
 
-// Both: the first workgroups one product's, the others the other's.
+// Both: workgroups from `rows_from` on (as many as there are) take dX, the others dW.
 template <typename XR, typename ZR, int WAVES, int PARTS>
-__global__ __launch_bounds__(WAVES * 64, 2) void k_typed_few_bwd(DwArgs a, int accumulate, float* dW, FewArgs g, unsigned across, unsigned down, unsigned weights,
-                                                                 unsigned beside)
+__global__ __launch_bounds__(WAVES * 64, 2) void k_typed_few_bwd(DwArgs a, int accumulate, float* dW, FewArgs g, unsigned across, unsigned down, unsigned rows_from,
+                                                                 unsigned rows, unsigned beside)
 {
     __shared__ float sums[WAVES * 16 * 64];
-    unsigned i = blockIdx.x;
-    if (i < weights) {
-        few_weights<XR, ZR, WAVES>(a, accumulate, dW, i % across * 32, i / across % down * 32, i / across / down, sums);
-    } else {
-        i -= weights;
+    const unsigned i = blockIdx.x - rows_from;
+    if (i < rows) {
         few_rows<typename ZR::T, true, PARTS, WAVES>(g, i / beside, i % beside, sums);
+    } else {
+        const unsigned w = blockIdx.x < rows_from ? blockIdx.x : blockIdx.x - rows;
+        few_weights<XR, ZR, WAVES>(a, accumulate, dW, w % across * 32, w / across % down * 32, w / across / down, sums);
     }
 }
 
@@ -334,16 +334,22 @@ int weights(const TypedDw& g, hipStream_t st)
     return SAR_OK;
 }
 
+// One launch for both products as long as they are about what the chip holds at once (a wavefront of the one takes the registers of the other's; bf16 from 8
+// bits, together and apart: 300 x 256 -> 256 of 5 types 6.9 and 10.3 us, 2000 x 256 -> 256 of 8 types 18.1 and 23.3, 8000 x 256 -> 256 of 46 types 53.5 and 50.9, 4735 x 258 -> 400 of 46
+// 80.8 and 62.2).
+constexpr int64_t kBothWaves = 16384;
 template <typename XR, typename ZR, int WAVES, int PARTS>
 int both(const TypedDw& g, const FewArgs& a, hipStream_t st)
 {
     const unsigned across = (g.K + 31) / 32, down = (g.F + 31) / 32, beside = (a.N + 32 * (WAVES / PARTS) - 1) / (32 * (WAVES / PARTS));
-    const int64_t first = (int64_t)across * down * g.types.T, second = row_blocks(a.types) * beside;
-    if (first + second > 0x7fffffff) {
+    const int64_t dw = (int64_t)across * down * g.types.T, dx = row_blocks(a.types) * beside;
+    if ((dw + dx) * WAVES > kBothWaves) {
         SAR_TRY((weights<XR, ZR>(g, st)));
         return product<typename ZR::T, true>(a, st);
     }
-    k_typed_few_bwd<XR, ZR, WAVES, PARTS><<<(unsigned)(first + second), WAVES * 64, 0, st>>>(dw_args(g), g.accumulate, g.dW, a, across, down, (unsigned)first, beside);
+    // the longer contraction first: they need not all fit at once
+    k_typed_few_bwd<XR, ZR, WAVES, PARTS><<<(unsigned)(dw + dx), WAVES * 64, 0, st>>>(dw_args(g), g.accumulate, g.dW, a, across, down,
+                                                                                    g.types.n < g.F ? 0u : (unsigned)dw, (unsigned)dx, beside);
     SAR_LAUNCH_CHECK();
     return SAR_OK;
 }
@@ -361,13 +367,15 @@ int both(const TypedDw& g, const FewArgs& a, hipStream_t st)
 constexpr int kFewBlocks = 2560;
 bool few_blocks(const Types& types, int N) { return row_blocks(types) * ((N + 31) / 32) <= kFewBlocks; }
 
-// Whether these take a backward pass's sums over rows.  Every 32 x 32 weights read their columns anew, and of one type a wavefront takes every eighth 16 rows (256 x 256, fp32: 500
-// rows 6.5 us and 10.6 in shares of the rows (linear_typed_dw.hip), 1000 rows 10.6 and 11.6, 2000 rows 19.1 and 13.9); of several, whose shares are seldom even, twice as many rows (2000
-// rows of four even types 6.9 and 16.1, 4000 rows 12.1 and 20.5; were they all of one type, 35.0 and 16.4).
-constexpr int64_t kFewRows = 1024, kFewColumns = 1 << 18;
+// Whether these take a backward pass's sums over rows.  Of one type a wavefront takes every eighth 16 rows (256 x 256, fp32: 500 rows 6.5 us and 10.6 in shares
+// of the rows (linear_typed_dw.hip), 1000 rows 10.6 and 11.6, 2000 rows 19.1 and 13.9); of several, whose shares are seldom even, the largest may have a good part:
+// 256 rows a type (shares as the cubes of random numbers, 256 x 256 from 8 bits: 8 types, 2000 rows 14.9 and 18.4, 4000 rows 26.5 and 21.8; 46 types, 8000 rows 38.0
+// and 50.4; 64 x 100: 9.5 and 22.2, 16000 rows 16.7 and 22.5).  And every 32 x 32 weights read their columns anew (1000 rows, 1024 x 1024 from 8 bits 40.5 and 43.0, 2048 x 1024
+// 78.5 and 59.1).
+constexpr int64_t kFewRows = 1024, kFewOfType = 256, kFewRowsOfAll = 16384, kFewColumns = 1 << 20;
 bool few_rows_dw(int64_t n, int T, int K, int F)
 {
-    return n <= (T > 1 ? 2 * kFewRows : kFewRows) && n * ((K + 31) / 32) * ((F + 31) / 32) <= kFewColumns;
+    return n <= std::min(std::max(kFewRows, kFewOfType * T), kFewRowsOfAll) && n * ((K + 31) / 32) * ((F + 31) / 32) <= kFewColumns;
 }
 
 int few_product(int dtype, bool trans, const FewArgs& a, hipStream_t st)
