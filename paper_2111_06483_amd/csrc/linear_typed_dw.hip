@@ -14,8 +14,8 @@
 // next workgroup or the next type, so no two have the same place), and a second launch adds a type's places up in order: the result is the
 // same in every run.  Sums that are not finite are taken again there, from the operands.
 // What bounds it: 237500 x 256 x 256, fp32, 218 us = 143 TFLOP/s (the six products' 857 TFLOP/s of bf16, of 1170 that a large library product reaches); bf16 from
-// 8 bits, 867187 rows, 231 us: 680 MB once would be 141, its products 97; every chunk's way from memory through registers to LDS takes as many issue
-// slots as the products leave.
+// 8 bits, 867187 rows, 218 us: its 680 MB once would be 141, its products 97; every chunk's way from memory through registers to LDS is instructions between the
+// products (the matrix cores are busy a quarter of the cycles).
 #include <algorithm>
 
 #include "linear_pieces.h"
@@ -437,10 +437,12 @@ struct Shape {
 // again: the widest tile whose workgroups have chunks enough.  256 x 256 by tiles of 128 x 256 / 128 x 128 / 128 x 64, us:
 //   fp32, from 8 bits:  10 thousand rows 27.3 / 22.3 / 20.5, 40 thousand 43.3 / 39.3 / 40.7, 160 thousand 107 / 111 / 122
 //   bf16, from 8 bits:  10 thousand rows 24.3 / 22.9 / 18.0, 80 thousand 41.5 / 37.8 / 40.7, 160 thousand 56.8 / 58.0 / 67.9
+// From 8 bits rather 256 x 128 than 128 x 256, so that it is the short rows that two tiles read (867187 rows, bf16: 218 us and 226; 200 thousand, fp32: 133 and 137; of plain bf16
+// rows 82 and 72).
 // A compute unit holds two workgroups of 128 x 128 with fp32 rows (three asked for: 160 thousand rows 128 x 128, 60.1 us, two 50.8) and three with bf16 ones
 // (256 x 256: 58.0, two 66.1), three of 64 columns or rows (256 x 47, fp32: four 61.8, three 56.3).  Four chunks are a share's least (100 x 47, fp32: two, four, eight chunks, 4
 // thousand rows 10.5, 10.6, 13.6 us, 16 thousand 20.5, 15.5, 15.9).
-Shape shape_of(int64_t n, int K, int F, int chunk)
+Shape shape_of(int64_t n, int K, int F, int chunk, bool packed)
 {
     auto shape = [&](int tk, int tf, int resident) {
         const int tiles = ((K + tk - 1) / tk) * ((F + tf - 1) / tf);
@@ -452,8 +454,9 @@ Shape shape_of(int64_t n, int K, int F, int chunk)
     };
     if (F > 64 && K > 64) {
         Shape s{};
-        if ((F + 127) / 128 % 2 == 0) s = shape(128, 256, 2);
-        else if ((K + 127) / 128 % 2 == 0) s = shape(256, 128, 2);
+        const bool wide_K = (K + 127) / 128 % 2 == 0, wide_F = (F + 127) / 128 % 2 == 0;
+        if (wide_K && (packed || !wide_F)) s = shape(256, 128, 2);
+        else if (wide_F) s = shape(128, 256, 2);
         if (s.share >= 16 * chunk) return s;
         s = shape(128, 128, chunk == kChunk32 ? 2 : 3);
         if (s.share >= 8 * chunk) return s;
@@ -499,13 +502,14 @@ int run_all(const DwArgs& a, const Shape& s, int accumulate, float* dW, hipStrea
 
 size_t typed_dw_bytes(int64_t n, int K, int F, int T)
 {
-    return (size_t)(std::max(shape_of(n, K, F, kChunk32).groups, shape_of(n, K, F, kChunk16).groups) + T) * K * F * sizeof(float);
+    auto most = [&](int chunk) { return std::max(shape_of(n, K, F, chunk, false).groups, shape_of(n, K, F, chunk, true).groups); };
+    return (size_t)(std::max(most(kChunk32), most(kChunk16)) + T) * K * F * sizeof(float);
 }
 
 int typed_dw(int dtype, const TypedDw& g, hipStream_t st)
 {
     if (few_rows_dw(g.types.n, g.types.T, g.K, g.F)) return few_dw(dtype, g, st);
-    const Shape s = shape_of(g.types.n, g.K, g.F, dtype == SAR_F32 ? kChunk32 : kChunk16);
+    const Shape s = shape_of(g.types.n, g.K, g.F, dtype == SAR_F32 ? kChunk32 : kChunk16, g.Xq != nullptr);
     const DwArgs a{g.X, g.Xq, g.Xe, g.dZ, g.partial, g.types, g.K, g.F, s.share};
     if (dtype == SAR_F32)
         return g.Xq ? run_all<PackedRows, F32Rows, kChunk32 / 16, 2>(a, s, g.accumulate, g.dW, st)

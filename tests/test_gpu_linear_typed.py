@@ -100,6 +100,17 @@ def test_shapes(K, F, dtype, packed):
 
 
 @pytest.mark.parametrize("dtype,packed", KINDS)
+@pytest.mark.parametrize("n,K,F", [(140_003, 256, 256), (270_001, 100, 250), (270_001, 201, 70)])
+def test_weight_gradients_by_the_widest_tiles(n, K, F, dtype, packed):
+    X, dZ, W = inputs(n, K, F, 3, dtype)
+    p, x = packed_of(X) if packed else (X, nw.f64(X))
+    ends = [5, 100_000, 100_000, n - 7]
+    dW = torch.empty_like(W)
+    sar.sar_linear_typed_bwd(p, dZ, W, ptr_of(ends), False, dW, None, work_for(n, K, F, 3))
+    check_dw(x, dZ, dW, nw.spans(ends, n))
+
+
+@pytest.mark.parametrize("dtype,packed", KINDS)
 @pytest.mark.parametrize("K,F", [(1, 1), (1, 40), (3, 2), (7, 9), (16, 47), (31, 33), (47, 65), (63, 100), (64, 129), (129, 31)])
 def test_shapes_by_the_kernels_of_many_rows(K, F, dtype, packed):
     """Ragged widths where the calls of few rows are not taken: both products of rows, and the weights' gradients in shares."""
