@@ -295,8 +295,9 @@ __device__ SAR_INLINE inline void multiply_stage(const uint4* b, const uint4 (&p
     }
 }
 
-// A stage's products, while the next stage's pieces (`from`, null where there is none) go to `to`.  (A function of its own for its arguments' sake: it is by them that the compiler knows the two apart.  Otherwise every
-// first read of a stage waits for the copy that was just begun: 237500 x 256 -> 256, fp32, 226 us for 195.)
+// A stage's products, while the next stage's pieces (`from`, null where there is none) go to `to`.  (A function of its own for its arguments'
+// sake: it is by them that the compiler knows the two apart.  Otherwise every first read of a stage waits for the copy that was just begun:
+// 237500 x 256 -> 256, fp32, 226 us for 195.)
 template <typename T, int NT, int SP, typename Fetch>
 __device__ SAR_INLINE inline void stage_products(uint4* __restrict__ to, const uint4* from, const uint4* __restrict__ b,
                                                  const uint4 (&p)[Share<T, NT>::MR][Mode<T>::kStage][SP], float sign, bool works,
