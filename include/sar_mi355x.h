@@ -497,8 +497,8 @@ int sar_layernorm_workspace_bytes(int64_t n, int D, size_t* bytes);
 /* -------------------------------------- transforms with a weight per node type
  * Rows sorted by type: those of type t are [type_ptr[t], type_ptr[t+1]), type_ptr device int32 [T+1], ascending, with
  * values of 0..n (what lies outside is cut off; rows that no type has are neither read nor written).  T <= 65535; a
- * type may have no row.  n < 2^31 - 256; K, F <= 65536.  fp32 results are sums of products that are exact for operands of at
- * least 2^-110 in size (smaller ones count to within 2^-126); bf16 rows meet weights taken to 16 bits, and are rounded when stored.
+ * type may have no row.  n < 2^31 - 256; K, F <= 65536.  fp32 results are sums of products that are exact for operands of any
+ * size; bf16 rows meet weights taken to 16 bits (as in sar_linear_fwd; those below 2^-117 to within 2^-134), and are rounded when stored.
  * work: scratch of at least sar_linear_typed_workspace_bytes, 16-byte aligned.
  */
 

@@ -51,6 +51,13 @@ int few_product(int dtype, bool trans, const FewArgs& a, hipStream_t st);
 int few_dw(int dtype, const TypedDw& g, hipStream_t st);
 int few_dw_and_dx(int dtype, const TypedDw& g, const FewArgs& a, hipStream_t st);
 
+// Operands of fp32 products are multiplied by 2^24 before they are cut into pieces of bf16, and sums by what takes that back where they are added up.  An
+// fp32 value is a multiple of 2^-149, so its pieces are then multiples of 2^-125, each a normal bf16 value, and a value keeps its bits however small it
+// is (unscaled, the last bits of a value below 2^-110 have no bf16 value).  What this takes away is the other end: of values from 2^104 and sums from 2^80
+// on, which are formed again from the operands as all that are not finite are.  (A multiplication a value:
+// 237500 x 256 -> 256 of four types 191.3 us for 190.0, backward 405.7 for 403.5.)
+constexpr float kUp = 0x1p24f, kDown = 0x1p-24f;
+
 // What rows an operand has: pieces of a value, values a thread takes of a row, and their bytes.
 struct F32Rows {
     using T = float;

@@ -3,8 +3,8 @@
 // Both are rows (contraction index contiguous) times a small operand B [C, N] per type.
 //   - Few rows (linear_typed_few.hip): latency.  One launch.
 //   - Otherwise a first launch (k_typed_lay) lays B out in pieces of bf16, in the order in which a wavefront's lanes want them: fp32 rows three pieces a
-//     weight (exact products, linear_pieces.h), bf16 rows two (the weight to 16 bits), T K F values; and lists the row blocks of every type, as many
-//     as its rows need, which the workgroups of the main launch (k_typed_rows) share: 128 rows and up to 256 columns at a time, four wavefronts, the
+//     weight (24 bits, linear_pieces.h), bf16 rows two (as in linear.hip: the weight to 16 bits, below 2^-117 to
+//     within 2^-134; the result is rounded to 8), T K F values; and lists the row blocks of every type, as many as its rows need, which the workgroups of the main launch (k_typed_rows) share: 128 rows and up to 256 columns at a time, four wavefronts, the
 //     pieces by asynchronous copies to LDS, two buffers, a barrier a stage.  (Tried, with no gain beyond a twentieth either way: 256 rows by eight
 //     wavefronts, rows by asynchronous copies as well, both two stages ahead.)
 //   - Columns are dealt to the column tiles by turns (`column_of`), so that a lane ends up with four neighbours of a row and writes them at once:
@@ -12,8 +12,8 @@
 // fp32 sums: the matrix unit cuts (does not round) when it adds, so a chunk's 16 products are summed from zero there and added to the
 // running sum by vector instructions, which round to nearest; and every other chunk is multiplied by -B and subtracted, so that what is
 // cut leans to neither side.  bf16 products of at most a few hundred terms, whose sums are rounded to 8 bits, are added there.  A result that is not finite
-// (infinities and NaN have no such pieces, and the largest numbers round to infinity) sends the wavefront's tile back to the fp32 matrix instruction, from
-// the operands themselves.  Operands below 2^-110 in size are taken to within 2^-126.
+// (infinities and NaN have no such pieces, and numbers are scaled up first, kUp) sends the wavefront's tile back to the fp32 matrix instruction, from
+// the operands themselves.
 // What bounds them (256 -> 256, four types): fp32, 237500 rows, 191 us = 163 TFLOP/s: the six products, 978 TFLOP/s of bf16 (a large library product in
 // bf16 reaches 1170, one in fp32 154); bf16, 867187 rows, 276 us: its two products 823 TFLOP/s, its 888 MB 3.2 TB/s, neither alone (195 and 185 us).
 #include <algorithm>
@@ -114,7 +114,7 @@ __global__ __launch_bounds__(256) void k_typed_lay(LayArgs a)
     for (int j = 0; j < 8; ++j) {
         v[j] = 0.f;
         if (n < a.N && c + j < a.C) v[j] = TRANS ? W[(int64_t)n * a.F + c + j] : W[(int64_t)(c + j) * a.F + n];
-        if (P == 3 && (chunk & 1)) v[j] = -v[j];
+        if (P == 3) v[j] *= chunk & 1 ? -kUp : kUp;
     }
     uint4* out = a.out + (((int64_t)(t * a.blocks + block) * a.chunks + chunk) * S + s) * (P * NT * 64) + tile * 64 + lane;
     if constexpr (P == 3) {
@@ -391,7 +391,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs a)
         for (int m = 0; m < MR; ++m)
 #pragma unroll
             for (int i = 0; i < NW; ++i) acc[m][i] = float16_t{};
-        float sign = 1.f;
+        float sign = kDown * kDown;        // (fp32 products: rows' and weights' 2^24)
         for (int chunk = 0; chunk < a.chunks; ++chunk) {
             const bool more = chunk + 1 < a.chunks, coming = more ? here : there;
             uint4 p[S / SB][MR][SB][kSP];
@@ -403,9 +403,11 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs a)
 #pragma unroll
                     for (int s = 0; s < S; ++s) {
                         if constexpr (P == 3) {
-                            const float v[8] = {__uint_as_float(x[2 * s].x), __uint_as_float(x[2 * s].y), __uint_as_float(x[2 * s].z),
-                                                __uint_as_float(x[2 * s].w), __uint_as_float(x[2 * s + 1].x), __uint_as_float(x[2 * s + 1].y),
-                                                __uint_as_float(x[2 * s + 1].z), __uint_as_float(x[2 * s + 1].w)};
+                            float v[8] = {__uint_as_float(x[2 * s].x), __uint_as_float(x[2 * s].y), __uint_as_float(x[2 * s].z),
+                                          __uint_as_float(x[2 * s].w), __uint_as_float(x[2 * s + 1].x), __uint_as_float(x[2 * s + 1].y),
+                                          __uint_as_float(x[2 * s + 1].z), __uint_as_float(x[2 * s + 1].w)};
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) v[j] *= kUp;
                             split8(v, p[s / SB][m][s % SB]);
                         } else {
                             p[s / SB][m][s % SB][0] = x[s];

@@ -90,13 +90,13 @@ struct Unit {
             }
         }
         if constexpr (sizeof(T) == 4) {
-            const uint32_t flip = negate ? 0x80000000u : 0u;
+            const float scale = negate ? -kUp : kUp;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 float v[8];
                 uint4 p[3];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(w[2 * k + j] ^ flip);
+                for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(w[2 * k + j]) * scale;
                 split8(v, p);
 #pragma unroll
                 for (int t = 0; t < 3; ++t) out[t * stride + 32 * j] = p[t];
@@ -280,7 +280,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
                         }
                     }
                 } else {
-                    const float sign = minus(i) ? -1.f : 1.f;
+                    constexpr float kBack = (PX == 3 ? kDown : 1.f) * kDown;
+                    const float sign = minus(i) ? -kBack : kBack;
                     // one tile's products run while the sums of the one before are added; no more than these two are kept at once
                     auto add = [&](int i, const float16_t& sum) SAR_INLINE {
 #pragma unroll
@@ -363,7 +364,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
 }
 
 // What a workgroup's place w + t should hold where it holds no finite number: three pieces of bf16 are no infinity, no NaN and none of the
-// largest numbers, whose rounding up is an infinity.  Summed again from the operands, by multiply-adds.
+// numbers that are too large to be scaled up (kUp).  Summed again from the operands, by multiply-adds.
 template <typename XR, typename ZR>
 __device__ float sum_again(const DwArgs& a, int64_t w, int64_t lo, int64_t hi, int64_t element)
 {

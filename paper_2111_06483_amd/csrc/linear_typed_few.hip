@@ -107,20 +107,20 @@ __device__ SAR_INLINE inline void few_rows(const FewArgs& a, int64_t row_block, 
             if (k0 + u * 16 >= a.C) break;
             float w[8], x[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = c + j < a.C ? g.w[u][j] : 0.f;
+            for (int j = 0; j < 8; ++j) w[j] = c + j < a.C ? g.w[u][j] * (sizeof(T) == 4 ? kUp : 1.f) : 0.f;
             if constexpr (sizeof(T) == 4) {
                 float lo[4], hi[4];
                 Cols<T>::values(g.x[u][0], c, a.C, lo);
                 Cols<T>::values(g.x[u][1 % kRaw], c + 4, a.C, hi);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = lo[j], x[4 + j] = hi[j];
+                for (int j = 0; j < 4; ++j) x[j] = lo[j] * kUp, x[4 + j] = hi[j] * kUp;
                 uint4 p[3], q[3];
                 split8(x, p);
                 split8(w, q);
                 float16_t sum;
                 multiply_split(p, q, sum);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[0][r] += sum[r];
+                for (int r = 0; r < 16; ++r) acc[0][r] = fmaf(sum[r], kDown * kDown, acc[0][r]);
             } else {
                 const uint4 m = Cols<T>::within(c, a.C), v = g.x[u][0];
                 const uint4 p = make_uint4(v.x & m.x, v.y & m.y, v.z & m.z, v.w & m.w);
@@ -221,10 +221,20 @@ __device__ SAR_INLINE inline void few_weights(const DwArgs& a, int accumulate, f
             auto whole = [](const float (&v)[8]) SAR_INLINE {        // (bf16 values: not rounded)
                 return make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
             };
-            if constexpr (PX == 3) split8(x, p);
-            else p[0] = whole(x);
-            if constexpr (PZ == 3) split8(z, q);
-            else q[0] = whole(z);
+            if constexpr (PX == 3) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] *= kUp;
+                split8(x, p);
+            } else {
+                p[0] = whole(x);
+            }
+            if constexpr (PZ == 3) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[j] *= kUp;
+                split8(z, q);
+            } else {
+                q[0] = whole(z);
+            }
             float16_t sum = {};
 #pragma unroll
             for (int i = 0; i < 6; ++i)
@@ -232,7 +242,7 @@ __device__ SAR_INLINE inline void few_weights(const DwArgs& a, int accumulate, f
                     sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p[kTerm[i][0] < PX ? kTerm[i][0] : 0]),
                                                                   __builtin_bit_cast(bf16x8_t, q[kTerm[i][1] < PZ ? kTerm[i][1] : 0]), sum, 0, 0, 0);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) acc[r] += sum[r];
+            for (int r = 0; r < 16; ++r) acc[r] = fmaf(sum[r], (PX == 3 ? kDown : 1.f) * (PZ == 3 ? kDown : 1.f), acc[r]);
         }
     };
     const int64_t from = lo + wave * 16;
