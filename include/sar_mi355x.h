@@ -499,7 +499,7 @@ int sar_layernorm_workspace_bytes(int64_t n, int D, size_t* bytes);
  * values of 0..n (what lies outside is cut off; rows that no type has are neither read nor written).  T <= 65535; a
  * type may have no row.  n < 2^31 - 256; K, F <= 65536.  fp32 results are sums of products that are exact for operands of any
  * size; bf16 rows meet weights taken to 16 bits (as in sar_linear_fwd; those below 2^-117 to within 2^-134), and are rounded when stored.
- * work: scratch of at least sar_linear_typed_workspace_bytes, 16-byte aligned.
+ * work: scratch of at least sar_linear_typed_workspace_bytes, 16-byte aligned; that of n rows serves fewer as well.
  */
 
 /* Z[i] = X[i] W[t(i)]: X [n,K], Z [n,F] of `dtype` (no alias), W fp32 [T,K,F]. */

@@ -443,26 +443,48 @@ struct Shape {
 // A compute unit holds two workgroups of 128 x 128 with fp32 rows (three asked for: 160 thousand rows 128 x 128, 60.1 us, two 50.8) and three with bf16 ones
 // (256 x 256: 58.0, two 66.1), three of 64 columns or rows (256 x 47, fp32: four 61.8, three 56.3).  Four chunks are a share's least (100 x 47, fp32: two, four, eight chunks, 4
 // thousand rows 10.5, 10.6, 13.6 us, 16 thousand 20.5, 15.5, 15.9).
+struct Tile {
+    int tk, tf, resident, least;       // weights; workgroups of a compute unit; the chunks that a share has at least
+};
+// The tiles that may take K x F weights, widest first, a narrow one last.
+int tiles_of(int K, int F, int chunk, bool packed, Tile (&t)[3])
+{
+    int count = 0;
+    if (F > 64 && K > 64) {
+        const bool wide_K = (K + 127) / 128 % 2 == 0, wide_F = (F + 127) / 128 % 2 == 0;
+        if (wide_K && (packed || !wide_F)) t[count++] = {256, 128, 2, 16};
+        else if (wide_F) t[count++] = {128, 256, 2, 16};
+        t[count++] = {128, 128, chunk == kChunk32 ? 2 : 3, 8};
+    }
+    t[count++] = K <= 64 && F > 64 ? Tile{64, 128, 3, 4} : Tile{128, 64, 3, 4};
+    return count;
+}
+int64_t most_at_once(const Tile& t, int K, int F) { return std::max(1, 256 * t.resident / (((K + t.tk - 1) / t.tk) * ((F + t.tf - 1) / t.tf))); }
+
 Shape shape_of(int64_t n, int K, int F, int chunk, bool packed)
 {
-    auto shape = [&](int tk, int tf, int resident) {
-        const int tiles = ((K + tk - 1) / tk) * ((F + tf - 1) / tf);
+    Tile t[3];
+    const int count = tiles_of(K, F, chunk, packed, t);
+    for (int i = 0;; ++i) {
         const int64_t least = 4 * chunk;
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>((n + least - 1) / least, std::max(1, 256 * resident / tiles)));
-        Shape s{tk, tf, std::max<int64_t>(least, ((n + want - 1) / want + 31) / 32 * 32), 0};
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>((n + least - 1) / least, most_at_once(t[i], K, F)));
+        Shape s{t[i].tk, t[i].tf, std::max<int64_t>(least, ((n + want - 1) / want + 31) / 32 * 32), 0};
         s.groups = std::max<int64_t>(1, (n + s.share - 1) / s.share);
-        return s;
-    };
-    if (F > 64 && K > 64) {
-        Shape s{};
-        const bool wide_K = (K + 127) / 128 % 2 == 0, wide_F = (F + 127) / 128 % 2 == 0;
-        if (wide_K && (packed || !wide_F)) s = shape(256, 128, 2);
-        else if (wide_F) s = shape(128, 256, 2);
-        if (s.share >= 16 * chunk) return s;
-        s = shape(128, 128, chunk == kChunk32 ? 2 : 3);
-        if (s.share >= 8 * chunk) return s;
+        if (i == count - 1 || s.share >= t[i].least * chunk) return s;
     }
-    return K <= 64 && F > 64 ? shape(64, 128, 3) : shape(128, 64, 3);
+}
+
+// No fewer workgroups than any call of up to n rows has: what that is grows with n, though their number need not (shares are whole 32 rows, and
+// wider tiles are fewer).  Scratch for a batch's most rows then serves all of its batches.
+int64_t most_groups(int64_t n, int K, int F, int chunk, bool packed)
+{
+    Tile t[3];
+    int64_t most = 1;
+    for (int i = tiles_of(K, F, chunk, packed, t) - 1; i >= 0; --i) {
+        const int64_t share = t[i].least * chunk;
+        most = std::max(most, std::min((n + share - 1) / share, most_at_once(t[i], K, F)));
+    }
+    return most;
 }
 
 template <typename XR, typename ZR, int MT, int NT, int WM, int WN, int S, int AHEAD>
@@ -503,7 +525,7 @@ int run_all(const DwArgs& a, const Shape& s, int accumulate, float* dW, hipStrea
 
 size_t typed_dw_bytes(int64_t n, int K, int F, int T)
 {
-    auto most = [&](int chunk) { return std::max(shape_of(n, K, F, chunk, false).groups, shape_of(n, K, F, chunk, true).groups); };
+    auto most = [&](int chunk) { return std::max(most_groups(n, K, F, chunk, false), most_groups(n, K, F, chunk, true)); };
     return (size_t)(std::max(most(kChunk32), most(kChunk16)) + T) * K * F * sizeof(float);
 }
 
