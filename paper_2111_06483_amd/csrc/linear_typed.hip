@@ -452,8 +452,6 @@ template <typename T, int NT, bool TRANS>
 int run_rows(const RowsArgs& a, LayArgs l, hipStream_t st)
 {
     const int64_t units = (int64_t)l.T * l.blocks * l.chunks * Mode<T>::kSteps * NT * 64, lay = (units + 255) / 256;
-    if (lay > 0x7fffffff - 65536 || l.blocks > 65535)
-        return fail(SAR_ERR_UNSUPPORTED, "typed products: %d x %d weights of %d types are too many for one launch", a.K, a.F, l.T);
     l.lay = (unsigned)lay;
     k_typed_lay<T, NT, TRANS><<<(unsigned)lay + l.T, 256, 0, st>>>(l);
     SAR_LAUNCH_CHECK();
@@ -502,6 +500,9 @@ int check_shape(int64_t n, int K, int F, int T)
     if (n > 0x7fffffff - 256 || K > 65536 || F > 65536 || T > 65535)
         return fail(SAR_ERR_UNSUPPORTED, "typed products: n = %lld rows (below 2^31 - 256), K = %d, F = %d (at most 65536), T = %d types (at most 65535)",
                     (long long)n, K, F, T);
+    // (the launch that lays them out: a thread for two or three pieces of 16 bytes, and a workgroup for each type)
+    if (std::max(lay_bytes(K, F, T), lay_bytes(F, K, T)) / (2 * 16 * 256) + T > (size_t)most_workgroups(256))
+        return fail(SAR_ERR_UNSUPPORTED, "typed products: %d x %d weights of %d types are too many for one launch", K, F, T);
     return SAR_OK;
 }
 

@@ -469,7 +469,7 @@ extern "C" int sar_layernorm_fwd(const void* X, const float* gamma, const float*
     return with_shape(dtype, D, [&](auto T0, auto tpr, auto r, auto nr) {
         using T = decltype(T0);
         const int64_t rows = kThreads / tpr.value * nr.value, wgs = (n + rows - 1) / rows;
-        if (wgs > 0x7fffffff) return fail(SAR_ERR_UNSUPPORTED, "layer norm: %lld rows are too many for one launch", (long long)n);
+        if (wgs > most_workgroups(kThreads)) return fail(SAR_ERR_UNSUPPORTED, "layer norm: %lld rows are too many for one launch", (long long)n);
         k_norm_fwd<T, tpr.value, r.value, nr.value><<<(unsigned)wgs, kThreads, 0, as_stream(stream)>>>(a);
         SAR_LAUNCH_CHECK();
         return (int)SAR_OK;

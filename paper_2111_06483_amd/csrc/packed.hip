@@ -66,7 +66,7 @@ int run(T* X, int8_t* q, uint8_t* e, int64_t n, int K, hipStream_t st)
 {
     const uint32_t per_row = (uint32_t)packed_steps(K) * (kPackBlock / Cols<T>::N);
     const int64_t units = n * per_row, wgs = (units + kUnits * kThreads - 1) / (kUnits * kThreads);
-    if (wgs > 0x7fffffff) return fail(SAR_ERR_UNSUPPORTED, "packed rows: %lld rows of %d values are too many for one launch", (long long)n, K);
+    if (wgs > most_workgroups(kThreads)) return fail(SAR_ERR_UNSUPPORTED, "packed rows: %lld rows of %d values are too many for one launch", (long long)n, K);
     k_packed<T, PACK><<<(unsigned)wgs, kThreads, 0, st>>>(X, q, e, n, K, per_row);
     SAR_LAUNCH_CHECK();
     return SAR_OK;

@@ -36,6 +36,9 @@ int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
         if (sar_rc_ != SAR_OK) return sar_rc_;                                          \
     } while (0)
 
+// A launch's workgroups along one side: their threads are fewer than 2^32.
+constexpr int64_t most_workgroups(int threads) { return 0xffffffffll / threads; }
+
 #define SAR_LAUNCH_CHECK() SAR_HIP(hipGetLastError())
 
 // Rows (or sources) with at least this many edges in a block are "long": they
