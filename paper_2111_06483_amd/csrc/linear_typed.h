@@ -40,16 +40,16 @@ int typed_dw(int dtype, const TypedDw& g, hipStream_t st);
 // Calls of few rows (linear_typed_few.hip): whether they are, and one launch each, or one for both of a backward pass.
 bool few_blocks(const Types& types, int N);
 bool few_rows_dw(int64_t n, int T, int K, int F);
-struct FewArgs {
+struct TypedRows {
     const void* A;         // [n, C]
     const float* W;        // [T, K, F]
     void* out;             // [n, N]
     Types types;
     int C, N, K, F;
 };
-int few_product(int dtype, bool trans, const FewArgs& a, hipStream_t st);
+int few_product(int dtype, bool trans, const TypedRows& a, hipStream_t st);
 int few_dw(int dtype, const TypedDw& g, hipStream_t st);
-int few_dw_and_dx(int dtype, const TypedDw& g, const FewArgs& a, hipStream_t st);
+int few_dw_and_dx(int dtype, const TypedDw& g, const TypedRows& a, hipStream_t st);
 
 // Operands of fp32 products are multiplied by 2^24 before they are cut into pieces of bf16, and sums by what takes that back where they are added up.  An
 // fp32 value is a multiple of 2^-149, so its pieces are then multiples of 2^-125, each a normal bf16 value, and a value keeps its bits however small it

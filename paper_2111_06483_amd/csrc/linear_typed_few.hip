@@ -49,7 +49,7 @@ __device__ inline bool few_rows_of(const Types& types, int64_t index, int& t, in
 // PARTS: wavefronts that share one block's contraction, chunk by chunk, and add up in LDS (4), or one a block (1), of a workgroup of WAVES.  `row`: which
 // block of rows; `beside`: which of the groups of column tiles that a workgroup takes; `sums`: [WAVES][16][64].
 template <typename T, bool TRANS, int PARTS, int WAVES>
-__device__ SAR_INLINE inline void few_rows(const FewArgs& a, int64_t row_block, int beside, float* sums)
+__device__ SAR_INLINE inline void few_rows(const TypedRows& a, int64_t row_block, int beside, float* sums)
 {
     constexpr int N = Cols<T>::N, kRaw = 8 / N, U = 4;                // 16-byte pieces of a row a product of 16; products a chunk
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, share = wave % PARTS;
@@ -286,7 +286,7 @@ __device__ SAR_INLINE inline void few_weights(const DwArgs& a, int accumulate, f
 // ---- launches
 
 template <typename T, bool TRANS, int PARTS>
-__global__ __launch_bounds__(256, 2) void k_typed_few(FewArgs a)
+__global__ __launch_bounds__(256, 2) void k_typed_few(TypedRows a)
 {
     __shared__ float sums[PARTS == 4 ? 4 * 16 * 64 : 1];
     few_rows<T, TRANS, PARTS, 4>(a, blockIdx.x, blockIdx.y, sums);
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_dw_few(DwArgs a, int ac
 
 // Both: workgroups from `rows_from` on (as many as there are) take dX, the others dW.
 template <typename XR, typename ZR, int WAVES, int PARTS>
-__global__ __launch_bounds__(WAVES * 64, 2) void k_typed_few_bwd(DwArgs a, int accumulate, float* dW, FewArgs g, unsigned across, unsigned down, unsigned rows_from,
+__global__ __launch_bounds__(WAVES * 64, 2) void k_typed_few_bwd(DwArgs a, int accumulate, float* dW, TypedRows g, unsigned across, unsigned down, unsigned rows_from,
                                                                  unsigned rows, unsigned beside)
 {
     __shared__ float sums[WAVES * 16 * 64];
@@ -317,13 +317,13 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_few_bwd(DwArgs a, int a
 int64_t row_blocks(const Types& types) { return types.n / 32 + types.T; }
 // Four wavefronts a block where that is no more than four a SIMD (2000 rows 256 -> 256, fp32, 544 blocks 9.2 us, one a block 13.0; 8000 rows 25.2 and 21.4).
 constexpr int kFewShared = 1024;
-bool shared_blocks(const FewArgs& a) { return a.C > 64 && row_blocks(a.types) * ((a.N + 31) / 32) <= kFewShared; }
+bool shared_blocks(const TypedRows& a) { return a.C > 64 && row_blocks(a.types) * ((a.N + 31) / 32) <= kFewShared; }
 // Eight wavefronts for 32 x 32 weights where types have rows for them (2000 rows of 4 types, 256 x 256 from 8 bits, 7.2 us, by four 8.6; 300 rows of 20
 // types, 400 x 512, 30.7 and 15.7).
 bool eight_waves(const Types& types) { return types.n > 64 * (int64_t)types.T; }
 
 template <typename T, bool TRANS>
-int product(const FewArgs& a, hipStream_t st)
+int product(const TypedRows& a, hipStream_t st)
 {
     const unsigned groups = (unsigned)row_blocks(a.types);
     if (shared_blocks(a)) k_typed_few<T, TRANS, 4><<<dim3(groups, (a.N + 31) / 32), 256, 0, st>>>(a);
@@ -349,7 +349,7 @@ int weights(const TypedDw& g, hipStream_t st)
 // 80.8 and 62.2).
 constexpr int64_t kBothWaves = 16384;
 template <typename XR, typename ZR, int WAVES, int PARTS>
-int both(const TypedDw& g, const FewArgs& a, hipStream_t st)
+int both(const TypedDw& g, const TypedRows& a, hipStream_t st)
 {
     const unsigned across = (g.K + 31) / 32, down = (g.F + 31) / 32, beside = (a.N + 32 * (WAVES / PARTS) - 1) / (32 * (WAVES / PARTS));
     const int64_t dw = (int64_t)across * down * g.types.T, dx = row_blocks(a.types) * beside;
@@ -364,7 +364,7 @@ int both(const TypedDw& g, const FewArgs& a, hipStream_t st)
     return SAR_OK;
 }
 template <typename XR, typename ZR>
-int both(const TypedDw& g, const FewArgs& a, hipStream_t st)
+int both(const TypedDw& g, const TypedRows& a, hipStream_t st)
 {
     if (eight_waves(g.types)) return shared_blocks(a) ? both<XR, ZR, 8, 4>(g, a, st) : both<XR, ZR, 8, 1>(g, a, st);
     return shared_blocks(a) ? both<XR, ZR, 4, 4>(g, a, st) : both<XR, ZR, 4, 1>(g, a, st);
@@ -388,7 +388,7 @@ bool few_rows_dw(int64_t n, int T, int K, int F)
     return n <= std::min(std::max(kFewRows, kFewOfType * T), kFewRowsOfAll) && n * ((K + 31) / 32) * ((F + 31) / 32) <= kFewColumns;
 }
 
-int few_product(int dtype, bool trans, const FewArgs& a, hipStream_t st)
+int few_product(int dtype, bool trans, const TypedRows& a, hipStream_t st)
 {
     if (dtype == SAR_F32) return trans ? product<float, true>(a, st) : product<float, false>(a, st);
     return trans ? product<bf16_t, true>(a, st) : product<bf16_t, false>(a, st);
@@ -401,7 +401,7 @@ int few_dw(int dtype, const TypedDw& g, hipStream_t st)
 }
 
 // (the same bits as by two launches)
-int few_dw_and_dx(int dtype, const TypedDw& g, const FewArgs& a, hipStream_t st)
+int few_dw_and_dx(int dtype, const TypedDw& g, const TypedRows& a, hipStream_t st)
 {
     if (dtype == SAR_F32) return g.Xq ? both<PackedRows, F32Rows>(g, a, st) : both<F32Rows, F32Rows>(g, a, st);
     return g.Xq ? both<PackedRows, Bf16Rows>(g, a, st) : both<Bf16Rows, Bf16Rows>(g, a, st);
