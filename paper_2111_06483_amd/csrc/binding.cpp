@@ -13,6 +13,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <initializer_list>
+#include <limits>
 #include <string>
 #include <vector>
 
@@ -623,6 +624,14 @@ T* at_if(PyObject* o, const char* what, at::ScalarType dtype, std::initializer_l
     return o == Py_None ? nullptr : at_of<T>(o, what, dtype, shape);
 }
 
+// (the library takes widths and numbers of types as int)
+int64_t within_int(int64_t v)
+{
+    if (v > std::numeric_limits<int>::max())
+        raise_sar(SAR_ERR_UNSUPPORTED, ("a size of " + std::to_string(v) + " is more than the call takes").c_str());
+    return v;
+}
+
 // The first of a call's tensors, which says how many rows and columns there are, and of which type.
 struct Rows {
     at::ScalarType dtype;
@@ -636,7 +645,7 @@ Rows rows_of(PyObject* o, const char* what)
     const int code = dtype_code(t.scalar_type());
     int64_t s[2];
     unpack_sizes(t, s);
-    return {t.scalar_type(), code, s[0], s[1], at_of(o, what, t.scalar_type(), {s[0], s[1]})};
+    return {t.scalar_type(), code, s[0], within_int(s[1]), at_of(o, what, t.scalar_type(), {s[0], s[1]})};
 }
 
 // Rows in 8 bits: a pair (q, e), or None.
@@ -740,7 +749,7 @@ TypedW typed_w(PyObject* W, PyObject* ptr, int64_t K, int64_t F)
     unpack_sizes(tensor(W), s);
     if (K < 0) K = s[1];
     if (F < 0) F = s[2];
-    return {s[0], K, F, at_of<float>(W, "W", at::kFloat, {s[0], K, F}), at_of<int32_t>(ptr, "type_ptr", at::kInt, {s[0] + 1})};
+    return {within_int(s[0]), within_int(K), within_int(F), at_of<float>(W, "W", at::kFloat, {s[0], K, F}), at_of<int32_t>(ptr, "type_ptr", at::kInt, {s[0] + 1})};
 }
 
 // X, W, type_ptr, Z, work
@@ -775,7 +784,7 @@ SAR_CALL(linear_bwd_packed, 7)
     const Rows dZ = rows_of(a[1], "dZ");
     int64_t kf[2];
     unpack_sizes(tensor(a[2]), kf);
-    const int64_t K = kf[0], F = dZ.width;
+    const int64_t K = within_int(kf[0]), F = dZ.width;
     float* const W = at_of<float>(a[2], "W", at::kFloat, {K, F});
     const Packed xp = packed(a[0], "X", dZ.n, K);
     const int acc = truth(a[3]);

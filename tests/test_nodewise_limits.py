@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 from paper_2111_06483_amd import sar
 
@@ -36,3 +37,22 @@ def test_more_weights_than_a_launch_lays_out():
         assert "too many for one launch" in lib.sar_last_error().decode()
         assert lib.sar_linear_typed_workspace_bytes(1, K, F, 1024, ctypes.byref(n)) == 0
         assert lib.sar_linear_typed_bwd(at, none, none, at, at, at, 16384, 0, at + 16, at + 32, 0, 1, K, F, at, 1 << 62, none) == sar.SAR_ERR_UNSUPPORTED
+
+
+def test_sizes_beyond_an_int():
+    """A width of 2^32 + 8 is not one of 8.  (Tensors without rows or values: they take no memory.)"""
+    wide = (1 << 32) + 8
+    rows = lambda n, K: torch.empty(n, K)
+    w, ptr = torch.empty(64, dtype=torch.uint8), torch.zeros(3, dtype=torch.int32)
+    for call in (lambda: sar.sar_pack(rows(0, wide), sar.packed_empty(0, wide, "cpu")),
+                 lambda: sar.sar_unpack(sar.packed_empty(0, wide, "cpu"), rows(0, wide)),
+                 lambda: sar.sar_layernorm_fwd(rows(0, wide), None, None, 1e-5, rows(0, wide)),
+                 lambda: sar.sar_layernorm_bwd(rows(0, wide), rows(0, wide), rows(0, 2), None, False, rows(0, wide), None, None, None),
+                 lambda: sar.sar_linear_typed_fwd(rows(0, wide), torch.empty(2, wide, 0), ptr, rows(0, 0), w),
+                 lambda: sar.sar_linear_typed_fwd(rows(0, 0), torch.empty(2, 0, wide), ptr, rows(0, wide), w),
+                 lambda: sar.sar_linear_typed_fwd(rows(0, 0), torch.empty(wide, 0, 4), ptr, rows(0, 4), w),
+                 lambda: sar.sar_linear_typed_bwd(None, rows(0, 0), torch.empty(2, wide, 0), ptr, False, None, rows(0, wide), w),
+                 lambda: sar.sar_linear_bwd_packed(None, rows(0, 0), torch.empty(wide, 0), False, None, rows(0, wide), w)):
+        with pytest.raises(sar.SarError) as e:
+            call()
+        assert e.value.code == sar.SAR_ERR_UNSUPPORTED and str(wide) in str(e.value)
