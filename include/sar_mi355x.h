@@ -497,8 +497,9 @@ int sar_layernorm_workspace_bytes(int64_t n, int D, size_t* bytes);
 /* -------------------------------------- transforms with a weight per node type
  * Rows sorted by type: those of type t are [type_ptr[t], type_ptr[t+1]), type_ptr device int32 [T+1], ascending, with
  * values of 0..n (what lies outside is cut off; rows that no type has are neither read nor written).  T <= 65535; a
- * type may have no row.  n < 2^31 - 256; K, F <= 65536.  fp32 results are sums of products that are exact for operands of any
- * size; bf16 rows meet weights taken to 16 bits (as in sar_linear_fwd; those below 2^-117 to within 2^-134), and are rounded when stored.
+ * type may have no row.  n < 2^31 - 256; K, F <= 65536.  fp32 results are sums of products that are formed
+ * to within 2^-23 of their size, whatever the size of their operands; bf16 rows meet weights taken to 16 bits (as in sar_linear_fwd; those
+ * below 2^-117 to within 2^-134), and are rounded when stored.
  * work: scratch of at least sar_linear_typed_workspace_bytes, 16-byte aligned; that of n rows serves fewer as well.
  */
 
@@ -516,8 +517,9 @@ int sar_linear_typed_bwd(const void* X, const int8_t* Xq, const uint8_t* Xe, con
 
 int sar_linear_typed_workspace_bytes(int64_t n, int K, int F, int T, size_t* bytes);
 
-/* sar_linear_bwd from rows kept in 8 bits: dW (fp32 [K,F]) as sar_linear_typed_bwd forms it of one type that has all
- * rows, dX as sar_linear_bwd does (must not alias dZ).  work: sar_linear_typed_workspace_bytes with T = 1. */
+/* sar_linear_bwd from rows kept in 8 bits: dW (fp32 [K,F], OVERWRITTEN unless accumulate != 0) as sar_linear_typed_bwd forms it of one type
+ * that has all rows; dX = dZ W^T (must not alias dZ), of few rows as sar_linear_typed_bwd forms it, of more as sar_linear_bwd does (as
+ * precise; the last bits may differ).  work: sar_linear_typed_workspace_bytes with T = 1. */
 int sar_linear_bwd_packed(const int8_t* Xq, const uint8_t* Xe, const void* dZ, const float* W, int accumulate, float* dW,
                           void* dX, int dtype, int64_t n, int K, int F, void* work, size_t work_bytes, void* stream);
 

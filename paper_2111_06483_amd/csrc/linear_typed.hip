@@ -3,16 +3,17 @@
 // Both are rows (contraction index contiguous) times a small operand B [C, N] per type.
 //   - Few rows (linear_typed_few.hip): latency.  One launch.
 //   - Otherwise a first launch (k_typed_lay) lays B out in pieces of bf16, in the order in which a wavefront's lanes want them: fp32 rows three pieces a
-//     weight (24 bits, linear_pieces.h), bf16 rows two (as in linear.hip: the weight to 16 bits, below 2^-117 to
-//     within 2^-134; the result is rounded to 8), T K F values; and lists the row blocks of every type, as many as its rows need, which the workgroups of the main launch (k_typed_rows) share: 128 rows and up to 256 columns at a time, four wavefronts, the
-//     pieces by asynchronous copies to LDS, two buffers, a barrier a stage.  (Tried, with no gain beyond a twentieth either way: 256 rows by eight
+//     weight (24 bits, linear_pieces.h; products to within 2^-23, linear_split.hip), bf16 rows two (as in linear.hip: the weight to 16 bits, below 2^-117 to
+//     within 2^-134; the result is rounded to 8), T K F values; and lists the row blocks of every type, as many as its rows need, which the
+//     workgroups of the main launch (k_typed_rows) share: 128 rows and up to 256 columns at a time, four wavefronts, the pieces by asynchronous
+//     copies to LDS, two buffers, a barrier a stage.  (Tried, with no gain beyond a twentieth either way: 256 rows by eight
 //     wavefronts, rows by asynchronous copies as well, both two stages ahead.)
 //   - Columns are dealt to the column tiles by turns (`column_of`), so that a lane ends up with four neighbours of a row and writes them at once:
 //     a wavefront's store covers whole lines, with no turn through LDS.
 // fp32 sums: the matrix unit cuts (does not round) when it adds, so a chunk's 16 products are summed from zero there and added to the
 // running sum by vector instructions, which round to nearest; and every other chunk is multiplied by -B and subtracted, so that what is
-// cut leans to neither side.  bf16 products of at most a few hundred terms, whose sums are rounded to 8 bits, are added there.  A result that is not finite
-// (infinities and NaN have no such pieces, and numbers are scaled up first, kUp) sends the wavefront's tile back to the fp32 matrix instruction, from
+// cut leans to neither side.  bf16 products are added there: a unit of 2^-23 of the sum for eight terms, 2^-10 of the longest
+// contraction's (65536), which is rounded to 8 bits.  A result that is not finite (infinities and NaN have no such pieces, and numbers are scaled up first, kUp) sends the wavefront's tile back to the fp32 matrix instruction, from
 // the operands themselves.
 // What bounds them (256 -> 256, four types): fp32, 237500 rows, 191 us = 163 TFLOP/s: the six products, 978 TFLOP/s of bf16 (a large library product in
 // bf16 reaches 1170, one in fp32 154); bf16, 867187 rows, 276 us: its two products 823 TFLOP/s, its 888 MB 3.2 TB/s, neither alone (195 and 185 us).
@@ -587,7 +588,7 @@ extern "C" int sar_linear_bwd_packed(const int8_t* Xq, const uint8_t* Xe, const 
                                      int dtype, int64_t n, int K, int F, void* work, size_t work_bytes, void* stream)
 {
     SAR_TRY(check_call(dtype, n, K, F, 1, nullptr, work, work_bytes));
-    // of more than a few rows the product that sar_linear_bwd has: the errors of the rows do not depend on the form of the input
+    // few rows: both products in one launch; of more, dX by the kernels of sar_linear_bwd
     const bool few = few_bwd({nullptr, 1, n}, K, F);
     SAR_TRY(typed_bwd(nullptr, Xq, Xe, dZ, W, nullptr, 1, accumulate, dW, dX, few, dtype, n, K, F, work, as_stream(stream)));
     return dX && !few ? sar_linear_bwd(nullptr, dZ, W, nullptr, dX, dtype, n, K, F, nullptr, 0, stream) : SAR_OK;

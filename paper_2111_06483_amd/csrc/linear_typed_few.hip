@@ -3,7 +3,7 @@
 // Here a call is latency, a launch costs as much as the work, and the weights' pieces and lists that calls of many rows lay out first do not pay: one launch
 // a call, the backward pass's two products in the same one, operands straight from memory, the contraction shared by a workgroup's wavefronts,
 // which add up in LDS.  The numbers are formed as there (linear_pieces.h: fp32 as three bf16 pieces, six products, from zero, added by vector
-// instructions; sums that are not finite once more by the fp32 matrix instruction).
+// instructions; sums that are not finite once more by the fp32 matrix instruction).  Which kernel takes a call shows in the last bits alone.
 // 2000 x 128 -> 128, bf16, 4 types: 4.3 us, 10 with pieces and lists laid out first; 300 x 256 -> 256, fp32, 5 types: forward 5.1, backward, both products, 7.3, by a launch
 // each 11.2.
 #include <algorithm>
