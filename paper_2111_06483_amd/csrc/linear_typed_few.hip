@@ -380,7 +380,9 @@ bool few_blocks(const Types& types, int N) { return row_blocks(types) * ((N + 31
 // Whether these take a backward pass's sums over rows.  Of one type a wavefront takes every eighth 16 rows (256 x 256, fp32: 500 rows 6.5 us and 10.6 in shares
 // of the rows (linear_typed_dw.hip), 1000 rows 10.6 and 11.6, 2000 rows 19.1 and 13.9); of several, whose shares are seldom even, the largest may have a good part:
 // 256 rows a type (shares as the cubes of random numbers, 256 x 256 from 8 bits: 8 types, 2000 rows 14.9 and 18.4, 4000 rows 26.5 and 21.8; 46 types, 8000 rows 38.0
-// and 50.4; 64 x 100: 9.5 and 22.2, 16000 rows 16.7 and 22.5).  And every 32 x 32 weights read their columns anew (1000 rows, 1024 x 1024 from 8 bits 40.5 and 43.0, 2048 x 1024
+// and 50.4; 64 x 100: 9.5 and 22.2, 16000 rows 16.7 and 22.5).  How long the longest type is the host does not know, and its rows are walked by the wavefronts of
+// one workgroup: with 95% of 16384 rows in one of 64 types 147 us and 100 (even types 50 and 61, cubes 62 and 77), 64 x 100 133 and 29 (11 and 16, 17 and 25); of
+// 128 types and more 256 x 256 is faster here even so (162 and 185).  And every 32 x 32 weights read their columns anew (1000 rows, 1024 x 1024 from 8 bits 40.5 and 43.0, 2048 x 1024
 // 78.5 and 59.1).
 constexpr int64_t kFewRows = 1024, kFewOfType = 256, kFewRowsOfAll = 16384, kFewColumns = 1 << 20;
 bool few_rows_dw(int64_t n, int T, int K, int F)
