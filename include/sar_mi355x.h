@@ -478,7 +478,8 @@ int sar_unpack(const int8_t* q, const uint8_t* e, int dtype, int64_t n, int K, v
 
 /* Y[i] = (X[i] - mu_i) r_i gamma + beta with mu_i = mean(X[i]), r_i = 1 / sqrt(mean((X[i] - mu_i)^2) + eps).
  * X, Y [n,D] of `dtype` (Y may alias X), D <= 8192; gamma, beta fp32 [D], either NULL for 1 / 0; stats fp32 [n,2]
- * = (mu_i, r_i), what the backward pass reads, or NULL.
+ * = (mu_i, r_i), what the backward pass reads, or NULL.  Held in 32 bits: a row whose sum, or whose deviations' squares' sum, passes fp32's largest
+ * number is not normalised (deviations of 2^64 / sqrt(D) and more).
  * Xq,Xe and Yq,Ye: NULL, or where the input and the output (as stored) go in 8 bits as well, in the same pass: what
  * the backward passes of the norm and of the transform behind it need. */
 int sar_layernorm_fwd(const void* X, const float* gamma, const float* beta, float eps, void* Y, float* stats, int dtype,

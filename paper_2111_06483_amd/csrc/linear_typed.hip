@@ -15,7 +15,7 @@
 // cut leans to neither side.  bf16 products are added there: a unit of 2^-23 of the sum for eight terms, 2^-10 of the longest
 // contraction's (65536), which is rounded to 8 bits.  A result that is not finite (infinities and NaN have no such pieces, and numbers are scaled up first, kUp) sends the wavefront's tile back to the fp32 matrix instruction, from
 // the operands themselves.
-// What bounds them (256 -> 256, four types): fp32, 237500 rows, 191 us = 163 TFLOP/s: the six products, 978 TFLOP/s of bf16 (a large library product in
+// What bounds them (256 -> 256, four types): fp32, 237500 rows, 187 us = 166 TFLOP/s: the six products, 998 TFLOP/s of bf16 (a large library product in
 // bf16 reaches 1170, one in fp32 154); bf16, 867187 rows, 276 us: its two products 823 TFLOP/s, its 888 MB 3.2 TB/s, neither alone (195 and 185 us).
 #include <algorithm>
 

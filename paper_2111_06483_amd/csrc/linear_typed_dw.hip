@@ -14,8 +14,8 @@
 // anew, so no workgroup has more rows than another.  Workgroup w writes its sums of type t to place w + t (every step along the rows goes to the
 // next workgroup or the next type, so no two have the same place), and a second launch adds a type's places up in order: the result is the
 // same in every run.  fp32 sums that are not finite (kUp: nor that large) are taken again there, from the operands.
-// What bounds it: 237500 x 256 x 256, fp32, 218 us = 143 TFLOP/s (the six products' 857 TFLOP/s of bf16, of 1170 that a large library product reaches); bf16 from
-// 8 bits, 867187 rows, 218 us: its 680 MB once would be 141, its products 97; every chunk's way from memory through registers to LDS is instructions between the
+// What bounds it: 237500 x 256 x 256, fp32, 210 us = 148 TFLOP/s (the six products' 890 TFLOP/s of bf16, of 1170 that a large library product reaches); bf16 from
+// 8 bits, 867187 rows, 212 us: its 680 MB once would be 141, its products 97; every chunk's way from memory through registers to LDS is instructions between the
 // products (the matrix cores are busy a quarter of the cycles).
 #include <algorithm>
 

@@ -9,8 +9,9 @@
 // The backward pass keeps a lane's share of dg and db in registers over all rows that the lane meets; a workgroup's wavefronts add theirs up in
 // LDS, every workgroup writes one row of partial sums, and a second launch adds those in a fixed order (few rows: columns_of_few): the result is the same
 // in every run.
-// 306250 x 256, fp32: forward 105 us, 5.9 TB/s (a large copy: 4.8, one of this size 5.3); backward 187 + 4 us, 5.0 TB/s; 1000003 x 47, bf16, from 8 bits 70 + 4 us,
-// 3.5 TB/s of the bytes it needs, whose rows of 94 and 48 + 2 bytes are no whole lines.
+// 306250 x 256, fp32: forward 104 us, 6.0 TB/s (a large copy: 4.8, one of this size 5.3), with both forms in 8 bits 137; backward 177 + 5 us, 5.2 TB/s; 867187 x 256,
+// bf16: 148 us, with both 230; backward from 8 bits 223; 1000003 x 47, bf16, from 8 bits 64 + 5 us, 3.5 TB/s of the bytes it needs, whose rows of 94 and 48 + 2
+// bytes are no whole lines.
 #include <algorithm>
 #include <cmath>
 

@@ -11,8 +11,8 @@
 //     bits would cost a second one.  The price: steps are up to twice as long as they need to be (1.4 times on average).
 //   - 32 values: one more byte per block; a single large value spoils no more than its block.
 // Both kernels are bound by memory: a lane moves 16 bytes of the row and 4 or 8 of the packed one, rows one after the other in one
-// index space, so that short and odd rows leave no lanes idle but those behind a row's last piece.  1734375 x 256, bf16: 257 us to pack, 213 to unpack, 5.2 and
-// 6.3 TB/s (a large copy: 4.8); 306250 x 100, fp32: 39 and 25 us.
+// index space, so that short and odd rows leave no lanes idle but those behind a row's last piece.  1734375 x 256, bf16: 243 us to pack, 208 to unpack, 5.5 and
+// 6.5 TB/s (a large copy: 4.8); 306250 x 100, fp32: 39 and 25 us.
 #include "packed.h"
 #include "sar_internal.h"
 
