@@ -55,7 +55,8 @@ int few_dw_and_dx(int dtype, const TypedDw& g, const TypedRows& a, hipStream_t s
 // fp32 value is a multiple of 2^-149, so its pieces are then multiples of 2^-125, each a normal bf16 value, and a value keeps its bits however small it
 // is (unscaled, the last bits of a value below 2^-110 have no bf16 value).  What this takes away is the other end: of values from 2^104 and sums from 2^80
 // on, which are formed again from the operands as all that are not finite are.  (A multiplication a value:
-// 237500 x 256 -> 256 of four types 191.3 us for 190.0, backward 405.7 for 403.5.)
+// of four types, 237500 x 256 -> 256, 194.0 us for 192.6, backward 410 for 407; 8000 rows, one launch, 19.5 for 18.8; 60000 x 400 -> 400, backward from 8 bits,
+// 312 for 302.)
 constexpr float kUp = 0x1p24f, kDown = 0x1p-24f;
 
 // What rows an operand has: pieces of a value, values a thread takes of a row, and their bytes.
