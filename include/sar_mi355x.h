@@ -81,7 +81,10 @@ typedef enum { SAR_F32 = 0, SAR_BF16 = 1 } sar_dtype;
 
 /* The non-linearity sigma of Eq. 2 / Eq. 3.  The paper leaves sigma open; ReLU is
  * the one offered, its derivative being a function of the output alone. */
-typedef enum { SAR_ACT_NONE = 0, SAR_ACT_RELU = 1 } sar_act;
+typedef enum { SAR_ACT_NONE = 0, SAR_ACT_RELU = 1,
+               /* of sar_linear_act_fwd / _bwd alone, whose backward pass reads what the activation was taken of: a Phi(a) with the normal
+                * distribution's Phi, a / (1 + exp(-a)), and a for a > 0, else exp(a) - 1 */
+               SAR_ACT_GELU = 2, SAR_ACT_SILU = 3, SAR_ACT_ELU = 4 } sar_act;
 
 /* Most blocks one batched (..._all) call can take, hence most partitions of a handle built with
  * SAR_BUILD_FUSED; and most partitions of any handle.  A handle of more than SAR_MAX_BLOCKS
@@ -523,6 +526,63 @@ int sar_linear_typed_workspace_bytes(int64_t n, int K, int F, int T, size_t* byt
  * precise; the last bits may differ).  work: sar_linear_typed_workspace_bytes with T = 1. */
 int sar_linear_bwd_packed(const int8_t* Xq, const uint8_t* Xe, const void* dZ, const float* W, int accumulate, float* dW,
                           void* dX, int dtype, int64_t n, int K, int F, void* work, size_t work_bytes, void* stream);
+
+/* ------------------------- the transform with bias, activation and residual */
+
+/* a = X W + bias, Y = act(a), with a residual row R inside (res_after == 0: a = X W + bias + R) or behind the activation
+ * (res_after != 0: Y = act(a) + R).  X [n,K], Y, res [n,F] of `dtype`, W fp32 [K,F], bias fp32 [F]; bias and res may be NULL.  A
+ * ([n,F] of `dtype`, or NULL) receives a, which the backward pass reads; of ReLU with no residual behind it Y serves there as
+ * well.  Sums and activation in 32 bits, rounded once when stored; the products as precise as those of sar_linear_typed_fwd.  Y may be res (A too, of a
+ * residual inside), and must not overlap X, W or A.  n < 2^31 - 256; K, F <= 65536.  act: any sar_act.
+ * work: scratch of at least sar_linear_act_workspace_bytes, 16-byte aligned; that of n rows serves fewer as well. */
+int sar_linear_act_fwd(const void* X, const float* W, const float* bias, const void* res, int act, int res_after, void* Y, void* A, int dtype, int64_t n,
+                       int K, int F, void* work, size_t work_bytes, void* stream);
+
+/* With dA = dY act'(A):  dW = X^T dA (fp32 [K,F]), db = sum_i dA_i (fp32 [F]), both added to what is there where accumulate != 0, else
+ * overwritten, and summed in a fixed order; dX = dA W^T ([n,K] of `dtype`, OVERWRITTEN); dA ([n,F] of `dtype`, OVERWRITTEN: the gradient of a residual inside
+ * the activation; that of one behind it is dY).  Each of the four may be NULL.  A as sar_linear_act_fwd wrote it (not read with SAR_ACT_NONE); X only for
+ * dW, W only for dX.  The derivative is taken of A as it is stored, in 32 bits.  Of bf16 rows dW sums products of dA to 16 bits (2^-17 of it), db dA in 32, and dX
+ * products of dA rounded to bf16 as dX itself is.  dX and dA must not overlap what is read or each other. */
+int sar_linear_act_bwd(const void* dY, const void* A, const void* X, const float* W, int act, int accumulate, float* dW, float* db, void* dX, void* dA,
+                       int dtype, int64_t n, int K, int F, void* work, size_t work_bytes, void* stream);
+
+int sar_linear_act_workspace_bytes(int64_t n, int K, int F, size_t* bytes);
+
+/* ------------------------------------ rows of class scores: losses, predictions
+ * X [n,C] of `dtype`: a row's scores, by which p = softmax(x) (at a temperature T: softmax(x / T)).  C <= 2^30.  A class with a score of -inf is out: it has
+ * no probability, and no gradient but what it has as a label.  A row of -inf alone has lse = -inf, entropy 0, log probability -inf, no top class, a distillation loss of
+ * +inf and no gradient.  A NaN or +inf makes a row's results and gradient NaN (but for classes out of -inf, 0 or NaN; its top classes
+ * are then any of the row's).  Sums in 32 bits.
+ * work: scratch of at least the call's ..._workspace_bytes, 16-byte aligned (NULL where that is 0); that of n rows serves fewer as well. */
+
+/* lse[i] = log sum_c exp(x_c), logp[i] = x_label - lse (0 for a label that is no class: one outside 0..C-1, such as -1), entropy[i] = -sum_c p_c log p_c
+ * (fp32 [n], each may be NULL; label int32 [n], read for logp), and the k classes of the highest scores, in descending order, of equal scores the lower class
+ * first: top_index int32 [n,k] and their log probabilities top_value fp32 [n,k]; -1 and -inf where a row has fewer than k.  0 <= k <= 64; NULL for k = 0. */
+int sar_logprob_fwd(const void* X, const int32_t* label, float* logp, float* lse, float* entropy, int k, float* top_value, int32_t* top_index, int dtype,
+                    int64_t n, int C, void* work, size_t work_bytes, void* stream);
+
+/* dX[i,c] = dlogp[i] ([c = label] - p_c) - dentropy[i] p_c (log p_c + entropy[i])  (OVERWRITTEN, `dtype`, may be X), with p_c = exp(x_c - lse[i]); rows
+ * whose label is no class have no part of dlogp.  lse, entropy from sar_logprob_fwd; dlogp, dentropy fp32 [n], either may be NULL (0); label only for
+ * dlogp, entropy only for dentropy. */
+int sar_logprob_bwd(const void* X, const int32_t* label, const float* lse, const float* entropy, const float* dlogp, const float* dentropy, void* dX, int dtype,
+                    int64_t n, int C, void* stream);
+
+int sar_logprob_workspace_bytes(int64_t n, int C, int k, size_t* bytes);
+
+/* Distillation: the teacher has k classes of every row, top_index int32 [n,k], with scores top_value fp32 [n,k] (logits or log probabilities: a number
+ * added to a row's changes nothing), as sar_logprob_fwd lists them.  q = softmax of a row's top_value / T, s = softmax(x / T):
+ *   loss[i] = sum_j q_j (log q_j - log s_{top_index_j}),  lse[i] = log sum_c exp(x_c / T)   (fp32 [n], either may be NULL)
+ * An index outside 0..C-1 is no entry, nor is a value of -inf; a class listed twice counts twice; a row without entries has loss 0.  0 <= k <= 64;
+ * T > 0. */
+int sar_distill_fwd(const void* X, int k, const float* top_value, const int32_t* top_index, float temperature, float* loss, float* lse, int dtype, int64_t n,
+                    int C, void* work, size_t work_bytes, void* stream);
+
+/* dX[i,c] = dloss[i] / T (s_c - sum of the q_j whose class is c)  (OVERWRITTEN, `dtype`, may be X; 0 in a row without entries); lse from sar_distill_fwd at the
+ * same T, dloss fp32 [n]. */
+int sar_distill_bwd(const void* X, int k, const float* top_value, const int32_t* top_index, float temperature, const float* lse, const float* dloss, void* dX,
+                    int dtype, int64_t n, int C, void* stream);
+
+int sar_distill_workspace_bytes(int64_t n, int C, int k, size_t* bytes);
 
 #ifdef __cplusplus
 }

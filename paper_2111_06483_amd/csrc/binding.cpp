@@ -795,6 +795,122 @@ SAR_CALL(linear_bwd_packed, 7)
     call([&] { return sar_linear_bwd_packed(xp.q, xp.e, dZ.p, W, acc, dW, dX, dZ.code, dZ.n, (int)K, (int)F, work, wb, st); });
 SAR_CALL_END
 
+// W [K, F]; what is not known of it otherwise (-1) it says itself.
+struct PlainW {
+    int64_t K, F;
+    float* W;
+};
+PlainW plain_w(PyObject* W, int64_t K, int64_t F)
+{
+    int64_t s[2];
+    unpack_sizes(tensor(W), s);
+    if (K < 0) K = s[0];
+    if (F < 0) F = s[1];
+    return {within_int(K), within_int(F), at_of<float>(W, "W", at::kFloat, {K, F})};
+}
+
+// (an enumeration's number)
+int whole(PyObject* o)
+{
+    const int64_t v = integer(o);
+    if (v < std::numeric_limits<int>::min() || v > std::numeric_limits<int>::max())
+        raise_sar(SAR_ERR_UNSUPPORTED, ("a number of " + std::to_string(v) + " is more than the call takes").c_str());
+    return (int)v;
+}
+
+// X, W, bias, res, act, res_after, Y, A, work
+SAR_CALL(linear_act_fwd, 9)
+    const Rows X = rows_of(a[0], "X");
+    const PlainW w = plain_w(a[1], X.width, -1);
+    float* const bias = at_if<float>(a[2], "bias", at::kFloat, {w.F});
+    void* const res = at_if(a[3], "res", X.dtype, {X.n, w.F});
+    const int act = whole(a[4]), after = truth(a[5]);
+    void *const Y = at_of(a[6], "Y", X.dtype, {X.n, w.F}), *const A = at_if(a[7], "A", X.dtype, {X.n, w.F});
+    void *const work = scratch(a[8]), *const st = stream();
+    const size_t wb = bytes_if(a[8]);
+    all_here(a, 9);
+    call([&] { return sar_linear_act_fwd(X.p, w.W, bias, res, act, after, Y, A, X.code, X.n, (int)w.K, (int)w.F, work, wb, st); });
+SAR_CALL_END
+
+// dY, A, X or None, W, act, accumulate, dW, db, dX, dA, work
+SAR_CALL(linear_act_bwd, 11)
+    const Rows dY = rows_of(a[0], "dY");
+    const PlainW w = plain_w(a[3], -1, dY.width);
+    void *const A = at_if(a[1], "A", dY.dtype, {dY.n, w.F}), *const X = at_if(a[2], "X", dY.dtype, {dY.n, w.K});
+    const int act = whole(a[4]), acc = truth(a[5]);
+    float *const dW = at_if<float>(a[6], "dW", at::kFloat, {w.K, w.F}), *const db = at_if<float>(a[7], "db", at::kFloat, {w.F});
+    void *const dX = at_if(a[8], "dX", dY.dtype, {dY.n, w.K}), *const dA = at_if(a[9], "dA", dY.dtype, {dY.n, w.F});
+    void *const work = scratch(a[10]), *const st = stream();
+    const size_t wb = bytes_if(a[10]);
+    all_here(a, 11);
+    call([&] { return sar_linear_act_bwd(dY.p, A, X, w.W, act, acc, dW, db, dX, dA, dY.code, dY.n, (int)w.K, (int)w.F, work, wb, st); });
+SAR_CALL_END
+
+// Top classes: a pair (values [n, k], classes [n, k]), or None.
+struct Top {
+    int k = 0;
+    float* value = nullptr;
+    int32_t* index = nullptr;
+};
+Top top_of(PyObject* o, int64_t n)
+{
+    if (o == Py_None) return {};
+    if (!is_pair(o) || PySequence_Fast_GET_SIZE(o) != 2) refuse("top classes are a pair (values, classes)");
+    PyObject* const* const items = PySequence_Fast_ITEMS(o);
+    int64_t s[2];
+    unpack_sizes(tensor(items[0]), s);
+    return {(int)within_int(s[1]), at_of<float>(items[0], "top values", at::kFloat, {n, s[1]}), at_of<int32_t>(items[1], "top classes", at::kInt, {n, s[1]})};
+}
+
+// X, label, logp, lse, entropy, (values, classes), work
+SAR_CALL(logprob_fwd, 7)
+    const Rows X = rows_of(a[0], "X");
+    int32_t* const label = at_if<int32_t>(a[1], "label", at::kInt, {X.n});
+    float *const logp = at_if<float>(a[2], "logp", at::kFloat, {X.n}), *const lse = at_if<float>(a[3], "lse", at::kFloat, {X.n});
+    float* const entropy = at_if<float>(a[4], "entropy", at::kFloat, {X.n});
+    const Top top = top_of(a[5], X.n);
+    void *const work = scratch(a[6]), *const st = stream();
+    const size_t wb = bytes_if(a[6]);
+    all_here(a, 7);
+    call([&] { return sar_logprob_fwd(X.p, label, logp, lse, entropy, top.k, top.value, top.index, X.code, X.n, (int)X.width, work, wb, st); });
+SAR_CALL_END
+
+// X, label, lse, entropy, dlogp, dentropy, dX
+SAR_CALL(logprob_bwd, 7)
+    const Rows X = rows_of(a[0], "X");
+    int32_t* const label = at_if<int32_t>(a[1], "label", at::kInt, {X.n});
+    float *const lse = at_of<float>(a[2], "lse", at::kFloat, {X.n}), *const entropy = at_if<float>(a[3], "entropy", at::kFloat, {X.n});
+    float *const dlogp = at_if<float>(a[4], "dlogp", at::kFloat, {X.n}), *const dentropy = at_if<float>(a[5], "dentropy", at::kFloat, {X.n});
+    void *const dX = at_of(a[6], "dX", X.dtype, {X.n, X.width}), *const st = stream();
+    all_here(a, 7);
+    call([&] { return sar_logprob_bwd(X.p, label, lse, entropy, dlogp, dentropy, dX, X.code, X.n, (int)X.width, st); });
+SAR_CALL_END
+
+// X, (values, classes), temperature, loss, lse, work
+SAR_CALL(distill_fwd, 6)
+    const Rows X = rows_of(a[0], "X");
+    if (a[1] == Py_None) refuse("top classes are a pair (values, classes)");
+    const Top top = top_of(a[1], X.n);
+    const float temperature = real(a[2]);
+    float *const loss = at_if<float>(a[3], "loss", at::kFloat, {X.n}), *const lse = at_if<float>(a[4], "lse", at::kFloat, {X.n});
+    void *const work = scratch(a[5]), *const st = stream();
+    const size_t wb = bytes_if(a[5]);
+    all_here(a, 6);
+    call([&] { return sar_distill_fwd(X.p, top.k, top.value, top.index, temperature, loss, lse, X.code, X.n, (int)X.width, work, wb, st); });
+SAR_CALL_END
+
+// X, (values, classes), temperature, lse, dloss, dX
+SAR_CALL(distill_bwd, 6)
+    const Rows X = rows_of(a[0], "X");
+    if (a[1] == Py_None) refuse("top classes are a pair (values, classes)");
+    const Top top = top_of(a[1], X.n);
+    const float temperature = real(a[2]);
+    float *const lse = at_of<float>(a[3], "lse", at::kFloat, {X.n}), *const dloss = at_of<float>(a[4], "dloss", at::kFloat, {X.n});
+    void *const dX = at_of(a[5], "dX", X.dtype, {X.n, X.width}), *const st = stream();
+    all_here(a, 6);
+    call([&] { return sar_distill_bwd(X.p, top.k, top.value, top.index, temperature, lse, dloss, dX, X.code, X.n, (int)X.width, st); });
+SAR_CALL_END
+
 #define SAR_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     SAR_METHOD(spmm_all), SAR_METHOD(act_bwd), SAR_METHOD(spmm_bwd_all), SAR_METHOD(error_add), SAR_METHOD(gat_scores),
@@ -802,7 +918,8 @@ PyMethodDef methods[] = {
     SAR_METHOD(gat_bwd_begin), SAR_METHOD(gat_bwd_block), SAR_METHOD(gat_bwd_all), SAR_METHOD(gat_bwd_end),
     SAR_METHOD(linear_fwd), SAR_METHOD(linear_bwd), SAR_METHOD(linear_bwd_rows), SAR_METHOD(pack), SAR_METHOD(unpack),
     SAR_METHOD(layernorm_fwd), SAR_METHOD(layernorm_bwd), SAR_METHOD(linear_typed_fwd), SAR_METHOD(linear_typed_bwd),
-    SAR_METHOD(linear_bwd_packed), {nullptr, nullptr, 0, nullptr}};
+    SAR_METHOD(linear_bwd_packed), SAR_METHOD(linear_act_fwd), SAR_METHOD(linear_act_bwd), SAR_METHOD(logprob_fwd), SAR_METHOD(logprob_bwd),
+    SAR_METHOD(distill_fwd), SAR_METHOD(distill_bwd), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,447 @@
+// Rows of class scores (logprob.hip, distill.hip): the largest of a row, the sum of exponentials below it and the row's top classes, in one
+// pass over the scores, and the gradient's tiles.
+#pragma once
+
+#include <algorithm>
+#include <cmath>
+
+#include "packed.h"
+#include "sar_internal.h"
+
+namespace sar {
+
+constexpr int kClassThreads = 256, kClassWaves = kClassThreads / kWave;
+constexpr int kMostTop = 64;                           // a lane of a wavefront for each
+constexpr float kLeast = -1e4f;                        // a difference whose exponential is zero: times that it is zero, where -inf would be NaN
+
+// ---- over the L neighbouring lanes that share a row
+
+template <int CTRL>
+__device__ inline uint32_t dpp_of(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false); }
+
+template <int L, typename V, typename Op>
+__device__ inline V over_lanes(V v, Op op)
+{
+    static_assert(sizeof(V) == 4, "a register");
+    auto other = [&](auto ctrl) { return __builtin_bit_cast(V, dpp_of<decltype(ctrl)::value>(__builtin_bit_cast(uint32_t, v))); };
+    if constexpr (L >= 2) v = op(v, other(std::integral_constant<int, 0xB1>{}));       // lane ^ 1
+    if constexpr (L >= 4) v = op(v, other(std::integral_constant<int, 0x4E>{}));       // lane ^ 2
+    if constexpr (L >= 8) v = op(v, other(std::integral_constant<int, 0x141>{}));      // the other four of eight
+    if constexpr (L >= 16) v = op(v, other(std::integral_constant<int, 0x140>{}));     // the other eight of sixteen
+    if constexpr (L >= 32) v = op(v, (V)__shfl_xor(v, 16));
+    if constexpr (L >= 64) v = op(v, (V)__shfl_xor(v, 32));
+    return v;
+}
+template <int L>
+__device__ inline float lanes_largest(float v) { return over_lanes<L>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int L>
+__device__ inline float lanes_sum(float v) { return over_lanes<L>(v, [](float a, float b) { return a + b; }); }
+
+// ---- a row's sums
+
+// largest; sum of exp((x - largest) / T); sum of the same times (x - largest) / T
+struct RowSums {
+    float m, s, u;
+};
+__device__ inline float base_of(float m) { return m == -__builtin_inff() ? 0.f : m; }      // what is subtracted of a row without a score
+// log2(e) / T: exponentials are taken by the base 2
+__device__ inline float exp_below(float d, float by) { return __builtin_amdgcn_exp2f(d * by); }
+
+// Sums of parts of a row, with their largest score's place moved from r.m to `to`.
+__device__ inline void move_sums(RowSums& r, float to, float by, float over)
+{
+    const float d = fmaxf(r.m - base_of(to), kLeast), f = exp_below(r.m - base_of(to), by);
+    r.u = f * (r.u + r.s * (d * over));
+    r.s *= f;
+    r.m = to;
+}
+
+// ---- scores in order
+// A score's place among scores: numbers that ascend as the scores do (-0 and 0 alike, NaN last), never zero.
+__device__ inline uint32_t order_of(float x)
+{
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ inline float score_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order); }
+constexpr uint32_t kOrderOfNone = 0x007fffffu;         // that of -inf: such a class, and those behind the last one (0), are none of the top ones
+
+// The top classes of a wavefront's scores, the l-th in lane l; of equal scores the lower class first.
+struct TopList {
+    uint32_t order;
+    int cls;
+};
+__device__ inline TopList no_class() { return {0u, 0x7fffffff}; }
+__device__ inline bool ahead(const TopList& a, const TopList& b) { return a.order > b.order || (a.order == b.order && a.cls < b.cls); }
+__device__ inline TopList from_lane(const TopList& v, int l) { return {(uint32_t)__shfl((int)v.order, l), __shfl(v.cls, l)}; }
+
+// One candidate, the same for all lanes.
+__device__ inline void insert_top(TopList& list, const TopList& c)
+{
+    const int lane = threadIdx.x & 63, place = __builtin_popcountll(__ballot(ahead(list, c)));
+    const TopList before = {(uint32_t)__shfl_up((int)list.order, 1), __shfl_up(list.cls, 1)};
+    if (lane > place) list = before;
+    if (lane == place) list = c;
+}
+// A descending list of candidates.
+__device__ inline void merge_top(TopList& list, const TopList& sorted)
+{
+    const int lane = threadIdx.x & 63;
+    const TopList c = from_lane(sorted, 63 - lane);
+    if (ahead(c, list)) list = c;          // (the upper half of both, falling and then rising)
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+        const TopList p = {(uint32_t)__shfl_xor((int)list.order, o), __shfl_xor(list.cls, o)};
+        if (ahead(p, list) == ((lane & o) == 0)) list = p;
+    }
+}
+// One candidate of every lane.
+__device__ inline void sort_top(TopList& v)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int size = 2; size <= 64; size <<= 1)
+#pragma unroll
+        for (int o = size >> 1; o >= 1; o >>= 1) {
+            const TopList p = {(uint32_t)__shfl_xor((int)v.order, o), __shfl_xor(v.cls, o)};
+            const bool falls = (lane & size) == 0 || size == 64;
+            if (ahead(p, v) == (((lane & o) == 0) == falls)) v = p;
+        }
+}
+// Those of the candidates that belong among the first k.
+__device__ inline void offer_top(TopList& list, const TopList& c, int k)
+{
+    const TopList last = {(uint32_t)__builtin_amdgcn_readlane((int)list.order, k - 1), __builtin_amdgcn_readlane(list.cls, k - 1)};
+    uint64_t in = __ballot(c.order != 0u && ahead(c, last));
+    if (in == 0) return;
+    if (__builtin_popcountll(in) > 12) {               // (an insertion is a twelfth of a sort and a merge)
+        TopList all = c;
+        sort_top(all);
+        merge_top(list, all);
+        return;
+    }
+    while (in) {
+        const int l = __builtin_ctzll(in);
+        in &= in - 1;
+        insert_top(list, {(uint32_t)__builtin_amdgcn_readlane((int)c.order, l), __builtin_amdgcn_readlane(c.cls, l)});
+    }
+}
+
+// ---- how rows are laid over threads
+
+// Rows of up to 32 values a lane of a wavefront stay in registers.
+template <typename T>
+constexpr int kMostPieces = 32 / Cols<T>::N;
+constexpr int kMostInLanes = 64 * 32;
+
+struct ClassShape {
+    int tpr, r;            // lanes a row, pieces a lane
+};
+inline ClassShape class_shape(int dtype, int64_t n, int C)
+{
+    const int vec = dtype == SAR_F32 ? 4 : 8, pieces = (C + vec - 1) / vec, most = 32 / vec;
+    int tpr = 4;
+    while (tpr < 64 && pieces > tpr * most) tpr <<= 1;
+    // few rows are spread over more lanes
+    while (tpr < 64 && pieces > tpr && n * tpr < 64 * 2048) tpr <<= 1;
+    const int r = (pieces + tpr - 1) / tpr, step = dtype == SAR_F32 ? 2 : 1;
+    return {tpr, (r + step - 1) / step * step};
+}
+
+// Longer rows are cut into parts of whole pieces, a workgroup each; several parts a row where there are few rows, and a second launch that joins them.
+constexpr int64_t kWideGroups = 1024;
+inline int64_t least_part(int dtype) { return (int64_t)kClassThreads * 4 * (dtype == SAR_F32 ? 4 : 8); }
+inline int parts_of(int dtype, int64_t n, int C)
+{
+    if (C <= kMostInLanes) return 1;
+    const int64_t want = (kWideGroups + n - 1) / std::max<int64_t>(n, 1), most = (C + least_part(dtype) - 1) / least_part(dtype);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, 64}));
+}
+// Values of a part, a multiple of eight.
+inline int64_t part_width(int C, int parts) { return ((C + parts - 1) / parts + 7) / 8 * 8; }
+// Parts that any call of up to n rows has, where it has several a row.
+inline int64_t most_parts(int64_t n, int C)
+{
+    if (C <= kMostInLanes) return 0;
+    const int64_t most = std::min<int64_t>((C + least_part(SAR_F32) - 1) / least_part(SAR_F32), 64), rows = std::min(n, kWideGroups);
+    return most > 1 ? std::min(rows * most, rows + kWideGroups) : 0;
+}
+
+struct ClassRows {
+    const void* X;         // [n, C]
+    int64_t n;
+    int C, k;
+    float by, over;        // log2(e) / T, 1 / T
+    int parts;
+    int64_t width;
+    RowSums* sums;         // [n, parts]
+    TopList* lists;        // [n, parts, k]
+};
+
+// A row's pieces of `T` in the lanes t of TPR, -inf behind the row's end.
+template <typename T, int TPR, int R>
+__device__ inline void row_in_lanes(const ClassRows& a, int64_t row, int t, float (&v)[R][Cols<T>::N])
+{
+    constexpr int N = Cols<T>::N;
+    uint4 raw[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) raw[r] = Cols<T>::load(static_cast<const T*>(a.X) + row * a.C, (t + r * TPR) * N, a.C, (a.n - row) * a.C);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int c = (t + r * TPR) * N;
+        Cols<T>::unpack(raw[r], v[r]);
+        if (c + N > a.C) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (c + j >= a.C) v[r][j] = -__builtin_inff();
+        }
+    }
+}
+
+template <typename T, int TPR, int R, typename Job>
+__global__ __launch_bounds__(kClassThreads) void k_class_rows(ClassRows a, typename Job::Args job)
+{
+    constexpr int N = Cols<T>::N, kRows = kClassThreads / TPR;
+    const int t = threadIdx.x % TPR;
+    for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.n; base += (int64_t)gridDim.x * kRows) {
+        const int64_t row = base + threadIdx.x / TPR;
+        const bool there = row < a.n;
+        float v[R][N];
+        row_in_lanes<T, TPR, R>(a, min(row, a.n - 1), t, v);
+        RowSums sums{-__builtin_inff(), 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < N; ++j) sums.m = fmaxf(sums.m, v[r][j]);
+        sums.m = lanes_largest<TPR>(sums.m);
+        const float m = base_of(sums.m);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float d = v[r][j] - m, e = exp_below(d, a.by);
+                sums.s += e;
+                if constexpr (Job::kEntropy) sums.u = fmaf(e, fmaxf(d, kLeast), sums.u);
+            }
+        sums.s = lanes_sum<TPR>(sums.s);
+        if constexpr (Job::kEntropy) sums.u = lanes_sum<TPR>(sums.u) * a.over;
+        Job::template in_lanes<T, TPR, R>(a, job, min(row, a.n - 1), there, t, sums, v);
+    }
+}
+
+// A part of a row.
+template <typename T, typename Job>
+__global__ __launch_bounds__(kClassThreads) void k_class_wide(ClassRows a, typename Job::Args job)
+{
+    constexpr int N = Cols<T>::N, U = 4;
+    __shared__ RowSums wave_sums[kClassWaves];
+    __shared__ TopList wave_top[Job::kTop ? kClassWaves : 1][kMostTop];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int64_t index = blockIdx.x; index < a.n * a.parts; index += gridDim.x) {
+        const int64_t row = index / a.parts;
+        const int part = (int)(index - row * a.parts);
+        const T* x = static_cast<const T*>(a.X) + row * a.C;
+        const int64_t left = (a.n - row) * a.C;
+        const int64_t c0 = part * a.width, c1 = min(c0 + a.width, (int64_t)a.C);
+        RowSums sums{-__builtin_inff(), 0.f, 0.f};
+        TopList top = no_class();
+        for (int64_t at = c0; at < c1; at += kClassThreads * N * U) {
+            uint4 raw[U];
+            float v[U][N];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int64_t c = min(at + (i * kClassThreads + (int)threadIdx.x) * N, (int64_t)a.C);
+                raw[i] = Cols<T>::load(x, (int)c, a.C, left);
+            }
+            float most = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int64_t c = at + (i * kClassThreads + (int)threadIdx.x) * N;
+                Cols<T>::unpack(raw[i], v[i]);
+                if (c + N > c1) {
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        if (c + j >= c1) v[i][j] = -__builtin_inff();
+                }
+#pragma unroll
+                for (int j = 0; j < N; ++j) most = fmaxf(most, v[i][j]);
+            }
+            if (most > sums.m) move_sums(sums, most, a.by, 1.f);
+            const float m = base_of(sums.m);
+#pragma unroll
+            for (int i = 0; i < U; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float d = v[i][j] - m, e = exp_below(d, a.by);
+                    sums.s += e;
+                    if constexpr (Job::kEntropy) sums.u = fmaf(e, fmaxf(d, kLeast), sums.u);
+                }
+            if constexpr (Job::kTop) {
+                if (a.k > 0) {
+#pragma unroll 1
+                    for (int i = 0; i < U; ++i) {
+                        const uint32_t last = (uint32_t)__builtin_amdgcn_readlane((int)top.order, a.k - 1);
+                        float x[N];
+                        uint32_t best = 0;
+#pragma unroll
+                        for (int j = 0; j < N; ++j) {
+                            x[j] = i == 0 ? v[0][j] : i == 1 ? v[1][j] : i == 2 ? v[2][j] : v[3][j];
+                            best = max(best, order_of(x[j]));
+                        }
+                        if (!__any(best >= last)) continue;
+                        const int64_t c = at + (i * kClassThreads + (int)threadIdx.x) * N;
+#pragma unroll
+                        for (int j = 0; j < N; ++j) offer_top(top, {c + j < c1 ? order_of(x[j]) : 0u, (int)(c + j)}, a.k);
+                    }
+                }
+            }
+        }
+        // the wavefront's, then the workgroup's
+        const float largest = lanes_largest<64>(sums.m);
+        move_sums(sums, largest, a.by, 1.f);
+        sums.s = lanes_sum<64>(sums.s);
+        if constexpr (Job::kEntropy) sums.u = lanes_sum<64>(sums.u);
+        __syncthreads();               // (what the last part left there has been read)
+        if (lane == 0) wave_sums[wave] = sums;
+        if constexpr (Job::kTop) wave_top[wave][lane] = top;
+        __syncthreads();
+        if (wave != 0) continue;
+        RowSums all = wave_sums[0];
+#pragma unroll
+        for (int w = 1; w < kClassWaves; ++w) all.m = fmaxf(all.m, wave_sums[w].m);
+        const float m = all.m;
+        all = wave_sums[0];
+        move_sums(all, m, a.by, 1.f);
+#pragma unroll
+        for (int w = 1; w < kClassWaves; ++w) {
+            RowSums more = wave_sums[w];
+            move_sums(more, m, a.by, 1.f);
+            all.s += more.s, all.u += more.u;
+        }
+        if constexpr (Job::kTop) {
+            if (a.k > 0) {
+#pragma unroll 1
+                for (int w = 1; w < kClassWaves; ++w) merge_top(top, wave_top[w][lane]);
+            }
+        }
+        if (a.parts == 1) {
+            all.u *= a.over;
+            Job::template in_wave<T>(a, job, row, all, top);
+        } else {
+            if (lane == 0) a.sums[index] = all;
+            if constexpr (Job::kTop) {
+                if (lane < a.k) a.lists[index * a.k + lane] = top;
+            }
+        }
+    }
+}
+
+// The parts of a row, a wavefront each row.
+template <typename T, typename Job>
+__global__ __launch_bounds__(kClassThreads) void k_class_join(ClassRows a, typename Job::Args job)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * kClassWaves + (threadIdx.x >> 6);
+    if (row >= a.n) return;
+    RowSums all{-__builtin_inff(), 0.f, 0.f};
+    if (lane < a.parts) all = a.sums[row * a.parts + lane];
+    move_sums(all, lanes_largest<64>(all.m), a.by, 1.f);
+    all.s = lanes_sum<64>(all.s);
+    all.u = lanes_sum<64>(all.u) * a.over;
+    TopList top = no_class();
+    if constexpr (Job::kTop) {
+        if (a.k > 0) {
+            for (int p = 0; p < a.parts; ++p) merge_top(top, lane < a.k ? a.lists[(row * a.parts + p) * a.k + lane] : no_class());
+        }
+    }
+    Job::template in_wave<T>(a, job, row, all, top);
+}
+
+inline size_t class_work_bytes(int64_t n, int C, int k)
+{
+    return (size_t)most_parts(n, C) * (sizeof(RowSums) + (size_t)k * sizeof(TopList) + 8);
+}
+
+template <typename T, typename Job, int TPR>
+int run_in_lanes(int r, const ClassRows& a, const typename Job::Args& job, hipStream_t st)
+{
+    constexpr int kRows = kClassThreads / TPR, S = 4 / (int)sizeof(T) == 1 ? 2 : 1;       // pieces of 8 values
+    const unsigned groups = (unsigned)std::min<int64_t>((a.n + kRows - 1) / kRows, 1 << 20);
+    switch (r / S) {
+    case 1: k_class_rows<T, TPR, 1 * S, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
+    case 2: k_class_rows<T, TPR, 2 * S, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
+    case 3: k_class_rows<T, TPR, 3 * S, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
+    default: k_class_rows<T, TPR, 4 * S, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
+    }
+    SAR_LAUNCH_CHECK();
+    return SAR_OK;
+}
+
+// One pass over the scores X [n, C] of a job; work: class_work_bytes.
+template <typename T, typename Job>
+int run_classes(ClassRows a, const typename Job::Args& job, const char* what, void* work, size_t work_bytes, hipStream_t st)
+{
+    const int dtype = sizeof(T) == 4 ? SAR_F32 : SAR_BF16;
+    if (a.C <= kMostInLanes) {
+        const ClassShape s = class_shape(dtype, a.n, a.C);
+        switch (s.tpr) {
+        case 4: return run_in_lanes<T, Job, 4>(s.r, a, job, st);
+        case 8: return run_in_lanes<T, Job, 8>(s.r, a, job, st);
+        case 16: return run_in_lanes<T, Job, 16>(s.r, a, job, st);
+        case 32: return run_in_lanes<T, Job, 32>(s.r, a, job, st);
+        default: return run_in_lanes<T, Job, 64>(s.r, a, job, st);
+        }
+    }
+    a.parts = parts_of(dtype, a.n, a.C);
+    a.width = part_width(a.C, a.parts);
+    if (a.parts > 1) {
+        const size_t need = class_work_bytes(a.n, a.C, Job::kTop ? a.k : 0);
+        SAR_CHECK_ARG(work && work_bytes >= need, "%s: work has %zu bytes, needs %zu", what, work ? work_bytes : 0, need);
+        SAR_CHECK_ARG((reinterpret_cast<uintptr_t>(work) & 15) == 0, "%s: work must be 16-byte aligned", what);
+        a.lists = static_cast<TopList*>(work);
+        a.sums = reinterpret_cast<RowSums*>(a.lists + a.n * a.parts * (Job::kTop ? a.k : 0));
+    }
+    const unsigned groups = (unsigned)std::min<int64_t>(a.n * a.parts, 1 << 20);
+    k_class_wide<T, Job><<<groups, kClassThreads, 0, st>>>(a, job);
+    SAR_LAUNCH_CHECK();
+    if (a.parts > 1) {
+        k_class_join<T, Job><<<(unsigned)((a.n + kClassWaves - 1) / kClassWaves), kClassThreads, 0, st>>>(a, job);
+        SAR_LAUNCH_CHECK();
+    }
+    return SAR_OK;
+}
+
+// ---- gradients: tiles of up to kTileValues scores, whole rows where they are short, a piece of one row where they are long
+
+constexpr int kTileValues = 4096, kMostTileRows = 256;
+struct ClassTiles {
+    int64_t n;
+    int C;
+    int rows, width;       // of a tile
+    int across;            // tiles beside each other
+    int64_t tiles;
+    uint32_t magic;        // ceil(2^32 / C): a place in a tile of whole rows by it is its row
+};
+inline ClassTiles class_tiles(int64_t n, int C)
+{
+    ClassTiles t{n, C, 1, std::min(C, kTileValues), 0, 0, 0};
+    t.rows = std::max(1, std::min(kTileValues / C, kMostTileRows));
+    if (t.rows >= 8) t.rows = t.rows / 8 * 8;          // (whole pieces)
+    t.across = (C + t.width - 1) / t.width;
+    t.tiles = (n + t.rows - 1) / t.rows * t.across;
+    t.magic = C > 1 ? (uint32_t)(((1ull << 32) + C - 1) / C) : 0u;
+    return t;
+}
+__device__ inline int tile_row(const ClassTiles& t, int place) { return t.C > 1 ? (int)__umulhi((uint32_t)place, t.magic) : place; }
+
+// Refuses what no call takes.
+inline int check_classes(const char* what, int dtype, int64_t n, int C, int k)
+{
+    if (dtype != SAR_F32 && dtype != SAR_BF16) return fail(SAR_ERR_UNSUPPORTED, "dtype %d is neither SAR_F32 nor SAR_BF16", dtype);
+    SAR_CHECK_ARG(n >= 0 && C >= 1 && k >= 0, "%s: n = %lld rows of C = %d classes, k = %d", what, (long long)n, C, k);
+    if (k > kMostTop) return fail(SAR_ERR_UNSUPPORTED, "%s: k = %d classes of a row (at most %d)", what, k, kMostTop);
+    if (C > (1 << 30)) return fail(SAR_ERR_UNSUPPORTED, "%s: C = %d classes (at most 2^30)", what, C);
+    return SAR_OK;
+}
+
+}  // namespace sar

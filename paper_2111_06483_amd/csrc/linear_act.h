@@ -1,0 +1,111 @@
+// What is done to a row of X W before it is stored: bias, residual, activation (linear_act.hip); the activations and their derivatives.
+#pragma once
+
+#include "linear_common.h"
+#include "sar_internal.h"
+
+namespace sar {
+
+struct NoEpilogue {
+    static constexpr bool kAny = false;
+};
+// a = X W + bias (+ res), pre = a, Y = act(a) (+ res, `after`); null where there is none.
+struct Epilogue {
+    static constexpr bool kAny = true;
+    const float* bias;
+    const void* res;
+    void* pre;
+    int act, after;
+};
+
+__device__ inline float value_of(float v) { return v; }
+__device__ inline float value_of(bf16_t v) { return bf16_to_f32(v); }
+
+// ---- activations, in 32 bits.  Infinities have their limits, NaN stays.
+
+// Phi(a) and exp(-a^2 / 2).  The smaller side is t P(t) exp(-a^2 / 2) with t = 1 / (1 + 0.275 |a|), P of degree 5 fitted to it by least squares with weights
+// raised where it was furthest off (5e-9 of Phi); by fp32 operations 2e-7.
+__device__ inline float normal_share(float a, float& bell)
+{
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(a), 0.275f, 1.f));
+    bell = __builtin_amdgcn_exp2f(a * a * -0.72134752f);
+    float p = fmaf(t, -0.11485983431339264f, 0.45200487971305847f);
+    p = fmaf(t, p, -0.33100342750549316f);
+    p = fmaf(t, p, 0.3339403569698334f);
+    p = fmaf(t, p, 0.042108260095119476f);
+    p = fmaf(t, p, 0.11780976504087448f);
+    const float side = p * t * bell;
+    return a > 0.f ? 1.f - side : side;
+}
+__device__ inline float logistic(float a) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(a * -kLog2e)); }
+// Between them the derivatives of what follows are still to be told from their limits.
+__device__ inline float within(float a, float most) { return __builtin_amdgcn_fmed3f(a, -most, most); }
+// exp(a) - 1 for a <= 0: near zero by the series (its first term left out, a^7 / 8!, is 2^-26 of the sum at most).
+__device__ inline float below_one(float a)
+{
+    float s = fmaf(a, 1.f / 5040.f, 1.f / 720.f);
+    s = fmaf(a, s, 1.f / 120.f);
+    s = fmaf(a, s, 1.f / 24.f);
+    s = fmaf(a, s, 1.f / 6.f);
+    s = fmaf(a, s, 0.5f);
+    s = fmaf(a * a, s, a);
+    return a > -0.35f ? s : __builtin_amdgcn_exp2f(a * kLog2e) - 1.f;
+}
+
+template <int ACT>
+__device__ inline float act_of(float a)
+{
+    if constexpr (ACT == SAR_ACT_RELU) return a < 0.f ? 0.f : a;
+    if constexpr (ACT == SAR_ACT_GELU) {
+        float bell;
+        const float share = normal_share(a, bell);
+        return fmaxf(a, -64.f) * share;
+    }
+    if constexpr (ACT == SAR_ACT_SILU) return fmaxf(a, -256.f) * logistic(a);
+    if constexpr (ACT == SAR_ACT_ELU) return a > 0.f ? a : below_one(a);
+    return a;
+}
+// d act'(a)
+template <int ACT>
+__device__ inline float act_grad(float d, float a)
+{
+    if constexpr (ACT == SAR_ACT_RELU) return a > 0.f ? d : 0.f;
+    if constexpr (ACT == SAR_ACT_GELU) {
+        float bell;
+        const float share = normal_share(a, bell);
+        return d * fmaf(within(a, 64.f) * bell, 0.39894228040143267f, share);
+    }
+    if constexpr (ACT == SAR_ACT_SILU) {
+        const float s = logistic(a);
+        return d * (s * fmaf(within(a, 256.f), 1.f - s, 1.f));
+    }
+    if constexpr (ACT == SAR_ACT_ELU) return a > 0.f ? d : d * __builtin_amdgcn_exp2f(a * kLog2e);
+    return d;
+}
+
+// f with the activation as a constant.
+template <typename F>
+__device__ __attribute__((always_inline)) inline void with_act(int act, F&& f)
+{
+    switch (act) {
+    case SAR_ACT_RELU: f(std::integral_constant<int, SAR_ACT_RELU>{}); break;
+    case SAR_ACT_GELU: f(std::integral_constant<int, SAR_ACT_GELU>{}); break;
+    case SAR_ACT_SILU: f(std::integral_constant<int, SAR_ACT_SILU>{}); break;
+    case SAR_ACT_ELU: f(std::integral_constant<int, SAR_ACT_ELU>{}); break;
+    default: break;
+    }
+}
+
+// One value of the product, column n, place `at` of the rows.
+template <typename T>
+__device__ inline float finish_value(const Epilogue& e, float v, int64_t at, int n)
+{
+    if (e.bias) v += e.bias[n];
+    const float r = e.res ? value_of(static_cast<const T*>(e.res)[at]) : 0.f;
+    if (!e.after) v += r;
+    if (e.pre) static_cast<T*>(e.pre)[at] = from_f32<T>(v);
+    with_act(e.act, [&](auto act) { v = act_of<decltype(act)::value>(v); });
+    return e.after ? v + r : v;
+}
+
+}  // namespace sar

@@ -1,0 +1,206 @@
+// The transform with what stands around it in a layer: Y = act(X W + b + R) or act(X W + b) + R, and its backward pass.
+//
+//   a = X W + b (+ R),  Y = act(a) (+ R);   dA = dY act'(a):  dW = X^T dA,  db = sum over rows of dA,  dX = dA W^T
+//
+// Forward: the kernels of linear_typed_rows.h and linear_typed_few.hip with one type; bias, residual and activation meet the sums in registers, in 32
+// bits, and are rounded once.
+#include "linear_typed_rows.h"
+
+namespace sar {
+
+namespace {
+
+constexpr int kActThreads = 256;
+constexpr int kActGroups = 1024;
+
+// dA = dY act'(a) of rows, and sums of its columns.
+struct ActBwdArgs {
+    const void* dY;
+    const void* A;
+    void* dA;              // [n, F] of dtype, or null
+    void* low;             // bf16: what dA's rounding left, in bf16; or null
+    float* partial;        // [gridDim.x, F], or null
+    int64_t n;
+    int F, act, lanes;     // lanes: of a row, a power of two
+};
+
+template <typename T>
+__global__ __launch_bounds__(kActThreads) void k_act_bwd(ActBwdArgs a)
+{
+    constexpr int N = Cols<T>::N;
+    __shared__ float sums[kActThreads * N];
+    const int t = threadIdx.x & (a.lanes - 1), slice = threadIdx.x / a.lanes, rows = kActThreads / a.lanes;
+    const int c = (blockIdx.y * a.lanes + t) * N;
+    float total[N] = {};
+    for (int64_t row = (int64_t)blockIdx.x * rows + slice; row < a.n; row += (int64_t)gridDim.x * rows) {
+        const int64_t at = row * a.F, left = (a.n - row) * a.F;
+        float d[N];
+        Cols<T>::values(Cols<T>::load(static_cast<const T*>(a.dY) + at, c, a.F, left), c, a.F, d);
+        if (a.act != SAR_ACT_NONE) {
+            float x[N];
+            Cols<T>::values(Cols<T>::load(static_cast<const T*>(a.A) + at, c, a.F, left), c, a.F, x);
+            with_act(a.act, [&](auto act) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) d[j] = act_grad<decltype(act)::value>(d[j], x[j]);
+            });
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) total[j] += d[j];
+        if (a.dA) Cols<T>::store(static_cast<T*>(a.dA) + at, c, a.F, d);
+        if (a.low) {
+            float high[N];
+            Cols<T>::unpack(Cols<T>::round(d), high);
+#pragma unroll
+            for (int j = 0; j < N; ++j) d[j] -= high[j];
+            Cols<T>::store(static_cast<T*>(a.low) + at, c, a.F, d);
+        }
+    }
+    if (!a.partial) return;
+#pragma unroll
+    for (int j = 0; j < N; ++j) sums[(slice * N + j) * a.lanes + t] = total[j];
+    __syncthreads();
+    for (int k = threadIdx.x; k < a.lanes * N; k += kActThreads) {
+        const int col = (blockIdx.y * a.lanes + k % a.lanes) * N + k / a.lanes;
+        if (col >= a.F) continue;
+        float v = 0.f;
+        for (int s = 0; s < rows; ++s) v += sums[s * a.lanes * N + k];
+        a.partial[(int64_t)blockIdx.x * a.F + col] = v;
+    }
+}
+
+// db (+)= the partial sums of `groups` workgroups, in order: 32 columns a workgroup, whose 32 slices take every 32nd.
+__global__ __launch_bounds__(1024) void k_act_sum(const float* partial, int groups, int F, int accumulate, float* db)
+{
+    __shared__ float part[32][33];
+    const int k = threadIdx.x % 32, slice = threadIdx.x / 32, c = blockIdx.x * 32 + k;
+    float v = 0.f;
+    if (c < F)
+        for (int w = slice; w < groups; w += 32) v += partial[(int64_t)w * F + c];
+    part[slice][k] = v;
+    __syncthreads();
+    if (slice == 0 && c < F) {
+        float total = 0.f;
+#pragma unroll
+        for (int s = 0; s < 32; ++s) total += part[s][k];
+        db[c] = accumulate ? db[c] + total : total;
+    }
+}
+
+int lanes_of(int dtype, int F)
+{
+    const int vec = dtype == SAR_F32 ? 4 : 8;
+    int lanes = 1;
+    while (lanes < 64 && lanes * vec < F) lanes <<= 1;
+    return lanes;
+}
+int groups_of(int dtype, int64_t n, int F)
+{
+    const int64_t rows = kActThreads / lanes_of(dtype, F);
+    return (int)std::max<int64_t>(1, std::min<int64_t>((n + rows - 1) / rows, std::max(1, std::min(kActGroups, (1 << 22) / F))));
+}
+
+size_t rounded(size_t b) { return (b + 255) / 256 * 256; }
+size_t partial_bytes(int64_t n, int F)
+{
+    return rounded((size_t)std::max(groups_of(SAR_F32, n, F), groups_of(SAR_BF16, n, F)) * F * sizeof(float));
+}
+
+int check_act(int act)
+{
+    if (act < SAR_ACT_NONE || act > SAR_ACT_ELU) return fail(SAR_ERR_UNSUPPORTED, "act %d is none of SAR_ACT_NONE, _RELU, _GELU, _SILU, _ELU", act);
+    return SAR_OK;
+}
+
+int check_work(int dtype, int64_t n, int K, int F, const void* work, size_t work_bytes)
+{
+    if (dtype != SAR_F32 && dtype != SAR_BF16) return fail(SAR_ERR_UNSUPPORTED, "dtype %d is neither SAR_F32 nor SAR_BF16", dtype);
+    size_t need = 0;
+    SAR_TRY(sar_linear_act_workspace_bytes(n, K, F, &need));
+    SAR_CHECK_ARG(work && work_bytes >= need, "linear with activation: work has %zu bytes, needs %zu", work ? work_bytes : 0, need);
+    SAR_CHECK_ARG((reinterpret_cast<uintptr_t>(work) & 15) == 0, "linear with activation: work must be 16-byte aligned");
+    return SAR_OK;
+}
+
+template <typename T>
+int act_bwd(const void* dY, const void* A, const void* X, const float* W, int act, int accumulate, float* dW, float* db, void* dX, void* dA, int64_t n,
+            int K, int F, void* work, hipStream_t st)
+{
+    const int dtype = sizeof(T) == 4 ? SAR_F32 : SAR_BF16;
+    size_t products = 0;
+    SAR_TRY(sar_linear_typed_workspace_bytes(n, K, F, 1, &products));
+    char* const base = static_cast<char*>(work);
+    float* const partial = reinterpret_cast<float*>(base + rounded(products));
+    char* const high = reinterpret_cast<char*>(partial) + partial_bytes(n, F);
+    const bool formed = act != SAR_ACT_NONE;
+    void* rows = !formed ? const_cast<void*>(dY) : dA ? dA : high;
+    void* low = formed && dW && sizeof(T) == 2 ? high + rounded((size_t)n * F * sizeof(T)) : nullptr;
+    if (n > 0 && (formed || db || dA)) {
+        const int lanes = lanes_of(dtype, F), groups = groups_of(dtype, n, F);
+        const ActBwdArgs a{dY, A, formed ? rows : dA, low, db ? partial : nullptr, n, F, act, lanes};
+        const int across = (F + lanes * Cols<T>::N - 1) / (lanes * Cols<T>::N);
+        k_act_bwd<T><<<dim3(groups, across), kActThreads, 0, st>>>(a);
+        SAR_LAUNCH_CHECK();
+    }
+    if (db) {
+        k_act_sum<<<(F + 31) / 32, 1024, 0, st>>>(partial, n > 0 ? groups_of(dtype, n, F) : 0, F, accumulate, db);
+        SAR_LAUNCH_CHECK();
+    }
+    const Types types{nullptr, 1, n};
+    if (dW) {
+        SAR_TRY(typed_dw(dtype, {X, nullptr, nullptr, rows, dW, types, K, F, accumulate, static_cast<float*>(work)}, st));
+        if (low && n > 0) SAR_TRY(typed_dw(dtype, {X, nullptr, nullptr, low, dW, types, K, F, 1, static_cast<float*>(work)}, st));
+    }
+    if (dX && n > 0) return rows_product<T, true>(rows, W, types, dX, K, F, work, st);
+    return SAR_OK;
+}
+
+}  // namespace
+}  // namespace sar
+
+using namespace sar;
+
+extern "C" int sar_linear_act_workspace_bytes(int64_t n, int K, int F, size_t* bytes)
+{
+    SAR_CHECK_ARG(bytes, "bytes is null");
+    size_t products = 0;
+    SAR_TRY(sar_linear_typed_workspace_bytes(n, K, F, 1, &products));
+    *bytes = rounded(products) + partial_bytes(n, F) + 2 * rounded((size_t)n * F * 4);
+    return SAR_OK;
+}
+
+extern "C" int sar_linear_act_fwd(const void* X, const float* W, const float* bias, const void* res, int act, int res_after, void* Y, void* A, int dtype,
+                                  int64_t n, int K, int F, void* work, size_t work_bytes, void* stream)
+{
+    SAR_TRY(check_act(act));
+    SAR_TRY(check_work(dtype, n, K, F, work, work_bytes));
+    if (n == 0) return SAR_OK;
+    SAR_CHECK_ARG(X && W && Y, "null pointer (X, W, Y)");
+    const size_t b = dtype == SAR_F32 ? 4 : 2, in = (size_t)n * K * b, out = (size_t)n * F * b;
+    SAR_CHECK_ARG(apart(Y, out, X, in) && apart(Y, out, W, (size_t)K * F * 4) && apart(Y, out, A, out) && apart(X, in, A, out) && apart(W, (size_t)K * F * 4, A, out),
+                  "linear with activation: Y, A must not alias X, W or each other");
+    SAR_CHECK_ARG(Y == res || apart(Y, out, res, out), "linear with activation: Y overlaps res, and is not res");
+    SAR_CHECK_ARG((A == res && !res_after) || !A || apart(A, out, res, out), "linear with activation: A overlaps res");
+    const Types types{nullptr, 1, n};
+    const Epilogue e{bias, res, A, act, res_after};
+    return dtype == SAR_F32 ? rows_product<float, false>(X, W, types, Y, K, F, work, as_stream(stream), e)
+                            : rows_product<bf16_t, false>(X, W, types, Y, K, F, work, as_stream(stream), e);
+}
+
+extern "C" int sar_linear_act_bwd(const void* dY, const void* A, const void* X, const float* W, int act, int accumulate, float* dW, float* db, void* dX,
+                                  void* dA, int dtype, int64_t n, int K, int F, void* work, size_t work_bytes, void* stream)
+{
+    SAR_TRY(check_act(act));
+    SAR_TRY(check_work(dtype, n, K, F, work, work_bytes));
+    if (n > 0) {
+        const size_t b = dtype == SAR_F32 ? 4 : 2, in = (size_t)n * K * b, out = (size_t)n * F * b, w = (size_t)K * F * 4;
+        SAR_CHECK_ARG(dY && (act == SAR_ACT_NONE || A), "null pointer (dY, A)");
+        SAR_CHECK_ARG(!dW || X, "null pointer (X)");
+        SAR_CHECK_ARG(!dX || W, "null pointer (W)");
+        SAR_CHECK_ARG(!dX || (apart(dX, in, dY, out) && apart(dX, in, A, out) && apart(dX, in, X, in) && apart(dX, in, W, w) && apart(dX, in, dA, out)),
+                      "linear with activation: dX must not alias dY, A, X, W or dA");
+        SAR_CHECK_ARG(!dA || (apart(dA, out, dY, out) && apart(dA, out, A, out) && apart(dA, out, X, in)), "linear with activation: dA must not alias dY, A or X");
+        SAR_CHECK_ARG(!dW || !W || apart(dW, w, W, w), "linear with activation: dW must not alias W");
+    }
+    return dtype == SAR_F32 ? act_bwd<float>(dY, A, X, W, act, accumulate, dW, db, dX, dA, n, K, F, work, as_stream(stream))
+                            : act_bwd<bf16_t>(dY, A, X, W, act, accumulate, dW, db, dX, dA, n, K, F, work, as_stream(stream));
+}

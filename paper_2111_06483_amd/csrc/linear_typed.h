@@ -47,7 +47,10 @@ struct TypedRows {
     Types types;
     int C, N, K, F;
 };
-int few_product(int dtype, bool trans, const TypedRows& a, hipStream_t st);
+struct NoEpilogue;
+struct Epilogue;
+int few_product(int dtype, bool trans, const TypedRows& a, const NoEpilogue&, hipStream_t st);
+int few_product(int dtype, bool trans, const TypedRows& a, const Epilogue& e, hipStream_t st);      // (not of W^T)
 int few_dw(int dtype, const TypedDw& g, hipStream_t st);
 int few_dw_and_dx(int dtype, const TypedDw& g, const TypedRows& a, hipStream_t st);
 

@@ -8,6 +8,7 @@
 // each 11.2.
 #include <algorithm>
 
+#include "linear_act.h"
 #include "linear_pieces.h"
 #include "linear_typed.h"
 
@@ -48,8 +49,8 @@ __device__ inline bool few_rows_of(const Types& types, int64_t index, int& t, in
 
 // PARTS: wavefronts that share one block's contraction, chunk by chunk, and add up in LDS (4), or one a block (1), of a workgroup of WAVES.  `row`: which
 // block of rows; `beside`: which of the groups of column tiles that a workgroup takes; `sums`: [WAVES][16][64].
-template <typename T, bool TRANS, int PARTS, int WAVES>
-__device__ SAR_INLINE inline void few_rows(const TypedRows& a, int64_t row_block, int beside, float* sums)
+template <typename T, bool TRANS, int PARTS, int WAVES, typename E = NoEpilogue>
+__device__ SAR_INLINE inline void few_rows(const TypedRows& a, int64_t row_block, int beside, float* sums, const E& e = {})
 {
     constexpr int N = Cols<T>::N, kRaw = 8 / N, U = 4;                // 16-byte pieces of a row a product of 16; products a chunk
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, share = wave % PARTS;
@@ -162,7 +163,10 @@ __device__ SAR_INLINE inline void few_rows(const TypedRows& a, int64_t row_block
     }
     auto store = [&](int r, float v) SAR_INLINE {
         const int64_t o = first + 8 * (r / 4) + 4 * h + r % 4;
-        if (n < a.N && o < end) static_cast<T*>(a.out)[o * a.N + n] = from_f32<T>(v);
+        if (n < a.N && o < end) {
+            if constexpr (E::kAny) v = finish_value<T>(e, v, o * a.N + n, n);
+            static_cast<T*>(a.out)[o * a.N + n] = from_f32<T>(v);
+        }
     };
     if constexpr (PARTS == 4) {
         float(*part)[16][64] = reinterpret_cast<float(*)[16][64]>(sums) + wave / PARTS * PARTS;
@@ -285,11 +289,11 @@ __device__ SAR_INLINE inline void few_weights(const DwArgs& a, int accumulate, f
 
 // ---- launches
 
-template <typename T, bool TRANS, int PARTS>
-__global__ __launch_bounds__(256, 2) void k_typed_few(TypedRows a)
+template <typename T, bool TRANS, int PARTS, typename E>
+__global__ __launch_bounds__(256, 2) void k_typed_few(TypedRows a, E e)
 {
     __shared__ float sums[PARTS == 4 ? 4 * 16 * 64 : 1];
-    few_rows<T, TRANS, PARTS, 4>(a, blockIdx.x, blockIdx.y, sums);
+    few_rows<T, TRANS, PARTS, 4>(a, blockIdx.x, blockIdx.y, sums, e);
 }
 
 template <typename XR, typename ZR, int WAVES>
@@ -322,12 +326,12 @@ bool shared_blocks(const TypedRows& a) { return a.C > 64 && row_blocks(a.types) 
 // types, 400 x 512, 30.7 and 15.7).
 bool eight_waves(const Types& types) { return types.n > 64 * (int64_t)types.T; }
 
-template <typename T, bool TRANS>
-int product(const TypedRows& a, hipStream_t st)
+template <typename T, bool TRANS, typename E = NoEpilogue>
+int product(const TypedRows& a, hipStream_t st, const E& e = {})
 {
     const unsigned groups = (unsigned)row_blocks(a.types);
-    if (shared_blocks(a)) k_typed_few<T, TRANS, 4><<<dim3(groups, (a.N + 31) / 32), 256, 0, st>>>(a);
-    else k_typed_few<T, TRANS, 1><<<dim3(groups, (a.N + 127) / 128), 256, 0, st>>>(a);
+    if (shared_blocks(a)) k_typed_few<T, TRANS, 4, E><<<dim3(groups, (a.N + 31) / 32), 256, 0, st>>>(a, e);
+    else k_typed_few<T, TRANS, 1, E><<<dim3(groups, (a.N + 127) / 128), 256, 0, st>>>(a, e);
     SAR_LAUNCH_CHECK();
     return SAR_OK;
 }
@@ -390,10 +394,15 @@ bool few_rows_dw(int64_t n, int T, int K, int F)
     return n <= std::min(std::max(kFewRows, kFewOfType * T), kFewRowsOfAll) && n * ((K + 31) / 32) * ((F + 31) / 32) <= kFewColumns;
 }
 
-int few_product(int dtype, bool trans, const TypedRows& a, hipStream_t st)
+int few_product(int dtype, bool trans, const TypedRows& a, const NoEpilogue&, hipStream_t st)
 {
     if (dtype == SAR_F32) return trans ? product<float, true>(a, st) : product<float, false>(a, st);
     return trans ? product<bf16_t, true>(a, st) : product<bf16_t, false>(a, st);
+}
+
+int few_product(int dtype, bool, const TypedRows& a, const Epilogue& e, hipStream_t st)
+{
+    return dtype == SAR_F32 ? product<float, false>(a, st, e) : product<bf16_t, false>(a, st, e);
 }
 
 int few_dw(int dtype, const TypedDw& g, hipStream_t st)

@@ -1,0 +1,237 @@
+// Log probabilities of given classes, with the distribution's entropy and its top classes, and their gradient.
+//
+//   m = max x, S = sum exp(x - m), U = sum exp(x - m) (x - m):  lse = m + log S, log p_c = (x_c - m) - log S, H = log S - U / S
+//   dx_c = g ([c = label] - p_c) - h p_c (log p_c + H)
+//
+// One pass over the scores each way (class_rows.h).
+#include "class_rows.h"
+
+namespace sar {
+
+namespace {
+
+struct LogprobJob {
+    static constexpr bool kEntropy = true, kTop = true;
+    struct Args {
+        const int32_t* label;
+        float *logp, *lse, *entropy, *value;
+        int32_t* index;
+    };
+
+    // What a row has beside its top classes; by one lane.
+    template <typename T>
+    static __device__ inline void results(const ClassRows& a, const Args& o, int64_t row, const RowSums& r, float log)
+    {
+        const bool none = r.m == -__builtin_inff() && r.s == 0.f;
+        if (o.lse) o.lse[row] = base_of(r.m) + log;
+        if (o.entropy) o.entropy[row] = none ? 0.f : log - r.u / r.s;
+        if (o.logp) {
+            const int32_t c = o.label[row];
+            float v = 0.f;
+            if ((uint32_t)c < (uint32_t)a.C) {
+                const T x = static_cast<const T*>(a.X)[row * a.C + c];
+                v = none ? -__builtin_inff() : (to_f32(x) - base_of(r.m)) - log;
+            }
+            o.logp[row] = v;
+        }
+    }
+    static __device__ inline float to_f32(float v) { return v; }
+    static __device__ inline float to_f32(bf16_t v) { return bf16_to_f32(v); }
+
+    template <typename T, int TPR, int R>
+    static __device__ inline void in_lanes(const ClassRows& a, const Args& o, int64_t row, bool there, int t, const RowSums& r,
+                                           const float (&v)[R][Cols<T>::N])
+    {
+        constexpr int N = Cols<T>::N;
+        const float log = logf(r.s);
+        if (there && t == 0) results<T>(a, o, row, r, log);
+        if (a.k == 0) return;
+        // Whichever class is the largest is written and taken out, k times over.  A bf16 score's order and its class fit one number.
+        uint32_t key[R][N];
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int c = (t + i * TPR) * N + j;
+                key[i][j] = order_of(v[i][j]);
+                if constexpr (N == 8) key[i][j] = (key[i][j] & 0xffff0000u) | (0xffffu - (uint32_t)c);
+                if (c >= a.C) key[i][j] = 0u;
+            }
+        for (int k = 0; k < a.k; ++k) {
+            uint32_t best = 0;
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) best = max(best, key[i][j]);
+            best = over_lanes<TPR>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
+            int cls;
+            if constexpr (N == 8) {
+                cls = (int)(0xffffu - (best & 0xffffu));
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) key[i][j] = key[i][j] == best ? 0u : key[i][j];
+                best &= 0xffff0000u;
+                if (best & 0x80000000u) best = best;
+                else best |= 0xffffu;          // (the low half of a negative number's order)
+            } else {
+                cls = 0x7fffffff;
+#pragma unroll
+                for (int i = R - 1; i >= 0; --i)
+#pragma unroll
+                    for (int j = N - 1; j >= 0; --j) cls = key[i][j] == best ? (t + i * TPR) * N + j : cls;
+                cls = over_lanes<TPR>(cls, [](int x, int y) { return min(x, y); });
+#pragma unroll
+                for (int i = 0; i < R; ++i)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) key[i][j] = (t + i * TPR) * N + j == cls ? 0u : key[i][j];
+            }
+            if (there && t == 0) {
+                const bool is = best > kOrderOfNone;
+                o.value[row * a.k + k] = is ? (score_of(best) - base_of(r.m)) - log : -__builtin_inff();
+                o.index[row * a.k + k] = is ? cls : -1;
+            }
+        }
+    }
+
+    template <typename T>
+    static __device__ inline void in_wave(const ClassRows& a, const Args& o, int64_t row, const RowSums& r, const TopList& top)
+    {
+        const int lane = threadIdx.x & 63;
+        const float log = logf(r.s);
+        if (lane == 0) results<T>(a, o, row, r, log);
+        if (lane < a.k) {
+            const bool is = top.order > kOrderOfNone;
+            o.value[row * a.k + lane] = is ? (score_of(top.order) - base_of(r.m)) - log : -__builtin_inff();
+            o.index[row * a.k + lane] = is ? top.cls : -1;
+        }
+    }
+};
+
+struct GradArgs {
+    ClassTiles t;
+    const void* X;
+    const int32_t* label;
+    const float *lse, *entropy, *dlogp, *dentropy;
+    void* dX;
+};
+
+// What a row's gradient takes: p = exp(x - lse), dx = -p (g + h (x - lse + H)), and g more at the label.
+struct RowGrad {
+    float lse, g, h, entropy;
+};
+__device__ inline float grad_of(float x, const RowGrad& r)
+{
+    const float d = x - r.lse, p = exp_below(d, kLog2e);
+    return -p * fmaf(r.h, fmaxf(d, kLeast) + r.entropy, r.g);
+}
+
+// ROWS: how many rows a piece of N scores may meet: 1, 2, or any number.
+template <typename T, int ROWS>
+__global__ __launch_bounds__(kClassThreads) void k_logprob_bwd(GradArgs a)
+{
+    constexpr int N = Cols<T>::N;
+    __shared__ RowGrad rows[kMostTileRows + 1];
+    __shared__ int labels[kMostTileRows + 1];
+    for (int64_t index = blockIdx.x; index < a.t.tiles; index += gridDim.x) {
+        const int64_t down = index / a.t.across, row0 = down * a.t.rows;
+        const int c0 = (int)(index - down * a.t.across) * a.t.width;
+        const int count = (int)min((int64_t)a.t.rows, a.t.n - row0);
+        __syncthreads();               // (the last tile's rows have been read)
+        if ((int)threadIdx.x < count) {
+            const int64_t row = row0 + threadIdx.x;
+            const int32_t c = a.label ? a.label[row] : -1;
+            const bool has = (uint32_t)c < (uint32_t)a.t.C;
+            RowGrad r{a.lse[row], has && a.dlogp ? a.dlogp[row] : 0.f, a.dentropy ? a.dentropy[row] : 0.f, a.dentropy ? a.entropy[row] : 0.f};
+            int at = has ? c - c0 : -1;
+            if (r.lse == -__builtin_inff()) r = {__builtin_inff(), 0.f, 0.f, 0.f};        // nothing but -inf: no gradient
+            else if (r.lse == __builtin_inff()) r.lse = __builtin_nanf("");
+            rows[threadIdx.x] = r, labels[threadIdx.x] = at;
+        }
+        __syncthreads();
+        const int width = min(a.t.width, a.t.C - c0), values = count * width;
+        const int64_t at = row0 * a.t.C + c0;
+        const T* X = static_cast<const T*>(a.X) + at;
+        T* dX = static_cast<T*>(a.dX) + at;
+        const int64_t left = a.t.n * a.t.C - at;
+        for (int e = threadIdx.x * N; e < values; e += kClassThreads * N) {
+            float x[N];
+            Cols<T>::unpack(Cols<T>::load(X, e, values, left), x);
+            int r = a.t.across > 1 ? 0 : tile_row(a.t, e);
+            int c = e - r * width;
+            if constexpr (ROWS == 1) {
+                const RowGrad g = rows[r];
+                const int label = labels[r] - c;
+#pragma unroll
+                for (int j = 0; j < N; ++j) x[j] = grad_of(x[j], g) + (j == label ? g.g : 0.f);
+            } else if constexpr (ROWS == 2) {
+                const RowGrad g0 = rows[r], g1 = rows[r + 1];
+                const int end = width - c, l0 = labels[r] - c, l1 = labels[r + 1] + end;
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const bool next = j >= end;
+                    const RowGrad g{next ? g1.lse : g0.lse, next ? g1.g : g0.g, next ? g1.h : g0.h, next ? g1.entropy : g0.entropy};
+                    x[j] = grad_of(x[j], g) + (j == (next ? l1 : l0) ? g.g : 0.f);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    if (e + j < values) x[j] = grad_of(x[j], rows[r]) + (c == labels[r] ? rows[r].g : 0.f);
+                    if (++c == width) c = 0, ++r;
+                }
+            }
+            Cols<T>::store(dX, e, values, x);
+        }
+    }
+}
+
+template <typename T>
+int logprob_bwd(const GradArgs& a, hipStream_t st)
+{
+    constexpr int N = Cols<T>::N;
+    const unsigned groups = (unsigned)std::min<int64_t>(a.t.tiles, 1 << 20);
+    if (a.t.rows == 1 || a.t.C % N == 0) k_logprob_bwd<T, 1><<<groups, kClassThreads, 0, st>>>(a);
+    else if (a.t.C >= N) k_logprob_bwd<T, 2><<<groups, kClassThreads, 0, st>>>(a);
+    else k_logprob_bwd<T, 0><<<groups, kClassThreads, 0, st>>>(a);
+    SAR_LAUNCH_CHECK();
+    return SAR_OK;
+}
+
+}  // namespace
+}  // namespace sar
+
+using namespace sar;
+
+extern "C" int sar_logprob_workspace_bytes(int64_t n, int C, int k, size_t* bytes)
+{
+    SAR_CHECK_ARG(bytes, "bytes is null");
+    SAR_TRY(check_classes("log probabilities", SAR_F32, n, C, k));
+    *bytes = class_work_bytes(n, C, k);
+    return SAR_OK;
+}
+
+extern "C" int sar_logprob_fwd(const void* X, const int32_t* label, float* logp, float* lse, float* entropy, int k, float* top_value,
+                               int32_t* top_index, int dtype, int64_t n, int C, void* work, size_t work_bytes, void* stream)
+{
+    SAR_TRY(check_classes("log probabilities", dtype, n, C, k));
+    SAR_CHECK_ARG(k == 0 || n == 0 || (top_value && top_index), "null pointer (top_value, top_index)");
+    SAR_CHECK_ARG(!logp || label || n == 0, "null pointer (label)");
+    if (n == 0) return SAR_OK;
+    SAR_CHECK_ARG(X, "null pointer (X)");
+    ClassRows a{X, n, C, k, kLog2e, 1.f, 1, C, nullptr, nullptr};
+    const LogprobJob::Args job{label, logp, lse, entropy, top_value, top_index};
+    return dtype == SAR_F32 ? run_classes<float, LogprobJob>(a, job, "log probabilities", work, work_bytes, as_stream(stream))
+                            : run_classes<bf16_t, LogprobJob>(a, job, "log probabilities", work, work_bytes, as_stream(stream));
+}
+
+extern "C" int sar_logprob_bwd(const void* X, const int32_t* label, const float* lse, const float* entropy, const float* dlogp,
+                               const float* dentropy, void* dX, int dtype, int64_t n, int C, void* stream)
+{
+    SAR_TRY(check_classes("log probabilities", dtype, n, C, 0));
+    if (n == 0) return SAR_OK;
+    SAR_CHECK_ARG(X && lse && dX, "null pointer (X, lse, dX)");
+    SAR_CHECK_ARG(!dlogp || label, "null pointer (label)");
+    SAR_CHECK_ARG(!dentropy || entropy, "null pointer (entropy)");
+    const GradArgs a{class_tiles(n, C), X, label, lse, entropy, dlogp, dentropy, dX};
+    return dtype == SAR_F32 ? logprob_bwd<float>(a, as_stream(stream)) : logprob_bwd<bf16_t>(a, as_stream(stream));
+}

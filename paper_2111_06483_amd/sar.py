@@ -26,6 +26,9 @@ SAR_F32 = 0
 SAR_BF16 = 1
 SAR_ACT_NONE = 0
 SAR_ACT_RELU = 1
+SAR_ACT_GELU = 2         # (these three: sar_linear_act_fwd and its backward pass)
+SAR_ACT_SILU = 3
+SAR_ACT_ELU = 4
 SAR_MAX_BLOCKS = 64      # blocks of an all-blocks call (handles built with SAR_BUILD_FUSED)
 SAR_MAX_PARTS = 256      # partitions of any handle
 SAR_BUILD_TRANSPOSE = 1
@@ -115,6 +118,9 @@ _SIGNATURES = {
     "sar_layernorm_bwd": "ppppppipppilipzp", "sar_layernorm_workspace_bytes": "lip",
     "sar_linear_typed_fwd": "pppipiliipzp", "sar_linear_typed_bwd": "ppppppiippiliipzp", "sar_linear_typed_workspace_bytes": "liiip",
     "sar_linear_bwd_packed": "ppppippiliipzp",
+    "sar_linear_act_fwd": "ppppiippiliipzp", "sar_linear_act_bwd": "ppppiippppiliipzp", "sar_linear_act_workspace_bytes": "liip",
+    "sar_logprob_fwd": "pppppippilipzp", "sar_logprob_bwd": "pppppppilip", "sar_logprob_workspace_bytes": "liip",
+    "sar_distill_fwd": "pippfppilipzp", "sar_distill_bwd": "pippfpppilip", "sar_distill_workspace_bytes": "liip",
 }
 _CTYPES = {"p": _vp, "i": _c_int, "l": _c_i64, "z": ctypes.c_size_t, "f": ctypes.c_float}
 EXPORTS = list(_SIGNATURES)
@@ -538,3 +544,59 @@ def sar_linear_bwd_packed(packed, dZ: torch.Tensor, W: torch.Tensor, accumulate:
                           dX: Optional[torch.Tensor], work: torch.Tensor) -> None:
     """packed: the pair (q, e) of the input, or None without dW."""
     native().linear_bwd_packed(packed, dZ, W, accumulate, dW, dX, work)
+
+
+# ------------------------------------------------------ the transform with bias, activation and residual
+
+def sar_linear_act_fwd(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor], res: Optional[torch.Tensor], act: int, res_after: bool,
+                       Y: torch.Tensor, A: Optional[torch.Tensor], work: torch.Tensor) -> None:
+    """Y = act(X W + bias + res), or, with res_after, act(X W + bias) + res; A receives what the activation was taken of."""
+    native().linear_act_fwd(X, W, bias, res, act, res_after, Y, A, work)
+
+
+def sar_linear_act_bwd(dY: torch.Tensor, A: Optional[torch.Tensor], X: Optional[torch.Tensor], W: torch.Tensor, act: int, accumulate: bool,
+                       dW: Optional[torch.Tensor], db: Optional[torch.Tensor], dX: Optional[torch.Tensor], dA: Optional[torch.Tensor],
+                       work: torch.Tensor) -> None:
+    """dA receives dY act'(A), the gradient of a residual inside the activation; X None without dW."""
+    native().linear_act_bwd(dY, A, X, W, act, accumulate, dW, db, dX, dA, work)
+
+
+def sar_linear_act_workspace_bytes(n: int, K: int, F: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().sar_linear_act_workspace_bytes(n, K, F, ctypes.byref(out)))
+    return out.value
+
+
+# ------------------------------------------------------ rows of class scores: log probabilities, distillation
+
+def sar_logprob_fwd(X: torch.Tensor, label: Optional[torch.Tensor], logp: Optional[torch.Tensor], lse: Optional[torch.Tensor],
+                    entropy: Optional[torch.Tensor], top=None, work: Optional[torch.Tensor] = None) -> None:
+    """label int32 [n], a row without a class -1; top: a pair (values fp32 [n, k], classes int32 [n, k]) that receives the k likeliest classes."""
+    native().logprob_fwd(X, label, logp, lse, entropy, top, work)
+
+
+def sar_logprob_bwd(X: torch.Tensor, label: Optional[torch.Tensor], lse: torch.Tensor, entropy: Optional[torch.Tensor],
+                    dlogp: Optional[torch.Tensor], dentropy: Optional[torch.Tensor], dX: torch.Tensor) -> None:
+    native().logprob_bwd(X, label, lse, entropy, dlogp, dentropy, dX)
+
+
+def sar_logprob_workspace_bytes(n: int, C: int, k: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().sar_logprob_workspace_bytes(n, C, k, ctypes.byref(out)))
+    return out.value
+
+
+def sar_distill_fwd(X: torch.Tensor, top, temperature: float, loss: Optional[torch.Tensor], lse: Optional[torch.Tensor],
+                    work: Optional[torch.Tensor] = None) -> None:
+    """top: the teacher's classes, a pair (values fp32 [n, k], classes int32 [n, k]) as sar_logprob_fwd makes it."""
+    native().distill_fwd(X, top, temperature, loss, lse, work)
+
+
+def sar_distill_bwd(X: torch.Tensor, top, temperature: float, lse: torch.Tensor, dloss: torch.Tensor, dX: torch.Tensor) -> None:
+    native().distill_bwd(X, top, temperature, lse, dloss, dX)
+
+
+def sar_distill_workspace_bytes(n: int, C: int, k: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check(lib().sar_distill_workspace_bytes(n, C, k, ctypes.byref(out)))
+    return out.value

@@ -1,0 +1,235 @@
+"""The transform with bias, residual and activation, and its backward pass, against 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+from scipy.special import erfc
+
+from paper_2111_06483_amd import sar
+from tests import nodewise as nw
+from tests.test_gpu_linear_typed import dw_off, rows_off
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+DTYPES = [F32, BF16]
+ACTS = {"none": sar.SAR_ACT_NONE, "relu": sar.SAR_ACT_RELU, "gelu": sar.SAR_ACT_GELU, "silu": sar.SAR_ACT_SILU, "elu": sar.SAR_ACT_ELU}
+# no activation here is steeper than this, nor its slope's slope
+STEEP, BEND = 1.13, 1.0
+
+
+def act(name, a):
+    """(activation, slope, what 32 bits may be off of either): a few units of a result, the normal share to within 2e-7, an exponential's argument off
+    by a unit of its size."""
+    if name == "relu":
+        return np.maximum(a, 0), (a > 0) * 1.0, 0 * a, 0 * a
+    if name == "gelu":
+        share, bell = 0.5 * erfc(-a / math.sqrt(2)), np.exp(-a * a / 2) / math.sqrt(2 * math.pi)
+        off = 2.5e-7 + 4 * nw.U * a * a * bell
+        return a * share, share + a * bell, np.abs(a) * off + 2 * nw.U * np.abs(a * share), off + (4 + 4 * a * a) * nw.U * np.abs(a) * bell + 4 * nw.U
+    if name == "silu":
+        s = 1 / (1 + np.exp(-a))
+        off = (4 + 4 * np.abs(a)) * nw.U * s
+        return a * s, s * (1 + a * (1 - s)), np.abs(a) * off, (1 + np.abs(a)) * (off + 4 * nw.U * s)
+    if name == "elu":
+        e = np.exp(np.minimum(a, 0))
+        small = a > -0.35
+        return (np.where(a > 0, a, np.expm1(np.minimum(a, 0))), e, np.where(a > 0, 0, np.where(small, 12 * nw.U * np.abs(a), (4 + 4 * np.abs(a)) * nw.U * e + nw.U)),
+                (3 + 4 * np.abs(a)) * nw.U * e * (a <= 0))
+    return a, np.ones_like(a), 0 * a, 0 * a
+
+
+def inputs(n, K, F, dtype, seed=0):
+    g = torch.Generator().manual_seed(seed * 104729 + n * 131 + K * 17 + F)
+    rn = lambda *s: torch.randn(*s, generator=g)
+    return (rn(n, K).to(dtype).cuda(), (rn(K, F) / K ** 0.5).cuda(), rn(F).cuda(), rn(n, F).to(dtype).cuda())
+
+
+def scratch(n, K, F):
+    size = sar.sar_linear_act_workspace_bytes(n, K, F)
+    room = torch.full((size + 4096,), 77, dtype=torch.uint8, device="cuda")
+    return room[:size], room[size:]
+
+
+def stored(t, off, want):
+    return off + (nw.half_step(t)(np.abs(want) + off) if t == BF16 else 2 * nw.U * np.abs(want))
+
+
+def check_fwd(n, K, F, dtype, name, bias, res, keep, seed=0):
+    X, W, b, R = inputs(n, K, F, dtype, seed)
+    Y, A = torch.full((n, F), 7, dtype=dtype, device="cuda"), torch.full((n, F), 7, dtype=dtype, device="cuda")
+    work, behind = scratch(n, K, F)
+    sar.sar_linear_act_fwd(X, W, b if bias else None, R if res else None, ACTS[name], res == "after", Y, A if keep else None, work)
+    assert bool((behind == 77).all())
+    x, w = nw.f64(X), nw.f64(W)
+    a, size = x @ w, np.abs(x) @ np.abs(w)
+    off = rows_off(size, K, dtype)
+    if bias:
+        a, off = a + nw.f64(b), off + 2 * nw.U * (size + np.abs(nw.f64(b)))
+    if res == "first":
+        a, off = a + nw.f64(R), off + 2 * nw.U * (size + np.abs(nw.f64(b)) + np.abs(nw.f64(R)))
+    if keep:
+        assert (np.abs(nw.f64(A) - a) <= stored(dtype, off, a)).all()
+    y, _, off_act, _ = act(name, a)
+    off = STEEP * off + off_act
+    if res == "after":
+        y, off = y + nw.f64(R), off + 2 * nw.U * (np.abs(y) + np.abs(nw.f64(R)))
+    assert (np.abs(nw.f64(Y) - y) <= stored(dtype, off, y)).all()
+    # the residual's own rows as the result's
+    same = R.clone()
+    if res:
+        sar.sar_linear_act_fwd(X, W, b if bias else None, same, ACTS[name], res == "after", same, None, work)
+        assert torch.equal(same, Y)
+
+
+SHAPES = [(1, 1, 1), (3, 7, 5), (33, 47, 31), (300, 100, 47), (500, 256, 256), (2000, 128, 128), (9000, 256, 256), (9001, 100, 200), (20_000, 64, 400),
+          (30_011, 47, 172), (40_000, 130, 257), (12_345, 513, 64)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("name", list(ACTS))
+@pytest.mark.parametrize("n,K,F", SHAPES)
+def test_forward(n, K, F, name, dtype):
+    check_fwd(n, K, F, dtype, name, True, "first", True)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("res", [None, "first", "after"])
+@pytest.mark.parametrize("n,K,F", [(700, 100, 47), (20_000, 100, 256), (9_000, 64, 33)])
+def test_forms_of_the_forward_pass(n, K, F, res, bias, dtype):
+    check_fwd(n, K, F, dtype, "gelu", bias, res, False, 1)
+    check_fwd(n, K, F, dtype, "none", bias, res, res == "after", 2)
+
+
+def check_bwd(n, K, F, dtype, name, accumulate=False, want=("dW", "db", "dX", "dA"), seed=0):
+    X, W, _, dY = inputs(n, K, F, dtype, seed)
+    g = torch.Generator().manual_seed(n + F)
+    A = (2 * torch.randn(n, F, generator=g)).to(dtype).cuda() if name != "none" else None
+    e = lambda *s, dt=F32: torch.full(s, 3.0, dtype=dt, device="cuda")
+    out = {"dW": e(K, F), "db": e(F), "dX": e(n, K, dt=dtype), "dA": e(n, F, dt=dtype)}
+    out = {k: v if k in want else None for k, v in out.items()}
+    work, behind = scratch(n, K, F)
+    sar.sar_linear_act_bwd(dY, A, X if "dW" in want else None, W, ACTS[name], accumulate, out["dW"], out["db"], out["dX"], out["dA"], work)
+    assert bool((behind == 77).all())
+    x, w, d = nw.f64(X), nw.f64(W), nw.f64(dY)
+    off = 0 * d
+    if name != "none":
+        a = nw.f64(A)
+        _, slope, _, off_slope = act(name, a)
+        # the derivative's own error and the product's rounding
+        off = np.abs(d) * (off_slope + 2 * nw.U * np.abs(slope))
+        d = d * slope
+    before = 3.0 if accumulate else 0.0
+    many = n / 256 + 64                                     # a workgroup's rows, the workgroups
+    if "dA" in want:
+        assert (np.abs(nw.f64(out["dA"]) - d) <= stored(dtype, off, d)).all()
+    if "db" in want:
+        tol = off.sum(0) + many * 2 * nw.U * (np.abs(d).sum(0) + before)
+        assert (np.abs(nw.f64(out["db"]) - before - d.sum(0)) <= tol).all()
+    if "dW" in want:
+        size = np.abs(x).T @ np.abs(d)
+        # (bf16: dA in two pieces, each rounded to 8 bits)
+        tol = np.abs(x).T @ off + 2 * dw_off(size + before, n) + (2.0 ** -17 * size if dtype == BF16 and name != "none" else 0) + 4 * nw.U * before
+        assert (np.abs(nw.f64(out["dW"]) - before - x.T @ d) <= tol).all()
+    if "dX" in want:
+        want_x, size = d @ w.T, np.abs(d) @ np.abs(w).T
+        tol = off @ np.abs(w).T + rows_off(size, F, dtype) + (2.0 ** -8 * size if dtype == BF16 and name != "none" else 0)
+        assert (np.abs(nw.f64(out["dX"]) - want_x) <= stored(dtype, tol, want_x)).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("name", list(ACTS))
+@pytest.mark.parametrize("n,K,F", SHAPES)
+def test_backward(n, K, F, name, dtype):
+    check_bwd(n, K, F, dtype, name)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("want", [("dW",), ("db",), ("dX",), ("dA",), ("dW", "db"), ("dX", "dA"), ("dW", "dX"), ("db", "dX"), ("dW", "db", "dX")])
+@pytest.mark.parametrize("n,K,F", [(700, 100, 47), (20_000, 100, 256)])
+def test_forms_of_the_backward_pass(n, K, F, want, dtype):
+    for name in ("none", "silu"):
+        check_bwd(n, K, F, dtype, name, want=want, seed=1)
+        check_bwd(n, K, F, dtype, name, accumulate=True, want=want, seed=2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("name", list(ACTS))
+def test_activations_over_their_range(name, dtype):
+    """By a transform that hands its input on (X e_1 = x): small, large and infinite arguments, and NaN."""
+    v = torch.cat([torch.linspace(-30, 30, 4001), torch.logspace(-30, 38, 500), -torch.logspace(-30, 38, 500), torch.tensor([0.0, -0.0])])
+    X = torch.stack([v, torch.zeros_like(v)], 1).to(dtype).cuda()
+    W = torch.tensor([[1.0, 0.0], [0.0, 1.0]], device="cuda")
+    n = len(v)
+    Y = torch.empty(n, 2, dtype=dtype, device="cuda")
+    work, _ = scratch(n, 2, 2)
+    sar.sar_linear_act_fwd(X, W, None, None, ACTS[name], False, Y, None, work)
+    a = nw.f64(X)[:, 0]
+    with np.errstate(over="ignore"):
+        y, slope, off_y, off_slope = act(name, a)
+    tol = off_y + 4 * nw.U * np.abs(a) + 1e-37
+    assert (np.abs(nw.f64(Y)[:, 0] - y) <= stored(dtype, tol, y)).all()
+    assert (nw.f64(Y)[:, 1] == 0).all()
+    dA, one = torch.empty_like(X), torch.ones_like(X)
+    sar.sar_linear_act_bwd(one, X, None, W, ACTS[name], False, None, None, None, dA, work)
+    assert (np.abs(nw.f64(dA)[:, 0] - slope) <= stored(dtype, off_slope + 1e-37, slope)).all()
+    odd = torch.tensor([[float("inf"), 0], [-float("inf"), 0], [float("nan"), 0]]).to(dtype).cuda()
+    b = torch.zeros(2, device="cuda")
+    Y, A = torch.empty_like(odd), odd.clone()
+    # (infinities reach the activation by the residual: in a product they would meet zeros)
+    sar.sar_linear_act_fwd(torch.zeros_like(odd), W, b, odd, ACTS[name], False, Y, None, work)
+    low = {"none": -float("inf"), "elu": -1.0}.get(name, 0.0)
+    assert Y[0, 0] == float("inf") and Y[1, 0] == low and torch.isnan(Y[2, 0])
+    dA = torch.empty_like(odd)
+    sar.sar_linear_act_bwd(torch.ones_like(odd), A, None, W, ACTS[name], False, None, None, None, dA, work)
+    assert dA[0, 0] == 1 and dA[1, 0] == (1 if name == "none" else 0)
+
+
+def test_relu_takes_its_output_as_what_it_was_taken_of():
+    X, W, b, R = inputs(3000, 64, 96, F32)
+    Y, A = torch.empty(3000, 96, device="cuda"), torch.empty(3000, 96, device="cuda")
+    work, _ = scratch(3000, 64, 96)
+    sar.sar_linear_act_fwd(X, W, b, R, sar.SAR_ACT_RELU, False, Y, A, work)
+    got = []
+    for a in (Y, A):
+        dW, dX = torch.empty_like(W), torch.empty_like(X)
+        sar.sar_linear_act_bwd(R, a, X, W, sar.SAR_ACT_RELU, False, dW, None, dX, None, work)
+        got.append((dW, dX))
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+
+
+def test_no_rows():
+    for dtype in DTYPES:
+        X, Y, W = torch.empty(0, 8, dtype=dtype, device="cuda"), torch.empty(0, 6, dtype=dtype, device="cuda"), torch.ones(8, 6, device="cuda")
+        work, _ = scratch(0, 8, 6)
+        sar.sar_linear_act_fwd(X, W, None, Y, sar.SAR_ACT_GELU, False, Y, None, work)
+        dW, db = torch.full_like(W, 5), torch.full((6,), 5.0, device="cuda")
+        sar.sar_linear_act_bwd(Y, Y, X, W, sar.SAR_ACT_GELU, True, dW, db, X, Y, work)
+        assert (dW == 5).all() and (db == 5).all()
+        sar.sar_linear_act_bwd(Y, Y, X, W, sar.SAR_ACT_GELU, False, dW, db, X, Y, work)
+        assert (dW == 0).all() and (db == 0).all()
+
+
+def test_gradients_by_differences():
+    """The smooth ones, of a sum of the outputs by weights (formula in 64 bits, central differences)."""
+    n, K, F = 3, 4, 5
+    X, W, b, R = inputs(n, K, F, F32)
+    work, _ = scratch(n, K, F)
+    x, w, bb, g = nw.f64(X), nw.f64(W), nw.f64(b), nw.f64(R)
+    step = 1e-5
+    for name in ("gelu", "silu", "none"):
+        Y, A, dW, db, dX = torch.empty_like(R), torch.empty_like(R), torch.empty_like(W), torch.empty_like(b), torch.empty_like(X)
+        sar.sar_linear_act_fwd(X, W, b, None, ACTS[name], False, Y, A, work)
+        sar.sar_linear_act_bwd(R, A, X, W, ACTS[name], False, dW, db, dX, None, work)
+        total = lambda x, w, bb: (act(name, x @ w + bb)[0] * g).sum()
+        for v, got in ((0, dX), (1, dW), (2, db)):
+            args = [x, w, bb]
+            flat = nw.f64(got).ravel()
+            for i in range(flat.size):
+                s = []
+                for sign in (1, -1):
+                    moved = [t.copy() for t in args]
+                    moved[v].flat[i] += sign * step
+                    s.append(total(*moved))
+                assert abs((s[0] - s[1]) / (2 * step) - flat[i]) < 1e-5
