@@ -37,6 +37,9 @@ __device__ inline float lanes_largest(float v) { return over_lanes<L>(v, [](floa
 template <int L>
 __device__ inline float lanes_sum(float v) { return over_lanes<L>(v, [](float a, float b) { return a + b; }); }
 
+__device__ inline float value_in(float v) { return v; }
+__device__ inline float value_in(bf16_t v) { return bf16_to_f32(v); }
+
 // ---- a row's sums
 
 // largest; sum of exp((x - largest) / T); sum of the same times (x - largest) / T
@@ -66,64 +69,88 @@ __device__ inline uint32_t order_of(float x)
 __device__ inline float score_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order); }
 constexpr uint32_t kOrderOfNone = 0x007fffffu;         // that of -inf: such a class, and those behind the last one (0), are none of the top ones
 
-// The top classes of a wavefront's scores, the l-th in lane l; of equal scores the lower class first.
-struct TopList {
-    uint32_t order;
-    int cls;
-};
-__device__ inline TopList no_class() { return {0u, 0x7fffffff}; }
-__device__ inline bool ahead(const TopList& a, const TopList& b) { return a.order > b.order || (a.order == b.order && a.cls < b.cls); }
-__device__ inline TopList from_lane(const TopList& v, int l) { return {(uint32_t)__shfl((int)v.order, l), __shfl(v.cls, l)}; }
-
-// One candidate, the same for all lanes.
-__device__ inline void insert_top(TopList& list, const TopList& c)
+// A score and its class as one number: a higher score is a larger number, of equal scores the lower class.  0: none.
+typedef unsigned long long TopKey;
+__device__ inline TopKey key_of(uint32_t order, int cls) { return (TopKey)order << 32 | (uint32_t)~cls; }
+__device__ inline uint32_t order_in(TopKey k) { return (uint32_t)(k >> 32); }
+__device__ inline int class_in(TopKey k) { return (int)~(uint32_t)k; }
+__device__ inline TopKey key_at(TopKey k, int lane)        // (lane: the same for all)
 {
-    const int lane = threadIdx.x & 63, place = __builtin_popcountll(__ballot(ahead(list, c)));
-    const TopList before = {(uint32_t)__shfl_up((int)list.order, 1), __shfl_up(list.cls, 1)};
+    return (TopKey)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, lane);
+}
+
+// What lane ^ O holds, by vector instructions (through LDS a list's sort was most of a call of few rows).
+template <int O>
+__device__ inline uint32_t lane_xor(uint32_t v)
+{
+    if constexpr (O == 1) return dpp_of<0xB1>(v);
+    else if constexpr (O == 2) return dpp_of<0x4E>(v);
+    else if constexpr (O == 3) return dpp_of<0x1B>(v);
+    else if constexpr (O == 4) return dpp_of<0x1B>(dpp_of<0x141>(v));
+    else if constexpr (O == 8) return dpp_of<0x128>(v);
+    else if constexpr (O == 15) return dpp_of<0x140>(v);
+    else if constexpr (O == 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return threadIdx.x & 16 ? r[0] : r[1];
+    } else if constexpr (O == 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return threadIdx.x & 32 ? r[0] : r[1];
+    } else {
+        static_assert(O == 63, "a distance that the sort has");
+        return lane_xor<32>(lane_xor<16>(lane_xor<15>(v)));
+    }
+}
+template <int O>
+__device__ inline TopKey lane_xor64(TopKey k) { return (TopKey)lane_xor<O>((uint32_t)(k >> 32)) << 32 | lane_xor<O>((uint32_t)k); }
+
+// The top classes of a wavefront's scores, the l-th in lane l.
+// One candidate, the same for all lanes.
+__device__ inline void insert_top(TopKey& list, TopKey c)
+{
+    const int lane = threadIdx.x & 63, place = __builtin_popcountll(__ballot(list > c));
+    const TopKey before = (TopKey)dpp_of<0x138>((uint32_t)(list >> 32)) << 32 | dpp_of<0x138>((uint32_t)list);       // lane - 1
     if (lane > place) list = before;
     if (lane == place) list = c;
 }
+// Larger keys towards lane 0, along distances O, O / 2 ... 1; the other way round in lanes that `rises`.
+template <int O>
+__device__ inline void merge_lanes(TopKey& v, bool rises)
+{
+    const TopKey p = lane_xor64<O>(v);
+    if ((p > v) == (((threadIdx.x & O) == 0) != rises)) v = p;
+    if constexpr (O > 1) merge_lanes<O / 2>(v, rises);
+}
+// One candidate of every lane, sorted.
+__device__ inline void sort_top(TopKey& v)
+{
+    const int lane = threadIdx.x;
+    merge_lanes<1>(v, lane & 2);
+    merge_lanes<2>(v, lane & 4);
+    merge_lanes<4>(v, lane & 8);
+    merge_lanes<8>(v, lane & 16);
+    merge_lanes<16>(v, lane & 32);
+    merge_lanes<32>(v, false);
+}
 // A descending list of candidates.
-__device__ inline void merge_top(TopList& list, const TopList& sorted)
+__device__ inline void merge_top(TopKey& list, TopKey sorted)
 {
-    const int lane = threadIdx.x & 63;
-    const TopList c = from_lane(sorted, 63 - lane);
-    if (ahead(c, list)) list = c;          // (the upper half of both, falling and then rising)
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-        const TopList p = {(uint32_t)__shfl_xor((int)list.order, o), __shfl_xor(list.cls, o)};
-        if (ahead(p, list) == ((lane & o) == 0)) list = p;
-    }
+    const TopKey c = lane_xor64<63>(sorted);
+    if (c > list) list = c;                // (the upper half of both, falling and then rising)
+    merge_lanes<32>(list, false);
 }
-// One candidate of every lane.
-__device__ inline void sort_top(TopList& v)
+// Those of one candidate a lane that are beyond `last`, the k-th of the list.
+__device__ inline void offer_top(TopKey& list, TopKey c, TopKey last)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int size = 2; size <= 64; size <<= 1)
-#pragma unroll
-        for (int o = size >> 1; o >= 1; o >>= 1) {
-            const TopList p = {(uint32_t)__shfl_xor((int)v.order, o), __shfl_xor(v.cls, o)};
-            const bool falls = (lane & size) == 0 || size == 64;
-            if (ahead(p, v) == (((lane & o) == 0) == falls)) v = p;
-        }
-}
-// Those of the candidates that belong among the first k.
-__device__ inline void offer_top(TopList& list, const TopList& c, int k)
-{
-    const TopList last = {(uint32_t)__builtin_amdgcn_readlane((int)list.order, k - 1), __builtin_amdgcn_readlane(list.cls, k - 1)};
-    uint64_t in = __ballot(c.order != 0u && ahead(c, last));
-    if (in == 0) return;
-    if (__builtin_popcountll(in) > 12) {               // (an insertion is a twelfth of a sort and a merge)
-        TopList all = c;
-        sort_top(all);
-        merge_top(list, all);
+    uint64_t in = __ballot(c > last);
+    if (__builtin_popcountll(in) > 8) {                // (a sort and a merge are some eight insertions)
+        sort_top(c);
+        merge_top(list, c);
         return;
     }
     while (in) {
         const int l = __builtin_ctzll(in);
         in &= in - 1;
-        insert_top(list, {(uint32_t)__builtin_amdgcn_readlane((int)c.order, l), __builtin_amdgcn_readlane(c.cls, l)});
+        insert_top(list, key_at(c, l));
     }
 }
 
@@ -175,7 +202,7 @@ struct ClassRows {
     int parts;
     int64_t width;
     RowSums* sums;         // [n, parts]
-    TopList* lists;        // [n, parts, k]
+    TopKey* lists;         // [n, parts, k]
 };
 
 // A row's pieces of `T` in the lanes t of TPR, -inf behind the row's end.
@@ -235,7 +262,7 @@ __global__ __launch_bounds__(kClassThreads) void k_class_wide(ClassRows a, typen
 {
     constexpr int N = Cols<T>::N, U = 4;
     __shared__ RowSums wave_sums[kClassWaves];
-    __shared__ TopList wave_top[Job::kTop ? kClassWaves : 1][kMostTop];
+    __shared__ TopKey wave_top[Job::kTop ? kClassWaves : 1][kMostTop];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int64_t index = blockIdx.x; index < a.n * a.parts; index += gridDim.x) {
         const int64_t row = index / a.parts;
@@ -244,7 +271,7 @@ __global__ __launch_bounds__(kClassThreads) void k_class_wide(ClassRows a, typen
         const int64_t left = (a.n - row) * a.C;
         const int64_t c0 = part * a.width, c1 = min(c0 + a.width, (int64_t)a.C);
         RowSums sums{-__builtin_inff(), 0.f, 0.f};
-        TopList top = no_class();
+        TopKey top = 0;
         for (int64_t at = c0; at < c1; at += kClassThreads * N * U) {
             uint4 raw[U];
             float v[U][N];
@@ -277,21 +304,28 @@ __global__ __launch_bounds__(kClassThreads) void k_class_wide(ClassRows a, typen
                     if constexpr (Job::kEntropy) sums.u = fmaf(e, fmaxf(d, kLeast), sums.u);
                 }
             if constexpr (Job::kTop) {
+                // Every lane's largest score that is among the wavefront's first k so far, one a lane at a time.
                 if (a.k > 0) {
-#pragma unroll 1
-                    for (int i = 0; i < U; ++i) {
-                        const uint32_t last = (uint32_t)__builtin_amdgcn_readlane((int)top.order, a.k - 1);
-                        float x[N];
-                        uint32_t best = 0;
+                    for (;;) {
+                        const TopKey last = key_at(top, a.k - 1);
+                        if (!__any(most > -__builtin_inff() && order_of(most) >= order_in(last))) break;
+                        int cls = 0;
 #pragma unroll
-                        for (int j = 0; j < N; ++j) {
-                            x[j] = i == 0 ? v[0][j] : i == 1 ? v[1][j] : i == 2 ? v[2][j] : v[3][j];
-                            best = max(best, order_of(x[j]));
-                        }
-                        if (!__any(best >= last)) continue;
-                        const int64_t c = at + (i * kClassThreads + (int)threadIdx.x) * N;
+                        for (int i = U - 1; i >= 0; --i)
 #pragma unroll
-                        for (int j = 0; j < N; ++j) offer_top(top, {c + j < c1 ? order_of(x[j]) : 0u, (int)(c + j)}, a.k);
+                            for (int j = N - 1; j >= 0; --j) cls = v[i][j] == most ? i * (kClassThreads * N) + j : cls;
+                        const TopKey c = most > -__builtin_inff() ? key_of(order_of(most), (int)at + (int)threadIdx.x * N + cls) : 0ull;
+                        const bool in = c > last;
+                        if (!__any(in)) break;
+                        offer_top(top, c, last);
+                        most = -__builtin_inff();
+#pragma unroll
+                        for (int i = 0; i < U; ++i)
+#pragma unroll
+                            for (int j = 0; j < N; ++j) {
+                                if (in && cls == i * (kClassThreads * N) + j) v[i][j] = -__builtin_inff();
+                                most = fmaxf(most, v[i][j]);
+                            }
                     }
                 }
             }
@@ -348,10 +382,15 @@ __global__ __launch_bounds__(kClassThreads) void k_class_join(ClassRows a, typen
     move_sums(all, lanes_largest<64>(all.m), a.by, 1.f);
     all.s = lanes_sum<64>(all.s);
     all.u = lanes_sum<64>(all.u) * a.over;
-    TopList top = no_class();
+    TopKey top = 0;
     if constexpr (Job::kTop) {
-        if (a.k > 0) {
-            for (int p = 0; p < a.parts; ++p) merge_top(top, lane < a.k ? a.lists[(row * a.parts + p) * a.k + lane] : no_class());
+        const int count = a.parts * a.k;
+        const TopKey* lists = a.lists + row * count;
+        for (int i = 0; i < count; i += 64) {
+            TopKey c = i + lane < count ? lists[i + lane] : 0ull;
+            sort_top(c);
+            if (i == 0) top = c;
+            else merge_top(top, c);
         }
     }
     Job::template in_wave<T>(a, job, row, all, top);
@@ -359,7 +398,7 @@ __global__ __launch_bounds__(kClassThreads) void k_class_join(ClassRows a, typen
 
 inline size_t class_work_bytes(int64_t n, int C, int k)
 {
-    return (size_t)most_parts(n, C) * (sizeof(RowSums) + (size_t)k * sizeof(TopList) + 8);
+    return (size_t)most_parts(n, C) * (sizeof(RowSums) + (size_t)k * sizeof(TopKey) + 8);
 }
 
 template <typename T, typename Job, int TPR>
@@ -398,7 +437,7 @@ int run_classes(ClassRows a, const typename Job::Args& job, const char* what, vo
         const size_t need = class_work_bytes(a.n, a.C, Job::kTop ? a.k : 0);
         SAR_CHECK_ARG(work && work_bytes >= need, "%s: work has %zu bytes, needs %zu", what, work ? work_bytes : 0, need);
         SAR_CHECK_ARG((reinterpret_cast<uintptr_t>(work) & 15) == 0, "%s: work must be 16-byte aligned", what);
-        a.lists = static_cast<TopList*>(work);
+        a.lists = static_cast<TopKey*>(work);
         a.sums = reinterpret_cast<RowSums*>(a.lists + a.n * a.parts * (Job::kTop ? a.k : 0));
     }
     const unsigned groups = (unsigned)std::min<int64_t>(a.n * a.parts, 1 << 20);
@@ -413,7 +452,7 @@ int run_classes(ClassRows a, const typename Job::Args& job, const char* what, vo
 
 // ---- gradients: tiles of up to kTileValues scores, whole rows where they are short, a piece of one row where they are long
 
-constexpr int kTileValues = 4096, kMostTileRows = 256;
+constexpr int kTileValues = 4096, kWideTile = 8192, kMostTileRows = 256;
 struct ClassTiles {
     int64_t n;
     int C;
@@ -422,10 +461,10 @@ struct ClassTiles {
     int64_t tiles;
     uint32_t magic;        // ceil(2^32 / C): a place in a tile of whole rows by it is its row
 };
-inline ClassTiles class_tiles(int64_t n, int C)
+inline ClassTiles class_tiles(int64_t n, int C, int values = kTileValues, int most_rows = kMostTileRows)
 {
-    ClassTiles t{n, C, 1, std::min(C, kTileValues), 0, 0, 0};
-    t.rows = std::max(1, std::min(kTileValues / C, kMostTileRows));
+    ClassTiles t{n, C, 1, std::min(C, values), 0, 0, 0};
+    t.rows = std::max(1, std::min(values / C, std::min(most_rows, kMostTileRows)));
     if (t.rows >= 8) t.rows = t.rows / 8 * 8;          // (whole pieces)
     t.across = (C + t.width - 1) / t.width;
     t.tiles = (n + t.rows - 1) / t.rows * t.across;

@@ -46,16 +46,13 @@ struct DistillJob {
             if (!q.is(c)) continue;
             const float d = value[j] - top, e = exp_below(d, q.by);
             s += e;
-            if (e != 0.f) w = fmaf(e, (d - (to_f32(static_cast<const T*>(a.X)[row * a.C + c]) - base)) * q.over, w);
+            if (e != 0.f) w = fmaf(e, (d - (value_in(static_cast<const T*>(a.X)[row * a.C + c]) - base)) * q.over, w);
         }
         s = lanes_sum<L>(s);
         w = lanes_sum<L>(w);
         const bool empty = r.m == -__builtin_inff() && r.s == 0.f;
         if (there && t == 0) o.loss[row] = s == 0.f ? 0.f : empty ? __builtin_inff() : w / s - logf(s) + log;
     }
-    static __device__ inline float to_f32(float v) { return v; }
-    static __device__ inline float to_f32(bf16_t v) { return bf16_to_f32(v); }
-
     template <typename T, int TPR, int R>
     static __device__ inline void in_lanes(const ClassRows& a, const Args& o, int64_t row, bool there, int t, const RowSums& r,
                                            const float (&)[R][Cols<T>::N])
@@ -63,7 +60,7 @@ struct DistillJob {
         by_lanes<T, TPR>(a, o, row, there, t, r);
     }
     template <typename T>
-    static __device__ inline void in_wave(const ClassRows& a, const Args& o, int64_t row, const RowSums& r, const TopList&)
+    static __device__ inline void in_wave(const ClassRows& a, const Args& o, int64_t row, const RowSums& r, TopKey)
     {
         by_lanes<T, 64>(a, o, row, true, threadIdx.x & 63, r);
     }
@@ -73,94 +70,186 @@ struct GradArgs {
     ClassTiles t;
     const void* X;
     Teacher teacher;
+    int lanes;             // of a row's list: a power of two, k at least
     const float *lse, *dloss;
     void* dX;
 };
 
-// A row's share of the gradient: s = 2^(x by - lse), times g; the teacher's probabilities are e over.
-struct RowGrad {
-    float lse, g, top, over;
-};
+// Over `lanes` neighbours, a power of two.
+template <typename Op>
+__device__ inline float over_some(float v, int lanes, Op op)
+{
+    if (lanes >= 2) v = op(v, __uint_as_float(lane_xor<1>(__float_as_uint(v))));
+    if (lanes >= 4) v = op(v, __uint_as_float(lane_xor<2>(__float_as_uint(v))));
+    if (lanes >= 8) v = op(v, __uint_as_float(lane_xor<4>(__float_as_uint(v))));
+    if (lanes >= 16) v = op(v, __uint_as_float(lane_xor<8>(__float_as_uint(v))));
+    if (lanes >= 32) v = op(v, __uint_as_float(lane_xor<16>(__float_as_uint(v))));
+    if (lanes >= 64) v = op(v, __uint_as_float(lane_xor<32>(__float_as_uint(v))));
+    return v;
+}
 
-// The gradient of a tile without the teacher's part goes to LDS, the teacher's is subtracted there (a class that is listed twice, twice, in the
-// list's order), and the tile is written as a whole.
+// A row's part of the gradient: s = 2^(x by - lse), times g.
+struct RowGrad {
+    float lse, g;
+};
+// ... and a listed class's, p = g q, of the entry that this lane has: the row's lanes together.
+__device__ inline RowGrad row_grad(const GradArgs& a, int64_t row, bool is, float value, float& p)
+{
+    const Teacher& q = a.teacher;
+    const float top = base_of(over_some(is ? value : -__builtin_inff(), a.lanes, [](float x, float y) { return fmaxf(x, y); }));
+    const float e = is ? exp_below(value - top, q.by) : 0.f;
+    const float s = over_some(e, a.lanes, [](float x, float y) { return x + y; });
+    const float lse = a.lse[row], g = a.dloss[row] * q.over;
+    // no class, or no score: no gradient
+    const bool none = s == 0.f || lse == -__builtin_inff();
+    p = none ? 0.f : e * (g / s);
+    return none ? RowGrad{__builtin_inff(), 0.f} : RowGrad{lse == __builtin_inff() ? __builtin_nanf("") : lse * kLog2e, g};
+}
+__device__ inline float student_part(float x, const RowGrad& r, float by) { return r.g * __builtin_amdgcn_exp2f(fmaf(x, by, -r.lse)); }
+
+// Short rows, several a tile: the student's part goes to LDS, the teacher's is subtracted there, the tile is written as a whole.  Lists are read
+// as they lie, a lane an entry, up to kEntries a thread.
+constexpr int kEntries = 4;
 template <typename T>
 __global__ __launch_bounds__(kClassThreads) void k_distill_bwd(GradArgs a)
 {
-    constexpr int N = Cols<T>::N;
-    __shared__ RowGrad rows[kMostTileRows];
-    __shared__ __attribute__((aligned(16))) float tile[kTileValues + 8];
+    constexpr int N = Cols<T>::N, U = kTileValues / (kClassThreads * N);
+    __shared__ RowGrad rows[kMostTileRows + 1];
+    __shared__ __attribute__((aligned(16))) float tile[kTileValues];
+    __shared__ uint8_t named[kTileValues];
     const Teacher& q = a.teacher;
+    const int j = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes, groups = kClassThreads / a.lanes;
     for (int64_t index = blockIdx.x; index < a.t.tiles; index += gridDim.x) {
-        const int64_t down = index / a.t.across, row0 = down * a.t.rows;
-        const int c0 = (int)(index - down * a.t.across) * a.t.width;
-        const int count = (int)min((int64_t)a.t.rows, a.t.n - row0);
-        const int width = min(a.t.width, a.t.C - c0), values = count * width;
-        __syncthreads();               // (the last tile has been read)
-        if ((int)threadIdx.x < count) {
-            const int64_t row = row0 + threadIdx.x;
-            float most = -__builtin_inff(), s = 0.f;
-            for (int j = 0; j < q.k; ++j)
-                if (q.is(q.index[row * q.k + j])) most = fmaxf(most, q.value[row * q.k + j]);
-            const float top = base_of(most);
-            for (int j = 0; j < q.k; ++j)
-                if (q.is(q.index[row * q.k + j])) s += exp_below(q.value[row * q.k + j] - top, q.by);
-            const float lse = a.lse[row], g = a.dloss[row] * q.over;
-            RowGrad r{lse * kLog2e, g, top, g / s};
-            if (s == 0.f || lse == -__builtin_inff()) r = {__builtin_inff(), 0.f, 0.f, 0.f};       // no class, or no score: no gradient
-            else if (lse == __builtin_inff()) r.lse = __builtin_nanf("");
-            rows[threadIdx.x] = r;
-        }
-        __syncthreads();
-        const int64_t at = row0 * a.t.C + c0;
+        const int64_t row0 = index * a.t.rows;
+        const int C = a.t.C, count = (int)min((int64_t)a.t.rows, a.t.n - row0), values = count * C;
+        const int64_t at = row0 * C;
         const T* X = static_cast<const T*>(a.X) + at;
         T* dX = static_cast<T*>(a.dX) + at;
-        const int64_t left = a.t.n * a.t.C - at;
-        for (int e = threadIdx.x * N; e < values; e += kClassThreads * N) {
-            float x[N];
-            Cols<T>::unpack(Cols<T>::load(X, e, values, left), x);
-            int r = a.t.across > 1 ? 0 : tile_row(a.t, e), c = e - r * width;
-            RowGrad g = rows[r];
+        const int64_t left = a.t.n * C - at;
+        uint4 raw[U];
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                if (e + j < values) {
-                    if (c == width) c = 0, g = rows[++r];
-                    ++c;
-                    x[j] = g.g * __builtin_amdgcn_exp2f(fmaf(x[j], q.by, -g.lse));
-                }
-            }
+        for (int u = 0; u < U; ++u) raw[u] = Cols<T>::load(X, (u * kClassThreads + (int)threadIdx.x) * N, values, left);
+        int place[kEntries];           // of the entry's class in the tile, -1 without one
+        float p[kEntries];
 #pragma unroll
-            for (int j = 0; j < N; j += 4) *reinterpret_cast<float4*>(tile + e + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+        for (int k = 0; k < kEntries; ++k) {
+            const int r = k * groups + group;
+            place[k] = -1;
+            if (k * groups >= count) continue;
+            const int64_t row = row0 + min(r, count - 1), entry = row * q.k + min(j, q.k - 1);
+            const int32_t c = q.k > 0 ? q.index[entry] : -1;
+            const float value = q.k > 0 ? q.value[entry] : 0.f;
+            const bool is = j < q.k && q.is(c);
+            const RowGrad g = row_grad(a, row, is, value, p[k]);
+            if (r >= count) continue;
+            if (j == 0) rows[r] = g;
+            if (!is) continue;
+            place[k] = r * C + c;
+            named[place[k]] = (uint8_t)j;
         }
         __syncthreads();
-        if (a.t.rows > 1) {
-            if ((int)threadIdx.x < count) {
-                const RowGrad g = rows[threadIdx.x];
-                const int64_t row = row0 + threadIdx.x;
-                for (int j = 0; j < q.k; ++j) {
-                    const int32_t c = q.index[row * q.k + j];
-                    if (q.is(c)) tile[threadIdx.x * width + c] -= g.over * exp_below(q.value[row * q.k + j] - g.top, q.by);
+        // A class that is named twice takes the sum of its entries, in the list's order, by the first of them.
+#pragma unroll
+        for (int k = 0; k < kEntries; ++k) {
+            if (k * groups >= count) continue;
+            if (!__any(place[k] >= 0 && named[place[k]] != j)) continue;
+            float sum = 0.f;
+            bool first = true;
+            for (int l = 0; l < q.k; ++l) {
+                const int from = ((int)threadIdx.x & 63 & ~(a.lanes - 1)) + l, other = __shfl(place[k], from);
+                const float more = __shfl(p[k], from);
+                if (other == place[k]) {
+                    sum += more;
+                    first &= l >= j;
                 }
             }
-        } else if (threadIdx.x < 64) {
-            const int j = threadIdx.x;
-            const int32_t c = j < q.k ? q.index[row0 * q.k + j] : -1;
-            const float p = j < q.k ? rows[0].over * exp_below(q.value[row0 * q.k + j] - rows[0].top, q.by) : 0.f;
-            for (uint64_t in = __ballot(q.is(c) && c >= c0 && c < c0 + width); in; in &= in - 1) {
-                const int l = __builtin_ctzll(in);
-                if (j == l) tile[c - c0] -= p;
-                // (the next one may be the same class: behind this one's write)
-                __builtin_amdgcn_wave_barrier();
-                __threadfence_block();
+            p[k] = sum;
+            if (!first) place[k] = -1;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int e = (u * kClassThreads + (int)threadIdx.x) * N;
+            if (e >= values) continue;
+            float x[N];
+            Cols<T>::unpack(raw[u], x);
+            const int r = tile_row(a.t, e), end = (r + 1) * C - e;
+            if (C >= N) {
+                const RowGrad g0 = rows[r], g1 = rows[r + 1];          // (behind the last row: for values that are not stored)
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = student_part(x[i], i < end ? g0 : g1, q.by);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = student_part(x[i], rows[min(tile_row(a.t, e + i), count - 1)], q.by);
             }
+#pragma unroll
+            for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(tile + e + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
         }
         __syncthreads();
-        for (int e = threadIdx.x * N; e < values; e += kClassThreads * N) {
+#pragma unroll
+        for (int k = 0; k < kEntries; ++k)
+            if (place[k] >= 0) tile[place[k]] -= p[k];
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int e = (u * kClassThreads + (int)threadIdx.x) * N;
+            if (e >= values) continue;
             float x[N];
 #pragma unroll
-            for (int j = 0; j < N; ++j) x[j] = tile[e + j];
+            for (int i = 0; i < N; i += 4) {
+                const float4 v = *reinterpret_cast<const float4*>(tile + e + i);
+                x[i] = v.x, x[i + 1] = v.y, x[i + 2] = v.z, x[i + 3] = v.w;
+            }
             Cols<T>::store(dX, e, values, x);
         }
+    }
+}
+
+// Long rows, a piece of one a workgroup: the student's part is written, then the few listed classes of the piece once more, with the teacher's.
+template <typename T>
+__global__ __launch_bounds__(kClassThreads) void k_distill_bwd_wide(GradArgs a)
+{
+    constexpr int N = Cols<T>::N, U = kWideTile / (kClassThreads * N);
+    const Teacher& q = a.teacher;
+    const int j = threadIdx.x & 63;
+    for (int64_t index = blockIdx.x; index < a.t.tiles; index += gridDim.x) {
+        const int64_t row = index / a.t.across;
+        const int c0 = (int)(index - row * a.t.across) * a.t.width, width = min(a.t.width, a.t.C - c0);
+        const int64_t at = row * a.t.C + c0, left = a.t.n * a.t.C - at;
+        const T* X = static_cast<const T*>(a.X) + at;
+        T* dX = static_cast<T*>(a.dX) + at;
+        uint4 raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = Cols<T>::load(X, (u * kClassThreads + (int)threadIdx.x) * N, width, left);
+        const int32_t c = j < q.k ? q.index[row * q.k + j] : -1;
+        const float value = j < q.k ? q.value[row * q.k + j] : 0.f;
+        const bool in = q.is(c) && c >= c0 && c < c0 + width;
+        float own = 0.f, p;
+        if (threadIdx.x < 64 && in) own = value_in(X[c - c0]);
+        const RowGrad g = row_grad(a, row, q.is(c), value, p);
+        own = student_part(own, g, q.by);
+        // (of scores in place: they have been read before any is written)
+        asm volatile("s_waitcnt vmcnt(0)" : "+v"(own)::"memory");
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int e = (u * kClassThreads + (int)threadIdx.x) * N;
+            float x[N];
+            Cols<T>::unpack(raw[u], x);
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = student_part(x[i], g, q.by);
+            Cols<T>::store(dX, e, width, x);
+        }
+        __syncthreads();
+        if (threadIdx.x >= 64) continue;
+        // a class that is named twice: the sum of its entries, in the list's order, by the first of them
+        float sum = 0.f;
+        int first = 64;
+        for (uint64_t left_in = __ballot(in); left_in; left_in &= left_in - 1) {
+            const int l = __builtin_ctzll(left_in);
+            const float more = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(p), l));
+            if (__builtin_amdgcn_readlane(c, l) == c) sum += more, first = min(first, l);
+        }
+        if (first == j) dX[c - c0] = from_f32<T>(own - sum);
     }
 }
 
@@ -205,9 +294,15 @@ extern "C" int sar_distill_bwd(const void* X, int k, const float* top_value, con
     SAR_TRY(check_temperature(temperature));
     if (n == 0) return SAR_OK;
     SAR_CHECK_ARG(X && lse && dloss && dX && (k == 0 || (top_value && top_index)), "null pointer (X, top_value, top_index, lse, dloss, dX)");
-    const GradArgs a{class_tiles(n, C), X, teacher_of(top_value, top_index, k, C, temperature), lse, dloss, dX};
+    int lanes = 1;
+    while (lanes < k) lanes <<= 1;
+    const bool wide = C > kTileValues / 2;
+    const GradArgs a{wide ? class_tiles(n, C, kWideTile, 1) : class_tiles(n, C, kTileValues, kEntries * kClassThreads / lanes), X,
+                     teacher_of(top_value, top_index, k, C, temperature), wide ? 64 : lanes, lse, dloss, dX};
     const unsigned groups = (unsigned)std::min<int64_t>(a.t.tiles, 1 << 20);
-    if (dtype == SAR_F32) k_distill_bwd<float><<<groups, kClassThreads, 0, as_stream(stream)>>>(a);
+    if (wide && dtype == SAR_F32) k_distill_bwd_wide<float><<<groups, kClassThreads, 0, as_stream(stream)>>>(a);
+    else if (wide) k_distill_bwd_wide<bf16_t><<<groups, kClassThreads, 0, as_stream(stream)>>>(a);
+    else if (dtype == SAR_F32) k_distill_bwd<float><<<groups, kClassThreads, 0, as_stream(stream)>>>(a);
     else k_distill_bwd<bf16_t><<<groups, kClassThreads, 0, as_stream(stream)>>>(a);
     SAR_LAUNCH_CHECK();
     return SAR_OK;

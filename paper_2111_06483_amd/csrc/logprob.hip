@@ -30,14 +30,11 @@ struct LogprobJob {
             float v = 0.f;
             if ((uint32_t)c < (uint32_t)a.C) {
                 const T x = static_cast<const T*>(a.X)[row * a.C + c];
-                v = none ? -__builtin_inff() : (to_f32(x) - base_of(r.m)) - log;
+                v = none ? -__builtin_inff() : (value_in(x) - base_of(r.m)) - log;
             }
             o.logp[row] = v;
         }
     }
-    static __device__ inline float to_f32(float v) { return v; }
-    static __device__ inline float to_f32(bf16_t v) { return bf16_to_f32(v); }
-
     template <typename T, int TPR, int R>
     static __device__ inline void in_lanes(const ClassRows& a, const Args& o, int64_t row, bool there, int t, const RowSums& r,
                                            const float (&v)[R][Cols<T>::N])
@@ -95,15 +92,15 @@ struct LogprobJob {
     }
 
     template <typename T>
-    static __device__ inline void in_wave(const ClassRows& a, const Args& o, int64_t row, const RowSums& r, const TopList& top)
+    static __device__ inline void in_wave(const ClassRows& a, const Args& o, int64_t row, const RowSums& r, TopKey top)
     {
         const int lane = threadIdx.x & 63;
         const float log = logf(r.s);
         if (lane == 0) results<T>(a, o, row, r, log);
         if (lane < a.k) {
-            const bool is = top.order > kOrderOfNone;
-            o.value[row * a.k + lane] = is ? (score_of(top.order) - base_of(r.m)) - log : -__builtin_inff();
-            o.index[row * a.k + lane] = is ? top.cls : -1;
+            const bool is = top != 0;
+            o.value[row * a.k + lane] = is ? (score_of(order_in(top)) - base_of(r.m)) - log : -__builtin_inff();
+            o.index[row * a.k + lane] = is ? class_in(top) : -1;
         }
     }
 };
@@ -133,31 +130,37 @@ __global__ __launch_bounds__(kClassThreads) void k_logprob_bwd(GradArgs a)
     constexpr int N = Cols<T>::N;
     __shared__ RowGrad rows[kMostTileRows + 1];
     __shared__ int labels[kMostTileRows + 1];
+    constexpr int U = kTileValues / (kClassThreads * N);
     for (int64_t index = blockIdx.x; index < a.t.tiles; index += gridDim.x) {
         const int64_t down = index / a.t.across, row0 = down * a.t.rows;
         const int c0 = (int)(index - down * a.t.across) * a.t.width;
         const int count = (int)min((int64_t)a.t.rows, a.t.n - row0);
+        const int width = min(a.t.width, a.t.C - c0), values = count * width;
+        const int64_t at = row0 * a.t.C + c0;
+        const T* X = static_cast<const T*>(a.X) + at;
+        T* dX = static_cast<T*>(a.dX) + at;
+        const int64_t left = a.t.n * a.t.C - at;
+        uint4 raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = Cols<T>::load(X, (u * kClassThreads + (int)threadIdx.x) * N, values, left);
         __syncthreads();               // (the last tile's rows have been read)
         if ((int)threadIdx.x < count) {
             const int64_t row = row0 + threadIdx.x;
             const int32_t c = a.label ? a.label[row] : -1;
             const bool has = (uint32_t)c < (uint32_t)a.t.C;
             RowGrad r{a.lse[row], has && a.dlogp ? a.dlogp[row] : 0.f, a.dentropy ? a.dentropy[row] : 0.f, a.dentropy ? a.entropy[row] : 0.f};
-            int at = has ? c - c0 : -1;
             if (r.lse == -__builtin_inff()) r = {__builtin_inff(), 0.f, 0.f, 0.f};        // nothing but -inf: no gradient
             else if (r.lse == __builtin_inff()) r.lse = __builtin_nanf("");
-            rows[threadIdx.x] = r, labels[threadIdx.x] = at;
+            rows[threadIdx.x] = r, labels[threadIdx.x] = has ? c - c0 : -1;
         }
         __syncthreads();
-        const int width = min(a.t.width, a.t.C - c0), values = count * width;
-        const int64_t at = row0 * a.t.C + c0;
-        const T* X = static_cast<const T*>(a.X) + at;
-        T* dX = static_cast<T*>(a.dX) + at;
-        const int64_t left = a.t.n * a.t.C - at;
-        for (int e = threadIdx.x * N; e < values; e += kClassThreads * N) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int e = (u * kClassThreads + (int)threadIdx.x) * N;
+            if (e >= values) continue;
             float x[N];
-            Cols<T>::unpack(Cols<T>::load(X, e, values, left), x);
-            int r = a.t.across > 1 ? 0 : tile_row(a.t, e);
+            Cols<T>::unpack(raw[u], x);
+            int r = a.t.rows == 1 ? 0 : tile_row(a.t, e);
             int c = e - r * width;
             if constexpr (ROWS == 1) {
                 const RowGrad g = rows[r];
@@ -165,6 +168,7 @@ __global__ __launch_bounds__(kClassThreads) void k_logprob_bwd(GradArgs a)
 #pragma unroll
                 for (int j = 0; j < N; ++j) x[j] = grad_of(x[j], g) + (j == label ? g.g : 0.f);
             } else if constexpr (ROWS == 2) {
+                // (behind the last row: whatever is there, for values that are not stored)
                 const RowGrad g0 = rows[r], g1 = rows[r + 1];
                 const int end = width - c, l0 = labels[r] - c, l1 = labels[r + 1] + end;
 #pragma unroll
