@@ -161,99 +161,112 @@ __device__ inline void exact_tiles(const RowsArgs<E>& a, int t, const T* row, in
     }
 }
 
-// The bias, residual and activation of a wavefront's tiles, which are stored.  Residuals are read as the results are stored, four rows at a time (whole
-// lines of a tile's columns).
+// The bias, residual and activation of a wavefront's tiles, which are stored: four rows of a group of column tiles at a time, from their residuals (which
+// are under way some steps before) to the results, so that few values are in work at once beside the sums.
 template <typename T, int IL>
 struct __attribute__((packed, aligned(sizeof(T)))) Neighbours {
-    T x[IL];
+    uint32_t x[IL * sizeof(T) / 4];
+    __device__ inline void values(float (&v)[IL]) const
+    {
+#pragma unroll
+        for (int j = 0; j < IL; ++j) {
+            if constexpr (sizeof(T) == 4) v[j] = __uint_as_float(x[j]);
+            else v[j] = __uint_as_float(j % 2 ? x[j / 2] & 0xffff0000u : x[j / 2] << 16);
+        }
+    }
+    __device__ inline void set(const float (&v)[IL])
+    {
+#pragma unroll
+        for (int j = 0; j < IL * (int)sizeof(T) / 4; ++j) {
+            if constexpr (sizeof(T) == 4) x[j] = __float_as_uint(v[j]);
+            else x[j] = pack2_bf16(v[2 * j], v[2 * j + 1]);
+        }
+    }
 };
 template <typename T, int NT, int NW>
 __device__ SAR_INLINE inline void finish_tiles(const Epilogue& e, void* out, int N, int64_t r0, int64_t end, int n0, int first, int lane, float16_t (&acc)[NW])
 {
-    constexpr int IL = Share<T, NT>::IL;
+    constexpr int IL = Share<T, NT>::IL, kSteps = NW / IL * 4, kAhead = sizeof(T) == 4 ? 2 : 4;
     using V = Neighbours<T, IL>;
-    const int h = lane >> 5;
+    // (addresses are the tile's, the same for all lanes, and a lane's place in it: by 64 bits each they were a hundred registers)
+    const int h = lane >> 5, row0 = __builtin_amdgcn_readfirstlane((int)r0), rows = __builtin_amdgcn_readfirstlane((int)min(end - r0, (int64_t)32));
+    const int64_t tile = (int64_t)row0 * N;
     auto column = [&](int g) SAR_INLINE { return n0 + Share<T, NT>::column_of(first + g * IL, lane & 31); };
-    auto row = [&](int r) SAR_INLINE { return r0 + 8 * (r / 4) + 4 * h + r % 4; };
-    auto add_residual = [&](int g, int q) SAR_INLINE {
-        const int n = column(g);
-        if (n >= N) return;
-        float v[4][IL];
+    auto row = [&](int r) SAR_INLINE { return 8 * (r / 4) + 4 * h + r % 4; };
+    V res[kAhead][4];
+    auto fetch = [&](int s) SAR_INLINE {
+        const int n = column(s / 4);
+        const T* from = static_cast<const T*>(e.res) + tile;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const T* from = static_cast<const T*>(e.res) + min(row(4 * q + k), end - 1) * N + n;
+            const uint32_t at = (uint32_t)min(row(4 * (s % 4) + k), rows - 1) * (uint32_t)N;
             if (n + IL <= N) {
-                const V w = *reinterpret_cast<const V*>(from);
-#pragma unroll
-                for (int j = 0; j < IL; ++j) v[k][j] = value_of(w.x[j]);
+                res[s % kAhead][k] = *reinterpret_cast<const V*>(from + (at + (uint32_t)n));
             } else {
+                float v[IL];
 #pragma unroll
-                for (int j = 0; j < IL; ++j) v[k][j] = n + j < N ? value_of(from[j]) : 0.f;
+                for (int j = 0; j < IL; ++j) v[j] = value_of(from[at + (uint32_t)min(n + j, N - 1)]);
+                res[s % kAhead][k].set(v);
             }
         }
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-            for (int j = 0; j < IL; ++j) acc[g * IL + j][4 * q + k] += v[k][j];
     };
-    auto store = [&](void* to, int g, int q) SAR_INLINE {
+    auto store = [&](void* to, int g, int q, const float (&v)[4][IL]) SAR_INLINE {
         const int n = column(g);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int64_t i = row(4 * q + k);
-            if (i >= end || n >= N) continue;
-            T* p = static_cast<T*>(to) + i * N + n;
+            const int i = row(4 * q + k);
+            if (i >= rows || n >= N) continue;
+            T* p = static_cast<T*>(to) + tile + ((uint32_t)i * (uint32_t)N + (uint32_t)n);
             if (n + IL <= N) {
                 V w;
-                if constexpr (sizeof(T) == 4) {
-#pragma unroll
-                    for (int j = 0; j < IL; ++j) w.x[j] = acc[g * IL + j][4 * q + k];
-                } else {
-#pragma unroll
-                    for (int j = 0; j < IL; j += 2) {
-                        const uint32_t two = pack2_bf16(acc[g * IL + j][4 * q + k], acc[g * IL + j + 1][4 * q + k]);
-                        w.x[j].bits = (uint16_t)two, w.x[j + 1].bits = (uint16_t)(two >> 16);
-                    }
-                }
+                w.set(v[k]);
                 *reinterpret_cast<V*>(p) = w;
             } else {
 #pragma unroll
                 for (int j = 0; j < IL; ++j)
-                    if (n + j < N) p[j] = from_f32<T>(acc[g * IL + j][4 * q + k]);
+                    if (n + j < N) p[j] = from_f32<T>(v[k][j]);
             }
         }
     };
+    if (e.res) {
 #pragma unroll
-    for (int g = 0; g < NW / IL; ++g) {
-        const int n = column(g);
-        if (e.bias) {
+        for (int s = 0; s < kAhead - 1; ++s) fetch(s);
+    }
+    float bias[IL];
 #pragma unroll
-            for (int j = 0; j < IL; ++j) {
-                const float b = n + j < N ? e.bias[n + j] : 0.f;
+    for (int s = 0; s < kSteps; ++s) {
+        const int g = s / 4, q = s % 4;
+        if (e.res && s + kAhead - 1 < kSteps) fetch(s + kAhead - 1);
+        if (q == 0) {
+            const int n = column(g);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[g * IL + j][r] += b;
+            for (int j = 0; j < IL; ++j) bias[j] = e.bias && n + j < N ? e.bias[n + j] : 0.f;
+        }
+        float v[4][IL];
+        auto add_residual = [&]() SAR_INLINE {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                float r[IL];
+                res[s % kAhead][k].values(r);
+#pragma unroll
+                for (int j = 0; j < IL; ++j) v[k][j] += r[j];
             }
-        }
-        if (e.res && !e.after) {
+        };
 #pragma unroll
-            for (int q = 0; q < 4; ++q) add_residual(g, q);
-        }
-        if (e.pre) {
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) store(e.pre, g, q);
-        }
+            for (int j = 0; j < IL; ++j) v[k][j] = acc[g * IL + j][4 * q + k] + bias[j];
+        if (e.res && !e.after) add_residual();
+        if (e.pre) store(e.pre, g, q, v);
         with_act(e.act, [&](auto act) SAR_INLINE {
 #pragma unroll
-            for (int j = 0; j < IL; ++j)
+            for (int k = 0; k < 4; ++k)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[g * IL + j][r] = act_of<decltype(act)::value>(acc[g * IL + j][r]);
+                for (int j = 0; j < IL; ++j) v[k][j] = act_of<decltype(act)::value>(v[k][j]);
         });
-        if (e.res && e.after) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) add_residual(g, q);
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) store(out, g, q);
+        if (e.res && e.after) add_residual();
+        store(out, g, q, v);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
@@ -569,7 +582,7 @@ size_t list_bytes(int64_t n, int T) { return (size_t)(most_tiles(n, T) + 1) * si
 template <typename T, bool TRANS, typename E = NoEpilogue>
 int rows_product(const void* A, const float* W, const Types& types, void* out, int K, int F, void* work, hipStream_t st, const E& e = {})
 {
-    const int C = TRANS ? F : K, N = TRANS ? K : F, NT = tiles_of(types.n, N);
+    const int C = TRANS ? F : K, N = TRANS ? K : F, NT = E::kAny ? std::min(4, tiles_of(types.n, N)) : tiles_of(types.n, N);
     if (few_blocks(types, N)) return few_product(sizeof(T) == 4 ? SAR_F32 : SAR_BF16, TRANS, {A, W, out, types, C, N, K, F}, e, st);
     const int chunks = (C + kChunk<T> - 1) / kChunk<T>, blocks = (N + 32 * NT - 1) / (32 * NT);
     const int64_t most = most_tiles(types.n, types.T);
