@@ -4,7 +4,7 @@
 //
 // Forward: the kernels of linear_typed_rows.h and linear_typed_few.hip with one type; bias, residual and activation meet the sums in registers, in 32
 // bits, and are rounded once.
-#include "linear_typed_rows.h"
+#include "linear_kept.h"
 
 namespace sar {
 
@@ -99,6 +99,20 @@ int groups_of(int dtype, int64_t n, int F)
     return (int)std::max<int64_t>(1, std::min<int64_t>((n + rows - 1) / rows, std::max(1, std::min(kActGroups, (1 << 22) / F))));
 }
 
+// Whether a product's operand is kept: rows enough for the copies of it to pay.
+template <typename T>
+bool kept(int64_t n, int C)
+{
+    return n >= 65536 && fits_kept<T>(C);
+}
+
+template <typename T>
+int forward(const void* X, const float* W, int64_t n, void* Y, int K, int F, void* work, hipStream_t st, const Epilogue& e)
+{
+    if (kept<T>(n, K)) return run_kept<T, false>(X, W, n, Y, K, F, work, st, e, NoPrologue{});
+    return rows_product<T, false>(X, W, Types{nullptr, 1, n}, Y, K, F, work, st, e);
+}
+
 size_t rounded(size_t b) { return (b + 255) / 256 * 256; }
 size_t partial_bytes(int64_t n, int F)
 {
@@ -180,10 +194,8 @@ extern "C" int sar_linear_act_fwd(const void* X, const float* W, const float* bi
                   "linear with activation: Y, A must not alias X, W or each other");
     SAR_CHECK_ARG(Y == res || apart(Y, out, res, out), "linear with activation: Y overlaps res, and is not res");
     SAR_CHECK_ARG((A == res && !res_after) || !A || apart(A, out, res, out), "linear with activation: A overlaps res");
-    const Types types{nullptr, 1, n};
     const Epilogue e{bias, res, A, act, res_after};
-    return dtype == SAR_F32 ? rows_product<float, false>(X, W, types, Y, K, F, work, as_stream(stream), e)
-                            : rows_product<bf16_t, false>(X, W, types, Y, K, F, work, as_stream(stream), e);
+    return dtype == SAR_F32 ? forward<float>(X, W, n, Y, K, F, work, as_stream(stream), e) : forward<bf16_t>(X, W, n, Y, K, F, work, as_stream(stream), e);
 }
 
 extern "C" int sar_linear_act_bwd(const void* dY, const void* A, const void* X, const float* W, int act, int accumulate, float* dW, float* db, void* dX,

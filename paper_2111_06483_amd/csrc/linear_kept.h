@@ -1,0 +1,358 @@
+// Many rows times one small operand that a compute unit keeps whole: linear_act.hip says when.
+//
+// The operand's columns are dealt to workgroups in blocks whose pieces (k_typed_lay) fit LDS beside the rows'; a workgroup copies its block once and its
+// eight wavefronts then go their own ways, with no barrier: each takes every so-manyth 32 rows, brings them by whole lines, all of the next ones while it
+// multiplies these (a chunk ahead, memory was waited for half of the time), hands them to the lanes that multiply them through LDS of its own, and finishes
+// and stores its results while the others multiply.
+#pragma once
+
+#include "linear_typed_rows.h"
+
+namespace sar {
+
+namespace {
+
+constexpr int kKeptWaves = 8, kKeptThreads = kKeptWaves * 64;
+constexpr size_t kKeptLds = 160 * 1024;
+
+// What is done to a row's values before they are multiplied: nothing, or dA = dY act'(A) is formed of them.
+struct NoPrologue {
+    static constexpr bool kAny = false;
+};
+struct ActPrologue {
+    static constexpr bool kAny = true;
+    const void* pre;       // [n, C]: what the activation was taken of
+    void* formed;          // [n, C] or null: the rows as they are multiplied
+    int act;
+};
+
+template <typename E, typename P>
+struct KeptArgs {
+    RowsArgs<E> rows;
+    P prologue;
+    int64_t n;
+};
+
+template <typename T>
+__device__ SAR_INLINE inline void form_piece(int act, uint4& d, const uint4& pre)
+{
+    constexpr int N = Cols<T>::N;
+    float v[N], a[N];
+    Cols<T>::unpack(d, v);
+    Cols<T>::unpack(pre, a);
+    with_act(act, [&](auto which) SAR_INLINE {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = act_grad<decltype(which)::value>(v[j], a[j]);
+    });
+    d = Cols<T>::round(v);
+}
+
+// A wavefront's tiles once more by the fp32 matrix instruction, from the operands themselves (this lane's row: i).
+template <typename T, typename SH, bool TRANS, typename E, typename P>
+__device__ inline void exact_rows(const KeptArgs<E, P>& g, int64_t i, int n0, float16_t (&acc)[SH::NW])
+{
+    const RowsArgs<E>& a = g.rows;
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const T* row = static_cast<const T*>(a.A) + i * a.C;
+#pragma unroll
+    for (int t = 0; t < SH::NW; ++t) acc[t] = float16_t{};
+    for (int k = 0; k < a.C; k += 2) {
+        const bool in = k + h < a.C;
+        float x = in ? value_of(row[k + h]) : 0.f;
+        if constexpr (P::kAny) {
+            if (in) {
+                const float pre = value_of(static_cast<const T*>(g.prologue.pre)[i * a.C + k + h]);
+                with_act(g.prologue.act, [&](auto act) { x = act_grad<decltype(act)::value>(x, pre); });
+                x = value_of(from_f32<T>(x));
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < SH::NW; ++t) {
+            const int n = n0 + SH::column_of(t, lane & 31);
+            float w = 0.f;
+            if (in && n < a.N) w = TRANS ? a.W[(int64_t)n * a.F + k + h] : a.W[(int64_t)(k + h) * a.F + n];
+            acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w, acc[t], 0, 0, 0);
+        }
+    }
+}
+
+// The residuals of step s as fetch_residual has them, without a branch: what lies behind the last column or row is read from them.
+template <typename T, typename SH>
+__device__ SAR_INLINE inline void residual_of(const Epilogue& e, const Place<SH>& at, int s, Neighbours<T, SH::IL> (&out)[4])
+{
+    const T* from = static_cast<const T*>(e.res) + at.tile();
+    const uint32_t n = (uint32_t)min(at.column(s / 4), at.N - SH::IL);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        out[k] = *within_tile<const Neighbours<T, SH::IL>>(from, ((uint32_t)min(at.row(4 * (s % 4) + k), at.rows - 1) * (uint32_t)at.N + n) * (uint32_t)sizeof(T));
+}
+
+// A wavefront's results, from the sums to memory.  Loads and stores are waited for in the order in which they were sent, by counting those sent since, and
+// what a branch may have sent does not count: so that the next rows, which are under way, need not be waited for behind these results' stores,
+// whole tiles (FULL) are stored without a branch, and the bias is in registers from the beginning.
+template <typename T, typename SH, bool FULL, bool RES, typename E, int NW, int KNOWN>
+__device__ SAR_INLINE inline void finish_kept(const E& e, void* out, const Place<SH>& at, const float (&bias)[NW], float16_t (&acc)[NW],
+                                              Neighbours<T, SH::IL> (&res)[KNOWN][4])
+{
+    constexpr int IL = SH::IL, kSteps = NW / IL * 4;
+    const int64_t tile = at.tile();
+    auto store = [&](void* to, int s, const float (&v)[4][IL]) SAR_INLINE {
+        const int n = at.column(s / 4);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int i = at.row(4 * (s % 4) + k);
+            T* const p = within_tile<T>(static_cast<T*>(to) + tile, ((uint32_t)i * (uint32_t)at.N + (uint32_t)n) * (uint32_t)sizeof(T));
+            if (FULL || (i < at.rows && n + IL <= at.N)) {
+                Neighbours<T, IL> w;
+                w.set(v[k]);
+                *reinterpret_cast<Neighbours<T, IL>*>(p) = w;
+            } else if (i < at.rows) {
+#pragma unroll
+                for (int j = 0; j < IL; ++j)
+                    if (n + j < at.N) p[j] = from_f32<T>(v[k][j]);
+            }
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        float v[4][IL];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < IL; ++j) v[k][j] = acc[s / 4 * IL + j][4 * (s % 4) + k];
+        if constexpr (E::kAny) {
+            if constexpr (RES && !FULL) fetch_residual<T, SH>(e, at, s, res[s]);
+            auto add_residual = [&]() SAR_INLINE {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float r[IL];
+                    res[s][k].values(r);
+#pragma unroll
+                    for (int j = 0; j < IL; ++j) v[k][j] += r[j];
+                }
+            };
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < IL; ++j) v[k][j] += bias[s / 4 * IL + j];
+            if constexpr (RES) {
+                if (!e.after) add_residual();
+            }
+            if (e.pre) store(e.pre, s, v);
+            with_act(e.act, [&](auto act) SAR_INLINE {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int j = 0; j < IL; ++j) v[k][j] = act_of<decltype(act)::value>(v[k][j]);
+            });
+            if constexpr (RES) {
+                if (e.after) add_residual();
+            }
+        }
+        store(out, s, v);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// CHUNKS: of the contraction; RES: a residual.
+template <typename T, int NT, int CHUNKS, bool TRANS, bool RES, typename E, typename P>
+__global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E, P> g)
+{
+    using Sh = WholeShare<T, NT>;
+    const RowsArgs<E>& a = g.rows;
+    constexpr int PC = Mode<T>::kPieces, S = Mode<T>::kSteps, CH = kChunk<T>, N = Cols<T>::N, SB = Mode<T>::kStage, kSP = PC == 3 ? 3 : 1;
+    constexpr int kRaw = 4, kFrags = kStageFrags<T, NT>, kStages = CHUNKS * (S / SB);      // kRaw: 16-byte pieces of 32 rows' chunk that a lane brings
+    extern __shared__ __attribute__((aligned(16))) uint4 lds[];          // [kStages][kFrags][64] of B, [kKeptWaves][32][8] of rows
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    // workgroups of the same rows and other columns are neighbours on one XCD
+    const int turn = blockIdx.x / 8, block = turn % a.blocks, group = turn / a.blocks * 8 + blockIdx.x % 8, groups = gridDim.x / a.blocks;
+    const int n0 = block * (32 * NT);
+    const uint4* from = a.B + (int64_t)block * kStages * (kFrags * 64);
+    for (int f = wave; f < kStages * kFrags; f += kKeptWaves)
+        __builtin_amdgcn_global_load_lds((GlobalSrc*)(from + f * 64 + lane), (LdsPtr*)(lds + f * 64), 16, 0, 0);
+    float bias[NT] = {};
+    if constexpr (E::kAny) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int n = n0 + Sh::column_of(i, lane & 31);
+            if (a.epilogue.bias && n < a.N) bias[i] = a.epilogue.bias[n];
+        }
+    }
+
+    const int tiles = (int)((g.n + 31) / 32), step = groups * kKeptWaves;
+    uint4 raw[CHUNKS][kRaw], pre[P::kAny ? CHUNKS : 1][kRaw];
+    auto fetch = [&](int tile, int chunk) SAR_INLINE {
+        int own = lane;
+        asm volatile("" : "+v"(own));
+        const int c = chunk * CH + (own & 7) * N;
+        const int64_t r0 = (int64_t)tile * 32;
+        const uint32_t most = (uint32_t)min(g.n - 1 - r0, (int64_t)31);
+#pragma unroll
+        for (int k = 0; k < kRaw; ++k) {
+            const uint32_t row = min((uint32_t)(8 * k + (own >> 3)), most) * (uint32_t)a.C;
+            auto piece = [&](const void* p) SAR_INLINE {
+                const T* rows = static_cast<const T*>(p) + r0 * a.C;
+                // (rows of less than a piece: one chunk, value by value)
+                if (CHUNKS > 1 || a.C >= N) return load16(within_tile<const T>(rows, (row + (uint32_t)min(c, a.C - N)) * (uint32_t)sizeof(T)));
+                return Cols<T>::load(rows + row, c, a.C, a.C);
+            };
+            raw[chunk][k] = piece(a.A);
+            if constexpr (P::kAny) pre[chunk][k] = piece(g.prologue.pre);
+        }
+    };
+    uint4* const rows = lds + kStages * kFrags * 64 + wave * 256;
+    // a chunk, from the lanes that brought it to those that multiply it
+    auto hand_over = [&](int tile, int chunk, uint4 (&x)[kRaw]) SAR_INLINE {
+        const int c = chunk * CH + (lane & 7) * N;
+        if (chunk == CHUNKS - 1 && c + N > a.C) {
+            auto cut = [&](uint4& v) SAR_INLINE {
+                if (c >= a.C) v = make_uint4(0u, 0u, 0u, 0u);
+                else if (a.C >= N) v = front_of_piece<T>(v, a.C - c);
+            };
+#pragma unroll
+            for (int k = 0; k < kRaw; ++k) {
+                cut(raw[chunk][k]);
+                if constexpr (P::kAny) cut(pre[chunk][k]);
+            }
+        }
+        if constexpr (P::kAny) {
+#pragma unroll
+            for (int k = 0; k < kRaw; ++k) form_piece<T>(g.prologue.act, raw[chunk][k], pre[chunk][k]);
+            if (g.prologue.formed && block == 0) {
+#pragma unroll
+                for (int k = 0; k < kRaw; ++k) {
+                    const int64_t i = (int64_t)tile * 32 + 8 * k + (lane >> 3);
+                    float v[N];
+                    Cols<T>::unpack(raw[chunk][k], v);
+                    if (i < g.n) Cols<T>::store(static_cast<T*>(g.prologue.formed) + i * a.C, c, a.C, v);
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kRaw; ++k) rows[(8 * k + (lane >> 3)) * 8 + ((lane & 7) ^ (lane >> 3))] = raw[chunk][k];
+#pragma unroll
+        for (int k = 0; k < kRaw; ++k) x[k] = rows[(lane & 31) * 8 + ((h * kRaw + k) ^ (lane & 7))];
+    };
+
+    int tile = group * kKeptWaves + wave;
+    if (tile < tiles) {
+#pragma unroll
+        for (int chunk = 0; chunk < CHUNKS; ++chunk) fetch(tile, chunk);
+    }
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    // residuals read with the rows, and those that wait until there are registers for them
+    constexpr int kSteps = NT / Sh::IL * 4, kEarly = sizeof(T) == 2 ? kSteps : kSteps / 2;
+    for (; tile < tiles; tile += step) {
+        float16_t acc[NT];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) acc[i] = float16_t{};
+        const int64_t r0 = (int64_t)tile * 32;
+        // (places are worked out where they are used: carried through the loop they are dozens of registers)
+        auto place = [&]() SAR_INLINE {
+            int own = lane;
+            asm volatile("" : "+v"(own));
+            return Place<Sh>(r0, g.n, a.N, n0, 0, own);
+        };
+        Neighbours<T, Sh::IL> res[kSteps][4];
+        float sign = kDown * kDown;
+#pragma unroll
+        for (int chunk = 0; chunk < CHUNKS; ++chunk) {
+            uint4 p[S / SB][1][SB][kSP], x[kRaw];
+            hand_over(tile, chunk, x);
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                if constexpr (PC == 3) {
+                    float v[8] = {__uint_as_float(x[2 * s].x), __uint_as_float(x[2 * s].y), __uint_as_float(x[2 * s].z), __uint_as_float(x[2 * s].w),
+                                  __uint_as_float(x[2 * s + 1].x), __uint_as_float(x[2 * s + 1].y), __uint_as_float(x[2 * s + 1].z),
+                                  __uint_as_float(x[2 * s + 1].w)};
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] *= kUp;
+                    split8(v, p[s / SB][0][s % SB]);
+                } else {
+                    p[s / SB][0][s % SB][0] = x[s];
+                }
+            }
+            if constexpr (RES) {
+                if (chunk == 0) {
+                    const Place<Sh> at = place();
+#pragma unroll
+                    for (int s = 0; s < kEarly; ++s) residual_of<T, Sh>(a.epilogue, at, s, res[s]);
+                }
+            }
+            fetch(min(tile + step, tiles - 1), chunk);         // (the last one's are not looked at)
+#pragma unroll
+            for (int part = 0; part < S / SB; ++part) {
+                float16_t(&sums)[1][NT] = reinterpret_cast<float16_t(&)[1][NT]>(acc);
+                multiply_stage<T, NT, 1, NT>(lds + (chunk * (S / SB) + part) * (kFrags * 64) + lane, p[part], sign, sums);
+            }
+            sign = -sign;
+        }
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) odd |= not_finite(acc[i]);
+        if (__any(odd)) exact_rows<T, Sh, TRANS>(g, min(r0 + (lane & 31), g.n - 1), n0, acc);
+        const Place<Sh> at = place();
+        if constexpr (RES) {
+#pragma unroll
+            for (int s = kEarly; s < kSteps; ++s) residual_of<T, Sh>(a.epilogue, at, s, res[s]);
+        }
+        if (at.rows == 32 && n0 + 32 * NT <= a.N) {
+            finish_kept<T, Sh, true, RES>(a.epilogue, a.out, at, bias, acc, res);
+        } else {
+            finish_kept<T, Sh, false, RES>(a.epilogue, a.out, at, bias, acc, res);
+            __builtin_amdgcn_s_waitcnt(0);
+        }
+    }
+}
+
+// Four column tiles, eight wavefronts' rows: the chunks of a contraction that fit beside them.
+constexpr int kKeptTiles = 4;
+template <typename T>
+constexpr int kMostKeptChunks = (int)((kKeptLds - kKeptWaves * 4096) / (Mode<T>::kSteps * Mode<T>::kPieces * kKeptTiles * 1024));
+template <typename T>
+bool fits_kept(int C) { return (C + kChunk<T> - 1) / kChunk<T> <= kMostKeptChunks<T>; }
+
+// out [n, N] = (A [n, C], by the prologue) B; TRANS: B = W^T.  work: lay_bytes.
+template <typename T, int CHUNKS, bool TRANS, typename E, typename P>
+int run_kept_chunks(const void* A, const float* W, int64_t n, void* out, int K, int F, void* work, hipStream_t st, const E& e, const P& prologue)
+{
+    constexpr int NT = kKeptTiles;
+    const int C = TRANS ? F : K, N = TRANS ? K : F, blocks = (N + 32 * NT - 1) / (32 * NT);
+    uint4* const pieces = static_cast<uint4*>(work);
+    const int64_t units = (int64_t)blocks * CHUNKS * Mode<T>::kSteps * NT * 64, lay = (units + 255) / 256;
+    const LayArgs l{W, pieces, 1, K, F, C, N, CHUNKS, blocks, Types{nullptr, 1, n}, nullptr, 0, (unsigned)lay};
+    k_typed_lay<T, NT, TRANS, WholeShare<T, NT>><<<(unsigned)lay, 256, 0, st>>>(l);
+    SAR_LAUNCH_CHECK();
+    const KeptArgs<E, P> a{{A, pieces, W, out, nullptr, C, N, CHUNKS, blocks, K, F, e}, prologue, n};
+    constexpr size_t shared = ((size_t)CHUNKS * Mode<T>::kSteps * Mode<T>::kPieces * NT + kKeptWaves * 4) * 1024;
+    const int turns = std::max(1, (shared > kKeptLds / 2 ? 32 : 64) / blocks);
+    auto launch = [&](auto* fn) {
+        SAR_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)shared));
+        fn<<<(unsigned)(8 * blocks * turns), kKeptThreads, shared, st>>>(a);
+        SAR_LAUNCH_CHECK();
+        return (int)SAR_OK;
+    };
+    if constexpr (E::kAny) {
+        if (e.res) return launch(k_rows_kept<T, NT, CHUNKS, TRANS, true, E, P>);
+    }
+    return launch(k_rows_kept<T, NT, CHUNKS, TRANS, false, E, P>);
+}
+
+template <typename T, bool TRANS, typename E, typename P>
+int run_kept(const void* A, const float* W, int64_t n, void* out, int K, int F, void* work, hipStream_t st, const E& e, const P& p)
+{
+    static_assert(kMostKeptChunks<T> == (sizeof(T) == 4 ? 5 : 4), "the cases below");
+    switch (((TRANS ? F : K) + kChunk<T> - 1) / kChunk<T>) {
+    case 1: return run_kept_chunks<T, 1, TRANS>(A, W, n, out, K, F, work, st, e, p);
+    case 2: return run_kept_chunks<T, 2, TRANS>(A, W, n, out, K, F, work, st, e, p);
+    case 3: return run_kept_chunks<T, 3, TRANS>(A, W, n, out, K, F, work, st, e, p);
+    case 4: return run_kept_chunks<T, 4, TRANS>(A, W, n, out, K, F, work, st, e, p);
+    default:
+        if constexpr (sizeof(T) == 4) return run_kept_chunks<T, 5, TRANS>(A, W, n, out, K, F, work, st, e, p);
+        return fail(SAR_ERR_UNSUPPORTED, "a contraction of %d values is not kept", TRANS ? F : K);
+    }
+}
+
+}  // namespace
+}  // namespace sar

@@ -39,6 +39,13 @@ struct Share {
     static __host__ __device__ constexpr int column_of(int i, int c) { return i / IL * (32 * IL) + c * IL + i % IL; }
 };
 
+// A wavefront that has all columns of its rows (linear_kept.h).
+template <typename T, int NT>
+struct WholeShare {
+    static constexpr int MR = 1, WC = 1, WR = 1, NW = NT, IL = NT < 4 ? NT : 4;
+    static __host__ __device__ constexpr int column_of(int i, int c) { return i / IL * (32 * IL) + c * IL + i % IL; }
+};
+
 // ---- the small operand's pieces
 //
 // out [T, column blocks, chunks, steps, pieces, NT, 64 lanes] of 16 bytes: eight consecutive contraction values of a column.
@@ -78,7 +85,7 @@ __device__ inline void list_rows(const LayArgs& a, int t)
     if (t == a.T - 1 && threadIdx.x == 0) a.list[0] = make_int4((int)min(before + mine, a.most), 0, 0, 0);
 }
 
-template <typename T, int NT, bool TRANS>
+template <typename T, int NT, bool TRANS, typename SH = Share<T, NT>>
 __global__ __launch_bounds__(256) void k_typed_lay(LayArgs a)
 {
     constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps;
@@ -93,7 +100,7 @@ __global__ __launch_bounds__(256) void k_typed_lay(LayArgs a)
     const int block = (int)(rest % a.blocks);
     const int t = (int)(rest / a.blocks);
     if (t >= a.T) return;
-    const int n = block * (32 * NT) + Share<T, NT>::column_of(tile, lane & 31);
+    const int n = block * (32 * NT) + SH::column_of(tile, lane & 31);
     const int c = chunk * kChunk<T> + (lane >> 5) * (kChunk<T> / 2) + s * 8;
     const float* W = a.W + (int64_t)t * a.K * a.F;
     float v[8];
@@ -136,10 +143,11 @@ struct RowsArgs {
 };
 
 // A wavefront's tiles of 32 rows once more by the fp32 matrix instruction; column tiles from `first` on of the block that begins at n0.
-template <typename T, int NT, bool TRANS, typename E>
-__device__ inline void exact_tiles(const RowsArgs<E>& a, int t, const T* row, int n0, int first, float16_t (&acc)[Share<T, NT>::NW])
+template <typename T, typename SH, bool TRANS, typename E>
+__device__ inline void exact_tiles(const RowsArgs<E>& a, int t, int64_t i, int n0, int first, float16_t (&acc)[SH::NW])
 {
-    constexpr int NW = Share<T, NT>::NW;
+    constexpr int NW = SH::NW;
+    const T* row = static_cast<const T*>(a.A) + i * a.C;
     const int lane = threadIdx.x & 63, c = lane & 31, h = lane >> 5;
     const float* W = a.W + (int64_t)t * a.K * a.F;
 #pragma unroll
@@ -153,7 +161,7 @@ __device__ inline void exact_tiles(const RowsArgs<E>& a, int t, const T* row, in
         }
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
-            const int n = n0 + Share<T, NT>::column_of(first + i, c);
+            const int n = n0 + SH::column_of(first + i, c);
             float w = 0.f;
             if (in && n < a.N) w = TRANS ? W[(int64_t)n * a.F + k + h] : W[(int64_t)(k + h) * a.F + n];
             acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w, acc[i], 0, 0, 0);
@@ -183,40 +191,63 @@ struct __attribute__((packed, aligned(sizeof(T)))) Neighbours {
         }
     }
 };
-template <typename T, int NT, int NW>
-__device__ SAR_INLINE inline void finish_tiles(const Epilogue& e, void* out, int N, int64_t r0, int64_t end, int n0, int first, int lane, float16_t (&acc)[NW])
+// Where a wavefront's 32 rows lie: the first one, how many there are, the column tiles.  (Addresses are the tile's, the same for all lanes, and a lane's place
+// in it: by 64 bits each they were a hundred registers.)
+template <typename SH>
+struct Place {
+    int row0, rows, N, n0, first, lane;
+    __device__ SAR_INLINE inline Place(int64_t r0, int64_t end, int N, int n0, int first, int lane)
+        : row0(__builtin_amdgcn_readfirstlane((int)r0)), rows(__builtin_amdgcn_readfirstlane((int)min(end - r0, (int64_t)32))), N(N), n0(n0), first(first), lane(lane)
+    {
+    }
+    __device__ SAR_INLINE inline int64_t tile() const { return (int64_t)row0 * N; }
+    __device__ SAR_INLINE inline int column(int g) const { return n0 + SH::column_of(first + g * SH::IL, lane & 31); }
+    __device__ SAR_INLINE inline int row(int r) const { return 8 * (r / 4) + 4 * (lane >> 5) + r % 4; }
+};
+// (a byte's place within 32 rows fits 32 bits; said so, it is added to the tile's address by the access itself)
+template <typename V, typename T>
+__device__ SAR_INLINE inline V* within_tile(T* base, uint32_t bytes)
 {
-    constexpr int IL = Share<T, NT>::IL, kSteps = NW / IL * 4, kAhead = sizeof(T) == 4 ? 2 : 4;
-    using V = Neighbours<T, IL>;
-    // (addresses are the tile's, the same for all lanes, and a lane's place in it: by 64 bits each they were a hundred registers)
-    const int h = lane >> 5, row0 = __builtin_amdgcn_readfirstlane((int)r0), rows = __builtin_amdgcn_readfirstlane((int)min(end - r0, (int64_t)32));
-    const int64_t tile = (int64_t)row0 * N;
-    auto column = [&](int g) SAR_INLINE { return n0 + Share<T, NT>::column_of(first + g * IL, lane & 31); };
-    auto row = [&](int r) SAR_INLINE { return 8 * (r / 4) + 4 * h + r % 4; };
-    V res[kAhead][4];
-    auto fetch = [&](int s) SAR_INLINE {
-        const int n = column(s / 4);
-        const T* from = static_cast<const T*>(e.res) + tile;
+    return reinterpret_cast<V*>(reinterpret_cast<uintptr_t>(base) + bytes);
+}
+// The residuals of step s: four rows of a group of column tiles.
+template <typename T, typename SH>
+__device__ SAR_INLINE inline void fetch_residual(const Epilogue& e, const Place<SH>& at, int s, Neighbours<T, SH::IL> (&out)[4])
+{
+    constexpr int IL = SH::IL;
+    const int n = at.column(s / 4);
+    const T* from = static_cast<const T*>(e.res) + at.tile();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t at = (uint32_t)min(row(4 * (s % 4) + k), rows - 1) * (uint32_t)N;
-            if (n + IL <= N) {
-                res[s % kAhead][k] = *reinterpret_cast<const V*>(from + (at + (uint32_t)n));
-            } else {
-                float v[IL];
+    for (int k = 0; k < 4; ++k) {
+        const uint32_t place = (uint32_t)min(at.row(4 * (s % 4) + k), at.rows - 1) * (uint32_t)at.N;
+        if (n + IL <= at.N) {
+            out[k] = *within_tile<const Neighbours<T, IL>>(from, (place + (uint32_t)n) * (uint32_t)sizeof(T));
+        } else {
+            float v[IL];
 #pragma unroll
-                for (int j = 0; j < IL; ++j) v[j] = value_of(from[at + (uint32_t)min(n + j, N - 1)]);
-                res[s % kAhead][k].set(v);
-            }
+            for (int j = 0; j < IL; ++j) v[j] = value_of(from[place + (uint32_t)min(n + j, at.N - 1)]);
+            out[k].set(v);
         }
-    };
+    }
+}
+template <typename T, typename SH, int NW>
+__device__ SAR_INLINE inline void finish_tiles(const Epilogue& e, void* out, const Place<SH>& at, float16_t (&acc)[NW])
+{
+    constexpr int IL = SH::IL, kSteps = NW / IL * 4, kAhead = sizeof(T) == 4 ? 2 : 4;
+    using V = Neighbours<T, IL>;
+    const int N = at.N, rows = at.rows;
+    const int64_t tile = at.tile();
+    auto column = [&](int g) SAR_INLINE { return at.column(g); };
+    auto row = [&](int r) SAR_INLINE { return at.row(r); };
+    V res[kAhead][4];
+    auto fetch = [&](int s) SAR_INLINE { fetch_residual<T, SH>(e, at, s, res[s % kAhead]); };
     auto store = [&](void* to, int g, int q, const float (&v)[4][IL]) SAR_INLINE {
         const int n = column(g);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int i = row(4 * q + k);
             if (i >= rows || n >= N) continue;
-            T* p = static_cast<T*>(to) + tile + ((uint32_t)i * (uint32_t)N + (uint32_t)n);
+            T* p = within_tile<T>(static_cast<T*>(to) + tile, ((uint32_t)i * (uint32_t)N + (uint32_t)n) * (uint32_t)sizeof(T));
             if (n + IL <= N) {
                 V w;
                 w.set(v[k]);
@@ -271,22 +302,22 @@ __device__ SAR_INLINE inline void finish_tiles(const Epilogue& e, void* out, int
 }
 
 // A wavefront's tiles of rows r0..r0+31 (up to `end`), column tiles from `first` on.
-template <typename T, int NT, bool TRANS, int NW, typename E>
-__device__ SAR_INLINE inline void store_tiles(const RowsArgs<E>& a, int t, int64_t r0, int64_t end, int first, float16_t (&acc)[NW])
+template <typename T, typename SH, bool TRANS, int NW, typename E>
+__device__ SAR_INLINE inline void store_tiles(const RowsArgs<E>& a, int t, int64_t r0, int64_t end, int n0, int first, float16_t (&acc)[NW])
 {
-    constexpr int IL = Share<T, NT>::IL;
+    constexpr int IL = SH::IL;
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));         // (as above: nothing of this is carried through the products)
-    const int h = lane >> 5, n0 = blockIdx.y * (32 * NT);
+    const int h = lane >> 5;
     if (r0 >= end) return;
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < NW; ++i) odd |= not_finite(acc[i]);
     if (__any(odd))
-        exact_tiles<T, NT, TRANS>(a, t, static_cast<const T*>(a.A) + min(r0 + (lane & 31), end - 1) * a.C, n0, first, acc);
+        exact_tiles<T, SH, TRANS>(a, t, min(r0 + (lane & 31), end - 1), n0, first, acc);
 
     if constexpr (E::kAny) {
-        finish_tiles<T, NT, NW>(a.epilogue, a.out, a.N, r0, end, n0, first, lane, acc);
+        finish_tiles<T, SH, NW>(a.epilogue, a.out, Place<SH>(r0, end, a.N, n0, first, lane), acc);
         return;
     }
     // lane holds columns of its place; register r holds row 8*(r/4) + 4*h + r%4
@@ -297,7 +328,7 @@ __device__ SAR_INLINE inline void store_tiles(const RowsArgs<E>& a, int t, int64
         T* out = static_cast<T*>(a.out) + i * a.N;
 #pragma unroll
         for (int g = 0; g < NW / IL; ++g) {
-            const int n = n0 + Share<T, NT>::column_of(first + g * IL, lane & 31);
+            const int n = n0 + SH::column_of(first + g * IL, lane & 31);
             const float16_t* v = &acc[g * IL];
             if (n + IL <= a.N) {
                 if constexpr (sizeof(T) == 4) {
@@ -536,7 +567,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a
         tile = after;
 #pragma unroll
         for (int m = 0; m < MR; ++m)
-            store_tiles<T, NT, TRANS>(a, done.t, done.first + (wr * MR + m) * 32, done.end, wc * NW, acc[m]);
+            store_tiles<T, Sh, TRANS>(a, done.t, done.first + (wr * MR + m) * 32, done.end, blockIdx.y * (32 * NT), wc * NW, acc[m]);
     }
 }
 
@@ -582,7 +613,7 @@ size_t list_bytes(int64_t n, int T) { return (size_t)(most_tiles(n, T) + 1) * si
 template <typename T, bool TRANS, typename E = NoEpilogue>
 int rows_product(const void* A, const float* W, const Types& types, void* out, int K, int F, void* work, hipStream_t st, const E& e = {})
 {
-    const int C = TRANS ? F : K, N = TRANS ? K : F, NT = E::kAny ? std::min(4, tiles_of(types.n, N)) : tiles_of(types.n, N);
+    const int C = TRANS ? F : K, N = TRANS ? K : F, NT = tiles_of(types.n, N);
     if (few_blocks(types, N)) return few_product(sizeof(T) == 4 ? SAR_F32 : SAR_BF16, TRANS, {A, W, out, types, C, N, K, F}, e, st);
     const int chunks = (C + kChunk<T> - 1) / kChunk<T>, blocks = (N + 32 * NT - 1) / (32 * NT);
     const int64_t most = most_tiles(types.n, types.T);
