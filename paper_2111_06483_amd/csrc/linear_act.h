@@ -1,7 +1,7 @@
 // What is done to a row of X W before it is stored: bias, residual, activation (linear_act.hip); the activations and their derivatives.
 #pragma once
 
-#include "linear_common.h"
+#include "packed.h"
 #include "sar_internal.h"
 
 namespace sar {
@@ -94,6 +94,40 @@ __device__ __attribute__((always_inline)) inline void with_act(int act, F&& f)
     case SAR_ACT_ELU: f(std::integral_constant<int, SAR_ACT_ELU>{}); break;
     default: break;
     }
+}
+
+// What is done to a row's values before they are multiplied: nothing, or dA = dY act'(A) is formed of them.
+struct NoPrologue {
+    static constexpr bool kAny = false;
+};
+struct ActPrologue {
+    static constexpr bool kAny = true;
+    const void* pre;       // [n, C]: what the activation was taken of
+    void* formed;          // [n, C] or null: the rows as they are multiplied
+    int act;
+};
+
+template <typename T>
+__device__ __attribute__((always_inline)) inline void form_piece(int act, uint4& d, const uint4& pre)
+{
+    constexpr int N = Cols<T>::N;
+    float v[N], a[N];
+    Cols<T>::unpack(d, v);
+    Cols<T>::unpack(pre, a);
+    with_act(act, [&](auto which) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = act_grad<decltype(which)::value>(v[j], a[j]);
+    });
+    d = Cols<T>::round(v);
+}
+
+// ... of one value, at place `at` of the rows.
+template <typename T>
+__device__ inline float formed_value(const ActPrologue& p, float d, int64_t at)
+{
+    const float a = value_of(static_cast<const T*>(p.pre)[at]);
+    with_act(p.act, [&](auto which) { d = act_grad<decltype(which)::value>(d, a); });
+    return value_of(from_f32<T>(d));
 }
 
 // One value of the product, column n, place `at` of the rows.

@@ -100,16 +100,16 @@ int groups_of(int dtype, int64_t n, int F)
 }
 
 // Whether a product's operand is kept: rows enough for the copies of it to pay.
-template <typename T>
-bool kept(int64_t n, int C)
+template <typename T, typename P>
+bool kept(int64_t n, int C, int N)
 {
-    return n >= 65536 && fits_kept<T>(C);
+    return n >= 65536 && N >= 64 && fits_kept<T, P>(C);
 }
 
 template <typename T>
 int forward(const void* X, const float* W, int64_t n, void* Y, int K, int F, void* work, hipStream_t st, const Epilogue& e)
 {
-    if (kept<T>(n, K)) return run_kept<T, false>(X, W, n, Y, K, F, work, st, e, NoPrologue{});
+    if (kept<T, NoPrologue>(n, K, F)) return run_kept<T, false>(X, W, n, Y, K, F, work, st, e, NoPrologue{});
     return rows_product<T, false>(X, W, Types{nullptr, 1, n}, Y, K, F, work, st, e);
 }
 
@@ -146,11 +146,14 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
     float* const partial = reinterpret_cast<float*>(base + rounded(products));
     char* const high = reinterpret_cast<char*>(partial) + partial_bytes(n, F);
     const bool formed = act != SAR_ACT_NONE;
-    void* rows = !formed ? const_cast<void*>(dY) : dA ? dA : high;
+    const Types types{nullptr, 1, n};
+    // dA, where dW reads it
+    void* rows = !formed ? const_cast<void*>(dY) : dA ? dA : dW || (dX && few_blocks(types, K)) ? high : nullptr;
     void* low = formed && dW && sizeof(T) == 2 ? high + rounded((size_t)n * F * sizeof(T)) : nullptr;
-    if (n > 0 && (formed || db || dA)) {
+    const bool within = formed && dX && n > 0 && !few_blocks(types, K);       // the product for dX forms dA
+    if (n > 0 && ((rows && !within && formed) || low || db || (dA && !formed))) {
         const int lanes = lanes_of(dtype, F), groups = groups_of(dtype, n, F);
-        const ActBwdArgs a{dY, A, formed ? rows : dA, low, db ? partial : nullptr, n, F, act, lanes};
+        const ActBwdArgs a{dY, A, formed ? (within ? nullptr : rows) : dA, low, db ? partial : nullptr, n, F, act, lanes};
         const int across = (F + lanes * Cols<T>::N - 1) / (lanes * Cols<T>::N);
         k_act_bwd<T><<<dim3(groups, across), kActThreads, 0, st>>>(a);
         SAR_LAUNCH_CHECK();
@@ -159,12 +162,20 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
         k_act_sum<<<(F + 31) / 32, 1024, 0, st>>>(partial, n > 0 ? groups_of(dtype, n, F) : 0, F, accumulate, db);
         SAR_LAUNCH_CHECK();
     }
-    const Types types{nullptr, 1, n};
+    if (dX && n > 0) {
+        if (within) {
+            const ActPrologue q{A, rows, act};
+            if (kept<T, ActPrologue>(n, F, K)) SAR_TRY((run_kept<T, true>(dY, W, n, dX, K, F, work, st, NoEpilogue{}, q)));
+            else SAR_TRY((rows_product<T, true>(dY, W, types, dX, K, F, work, st, NoEpilogue{}, q)));
+        } else {
+            if (kept<T, NoPrologue>(n, F, K)) SAR_TRY((run_kept<T, true>(rows, W, n, dX, K, F, work, st, NoEpilogue{}, NoPrologue{})));
+            else SAR_TRY((rows_product<T, true>(rows, W, types, dX, K, F, work, st)));
+        }
+    }
     if (dW) {
         SAR_TRY(typed_dw(dtype, {X, nullptr, nullptr, rows, dW, types, K, F, accumulate, static_cast<float*>(work)}, st));
         if (low && n > 0) SAR_TRY(typed_dw(dtype, {X, nullptr, nullptr, low, dW, types, K, F, 1, static_cast<float*>(work)}, st));
     }
-    if (dX && n > 0) return rows_product<T, true>(rows, W, types, dX, K, F, work, st);
     return SAR_OK;
 }
 

@@ -15,66 +15,12 @@ namespace {
 constexpr int kKeptWaves = 8, kKeptThreads = kKeptWaves * 64;
 constexpr size_t kKeptLds = 160 * 1024;
 
-// What is done to a row's values before they are multiplied: nothing, or dA = dY act'(A) is formed of them.
-struct NoPrologue {
-    static constexpr bool kAny = false;
-};
-struct ActPrologue {
-    static constexpr bool kAny = true;
-    const void* pre;       // [n, C]: what the activation was taken of
-    void* formed;          // [n, C] or null: the rows as they are multiplied
-    int act;
-};
-
 template <typename E, typename P>
 struct KeptArgs {
     RowsArgs<E> rows;
     P prologue;
     int64_t n;
 };
-
-template <typename T>
-__device__ SAR_INLINE inline void form_piece(int act, uint4& d, const uint4& pre)
-{
-    constexpr int N = Cols<T>::N;
-    float v[N], a[N];
-    Cols<T>::unpack(d, v);
-    Cols<T>::unpack(pre, a);
-    with_act(act, [&](auto which) SAR_INLINE {
-#pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = act_grad<decltype(which)::value>(v[j], a[j]);
-    });
-    d = Cols<T>::round(v);
-}
-
-// A wavefront's tiles once more by the fp32 matrix instruction, from the operands themselves (this lane's row: i).
-template <typename T, typename SH, bool TRANS, typename E, typename P>
-__device__ inline void exact_rows(const KeptArgs<E, P>& g, int64_t i, int n0, float16_t (&acc)[SH::NW])
-{
-    const RowsArgs<E>& a = g.rows;
-    const int lane = threadIdx.x & 63, h = lane >> 5;
-    const T* row = static_cast<const T*>(a.A) + i * a.C;
-#pragma unroll
-    for (int t = 0; t < SH::NW; ++t) acc[t] = float16_t{};
-    for (int k = 0; k < a.C; k += 2) {
-        const bool in = k + h < a.C;
-        float x = in ? value_of(row[k + h]) : 0.f;
-        if constexpr (P::kAny) {
-            if (in) {
-                const float pre = value_of(static_cast<const T*>(g.prologue.pre)[i * a.C + k + h]);
-                with_act(g.prologue.act, [&](auto act) { x = act_grad<decltype(act)::value>(x, pre); });
-                x = value_of(from_f32<T>(x));
-            }
-        }
-#pragma unroll
-        for (int t = 0; t < SH::NW; ++t) {
-            const int n = n0 + SH::column_of(t, lane & 31);
-            float w = 0.f;
-            if (in && n < a.N) w = TRANS ? a.W[(int64_t)n * a.F + k + h] : a.W[(int64_t)(k + h) * a.F + n];
-            acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w, acc[t], 0, 0, 0);
-        }
-    }
-}
 
 // The residuals of step s as fetch_residual has them, without a branch: what lies behind the last column or row is read from them.
 template <typename T, typename SH>
@@ -219,12 +165,20 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E, P> g)
 #pragma unroll
             for (int k = 0; k < kRaw; ++k) form_piece<T>(g.prologue.act, raw[chunk][k], pre[chunk][k]);
             if (g.prologue.formed && block == 0) {
+                // (of whole tiles without a branch, as the results are stored)
+                T* const to = static_cast<T*>(g.prologue.formed) + (int64_t)tile * 32 * a.C;
+                if ((chunk + 1) * CH <= a.C && (int64_t)tile * 32 + 32 <= g.n) {
 #pragma unroll
-                for (int k = 0; k < kRaw; ++k) {
-                    const int64_t i = (int64_t)tile * 32 + 8 * k + (lane >> 3);
-                    float v[N];
-                    Cols<T>::unpack(raw[chunk][k], v);
-                    if (i < g.n) Cols<T>::store(static_cast<T*>(g.prologue.formed) + i * a.C, c, a.C, v);
+                    for (int k = 0; k < kRaw; ++k)
+                        store16(within_tile<T>(to, ((uint32_t)(8 * k + (lane >> 3)) * (uint32_t)a.C + (uint32_t)c) * (uint32_t)sizeof(T)), raw[chunk][k]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < kRaw; ++k) {
+                        float v[N];
+                        Cols<T>::unpack(raw[chunk][k], v);
+                        if ((int64_t)tile * 32 + 8 * k + (lane >> 3) < g.n) Cols<T>::store(to + (8 * k + (lane >> 3)) * a.C, c, a.C, v);
+                    }
+                    __builtin_amdgcn_s_waitcnt(0);
                 }
             }
         }
@@ -291,7 +245,7 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E, P> g)
         bool odd = false;
 #pragma unroll
         for (int i = 0; i < NT; ++i) odd |= not_finite(acc[i]);
-        if (__any(odd)) exact_rows<T, Sh, TRANS>(g, min(r0 + (lane & 31), g.n - 1), n0, acc);
+        if (__any(odd)) exact_tiles<T, Sh, TRANS>(a, g.prologue, 0, min(r0 + (lane & 31), g.n - 1), n0, 0, acc);
         const Place<Sh> at = place();
         if constexpr (RES) {
 #pragma unroll
@@ -306,12 +260,17 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E, P> g)
     }
 }
 
-// Four column tiles, eight wavefronts' rows: the chunks of a contraction that fit beside them.
+// Four column tiles, eight wavefronts' rows: the chunks of a contraction that fit beside them (bf16), or that a lane's registers take (fp32; with what
+// dA is formed of fewer).
 constexpr int kKeptTiles = 4;
-template <typename T>
-constexpr int kMostKeptChunks = (int)((kKeptLds - kKeptWaves * 4096) / (Mode<T>::kSteps * Mode<T>::kPieces * kKeptTiles * 1024));
-template <typename T>
-bool fits_kept(int C) { return (C + kChunk<T> - 1) / kChunk<T> <= kMostKeptChunks<T>; }
+template <typename T, typename P>
+constexpr int kMostKeptChunks = sizeof(T) == 2 || !P::kAny ? 4 : 3;
+template <typename T, typename P>
+bool fits_kept(int C)
+{
+    static_assert((kMostKeptChunks<T, P> * Mode<T>::kSteps * Mode<T>::kPieces * kKeptTiles + kKeptWaves * 4) * 1024 <= kKeptLds, "LDS of a compute unit");
+    return (C + kChunk<T> - 1) / kChunk<T> <= kMostKeptChunks<T, P>;
+}
 
 // out [n, N] = (A [n, C], by the prologue) B; TRANS: B = W^T.  work: lay_bytes.
 template <typename T, int CHUNKS, bool TRANS, typename E, typename P>
@@ -342,14 +301,12 @@ int run_kept_chunks(const void* A, const float* W, int64_t n, void* out, int K, 
 template <typename T, bool TRANS, typename E, typename P>
 int run_kept(const void* A, const float* W, int64_t n, void* out, int K, int F, void* work, hipStream_t st, const E& e, const P& p)
 {
-    static_assert(kMostKeptChunks<T> == (sizeof(T) == 4 ? 5 : 4), "the cases below");
     switch (((TRANS ? F : K) + kChunk<T> - 1) / kChunk<T>) {
     case 1: return run_kept_chunks<T, 1, TRANS>(A, W, n, out, K, F, work, st, e, p);
     case 2: return run_kept_chunks<T, 2, TRANS>(A, W, n, out, K, F, work, st, e, p);
     case 3: return run_kept_chunks<T, 3, TRANS>(A, W, n, out, K, F, work, st, e, p);
-    case 4: return run_kept_chunks<T, 4, TRANS>(A, W, n, out, K, F, work, st, e, p);
     default:
-        if constexpr (sizeof(T) == 4) return run_kept_chunks<T, 5, TRANS>(A, W, n, out, K, F, work, st, e, p);
+        if constexpr (kMostKeptChunks<T, P> == 4) return run_kept_chunks<T, 4, TRANS>(A, W, n, out, K, F, work, st, e, p);
         return fail(SAR_ERR_UNSUPPORTED, "a contraction of %d values is not kept", TRANS ? F : K);
     }
 }

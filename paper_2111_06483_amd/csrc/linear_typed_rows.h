@@ -143,8 +143,8 @@ struct RowsArgs {
 };
 
 // A wavefront's tiles of 32 rows once more by the fp32 matrix instruction; column tiles from `first` on of the block that begins at n0.
-template <typename T, typename SH, bool TRANS, typename E>
-__device__ inline void exact_tiles(const RowsArgs<E>& a, int t, int64_t i, int n0, int first, float16_t (&acc)[SH::NW])
+template <typename T, typename SH, bool TRANS, typename E, typename P>
+__device__ inline void exact_tiles(const RowsArgs<E>& a, const P& prologue, int t, int64_t i, int n0, int first, float16_t (&acc)[SH::NW])
 {
     constexpr int NW = SH::NW;
     const T* row = static_cast<const T*>(a.A) + i * a.C;
@@ -156,8 +156,8 @@ __device__ inline void exact_tiles(const RowsArgs<E>& a, int t, int64_t i, int n
         const bool in = k + h < a.C;
         float x = 0.f;
         if (in) {
-            if constexpr (sizeof(T) == 4) x = row[k + h];
-            else x = bf16_to_f32(row[k + h]);
+            x = value_of(row[k + h]);
+            if constexpr (P::kAny) x = formed_value<T>(prologue, x, i * a.C + k + h);
         }
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
@@ -302,8 +302,8 @@ __device__ SAR_INLINE inline void finish_tiles(const Epilogue& e, void* out, con
 }
 
 // A wavefront's tiles of rows r0..r0+31 (up to `end`), column tiles from `first` on.
-template <typename T, typename SH, bool TRANS, int NW, typename E>
-__device__ SAR_INLINE inline void store_tiles(const RowsArgs<E>& a, int t, int64_t r0, int64_t end, int n0, int first, float16_t (&acc)[NW])
+template <typename T, typename SH, bool TRANS, int NW, typename E, typename P>
+__device__ SAR_INLINE inline void store_tiles(const RowsArgs<E>& a, const P& prologue, int t, int64_t r0, int64_t end, int n0, int first, float16_t (&acc)[NW])
 {
     constexpr int IL = SH::IL;
     int lane = threadIdx.x & 63;
@@ -314,7 +314,7 @@ __device__ SAR_INLINE inline void store_tiles(const RowsArgs<E>& a, int t, int64
 #pragma unroll
     for (int i = 0; i < NW; ++i) odd |= not_finite(acc[i]);
     if (__any(odd))
-        exact_tiles<T, SH, TRANS>(a, t, min(r0 + (lane & 31), end - 1), n0, first, acc);
+        exact_tiles<T, SH, TRANS>(a, prologue, t, min(r0 + (lane & 31), end - 1), n0, first, acc);
 
     if constexpr (E::kAny) {
         finish_tiles<T, SH, NW>(a.epilogue, a.out, Place<SH>(r0, end, a.N, n0, first, lane), acc);
@@ -441,8 +441,8 @@ __device__ SAR_INLINE inline void stage_products(uint4* __restrict__ to, const u
     if (works) multiply_stage<T, NT, Share<T, NT>::MR, Share<T, NT>::NW>(b, p, sign, acc);
 }
 
-template <typename T, int NT, bool TRANS, typename E>
-__global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a)
+template <typename T, int NT, bool TRANS, typename E, typename Q>
+__global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a, Q prologue)
 {
     constexpr int P = Mode<T>::kPieces, S = Mode<T>::kSteps, CH = kChunk<T>, N = Cols<T>::N, SB = Mode<T>::kStage;
     using Sh = Share<T, NT>;
@@ -472,9 +472,9 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a
     // 64 rows a load, every line was asked for once for each of its pieces.)  They are handed to those lanes through LDS, pieces turned by the row
     // so that neither side meets a bank twice.
     auto brings = [&](const Tile& w) SAR_INLINE { return w.first + wave * 32 < w.end; };
-    auto fetch_a = [&](const Tile& w, int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
+    auto fetch_from = [&](const void* p, const Tile& w, int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
         const int64_t r0 = w.first + wave * 32;
-        const T* tile = static_cast<const T*>(a.A) + r0 * a.C;
+        const T* tile = static_cast<const T*>(p) + r0 * a.C;
         const uint32_t most = (uint32_t)min((int64_t)w.end - 1 - r0, (int64_t)31);
         const int c = chunk * CH + (lane & 7) * N;
         if (a.C >= N) {
@@ -486,14 +486,36 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a
             for (int p = 0; p < kRaw; ++p) v[p] = Cols<T>::load(tile + min((uint32_t)(8 * p + (lane >> 3)), most) * (uint32_t)a.C, c, a.C, a.C);
         }
     };
+    uint4 pre[Q::kAny ? kRaw : 1];
+    auto fetch_a = [&](const Tile& w, int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
+        fetch_from(a.A, w, chunk, v);
+        if constexpr (Q::kAny) fetch_from(prologue.pre, w, chunk, pre);
+    };
     uint4* const rows = lds + 2 * kFrags * 64;
-    auto hand_over = [&](int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
+    auto hand_over = [&](const Tile& w, int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
         const int c = chunk * CH + (lane & 7) * N;
         if ((chunk + 1) * CH > a.C && c + N > a.C) {
 #pragma unroll
             for (int p = 0; p < kRaw; ++p) {
-                if (c >= a.C) v[p] = make_uint4(0u, 0u, 0u, 0u);
-                else if (a.C >= N) v[p] = front_of_piece<T>(v[p], a.C - c);
+                auto cut = [&](uint4& u) SAR_INLINE {
+                    if (c >= a.C) u = make_uint4(0u, 0u, 0u, 0u);
+                    else if (a.C >= N) u = front_of_piece<T>(u, a.C - c);
+                };
+                cut(v[p]);
+                if constexpr (Q::kAny) cut(pre[p]);
+            }
+        }
+        if constexpr (Q::kAny) {
+#pragma unroll
+            for (int p = 0; p < kRaw; ++p) form_piece<T>(prologue.act, v[p], pre[p]);
+            if (prologue.formed && blockIdx.y == 0) {
+#pragma unroll
+                for (int p = 0; p < kRaw; ++p) {
+                    const int64_t i = w.first + wave * 32 + 8 * p + (lane >> 3);
+                    float u[N];
+                    Cols<T>::unpack(v[p], u);
+                    if (i < w.end) Cols<T>::store(static_cast<T*>(prologue.formed) + i * a.C, c, a.C, u);
+                }
             }
         }
 #pragma unroll
@@ -509,7 +531,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a
     copy_stage<T, NT>(lds, pieces_of(tile, 0));
     if (brings(tile)) {
         fetch_a(tile, 0, raw);
-        hand_over(0, raw);
+        hand_over(tile, 0, raw);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -556,7 +578,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a
                                       acc, [&]() SAR_INLINE {
                                           if (part == 0 && coming) fetch_a(more ? tile : after, more ? chunk + 1 : 0, raw);
                                       });
-                if (part == S / SB - 1 && coming) hand_over(more ? chunk + 1 : 0, raw);
+                if (part == S / SB - 1 && coming) hand_over(more ? tile : after, more ? chunk + 1 : 0, raw);
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
                 buffer ^= 1;
@@ -567,7 +589,7 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a
         tile = after;
 #pragma unroll
         for (int m = 0; m < MR; ++m)
-            store_tiles<T, Sh, TRANS>(a, done.t, done.first + (wr * MR + m) * 32, done.end, blockIdx.y * (32 * NT), wc * NW, acc[m]);
+            store_tiles<T, Sh, TRANS>(a, prologue, done.t, done.first + (wr * MR + m) * 32, done.end, blockIdx.y * (32 * NT), wc * NW, acc[m]);
     }
 }
 
@@ -581,8 +603,8 @@ int tiles_of(int64_t n, int N)
     return groups(4) <= 256 * 2 || (N + 127) / 128 % 2 ? 4 : 8;
 }
 
-template <typename T, int NT, bool TRANS, typename E>
-int run_rows(const RowsArgs<E>& a, LayArgs l, hipStream_t st)
+template <typename T, int NT, bool TRANS, typename E, typename Q>
+int run_rows(const RowsArgs<E>& a, const Q& prologue, LayArgs l, hipStream_t st)
 {
     const int64_t units = (int64_t)l.T * l.blocks * l.chunks * Mode<T>::kSteps * NT * 64, lay = (units + 255) / 256;
     l.lay = (unsigned)lay;
@@ -592,10 +614,10 @@ int run_rows(const RowsArgs<E>& a, LayArgs l, hipStream_t st)
     // them, so that no unit waits long for the last (100000 x 512 -> 512, fp32, 332 us by one turn, 302 by two, 301 by four; 237500 x 256 -> 256 197, 191, 193)
     constexpr int kGroups = NT == 2 ? 3 : NT == 4 ? 2 : 4;
     constexpr size_t shared = (size_t)(2 * kStageFrags<T, NT> + 4 * kTileWaves) * 1024;
-    auto* fn = k_typed_rows<T, NT, TRANS, E>;
+    auto* fn = k_typed_rows<T, NT, TRANS, E, Q>;
     if (shared > 65536) SAR_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)shared));
     const int64_t groups = std::min<int64_t>(l.types.n / kTileRows + l.T, std::max(1, 256 * kGroups / l.blocks));
-    fn<<<dim3((unsigned)groups, l.blocks), kTileWaves * 64, shared, st>>>(a);
+    fn<<<dim3((unsigned)groups, l.blocks), kTileWaves * 64, shared, st>>>(a, prologue);
     SAR_LAUNCH_CHECK();
     return SAR_OK;
 }
@@ -610,18 +632,18 @@ int64_t most_tiles(int64_t n, int T) { return n / kTileRows + T; }
 size_t list_bytes(int64_t n, int T) { return (size_t)(most_tiles(n, T) + 1) * sizeof(int4); }
 
 // out [n, N] = A [n, C] B; TRANS: B = W^T.
-template <typename T, bool TRANS, typename E = NoEpilogue>
-int rows_product(const void* A, const float* W, const Types& types, void* out, int K, int F, void* work, hipStream_t st, const E& e = {})
+template <typename T, bool TRANS, typename E = NoEpilogue, typename Q = NoPrologue>
+int rows_product(const void* A, const float* W, const Types& types, void* out, int K, int F, void* work, hipStream_t st, const E& e = {}, const Q& q = {})
 {
     const int C = TRANS ? F : K, N = TRANS ? K : F, NT = tiles_of(types.n, N);
-    if (few_blocks(types, N)) return few_product(sizeof(T) == 4 ? SAR_F32 : SAR_BF16, TRANS, {A, W, out, types, C, N, K, F}, e, st);
+    if (!Q::kAny && few_blocks(types, N)) return few_product(sizeof(T) == 4 ? SAR_F32 : SAR_BF16, TRANS, {A, W, out, types, C, N, K, F}, e, st);
     const int chunks = (C + kChunk<T> - 1) / kChunk<T>, blocks = (N + 32 * NT - 1) / (32 * NT);
     const int64_t most = most_tiles(types.n, types.T);
     int4* const list = static_cast<int4*>(work);
     uint4* const pieces = static_cast<uint4*>(work) + (most + 1);
     const RowsArgs<E> a{A, pieces, W, out, list, C, N, chunks, blocks, K, F, e};
     const LayArgs l{W, pieces, types.T, K, F, C, N, chunks, blocks, types, list, most, 0};
-    return NT == 2 ? run_rows<T, 2, TRANS>(a, l, st) : NT == 4 ? run_rows<T, 4, TRANS>(a, l, st) : run_rows<T, 8, TRANS>(a, l, st);
+    return NT == 2 ? run_rows<T, 2, TRANS>(a, q, l, st) : NT == 4 ? run_rows<T, 4, TRANS>(a, q, l, st) : run_rows<T, 8, TRANS>(a, q, l, st);
 }
 
 }  // namespace

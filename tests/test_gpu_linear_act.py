@@ -84,6 +84,9 @@ def check_fwd(n, K, F, dtype, name, bias, res, keep, seed=0):
 
 SHAPES = [(1, 1, 1), (3, 7, 5), (33, 47, 31), (300, 100, 47), (500, 256, 256), (2000, 128, 128), (9000, 256, 256), (9001, 100, 200), (20_000, 64, 400),
           (30_011, 47, 172), (40_000, 130, 257), (12_345, 513, 64)]
+# operands that are kept whole: every number of chunks, ragged rows and columns, fewer columns than a block
+MANY = [(65_536, 256, 256), (65_537, 100, 256), (66_001, 3, 64), (65_570, 31, 65), (70_000, 64, 200), (65_999, 128, 127), (68_000, 129, 131), (66_666, 200, 96),
+        (65_600, 90, 47), (65_601, 255, 129)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -91,6 +94,50 @@ SHAPES = [(1, 1, 1), (3, 7, 5), (33, 47, 31), (300, 100, 47), (500, 256, 256), (
 @pytest.mark.parametrize("n,K,F", SHAPES)
 def test_forward(n, K, F, name, dtype):
     check_fwd(n, K, F, dtype, name, True, "first", True)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,K,F", MANY)
+def test_forward_of_many_rows(n, K, F, dtype):
+    check_fwd(n, K, F, dtype, "elu", True, "first", True)
+    check_fwd(n, K, F, dtype, "gelu", False, "after", True)
+    check_fwd(n, K, F, dtype, "silu", True, None, False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,K,F", MANY + [(n, F, K) for n, K, F in MANY])
+def test_backward_of_many_rows(n, K, F, dtype):
+    check_bwd(n, K, F, dtype, "gelu")
+    check_bwd(n, K, F, dtype, "elu", accumulate=True, want=("dW", "db", "dX"))
+    check_bwd(n, K, F, dtype, "none")
+    check_bwd(n, K, F, dtype, "relu", want=("dX",))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,K,F", [(3000, 40, 70), (65_600, 40, 70)])
+def test_infinities_and_nan_in_rows(n, K, F, dtype):
+    """They reach their own row's results, forward and backward, and no other's."""
+    X, W, b, R = inputs(n, K, F, dtype, 4)
+    work, _ = scratch(n, K, F)
+    rows = [5, n - 7]
+    clean = torch.empty_like(R)
+    sar.sar_linear_act_fwd(X, W, b, None, ACTS["silu"], False, clean, None, work)
+    dX0, dX = torch.empty_like(X), torch.empty_like(X)
+    sar.sar_linear_act_bwd(R, R, X, W, ACTS["silu"], False, None, None, dX0, None, work)
+    X[rows[0], 3], X[rows[1], 0] = float("nan"), float("inf")
+    Y, D = torch.empty_like(R), R.clone()
+    sar.sar_linear_act_fwd(X, W, b, None, ACTS["silu"], False, Y, None, work)
+    want = torch.nn.functional.silu(X[rows].cpu().double() @ W.cpu().double() + b.cpu().double())
+    assert torch.isnan(Y[rows[0]]).all()
+    inf = torch.isinf(want[1])
+    assert (Y[rows[1]].cpu()[inf] == float("inf")).all() and (Y[rows[1]].cpu()[~inf] == 0).all()
+    D[rows[0], 1], D[rows[1], 2] = float("nan"), float("inf")
+    sar.sar_linear_act_bwd(D, R, X, W, ACTS["silu"], False, None, None, dX, None, work)
+    assert torch.isnan(dX[rows[0]]).all() and not torch.isfinite(dX[rows[1]]).any()
+    other = torch.ones(n, dtype=torch.bool, device="cuda")
+    other[rows] = False
+    near = lambda a, c: bool(((a.float() - c.float()).abs() <= 1e-5 + 2 * nw.HALF[dtype] * c.float().abs()).all())       # (their tiles are summed another way)
+    assert near(Y[other], clean[other]) and near(dX[other], dX0[other])
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
