@@ -13,7 +13,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsar_mi355x.so")
 SOURCES = ["builder.hip", "spmm.hip", "gat.hip", "gat_slices.hip", "gat_joint_f32.hip", "gat_joint_bf16.hip", "linear.hip",
            "linear_split.hip", "linear_few.hip", "packed.hip", "norm.hip",
-           "linear_typed.hip", "linear_typed_dw.hip", "linear_typed_few.hip", "linear_act.hip", "logprob.hip", "distill.hip"]
+           "linear_typed.hip", "linear_typed_dw.hip", "linear_typed_few.hip", "linear_act.hip", "linear_act_dw.hip", "logprob.hip", "distill.hip"]
 BENCH_LIB = os.path.join(HERE, "libsar_bench.so")
 BENCH_SOURCES = ["probe.hip"]
 BINDING = os.path.join(HERE, "_binding.so")

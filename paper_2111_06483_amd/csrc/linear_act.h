@@ -142,4 +142,21 @@ __device__ inline float finish_value(const Epilogue& e, float v, int64_t at, int
     return e.after ? v + r : v;
 }
 
+// dW (+)= X^T dA and db (+)= the sums of dA's columns, dA = dY act'(A) formed where it is read (bf16), or dY as it is (act 0, pre null); db may be
+// null.  work: act_dw_bytes.  (linear_act_dw.hip; more rows than few_rows_dw takes.)
+struct ActDw {
+    const void* X;         // [n, K]
+    const void* dY;        // [n, F]
+    const void* pre;
+    int act;
+    float *dW, *db;
+    int64_t n;
+    int K, F, accumulate;
+    void* work;
+};
+size_t act_dw_bytes(int64_t n, int K, int F);
+int act_dw(int dtype, const ActDw& g, hipStream_t st);
+// db (+)= the sums [groups, F] of workgroups, in order.
+int act_sum(const float* partial, int groups, int F, int accumulate, float* db, hipStream_t st);
+
 }  // namespace sar

@@ -68,24 +68,6 @@ __global__ __launch_bounds__(kActThreads) void k_act_bwd(ActBwdArgs a)
     }
 }
 
-// db (+)= the partial sums of `groups` workgroups, in order: 32 columns a workgroup, whose 32 slices take every 32nd.
-__global__ __launch_bounds__(1024) void k_act_sum(const float* partial, int groups, int F, int accumulate, float* db)
-{
-    __shared__ float part[32][33];
-    const int k = threadIdx.x % 32, slice = threadIdx.x / 32, c = blockIdx.x * 32 + k;
-    float v = 0.f;
-    if (c < F)
-        for (int w = slice; w < groups; w += 32) v += partial[(int64_t)w * F + c];
-    part[slice][k] = v;
-    __syncthreads();
-    if (slice == 0 && c < F) {
-        float total = 0.f;
-#pragma unroll
-        for (int s = 0; s < 32; ++s) total += part[s][k];
-        db[c] = accumulate ? db[c] + total : total;
-    }
-}
-
 int lanes_of(int dtype, int F)
 {
     const int vec = dtype == SAR_F32 ? 4 : 8;
@@ -119,6 +101,14 @@ size_t partial_bytes(int64_t n, int F)
     return rounded((size_t)std::max(groups_of(SAR_F32, n, F), groups_of(SAR_BF16, n, F)) * F * sizeof(float));
 }
 
+// Scratch of either product (one after the other).
+size_t product_bytes(int64_t n, int K, int F)
+{
+    size_t b = 0;
+    (void)sar_linear_typed_workspace_bytes(n, K, F, 1, &b);
+    return rounded(std::max(b, act_dw_bytes(n, K, F)));
+}
+
 int check_act(int act)
 {
     if (act < SAR_ACT_NONE || act > SAR_ACT_ELU) return fail(SAR_ERR_UNSUPPORTED, "act %d is none of SAR_ACT_NONE, _RELU, _GELU, _SILU, _ELU", act);
@@ -140,41 +130,43 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
             int K, int F, void* work, hipStream_t st)
 {
     const int dtype = sizeof(T) == 4 ? SAR_F32 : SAR_BF16;
-    size_t products = 0;
-    SAR_TRY(sar_linear_typed_workspace_bytes(n, K, F, 1, &products));
-    char* const base = static_cast<char*>(work);
-    float* const partial = reinterpret_cast<float*>(base + rounded(products));
+    const size_t products = product_bytes(n, K, F);
+    float* const partial = reinterpret_cast<float*>(static_cast<char*>(work) + products);
     char* const high = reinterpret_cast<char*>(partial) + partial_bytes(n, F);
     const bool formed = act != SAR_ACT_NONE;
     const Types types{nullptr, 1, n};
-    // dA, where dW reads it
-    void* rows = !formed ? const_cast<void*>(dY) : dA ? dA : dW || (dX && few_blocks(types, K)) ? high : nullptr;
-    void* low = formed && dW && sizeof(T) == 2 ? high + rounded((size_t)n * F * sizeof(T)) : nullptr;
-    const bool within = formed && dX && n > 0 && !few_blocks(types, K);       // the product for dX forms dA
-    if (n > 0 && ((rows && !within && formed) || low || db || (dA && !formed))) {
+    const bool few_dw = few_rows_dw(n, 1, K, F), few_dx = few_blocks(types, K);
+    // What forms dA: the product for dX of many rows, in bf16 the one for dW too; otherwise a launch of its own.
+    const bool within = formed && dX && n > 0 && !few_dx, again = formed && dW && !few_dw && sizeof(T) == 2;
+    const bool reads = (dW && !again) || (dX && !within);
+    void* const rows = !formed ? const_cast<void*>(dY) : dA ? dA : reads ? high : nullptr;
+    void* const low = formed && dW && few_dw && sizeof(T) == 2 ? high + rounded((size_t)n * F * sizeof(T)) : nullptr;
+    const bool sums = db && (!dW || few_dw);       // (otherwise with dW)
+    void* const written = formed ? (within ? nullptr : rows) : dA;
+    if (n > 0 && (written || low || sums)) {
         const int lanes = lanes_of(dtype, F), groups = groups_of(dtype, n, F);
-        const ActBwdArgs a{dY, A, formed ? (within ? nullptr : rows) : dA, low, db ? partial : nullptr, n, F, act, lanes};
+        const ActBwdArgs a{dY, A, written, low, sums ? partial : nullptr, n, F, act, lanes};
         const int across = (F + lanes * Cols<T>::N - 1) / (lanes * Cols<T>::N);
         k_act_bwd<T><<<dim3(groups, across), kActThreads, 0, st>>>(a);
         SAR_LAUNCH_CHECK();
     }
-    if (db) {
-        k_act_sum<<<(F + 31) / 32, 1024, 0, st>>>(partial, n > 0 ? groups_of(dtype, n, F) : 0, F, accumulate, db);
-        SAR_LAUNCH_CHECK();
-    }
+    if (sums) SAR_TRY(act_sum(partial, n > 0 ? groups_of(dtype, n, F) : 0, F, accumulate, db, st));
     if (dX && n > 0) {
         if (within) {
             const ActPrologue q{A, rows, act};
             if (kept<T, ActPrologue>(n, F, K)) SAR_TRY((run_kept<T, true>(dY, W, n, dX, K, F, work, st, NoEpilogue{}, q)));
             else SAR_TRY((rows_product<T, true>(dY, W, types, dX, K, F, work, st, NoEpilogue{}, q)));
+        } else if (kept<T, NoPrologue>(n, F, K)) {
+            SAR_TRY((run_kept<T, true>(rows, W, n, dX, K, F, work, st, NoEpilogue{}, NoPrologue{})));
         } else {
-            if (kept<T, NoPrologue>(n, F, K)) SAR_TRY((run_kept<T, true>(rows, W, n, dX, K, F, work, st, NoEpilogue{}, NoPrologue{})));
-            else SAR_TRY((rows_product<T, true>(rows, W, types, dX, K, F, work, st)));
+            SAR_TRY((rows_product<T, true>(rows, W, types, dX, K, F, work, st)));
         }
     }
-    if (dW) {
+    if (dW && few_dw) {
         SAR_TRY(typed_dw(dtype, {X, nullptr, nullptr, rows, dW, types, K, F, accumulate, static_cast<float*>(work)}, st));
         if (low && n > 0) SAR_TRY(typed_dw(dtype, {X, nullptr, nullptr, low, dW, types, K, F, 1, static_cast<float*>(work)}, st));
+    } else if (dW) {
+        SAR_TRY(act_dw(dtype, {X, again ? dY : rows, again ? A : nullptr, act, dW, db, n, K, F, accumulate, work}, st));
     }
     return SAR_OK;
 }
@@ -188,8 +180,8 @@ extern "C" int sar_linear_act_workspace_bytes(int64_t n, int K, int F, size_t* b
 {
     SAR_CHECK_ARG(bytes, "bytes is null");
     size_t products = 0;
-    SAR_TRY(sar_linear_typed_workspace_bytes(n, K, F, 1, &products));
-    *bytes = rounded(products) + partial_bytes(n, F) + 2 * rounded((size_t)n * F * 4);
+    SAR_TRY(sar_linear_typed_workspace_bytes(n, K, F, 1, &products));      // (refuses what no product takes)
+    *bytes = product_bytes(n, K, F) + partial_bytes(n, F) + 2 * rounded((size_t)n * F * 2);
     return SAR_OK;
 }
 

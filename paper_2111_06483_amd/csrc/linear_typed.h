@@ -84,6 +84,10 @@ struct DwArgs {
     Types types;
     int K, F;
     int64_t share;         // rows of a workgroup
+    // of linear_act_dw.hip alone: what dZ is formed with, and the sums of its columns, [workgroups, F], or null
+    const void* pre = nullptr;
+    int act = 0;
+    float* sums = nullptr;
 };
 
 // A value of X as fp32.
