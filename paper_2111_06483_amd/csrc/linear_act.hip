@@ -85,7 +85,7 @@ int groups_of(int dtype, int64_t n, int F)
 template <typename T, typename P>
 bool kept(int64_t n, int C, int N)
 {
-    return n >= 65536 && N >= 64 && fits_kept<T, P>(C);
+    return n >= 65536 && N >= 64 && (!P::kAny || N <= 32 * kKeptTiles) && fits_kept<T, P>(C);
 }
 
 template <typename T>
