@@ -154,6 +154,48 @@ __device__ inline void offer_top(TopKey& list, TopKey c, TopKey last)
     }
 }
 
+// ---- the eight largest of a lane's numbers, then of its row's lanes; numbers that differ, or zeros
+
+__device__ inline void falling(uint32_t& a, uint32_t& b)
+{
+    const uint32_t high = max(a, b);
+    b = min(a, b), a = high;
+}
+// Sorted, by a network of 19 exchanges.
+__device__ inline void sort8(uint32_t (&v)[8])
+{
+    constexpr int kPairs[19][2] = {{0, 2}, {1, 3}, {4, 6}, {5, 7}, {0, 4}, {1, 5}, {2, 6}, {3, 7}, {0, 1}, {2, 3},
+                                   {4, 5}, {6, 7}, {2, 4}, {3, 5}, {1, 4}, {3, 6}, {1, 2}, {3, 4}, {5, 6}};
+#pragma unroll
+    for (int k = 0; k < 19; ++k) falling(v[kPairs[k][0]], v[kPairs[k][1]]);
+}
+// Falls and then rises: sorted.
+__device__ inline void settle8(uint32_t (&v)[8])
+{
+#pragma unroll
+    for (int o = 4; o >= 1; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((i & o) == 0) falling(v[i], v[i + o]);
+}
+__device__ inline void merge8(uint32_t (&v)[8], const uint32_t (&sorted)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = max(v[i], sorted[7 - i]);
+    settle8(v);
+}
+template <int L, int O = 1>
+__device__ inline void merge8_lanes(uint32_t (&v)[8])
+{
+    if constexpr (O < L) {
+        uint32_t other[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) other[i] = lane_xor<O>(v[i]);
+        merge8(v, other);
+        merge8_lanes<L, O * 2>(v);
+    }
+}
+
 // ---- how rows are laid over threads
 
 // Rows of up to 32 values a lane of a wavefront stay in registers.
@@ -171,8 +213,8 @@ inline ClassShape class_shape(int dtype, int64_t n, int C)
     while (tpr < 64 && pieces > tpr * most) tpr <<= 1;
     // few rows are spread over more lanes
     while (tpr < 64 && pieces > tpr && n * tpr < 64 * 2048) tpr <<= 1;
-    const int r = (pieces + tpr - 1) / tpr, step = dtype == SAR_F32 ? 2 : 1;
-    return {tpr, (r + step - 1) / step * step};
+    const int r = (pieces + tpr - 1) / tpr;
+    return {tpr, r <= 4 ? r : (r + 1) / 2 * 2};
 }
 
 // Longer rows are cut into parts of whole pieces, a workgroup each; several parts a row where there are few rows, and a second launch that joins them.
@@ -234,6 +276,7 @@ __global__ __launch_bounds__(kClassThreads) void k_class_rows(ClassRows a, typen
         const int64_t row = base + threadIdx.x / TPR;
         const bool there = row < a.n;
         float v[R][N];
+        const auto other = Job::template begin<T>(a, job, min(row, a.n - 1), t);       // (what else is read of a row, under way with it)
         row_in_lanes<T, TPR, R>(a, min(row, a.n - 1), t, v);
         RowSums sums{-__builtin_inff(), 0.f, 0.f};
 #pragma unroll
@@ -252,7 +295,7 @@ __global__ __launch_bounds__(kClassThreads) void k_class_rows(ClassRows a, typen
             }
         sums.s = lanes_sum<TPR>(sums.s);
         if constexpr (Job::kEntropy) sums.u = lanes_sum<TPR>(sums.u) * a.over;
-        Job::template in_lanes<T, TPR, R>(a, job, min(row, a.n - 1), there, t, sums, v);
+        Job::template in_lanes<T, TPR, R>(a, job, min(row, a.n - 1), there, t, sums, other, v);
     }
 }
 
@@ -404,13 +447,18 @@ inline size_t class_work_bytes(int64_t n, int C, int k)
 template <typename T, typename Job, int TPR>
 int run_in_lanes(int r, const ClassRows& a, const typename Job::Args& job, hipStream_t st)
 {
-    constexpr int kRows = kClassThreads / TPR, S = 4 / (int)sizeof(T) == 1 ? 2 : 1;       // pieces of 8 values
+    constexpr int kRows = kClassThreads / TPR;
     const unsigned groups = (unsigned)std::min<int64_t>((a.n + kRows - 1) / kRows, 1 << 20);
-    switch (r / S) {
-    case 1: k_class_rows<T, TPR, 1 * S, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
-    case 2: k_class_rows<T, TPR, 2 * S, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
-    case 3: k_class_rows<T, TPR, 3 * S, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
-    default: k_class_rows<T, TPR, 4 * S, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
+    switch (r) {
+    case 1: k_class_rows<T, TPR, 1, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
+    case 2: k_class_rows<T, TPR, 2, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
+    case 3: k_class_rows<T, TPR, 3, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
+    case 4: k_class_rows<T, TPR, 4, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
+    default:
+        if constexpr (sizeof(T) == 4) {
+            if (r == 6) k_class_rows<T, TPR, 6, Job><<<groups, kClassThreads, 0, st>>>(a, job);
+            else k_class_rows<T, TPR, 8, Job><<<groups, kClassThreads, 0, st>>>(a, job);
+        }
     }
     SAR_LAUNCH_CHECK();
     return SAR_OK;

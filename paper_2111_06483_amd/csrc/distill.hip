@@ -27,42 +27,65 @@ struct DistillJob {
         float *loss, *lse;
     };
 
+    // An entry of the list, and the student's score of its class.
+    struct Entry {
+        bool is;
+        float value, score;
+    };
+    template <typename T>
+    static __device__ inline Entry entry_of(const ClassRows& a, const Teacher& q, int64_t row, int j)
+    {
+        Entry e{false, 0.f, 0.f};
+        if (j >= q.k) return e;
+        const int32_t c = q.index[row * q.k + j];
+        e.is = q.is(c);
+        e.value = q.value[row * q.k + j];
+        if (e.is) e.score = value_in(static_cast<const T*>(a.X)[row * a.C + c]);
+        return e;
+    }
+    // The first of a lane.
+    template <typename T>
+    static __device__ inline Entry begin(const ClassRows& a, const Args& o, int64_t row, int t)
+    {
+        return o.loss ? entry_of<T>(a, o.teacher, row, t) : Entry{false, 0.f, 0.f};
+    }
+
     template <typename T, int L>
-    static __device__ inline void by_lanes(const ClassRows& a, const Args& o, int64_t row, bool there, int t, const RowSums& r)
+    static __device__ inline void by_lanes(const ClassRows& a, const Args& o, int64_t row, bool there, int t, const RowSums& r, const Entry& first)
     {
         const Teacher& q = o.teacher;
         const float log = logf(r.s), base = base_of(r.m);
         if (there && t == 0 && o.lse) o.lse[row] = fmaf(base, q.over, log);
         if (!o.loss) return;
-        const float* value = q.value + row * q.k;
-        const int32_t* index = q.index + row * q.k;
-        float most = -__builtin_inff();
-        for (int j = t; j < q.k; j += L)
-            if (q.is(index[j])) most = fmaxf(most, value[j]);
+        float most = first.is ? first.value : -__builtin_inff();
+        for (int j = t + L; j < q.k; j += L)
+            if (q.is(q.index[row * q.k + j])) most = fmaxf(most, q.value[row * q.k + j]);
         const float top = base_of(lanes_largest<L>(most));
         float s = 0.f, w = 0.f;
-        for (int j = t; j < q.k; j += L) {
-            const int32_t c = index[j];
-            if (!q.is(c)) continue;
-            const float d = value[j] - top, e = exp_below(d, q.by);
+        auto add = [&](const Entry& x) {
+            const float d = x.value - top, e = exp_below(d, q.by);
+            if (!x.is) return;
             s += e;
-            if (e != 0.f) w = fmaf(e, (d - (value_in(static_cast<const T*>(a.X)[row * a.C + c]) - base)) * q.over, w);
-        }
+            if (e != 0.f) w = fmaf(e, (d - (x.score - base)) * q.over, w);
+        };
+        add(first);
+        for (int j = t + L; j < q.k; j += L) add(entry_of<T>(a, q, row, j));
         s = lanes_sum<L>(s);
         w = lanes_sum<L>(w);
         const bool empty = r.m == -__builtin_inff() && r.s == 0.f;
         if (there && t == 0) o.loss[row] = s == 0.f ? 0.f : empty ? __builtin_inff() : w / s - logf(s) + log;
     }
+
     template <typename T, int TPR, int R>
-    static __device__ inline void in_lanes(const ClassRows& a, const Args& o, int64_t row, bool there, int t, const RowSums& r,
+    static __device__ inline void in_lanes(const ClassRows& a, const Args& o, int64_t row, bool there, int t, const RowSums& r, const Entry& first,
                                            const float (&)[R][Cols<T>::N])
     {
-        by_lanes<T, TPR>(a, o, row, there, t, r);
+        by_lanes<T, TPR>(a, o, row, there, t, r, first);
     }
     template <typename T>
     static __device__ inline void in_wave(const ClassRows& a, const Args& o, int64_t row, const RowSums& r, TopKey)
     {
-        by_lanes<T, 64>(a, o, row, true, threadIdx.x & 63, r);
+        by_lanes<T, 64>(a, o, row, true, threadIdx.x & 63, r, begin<T>(a, o, row, threadIdx.x & 63));
     }
 };
 
