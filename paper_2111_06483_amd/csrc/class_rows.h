@@ -154,7 +154,7 @@ __device__ inline void offer_top(TopKey& list, TopKey c, TopKey last)
     }
 }
 
-// ---- the eight largest of a lane's numbers, then of its row's lanes; numbers that differ, or zeros
+// ---- the eight largest of a lane's numbers; numbers that differ, or zeros
 
 __device__ inline void falling(uint32_t& a, uint32_t& b)
 {
@@ -184,18 +184,6 @@ __device__ inline void merge8(uint32_t (&v)[8], const uint32_t (&sorted)[8])
     for (int i = 0; i < 8; ++i) v[i] = max(v[i], sorted[7 - i]);
     settle8(v);
 }
-template <int L, int O = 1>
-__device__ inline void merge8_lanes(uint32_t (&v)[8])
-{
-    if constexpr (O < L) {
-        uint32_t other[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) other[i] = lane_xor<O>(v[i]);
-        merge8(v, other);
-        merge8_lanes<L, O * 2>(v);
-    }
-}
-
 // ---- how rows are laid over threads
 
 // Rows of up to 32 values a lane of a wavefront stay in registers.
@@ -247,6 +235,10 @@ struct ClassRows {
     TopKey* lists;         // [n, parts, k]
 };
 
+// Whether a row may end in the lanes' r-th pieces: the last, where lanes have as few as cover it (class_shape).
+template <typename T, int R>
+constexpr bool ends_in(int r) { return r >= R - (R > 4 ? 2 : 1); }
+
 // A row's pieces of `T` in the lanes t of TPR, -inf behind the row's end.
 template <typename T, int TPR, int R>
 __device__ inline void row_in_lanes(const ClassRows& a, int64_t row, int t, float (&v)[R][Cols<T>::N])
@@ -257,13 +249,11 @@ __device__ inline void row_in_lanes(const ClassRows& a, int64_t row, int t, floa
     for (int r = 0; r < R; ++r) raw[r] = Cols<T>::load(static_cast<const T*>(a.X) + row * a.C, (t + r * TPR) * N, a.C, (a.n - row) * a.C);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int c = (t + r * TPR) * N;
         Cols<T>::unpack(raw[r], v[r]);
-        if (c + N > a.C) {
+        if (!ends_in<T, R>(r)) continue;
+        const int left = a.C - (t + r * TPR) * N;
 #pragma unroll
-            for (int j = 0; j < N; ++j)
-                if (c + j >= a.C) v[r][j] = -__builtin_inff();
-        }
+        for (int j = 0; j < N; ++j) v[r][j] = j < left ? v[r][j] : -__builtin_inff();
     }
 }
 
@@ -271,8 +261,10 @@ template <typename T, int TPR, int R, typename Job>
 __global__ __launch_bounds__(kClassThreads) void k_class_rows(ClassRows a, typename Job::Args job)
 {
     constexpr int N = Cols<T>::N, kRows = kClassThreads / TPR;
-    const int t = threadIdx.x % TPR;
     for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.n; base += (int64_t)gridDim.x * kRows) {
+        // (worked out for every row: which of its values lie behind the end was kept through the loop, in a hundred scalar registers that there are not)
+        int t = threadIdx.x % TPR;
+        asm volatile("" : "+v"(t));
         const int64_t row = base + threadIdx.x / TPR;
         const bool there = row < a.n;
         float v[R][N];
@@ -479,23 +471,26 @@ int run_classes(ClassRows a, const typename Job::Args& job, const char* what, vo
         default: return run_in_lanes<T, Job, 64>(s.r, a, job, st);
         }
     }
-    a.parts = parts_of(dtype, a.n, a.C);
-    a.width = part_width(a.C, a.parts);
-    if (a.parts > 1) {
-        const size_t need = class_work_bytes(a.n, a.C, Job::kTop ? a.k : 0);
-        SAR_CHECK_ARG(work && work_bytes >= need, "%s: work has %zu bytes, needs %zu", what, work ? work_bytes : 0, need);
-        SAR_CHECK_ARG((reinterpret_cast<uintptr_t>(work) & 15) == 0, "%s: work must be 16-byte aligned", what);
-        a.lists = static_cast<TopKey*>(work);
-        a.sums = reinterpret_cast<RowSums*>(a.lists + a.n * a.parts * (Job::kTop ? a.k : 0));
-    }
-    const unsigned groups = (unsigned)std::min<int64_t>(a.n * a.parts, 1 << 20);
-    k_class_wide<T, Job><<<groups, kClassThreads, 0, st>>>(a, job);
-    SAR_LAUNCH_CHECK();
-    if (a.parts > 1) {
-        k_class_join<T, Job><<<(unsigned)((a.n + kClassWaves - 1) / kClassWaves), kClassThreads, 0, st>>>(a, job);
+    if constexpr (Job::kWide) {
+        a.parts = parts_of(dtype, a.n, a.C);
+        a.width = part_width(a.C, a.parts);
+        if (a.parts > 1) {
+            const size_t need = class_work_bytes(a.n, a.C, Job::kTop ? a.k : 0);
+            SAR_CHECK_ARG(work && work_bytes >= need, "%s: work has %zu bytes, needs %zu", what, work ? work_bytes : 0, need);
+            SAR_CHECK_ARG((reinterpret_cast<uintptr_t>(work) & 15) == 0, "%s: work must be 16-byte aligned", what);
+            a.lists = static_cast<TopKey*>(work);
+            a.sums = reinterpret_cast<RowSums*>(a.lists + a.n * a.parts * (Job::kTop ? a.k : 0));
+        }
+        const unsigned groups = (unsigned)std::min<int64_t>(a.n * a.parts, 1 << 20);
+        k_class_wide<T, Job><<<groups, kClassThreads, 0, st>>>(a, job);
         SAR_LAUNCH_CHECK();
+        if (a.parts > 1) {
+            k_class_join<T, Job><<<(unsigned)((a.n + kClassWaves - 1) / kClassWaves), kClassThreads, 0, st>>>(a, job);
+            SAR_LAUNCH_CHECK();
+        }
+        return SAR_OK;
     }
-    return SAR_OK;
+    return fail(SAR_ERR_UNSUPPORTED, "%s: no kernel for %d classes", what, a.C);
 }
 
 // ---- gradients: tiles of up to kTileValues scores, whole rows where they are short, a piece of one row where they are long

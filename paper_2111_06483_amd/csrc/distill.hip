@@ -21,7 +21,7 @@ struct Teacher {
 };
 
 struct DistillJob {
-    static constexpr bool kEntropy = false, kTop = false;
+    static constexpr bool kEntropy = false, kTop = false, kWide = true;
     struct Args {
         Teacher teacher;
         float *loss, *lse;

@@ -10,13 +10,17 @@ namespace sar {
 
 namespace {
 
+struct LogprobArgs {
+    const int32_t* label;
+    float *logp, *lse, *entropy, *value;
+    int32_t* index;
+};
+
+// SHORT: up to eight top classes of bf16 rows that stay in registers.
+template <bool SHORT>
 struct LogprobJob {
-    static constexpr bool kEntropy = true, kTop = true;
-    struct Args {
-        const int32_t* label;
-        float *logp, *lse, *entropy, *value;
-        int32_t* index;
-    };
+    static constexpr bool kEntropy = true, kTop = true, kWide = !SHORT;
+    using Args = LogprobArgs;
 
     // The label and its score (0, a class that is none, where it is not asked for).
     struct Label {
@@ -45,7 +49,14 @@ struct LogprobJob {
         o.index[row * a.k + k] = is ? cls : -1;
     }
     // A bf16 score's order and its class in one number.
-    static __device__ inline uint32_t short_key(float v, int c, int C) { return c < C ? (order_of(v) & 0xffff0000u) | (0xffffu - (uint32_t)c) : 0u; }
+    static __device__ inline uint32_t short_key(float v, int c) { return (order_of(v) & 0xffff0000u) | (0xffffu - (uint32_t)c); }
+    // The number of the class c among a lane's i-th piece, 0 behind the last one.
+    template <typename T, int R>
+    static __device__ inline uint32_t key_in_lane(const ClassRows& a, float v, int i, int c)
+    {
+        const uint32_t key = Cols<T>::N == 8 ? short_key(v, c) : order_of(v);
+        return ends_in<T, R>(i) && c >= a.C ? 0u : key;
+    }
     static __device__ inline uint32_t order_of_short(uint32_t key) { return key & 0x80000000u ? key & 0xffff0000u : key | 0xffffu; }
     static __device__ inline int class_of_short(uint32_t key) { return (int)(0xffffu - (key & 0xffffu)); }
 
@@ -57,32 +68,38 @@ struct LogprobJob {
         const float log = logf(r.s);
         if (there && t == 0) results(a, o, row, r, label, log);
         if (a.k == 0) return;
-        if constexpr (N == 8) {
-            // Up to eight of bf16 scores: every lane's eight largest, merged piece by piece and lane by lane.  (1734375 rows of 172 classes, eight of them, one by one
-            // as below: 346 us.)
-            if (a.k <= 8) {
-                uint32_t top[8], piece[8];
+        if constexpr (SHORT) {
+            // Every lane's eight largest, sorted; the largest of the row's lanes is then taken from whichever lane has it, k times over.  (1734375 rows of 172 classes, eight
+            // of them, by the search below 346 us, lists merged lane by lane 295.)
+            uint32_t top[8], piece[8];
 #pragma unroll
-                for (int i = 0; i < R; ++i) {
+            for (int i = 0; i < R; ++i) {
 #pragma unroll
-                    for (int j = 0; j < N; ++j) (i == 0 ? top : piece)[j] = short_key(v[i][j], (t + i * TPR) * N + j, a.C);
-                    if (i == 0) {
-                        sort8(top);
-                    } else {
-                        sort8(piece);
-                        merge8(top, piece);
-                    }
+                for (int j = 0; j < 8; ++j) (i == 0 ? top : piece)[j] = key_in_lane<T, R>(a, v[i][j], i, (t + i * TPR) * N + j);
+                if (i == 0) {
+                    sort8(top);
+                } else {
+                    sort8(piece);
+                    merge8(top, piece);
                 }
-                merge8_lanes<TPR>(top);
-#pragma unroll
-                for (int k0 = 0; k0 < 8; k0 += TPR) {
-                    uint32_t key = 0;
-#pragma unroll
-                    for (int i = 0; i < (TPR < 8 ? TPR : 8); ++i) key = t == i ? top[k0 + i] : key;
-                    if (there && t < 8 && k0 + t < a.k) write_top(a, o, row, k0 + t, order_of_short(key) > kOrderOfNone, order_of_short(key), class_of_short(key), r, log);
-                }
-                return;
             }
+            uint32_t mine[(8 + TPR - 1) / TPR] = {};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (k >= a.k) break;
+                const uint32_t best = over_lanes<TPR>(top[0], [](uint32_t x, uint32_t y) { return max(x, y); });
+                const bool taken = top[0] == best;
+#pragma unroll
+                for (int i = 0; i + k < 7; ++i) top[i] = taken ? top[i + 1] : top[i];
+                mine[k / TPR] = t == k % TPR ? best : mine[k / TPR];
+            }
+#pragma unroll
+            for (int i = 0; i < (8 + TPR - 1) / TPR; ++i) {
+                const int k = t + i * TPR;
+                const uint32_t order = order_of_short(mine[i]);
+                if (there && k < a.k) write_top(a, o, row, k, order > kOrderOfNone, order, class_of_short(mine[i]), r, log);
+            }
+            return;
         }
         // Whichever class is the largest is written and taken out, k times over.  A bf16 score's order and its class fit one number.
         uint32_t key[R][N];
@@ -90,9 +107,7 @@ struct LogprobJob {
         for (int i = 0; i < R; ++i)
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const int c = (t + i * TPR) * N + j;
-                if constexpr (N == 8) key[i][j] = short_key(v[i][j], c, a.C);
-                else key[i][j] = c < a.C ? order_of(v[i][j]) : 0u;
+                key[i][j] = key_in_lane<T, R>(a, v[i][j], i, (t + i * TPR) * N + j);
             }
         for (int k = 0; k < a.k; ++k) {
             uint32_t best = 0;
@@ -252,10 +267,13 @@ extern "C" int sar_logprob_fwd(const void* X, const int32_t* label, float* logp,
     SAR_CHECK_ARG(!logp || label || n == 0, "null pointer (label)");
     if (n == 0) return SAR_OK;
     SAR_CHECK_ARG(X, "null pointer (X)");
-    ClassRows a{X, n, C, k, kLog2e, 1.f, 1, C, nullptr, nullptr};
-    const LogprobJob::Args job{label, logp, lse, entropy, top_value, top_index};
-    return dtype == SAR_F32 ? run_classes<float, LogprobJob>(a, job, "log probabilities", work, work_bytes, as_stream(stream))
-                            : run_classes<bf16_t, LogprobJob>(a, job, "log probabilities", work, work_bytes, as_stream(stream));
+    const ClassRows a{X, n, C, k, kLog2e, 1.f, 1, C, nullptr, nullptr};
+    const LogprobArgs job{label, logp, lse, entropy, top_value, top_index};
+    hipStream_t st = as_stream(stream);
+    const char* const what = "log probabilities";
+    if (dtype == SAR_F32) return run_classes<float, LogprobJob<false>>(a, job, what, work, work_bytes, st);
+    if (k > 0 && k <= 8 && C <= kMostInLanes) return run_classes<bf16_t, LogprobJob<true>>(a, job, what, work, work_bytes, st);
+    return run_classes<bf16_t, LogprobJob<false>>(a, job, what, work, work_bytes, st);
 }
 
 extern "C" int sar_logprob_bwd(const void* X, const int32_t* label, const float* lse, const float* entropy, const float* dlogp,
