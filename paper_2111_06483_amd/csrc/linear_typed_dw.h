@@ -134,11 +134,15 @@ struct FormedUnit {
         Plain::load(w, base, group, rows, full, c, width);
         Plain::load(w + Plain::kRegs, pre, group, rows, full, c, width);
     }
-    static __device__ SAR_INLINE inline void put(uint32_t* w, int act, uint4* out, int stride, int group, int rows, bool full, int c, int width, float (&sums)[2])
+    // `negate`: of dY's sign, which leaves X as it is (a quarter of the values to turn)
+    static __device__ SAR_INLINE inline void put(uint32_t* w, int act, uint4* out, int stride, int group, int rows, bool full, int c, int width, bool negate,
+                                                 float (&sums)[2])
     {
         float v[2][8];
+        const uint32_t flip = negate ? 0x80008000u : 0u;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
+            w[k] ^= flip;
             v[0][k] = __uint_as_float(w[k] << 16), v[1][k] = __uint_as_float(w[k] & 0xffff0000u);
         }
         with_act(act, [&](auto which) SAR_INLINE {
@@ -157,21 +161,34 @@ struct FormedUnit {
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[0][k] = v[1][k];
         }
+        uint32_t hi[2][4], lo[2][4];
+        float largest = 0.f;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            uint32_t hi[4], lo[4];
+            float sum = 0.f;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const float a = v[j][2 * k], b = v[j][2 * k + 1];
-                hi[k] = pack2_bf16(a, b);
-                float la = a - __uint_as_float(hi[k] << 16), lb = b - __uint_as_float(hi[k] & 0xffff0000u);
-                // (an infinity has no second piece)
-                la = fabsf(la) < __builtin_inff() ? la : 0.f, lb = fabsf(lb) < __builtin_inff() ? lb : 0.f;
-                lo[k] = pack2_bf16(la, lb);
-                sums[j] += a + b;
+                hi[j][k] = pack2_bf16(a, b);
+                lo[j][k] = pack2_bf16(a - __uint_as_float(hi[j][k] << 16), b - __uint_as_float(hi[j][k] & 0xffff0000u));
+                largest = fmaxf(largest, fmaxf(fabsf(a), fabsf(b)));
+                sum += a + b;
             }
-            out[32 * j] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            out[stride + 32 * j] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            sums[j] = negate ? sums[j] - sum : sums[j] + sum;
+        }
+        if (largest >= 0x1.fep127f) {          // an infinity (as bf16) has no second piece
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if ((hi[j][k] & 0x7fffu) == 0x7f80u) lo[j][k] &= 0xffff0000u;
+                    if ((hi[j][k] & 0x7fff0000u) == 0x7f800000u) lo[j][k] &= 0xffffu;
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            out[32 * j] = make_uint4(hi[j][0], hi[j][1], hi[j][2], hi[j][3]);
+            out[stride + 32 * j] = make_uint4(lo[j][0], lo[j][1], lo[j][2], lo[j][3]);
         }
     }
 };
@@ -306,7 +323,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
             if (first >= kXUnits || (kXUnits % 64 && id >= kXUnits)) continue;
             const int g = id / (TK / XR::kCols), c = id % (TK / XR::kCols) * XR::kCols;
             if constexpr (XR::kCols == 4) PackedUnit::put(raw.x[u], buf + g * TK + place_of(c), g, rows, full, negate);
-            else Unit<XR>::put(raw.x[u], buf + g * TK + place_of(c), kGroups * TK, g, rows, full, k0 + c, a.K, negate);
+            else Unit<XR>::put(raw.x[u], buf + g * TK + place_of(c), kGroups * TK, g, rows, full, k0 + c, a.K, negate && !ZTraits<ZR>::kFormed);
         }
 #pragma unroll
         for (int u = 0; u < kZSlots; ++u) {
@@ -314,7 +331,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
             if (first >= kZUnits || (kZUnits % 64 && id >= kZUnits)) continue;
             const int g = id / (TF / 2), c = id % (TF / 2) * 2;
             if constexpr (ZTraits<ZR>::kFormed) {
-                FormedUnit::put(raw.z[u], a.act, buf + kXSize + g * TF + place_of(c), kGroups * TF, g, rows, full, f0 + c, a.F, sums[u]);
+                FormedUnit::put(raw.z[u], a.act, buf + kXSize + g * TF + place_of(c), kGroups * TF, g, rows, full, f0 + c, a.F, negate, sums[u]);
             } else {
                 Unit<Plain>::put(raw.z[u], buf + kXSize + g * TF + place_of(c), kGroups * TF, g, rows, full, f0 + c, a.F, false);
                 if constexpr (ZTraits<ZR>::kSums) {
@@ -344,8 +361,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) acc[m][n] = float16_t{};
             // Which sign X has in chunk i, so that what the matrix unit cuts leans to neither side.  Bf16 products, which are added to the sums
-            // there: the other sign every four chunks and in every other workgroup, with the sums turned round where it changes.
-            auto minus = [&](int i) SAR_INLINE { return kThere ? (((i >> 2) + (int)blockIdx.x) & 1) != 0 : (i & 1) != 0; };
+            // there: the other sign every four chunks (of formed rows sixteen) and in every other workgroup, with the sums turned round where it changes.
+            auto minus = [&](int i) SAR_INLINE { return kThere ? (((i >> (ZTraits<ZR>::kFormed ? 4 : 2)) + (int)blockIdx.x) & 1) != 0 : (i & 1) != 0; };
             auto step = [&](int i, int64_t r0, Chunk& later, Chunk& next) SAR_INLINE {
                 constexpr int kRows = 16 * S;
                 if (r0 + AHEAD * kRows < end) fetch(later, r0 + AHEAD * kRows, end);
