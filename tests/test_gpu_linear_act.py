@@ -1,10 +1,8 @@
 """The transform with bias, residual and activation, and its backward pass, against 64 bits."""
 import math
 
-import numpy as np
 import pytest
 import torch
-from scipy.special import erfc
 
 from paper_2111_06483_amd import sar
 from tests import nodewise as nw
@@ -19,30 +17,35 @@ STEEP, BEND = 1.13, 1.0
 
 
 def act(name, a):
-    """(activation, slope, what 32 bits may be off of either): a few units of a result, the normal share to within 2e-7, an exponential's argument off
-    by a unit of its size."""
+    """(activation, slope, what 32 bits may be off of either) of float64 `a`: a few units of a result, the normal share to within 2e-7, an exponential's
+    argument off by a unit of its size."""
     if name == "relu":
-        return np.maximum(a, 0), (a > 0) * 1.0, 0 * a, 0 * a
+        return a.clamp(min=0), (a > 0).double(), 0 * a, 0 * a
     if name == "gelu":
-        share, bell = 0.5 * erfc(-a / math.sqrt(2)), np.exp(-a * a / 2) / math.sqrt(2 * math.pi)
+        share, bell = 0.5 * torch.special.erfc(-a / math.sqrt(2)), torch.exp(-a * a / 2) / math.sqrt(2 * math.pi)
         off = 2.5e-7 + 4 * nw.U * a * a * bell
-        return a * share, share + a * bell, np.abs(a) * off + 2 * nw.U * np.abs(a * share), off + (4 + 4 * a * a) * nw.U * np.abs(a) * bell + 4 * nw.U
+        return a * share, share + a * bell, a.abs() * off + 2 * nw.U * (a * share).abs(), off + (4 + 4 * a * a) * nw.U * a.abs() * bell + 4 * nw.U
     if name == "silu":
-        s = 1 / (1 + np.exp(-a))
-        off = (4 + 4 * np.abs(a)) * nw.U * s
-        return a * s, s * (1 + a * (1 - s)), np.abs(a) * off, (1 + np.abs(a)) * (off + 4 * nw.U * s)
+        s = torch.sigmoid(a)
+        off = (4 + 4 * a.abs()) * nw.U * s
+        return a * s, s * (1 + a * (1 - s)), a.abs() * off, (1 + a.abs()) * (off + 4 * nw.U * s)
     if name == "elu":
-        e = np.exp(np.minimum(a, 0))
-        small = a > -0.35
-        return (np.where(a > 0, a, np.expm1(np.minimum(a, 0))), e, np.where(a > 0, 0, np.where(small, 12 * nw.U * np.abs(a), (4 + 4 * np.abs(a)) * nw.U * e + nw.U)),
-                (3 + 4 * np.abs(a)) * nw.U * e * (a <= 0))
-    return a, np.ones_like(a), 0 * a, 0 * a
+        low = a.clamp(max=0)
+        e, none = torch.exp(low), 0 * a
+        return (torch.where(a > 0, a, torch.expm1(low)), e,
+                torch.where(a > 0, none, torch.where(a > -0.35, 12 * nw.U * a.abs(), (4 + 4 * a.abs()) * nw.U * e + nw.U)),
+                torch.where(a > 0, none, (3 + 4 * a.abs()) * nw.U * e))
+    return a, torch.ones_like(a), 0 * a, 0 * a
+
+
+def f64(t):
+    return t.detach().double()
 
 
 def inputs(n, K, F, dtype, seed=0):
-    g = torch.Generator().manual_seed(seed * 104729 + n * 131 + K * 17 + F)
-    rn = lambda *s: torch.randn(*s, generator=g)
-    return (rn(n, K).to(dtype).cuda(), (rn(K, F) / K ** 0.5).cuda(), rn(F).cuda(), rn(n, F).to(dtype).cuda())
+    g = torch.Generator("cuda").manual_seed(seed * 104729 + n * 131 + K * 17 + F)
+    rn = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    return (rn(n, K).to(dtype), rn(K, F) / K ** 0.5, rn(F), rn(n, F).to(dtype))
 
 
 def scratch(n, K, F):
@@ -52,7 +55,7 @@ def scratch(n, K, F):
 
 
 def stored(t, off, want):
-    return off + (nw.half_step(t)(np.abs(want) + off) if t == BF16 else 2 * nw.U * np.abs(want))
+    return off + (nw.HALF[t] * (want.abs() + off) + 2.0 ** -134 if t == BF16 else 2 * nw.U * want.abs())
 
 
 def check_fwd(n, K, F, dtype, name, bias, res, keep, seed=0):
@@ -61,20 +64,20 @@ def check_fwd(n, K, F, dtype, name, bias, res, keep, seed=0):
     work, behind = scratch(n, K, F)
     sar.sar_linear_act_fwd(X, W, b if bias else None, R if res else None, ACTS[name], res == "after", Y, A if keep else None, work)
     assert bool((behind == 77).all())
-    x, w = nw.f64(X), nw.f64(W)
-    a, size = x @ w, np.abs(x) @ np.abs(w)
+    x, w = f64(X), f64(W)
+    a, size = x @ w, x.abs() @ w.abs()
     off = rows_off(size, K, dtype)
     if bias:
-        a, off = a + nw.f64(b), off + 2 * nw.U * (size + np.abs(nw.f64(b)))
+        a, off = a + f64(b), off + 2 * nw.U * (size + f64(b).abs())
     if res == "first":
-        a, off = a + nw.f64(R), off + 2 * nw.U * (size + np.abs(nw.f64(b)) + np.abs(nw.f64(R)))
+        a, off = a + f64(R), off + 2 * nw.U * (size + f64(b).abs() + f64(R).abs())
     if keep:
-        assert (np.abs(nw.f64(A) - a) <= stored(dtype, off, a)).all()
+        assert ((f64(A) - a).abs() <= stored(dtype, off, a)).all()
     y, _, off_act, _ = act(name, a)
     off = STEEP * off + off_act
     if res == "after":
-        y, off = y + nw.f64(R), off + 2 * nw.U * (np.abs(y) + np.abs(nw.f64(R)))
-    assert (np.abs(nw.f64(Y) - y) <= stored(dtype, off, y)).all()
+        y, off = y + f64(R), off + 2 * nw.U * (y.abs() + f64(R).abs())
+    assert ((f64(Y) - y).abs() <= stored(dtype, off, y)).all()
     # the residual's own rows as the result's
     same = R.clone()
     if res:
@@ -151,38 +154,38 @@ def test_forms_of_the_forward_pass(n, K, F, res, bias, dtype):
 
 def check_bwd(n, K, F, dtype, name, accumulate=False, want=("dW", "db", "dX", "dA"), seed=0):
     X, W, _, dY = inputs(n, K, F, dtype, seed)
-    g = torch.Generator().manual_seed(n + F)
-    A = (2 * torch.randn(n, F, generator=g)).to(dtype).cuda() if name != "none" else None
+    g = torch.Generator("cuda").manual_seed(n + F)
+    A = (2 * torch.randn(n, F, generator=g, device="cuda")).to(dtype) if name != "none" else None
     e = lambda *s, dt=F32: torch.full(s, 3.0, dtype=dt, device="cuda")
     out = {"dW": e(K, F), "db": e(F), "dX": e(n, K, dt=dtype), "dA": e(n, F, dt=dtype)}
     out = {k: v if k in want else None for k, v in out.items()}
     work, behind = scratch(n, K, F)
     sar.sar_linear_act_bwd(dY, A, X if "dW" in want else None, W, ACTS[name], accumulate, out["dW"], out["db"], out["dX"], out["dA"], work)
     assert bool((behind == 77).all())
-    x, w, d = nw.f64(X), nw.f64(W), nw.f64(dY)
+    x, w, d = f64(X), f64(W), f64(dY)
     off = 0 * d
     if name != "none":
-        a = nw.f64(A)
+        a = f64(A)
         _, slope, _, off_slope = act(name, a)
         # the derivative's own error and the product's rounding
-        off = np.abs(d) * (off_slope + 2 * nw.U * np.abs(slope))
+        off = d.abs() * (off_slope + 2 * nw.U * slope.abs())
         d = d * slope
     before = 3.0 if accumulate else 0.0
     many = n / 256 + 64                                     # a workgroup's rows, the workgroups
     if "dA" in want:
-        assert (np.abs(nw.f64(out["dA"]) - d) <= stored(dtype, off, d)).all()
+        assert ((f64(out["dA"]) - d).abs() <= stored(dtype, off, d)).all()
     if "db" in want:
-        tol = off.sum(0) + many * 2 * nw.U * (np.abs(d).sum(0) + before)
-        assert (np.abs(nw.f64(out["db"]) - before - d.sum(0)) <= tol).all()
+        tol = off.sum(0) + many * 2 * nw.U * (d.abs().sum(0) + before)
+        assert ((f64(out["db"]) - before - d.sum(0)).abs() <= tol).all()
     if "dW" in want:
-        size = np.abs(x).T @ np.abs(d)
+        size = x.abs().T @ d.abs()
         # (bf16: dA in two pieces, each rounded to 8 bits)
-        tol = np.abs(x).T @ off + 2 * dw_off(size + before, n) + (2.0 ** -17 * size if dtype == BF16 and name != "none" else 0) + 4 * nw.U * before
-        assert (np.abs(nw.f64(out["dW"]) - before - x.T @ d) <= tol).all()
+        tol = x.abs().T @ off + 2 * dw_off(size + before, n) + (2.0 ** -17 * size if dtype == BF16 and name != "none" else 0) + 4 * nw.U * before
+        assert ((f64(out["dW"]) - before - x.T @ d).abs() <= tol).all()
     if "dX" in want:
-        want_x, size = d @ w.T, np.abs(d) @ np.abs(w).T
-        tol = off @ np.abs(w).T + rows_off(size, F, dtype) + (2.0 ** -8 * size if dtype == BF16 and name != "none" else 0)
-        assert (np.abs(nw.f64(out["dX"]) - want_x) <= stored(dtype, tol, want_x)).all()
+        want_x, size = d @ w.T, d.abs() @ w.abs().T
+        tol = off @ w.abs().T + rows_off(size, F, dtype) + (2.0 ** -8 * size if dtype == BF16 and name != "none" else 0)
+        assert ((f64(out["dX"]) - want_x).abs() <= stored(dtype, tol, want_x)).all()
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -212,15 +215,14 @@ def test_activations_over_their_range(name, dtype):
     Y = torch.empty(n, 2, dtype=dtype, device="cuda")
     work, _ = scratch(n, 2, 2)
     sar.sar_linear_act_fwd(X, W, None, None, ACTS[name], False, Y, None, work)
-    a = nw.f64(X)[:, 0]
-    with np.errstate(over="ignore"):
-        y, slope, off_y, off_slope = act(name, a)
-    tol = off_y + 4 * nw.U * np.abs(a) + 1e-37
-    assert (np.abs(nw.f64(Y)[:, 0] - y) <= stored(dtype, tol, y)).all()
-    assert (nw.f64(Y)[:, 1] == 0).all()
+    a = f64(X)[:, 0]
+    y, slope, off_y, off_slope = act(name, a)
+    tol = off_y + 4 * nw.U * a.abs() + 1e-37
+    assert ((f64(Y)[:, 0] - y).abs() <= stored(dtype, tol, y)).all()
+    assert (f64(Y)[:, 1] == 0).all()
     dA, one = torch.empty_like(X), torch.ones_like(X)
     sar.sar_linear_act_bwd(one, X, None, W, ACTS[name], False, None, None, None, dA, work)
-    assert (np.abs(nw.f64(dA)[:, 0] - slope) <= stored(dtype, off_slope + 1e-37, slope)).all()
+    assert ((f64(dA)[:, 0] - slope).abs() <= stored(dtype, off_slope + 1e-37, slope)).all()
     odd = torch.tensor([[float("inf"), 0], [-float("inf"), 0], [float("nan"), 0]]).to(dtype).cuda()
     b = torch.zeros(2, device="cuda")
     Y, A = torch.empty_like(odd), odd.clone()
@@ -263,7 +265,7 @@ def test_gradients_by_differences():
     n, K, F = 3, 4, 5
     X, W, b, R = inputs(n, K, F, F32)
     work, _ = scratch(n, K, F)
-    x, w, bb, g = nw.f64(X), nw.f64(W), nw.f64(b), nw.f64(R)
+    x, w, bb, g = f64(X), f64(W), f64(b), f64(R)
     step = 1e-5
     for name in ("gelu", "silu", "none"):
         Y, A, dW, db, dX = torch.empty_like(R), torch.empty_like(R), torch.empty_like(W), torch.empty_like(b), torch.empty_like(X)
@@ -272,11 +274,11 @@ def test_gradients_by_differences():
         total = lambda x, w, bb: (act(name, x @ w + bb)[0] * g).sum()
         for v, got in ((0, dX), (1, dW), (2, db)):
             args = [x, w, bb]
-            flat = nw.f64(got).ravel()
-            for i in range(flat.size):
+            flat = f64(got).flatten()
+            for i in range(flat.numel()):
                 s = []
                 for sign in (1, -1):
-                    moved = [t.copy() for t in args]
-                    moved[v].flat[i] += sign * step
+                    moved = [t.clone() for t in args]
+                    moved[v].view(-1)[i] += sign * step
                     s.append(total(*moved))
                 assert abs((s[0] - s[1]) / (2 * step) - flat[i]) < 1e-5
