@@ -52,24 +52,30 @@ struct Unit {
     using T = typename R::T;
     static constexpr int kRegs = 8 * (int)sizeof(T) * 2 / 4;
     // c: column of the tensor (its rows are `width` values wide)
-    static __device__ SAR_INLINE inline void load(uint32_t* w, const T* base, int group, int rows, bool full, int c, int width)
+    static __device__ SAR_INLINE inline void load_full(uint32_t* w, const T* base, int group, int c, int width)
     {
         const uint32_t bytes = (uint32_t)width * sizeof(T);
         const char* p = reinterpret_cast<const char*>(base);
-        if (full && width >= 2) {
-            const uint32_t at = (uint32_t)min(c, width - 2) * sizeof(T) + (uint32_t)group * 8 * bytes;
+        const uint32_t at = (uint32_t)min(c, width - 2) * sizeof(T) + (uint32_t)group * 8 * bytes;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                if constexpr (sizeof(T) == 4) {
-                    struct __attribute__((packed, aligned(4))) V { uint32_t x, y; };
-                    const V v = *reinterpret_cast<const V*>(p + (at + (uint32_t)k * bytes));
-                    w[2 * k] = v.x, w[2 * k + 1] = v.y;
-                } else {
-                    struct __attribute__((packed, aligned(2))) V { uint32_t x; };
-                    w[k] = reinterpret_cast<const V*>(p + (at + (uint32_t)k * bytes))->x;
-                }
+        for (int k = 0; k < 8; ++k) {
+            if constexpr (sizeof(T) == 4) {
+                struct __attribute__((packed, aligned(4))) V { uint32_t x, y; };
+                const V v = *reinterpret_cast<const V*>(p + (at + (uint32_t)k * bytes));
+                w[2 * k] = v.x, w[2 * k + 1] = v.y;
+            } else {
+                struct __attribute__((packed, aligned(2))) V { uint32_t x; };
+                w[k] = reinterpret_cast<const V*>(p + (at + (uint32_t)k * bytes))->x;
             }
+        }
+    }
+    static __device__ SAR_INLINE inline void load(uint32_t* w, const T* base, int group, int rows, bool full, int c, int width)
+    {
+        if (full && width >= 2) {
+            load_full(w, base, group, c, width);
         } else {
+            const uint32_t bytes = (uint32_t)width * sizeof(T);
+            const char* p = reinterpret_cast<const char*>(base);
             // value by value (a type's or a workgroup's last rows; rows of one value); addresses worked out here, not kept through the loop
             asm volatile("" : "+v"(c), "+v"(group));
             const uint32_t first = (uint32_t)min(c, max(width - 2, 0)) * sizeof(T), second = min(first + (uint32_t)sizeof(T), bytes - (uint32_t)sizeof(T));
@@ -129,6 +135,11 @@ struct Unit {
 struct FormedUnit {
     using Plain = Unit<Bf16Rows>;
     static constexpr int kRegs = 2 * Plain::kRegs;
+    static __device__ SAR_INLINE inline void load_full(uint32_t* w, const bf16_t* base, const bf16_t* pre, int group, int c, int width)
+    {
+        Plain::load_full(w, base, group, c, width);
+        Plain::load_full(w + Plain::kRegs, pre, group, c, width);
+    }
     static __device__ SAR_INLINE inline void load(uint32_t* w, const bf16_t* base, const bf16_t* pre, int group, int rows, bool full, int c, int width)
     {
         Plain::load(w, base, group, rows, full, c, width);
@@ -288,7 +299,9 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
         asm volatile("" : "+v"(v));
         return v;
     };
-    auto fetch = [&](Chunk& raw, int64_t r0, int64_t end) SAR_INLINE {
+    // (WHOLE: a full chunk of rows of at least two values)
+    auto fetch = [&](auto whole, Chunk& raw, int64_t r0, int64_t end) SAR_INLINE {
+        constexpr bool WHOLE = decltype(whole)::value;
         const int rows = (int)min(end - r0, (int64_t)(16 * S));
         const bool full = rows == 16 * S;
         const int lane = anew(threadIdx.x & 63);
@@ -299,6 +312,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
             const int g = id / (TK / XR::kCols), c = k0 + id % (TK / XR::kCols) * XR::kCols;
             if constexpr (XR::kCols == 4)
                 PackedUnit::load(raw.x[u], a.Xq + r0 * packed_stride(a.K), a.Xe + r0 * packed_steps(a.K), g, rows, full, c, a.K);
+            else if constexpr (WHOLE)
+                Unit<XR>::load_full(raw.x[u], static_cast<const typename XR::T*>(a.X) + r0 * a.K, g, c, a.K);
             else
                 Unit<XR>::load(raw.x[u], static_cast<const typename XR::T*>(a.X) + r0 * a.K, g, rows, full, c, a.K);
         }
@@ -307,14 +322,18 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
             const int first = wave * 64 + u * kThreads, id = first + lane;
             if (first >= kZUnits || (kZUnits % 64 && id >= kZUnits)) continue;
             const int g = id / (TF / 2), c = f0 + id % (TF / 2) * 2;
-            if constexpr (ZTraits<ZR>::kFormed)
+            if constexpr (ZTraits<ZR>::kFormed && WHOLE)
+                FormedUnit::load_full(raw.z[u], static_cast<const bf16_t*>(a.dZ) + r0 * a.F, static_cast<const bf16_t*>(a.pre) + r0 * a.F, g, c, a.F);
+            else if constexpr (WHOLE)
+                Unit<Plain>::load_full(raw.z[u], static_cast<const typename ZR::T*>(a.dZ) + r0 * a.F, g, c, a.F);
+            else if constexpr (ZTraits<ZR>::kFormed)
                 FormedUnit::load(raw.z[u], static_cast<const bf16_t*>(a.dZ) + r0 * a.F, static_cast<const bf16_t*>(a.pre) + r0 * a.F, g, rows, full, c, a.F);
             else
                 Unit<Plain>::load(raw.z[u], static_cast<const typename ZR::T*>(a.dZ) + r0 * a.F, g, rows, full, c, a.F);
         }
     };
-    auto put = [&](Chunk& raw, int64_t r0, int64_t end, uint4* buf, bool negate) SAR_INLINE {
-        const int rows = (int)min(end - r0, (int64_t)(16 * S));
+    auto put = [&](auto whole, Chunk& raw, int64_t r0, int64_t end, uint4* buf, bool negate) SAR_INLINE {
+        const int rows = decltype(whole)::value ? 16 * S : (int)min(end - r0, (int64_t)(16 * S));
         const bool full = rows == 16 * S;
         const int lane = anew(threadIdx.x & 63);
 #pragma unroll
@@ -363,9 +382,10 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
             // Which sign X has in chunk i, so that what the matrix unit cuts leans to neither side.  Bf16 products, which are added to the sums
             // there: the other sign every four chunks (of formed rows sixteen) and in every other workgroup, with the sums turned round where it changes.
             auto minus = [&](int i) SAR_INLINE { return kThere ? (((i >> (ZTraits<ZR>::kFormed ? 4 : 2)) + (int)blockIdx.x) & 1) != 0 : (i & 1) != 0; };
-            auto step = [&](int i, int64_t r0, Chunk& later, Chunk& next) SAR_INLINE {
+            constexpr std::integral_constant<bool, false> part{};
+            auto step = [&](auto whole, int i, int64_t r0, Chunk& later, Chunk& next) SAR_INLINE {
                 constexpr int kRows = 16 * S;
-                if (r0 + AHEAD * kRows < end) fetch(later, r0 + AHEAD * kRows, end);
+                if (decltype(whole)::value || r0 + AHEAD * kRows < end) fetch(whole, later, r0 + AHEAD * kRows, end);
                 const uint4* xb = lds + (i & 1) * kSize + wm * MT * 32 + (lane & 31);
                 const uint4* zb = lds + (i & 1) * kSize + kXSize + wn * NT * 32 + (lane & 31);
                 if constexpr (kThere) {
@@ -427,19 +447,30 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
                         add(MT * NT - 1, last);
                     }
                 }
-                if (r0 + kRows < end) put(next, r0 + kRows, end, lds + ((i & 1) ^ 1) * kSize, minus(i + 1));
+                if (decltype(whole)::value || r0 + kRows < end) put(whole, next, r0 + kRows, end, lds + ((i & 1) ^ 1) * kSize, minus(i + 1));
                 __syncthreads();
             };
-            fetch(raw[0], first, end);
-            if (AHEAD == 2 && first + 16 * S < end) fetch(raw[1 % AHEAD], first + 16 * S, end);
-            put(raw[0], first, end, lds, minus(0));
+            fetch(part, raw[0], first, end);
+            if (AHEAD == 2 && first + 16 * S < end) fetch(part, raw[1 % AHEAD], first + 16 * S, end);
+            put(part, raw[0], first, end, lds, minus(0));
             __syncthreads();
             int chunks = 0;
-            for (int64_t r0 = first; r0 < end;) {
-                step(chunks, r0, raw[0], raw[1 % AHEAD]);
+            int64_t r0 = first;
+            // As long as the chunks to come are full ones: loads without a branch, which would have all of them waited for (their number is not known behind it;
+            // 306250 x 256 -> 256 fp32, both products, 597 us for 617, 867187 bf16 835 for 850).
+            //
+            if (ZTraits<ZR>::kSums && a.K >= 2 && a.F >= 2) {
+                constexpr std::integral_constant<bool, true> whole{};
+                for (; r0 + (2 * AHEAD + 1) * 16 * S <= end; r0 += AHEAD * 16 * S) {
+                    step(whole, chunks++, r0, raw[0], raw[1 % AHEAD]);
+                    if (AHEAD == 2) step(whole, chunks++, r0 + 16 * S, raw[1 % AHEAD], raw[0]);
+                }
+            }
+            while (r0 < end) {
+                step(part, chunks, r0, raw[0], raw[1 % AHEAD]);
                 ++chunks, r0 += 16 * S;
                 if (AHEAD == 1 || r0 >= end) continue;
-                step(chunks, r0, raw[1 % AHEAD], raw[0]);
+                step(part, chunks, r0, raw[1 % AHEAD], raw[0]);
                 ++chunks, r0 += 16 * S;
             }
             if (kThere && minus(chunks - 1)) {
