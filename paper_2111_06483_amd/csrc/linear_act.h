@@ -130,16 +130,15 @@ __device__ inline float formed_value(const ActPrologue& p, float d, int64_t at)
     return value_of(from_f32<T>(d));
 }
 
-// One value of the product, column n, place `at` of the rows.
+// One value of the product, place `at` of the rows, with its bias and residual.
 template <typename T>
-__device__ inline float finish_value(const Epilogue& e, float v, int64_t at, int n)
+__device__ inline float finish_value(const Epilogue& e, float v, float bias, float res, int64_t at)
 {
-    if (e.bias) v += e.bias[n];
-    const float r = e.res ? value_of(static_cast<const T*>(e.res)[at]) : 0.f;
-    if (!e.after) v += r;
+    v += bias;
+    if (!e.after) v += res;
     if (e.pre) static_cast<T*>(e.pre)[at] = from_f32<T>(v);
     with_act(e.act, [&](auto act) { v = act_of<decltype(act)::value>(v); });
-    return e.after ? v + r : v;
+    return e.after ? v + res : v;
 }
 
 // dW (+)= X^T dA and db (+)= the sums of dA's columns, dA = dY act'(A) formed where it is read (bf16), or dY as it is (act 0, pre null); db may be

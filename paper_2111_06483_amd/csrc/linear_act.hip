@@ -136,6 +136,12 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
     const bool formed = act != SAR_ACT_NONE;
     const Types types{nullptr, 1, n};
     const bool few_dw = few_rows_dw(n, 1, K, F), few_dx = few_blocks(types, K);
+    // Few rows: one launch, but for what would have no kernel there to write it (db without dW, for which there need be no X; dA without dX, or of no
+    // activation).
+    if (few_dw && few_dx && n > 0 && (!db || dW) && (!dA || (formed && dX)) && (dW || dX)) {
+        const TypedDw g{X, nullptr, nullptr, dY, dW, types, K, F, accumulate, nullptr, formed ? A : nullptr, act, db};
+        return few_act_bwd(dtype, g, {dY, W, dX, types, F, K, K, F}, dA, st);
+    }
     // What forms dA: the product for dX of many rows, in bf16 the one for dW too; otherwise a launch of its own.
     const bool within = formed && dX && n > 0 && !few_dx, again = formed && dW && !few_dw && sizeof(T) == 2;
     const bool reads = (dW && !again) || (dX && !within);

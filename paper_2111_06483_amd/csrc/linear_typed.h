@@ -33,6 +33,9 @@ struct TypedDw {
     Types types;
     int K, F, accumulate;
     float* partial;
+    const void* pre = nullptr;     // (these three: few_act_bwd)
+    int act = 0;
+    float* sums = nullptr;
 };
 size_t typed_dw_bytes(int64_t n, int K, int F, int T);
 int typed_dw(int dtype, const TypedDw& g, hipStream_t st);
@@ -53,6 +56,9 @@ int few_product(int dtype, bool trans, const TypedRows& a, const NoEpilogue&, hi
 int few_product(int dtype, bool trans, const TypedRows& a, const Epilogue& e, hipStream_t st);      // (not of W^T)
 int few_dw(int dtype, const TypedDw& g, hipStream_t st);
 int few_dw_and_dx(int dtype, const TypedDw& g, const TypedRows& a, hipStream_t st);
+// ... of the transform with its activation, one type: dW (null: not wanted, and no sums) with the sums of dA's columns (null: not wanted), dX (a.out; null: not wanted, and
+// no dA) with dA (null: not wanted), dA = dY act'(pre) formed where it is read; pre null: dY as it is.
+int few_act_bwd(int dtype, const TypedDw& g, const TypedRows& a, void* dA, hipStream_t st);
 
 // Operands of fp32 products are multiplied by 2^24 before they are cut into pieces of bf16, and sums by what takes that back where they are added up.  An
 // fp32 value is a multiple of 2^-149, so its pieces are then multiples of 2^-125, each a normal bf16 value, and a value keeps its bits however small it
@@ -75,6 +81,36 @@ struct PackedRows {
     static constexpr int kPieces = 1, kCols = 4;
 };
 
+// Rows of dZ whose columns are summed as well, and rows that are formed where they are read, dA = dY act'(A); of bf16 as two pieces of bf16.
+struct F32Sums : F32Rows {
+    static constexpr bool kSums = true, kFormed = false;
+    using Plain = F32Rows;
+};
+struct F32Formed : F32Rows {
+    static constexpr bool kSums = true, kFormed = true;
+    using Plain = F32Rows;
+};
+struct Bf16Sums : Bf16Rows {
+    static constexpr bool kSums = true, kFormed = false;
+    using Plain = Bf16Rows;
+};
+struct Bf16Formed {
+    using T = bf16_t;
+    static constexpr int kPieces = 2, kCols = 2;
+    static constexpr bool kSums = true, kFormed = true;
+    using Plain = Bf16Rows;
+};
+template <typename ZR, typename = void>
+struct ZTraits {
+    static constexpr bool kSums = false, kFormed = false;
+    using Plain = ZR;
+};
+template <typename ZR>
+struct ZTraits<ZR, std::void_t<typename ZR::Plain>> {
+    static constexpr bool kSums = ZR::kSums, kFormed = ZR::kFormed;
+    using Plain = typename ZR::Plain;
+};
+
 struct DwArgs {
     const void* X;
     const int8_t* Xq;
@@ -84,7 +120,7 @@ struct DwArgs {
     Types types;
     int K, F;
     int64_t share;         // rows of a workgroup
-    // of linear_act_dw.hip alone: what dZ is formed with, and the sums of its columns, [workgroups, F], or null
+    // of the transform with its activation alone: what dZ is formed with, and the sums of its columns ([workgroups, F]; of few rows [F] itself), or null
     const void* pre = nullptr;
     int act = 0;
     float* sums = nullptr;

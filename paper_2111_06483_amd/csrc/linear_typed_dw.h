@@ -19,32 +19,6 @@ constexpr int kChunk32 = 16, kChunk16 = 32;          // rows of a chunk: fp32, b
 __device__ inline int place_of(int c) { return (c & ~63) | (c & 1) << 5 | (c >> 1 & 31); }
 __device__ inline int column_at(int p) { return (p & ~63) | (p & 31) << 1 | (p >> 5 & 1); }
 
-// Rows of dZ whose columns are summed as well, and rows of bf16 that are formed where they are read, dA = dY act'(A), and multiplied as two pieces of bf16.
-struct F32Sums : F32Rows {
-    static constexpr bool kSums = true, kFormed = false;
-    using Plain = F32Rows;
-};
-struct Bf16Sums : Bf16Rows {
-    static constexpr bool kSums = true, kFormed = false;
-    using Plain = Bf16Rows;
-};
-struct Bf16Formed {
-    using T = bf16_t;
-    static constexpr int kPieces = 2, kCols = 2;
-    static constexpr bool kSums = true, kFormed = true;
-    using Plain = Bf16Rows;
-};
-template <typename ZR, typename = void>
-struct ZTraits {
-    static constexpr bool kSums = false, kFormed = false;
-    using Plain = ZR;
-};
-template <typename ZR>
-struct ZTraits<ZR, std::void_t<typename ZR::Plain>> {
-    static constexpr bool kSums = ZR::kSums, kFormed = ZR::kFormed;
-    using Plain = typename ZR::Plain;
-};
-
 // Eight rows of kCols columns of a tile on their way from memory to LDS.  `base` is the chunk's first row, the same for all lanes; a chunk
 // that is not full reads its last row again in place of those that are not there, and counts them as zeros.
 template <typename R>

@@ -49,8 +49,8 @@ __device__ inline bool few_rows_of(const Types& types, int64_t index, int& t, in
 
 // PARTS: wavefronts that share one block's contraction, chunk by chunk, and add up in LDS (4), or one a block (1), of a workgroup of WAVES.  `row`: which
 // block of rows; `beside`: which of the groups of column tiles that a workgroup takes; `sums`: [WAVES][16][64].
-template <typename T, bool TRANS, int PARTS, int WAVES, typename E = NoEpilogue>
-__device__ SAR_INLINE inline void few_rows(const TypedRows& a, int64_t row_block, int beside, float* sums, const E& e = {})
+template <typename T, bool TRANS, int PARTS, int WAVES, typename E = NoEpilogue, typename Q = NoPrologue>
+__device__ SAR_INLINE inline void few_rows(const TypedRows& a, int64_t row_block, int beside, float* sums, const E& e = {}, const Q& prologue = {})
 {
     constexpr int N = Cols<T>::N, kRaw = 8 / N, U = 4;                // 16-byte pieces of a row a product of 16; products a chunk
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, share = wave % PARTS;
@@ -66,10 +66,17 @@ __device__ SAR_INLINE inline void few_rows(const TypedRows& a, int64_t row_block
     const float* W = a.W + (int64_t)t * a.K * a.F;
     const int nc = min(n, a.N - 1);
     struct Chunk {
-        uint4 x[U][kRaw];
+        uint4 x[U][kRaw], pre[Q::kAny ? U : 1][kRaw];
         float w[U][8];
     };
     auto load = [&](Chunk& g, int k0) SAR_INLINE {
+        if constexpr (Q::kAny) {
+            const T* pre = static_cast<const T*>(prologue.pre) + i * a.C;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int p = 0; p < kRaw; ++p) g.pre[u][p] = Cols<T>::load(pre, k0 + u * 16 + h * 8 + p * N, a.C, left);
+        }
         const float* w = TRANS ? W + (int64_t)nc * a.F : W + nc;
         if (k0 + 16 * U <= a.C) {          // the same for all lanes: one run of loads
 #pragma unroll
@@ -101,11 +108,26 @@ __device__ SAR_INLINE inline void few_rows(const TypedRows& a, int64_t row_block
         }
     };
     float16_t acc[1] = {};
-    auto multiply = [&](const Chunk& g, int k0) SAR_INLINE {
+    auto multiply = [&](Chunk& g, int k0) SAR_INLINE {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int c = k0 + u * 16 + h * 8;
             if (k0 + u * 16 >= a.C) break;
+            if constexpr (Q::kAny) {
+#pragma unroll
+                for (int p = 0; p < kRaw; ++p) {
+                    const uint4 m = Cols<T>::within(c + p * N, a.C);
+                    auto cut = [&](uint4& v) SAR_INLINE { v = make_uint4(v.x & m.x, v.y & m.y, v.z & m.z, v.w & m.w); };
+                    cut(g.x[u][p]);
+                    cut(g.pre[u][p]);
+                    form_piece<T>(prologue.act, g.x[u][p], g.pre[u][p]);
+                    if (prologue.formed && n0 == 0 && first + (lane & 31) < end) {
+                        float v[N];
+                        Cols<T>::unpack(g.x[u][p], v);
+                        Cols<T>::store(static_cast<T*>(prologue.formed) + i * a.C, c + p * N, a.C, v);
+                    }
+                }
+            }
             float w[8], x[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) w[j] = c + j < a.C ? g.w[u][j] * (sizeof(T) == 4 ? kUp : 1.f) : 0.f;
@@ -153,18 +175,33 @@ __device__ SAR_INLINE inline void few_rows(const TypedRows& a, int64_t row_block
                     const bool in = k + h < a.C;
                     float x = 0.f, w = 0.f;
                     if (in) {
-                        if constexpr (sizeof(T) == 4) x = row[k + h];
-                        else x = bf16_to_f32(row[k + h]);
+                        x = value_of(row[k + h]);
+                        if constexpr (Q::kAny) x = formed_value<T>(prologue, x, i * a.C + k + h);
                         w = TRANS ? W[(int64_t)nc * a.F + k + h] : W[(int64_t)(k + h) * a.F + nc];
                     }
                     acc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w, acc[0], 0, 0, 0);
                 }
         }
     }
-    auto store = [&](int r, float v) SAR_INLINE {
+    // (residuals are read together, before the first is waited for)
+    constexpr int kMine = PARTS == 4 ? 4 : 16;
+    const int r0 = PARTS == 4 ? share * 4 : 0;
+    float res[E::kAny ? kMine : 1] = {}, bias = 0.f;
+    if constexpr (E::kAny) {
+        if (e.bias) bias = e.bias[nc];
+        if (e.res) {
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) {
+                const int r = r0 + j;
+                res[j] = value_of(static_cast<const T*>(e.res)[min(first + 8 * (r / 4) + 4 * h + r % 4, end - 1) * a.N + nc]);
+            }
+        }
+    }
+    auto store = [&](int j, float v) SAR_INLINE {
+        const int r = r0 + j;
         const int64_t o = first + 8 * (r / 4) + 4 * h + r % 4;
         if (n < a.N && o < end) {
-            if constexpr (E::kAny) v = finish_value<T>(e, v, o * a.N + n, n);
+            if constexpr (E::kAny) v = finish_value<T>(e, v, bias, res[j], o * a.N + n);
             static_cast<T*>(a.out)[o * a.N + n] = from_f32<T>(v);
         }
     };
@@ -176,7 +213,7 @@ __device__ SAR_INLINE inline void few_rows(const TypedRows& a, int64_t row_block
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int r = share * 4 + j;
-            store(r, (part[0][r][lane] + part[1][r][lane]) + (part[2][r][lane] + part[3][r][lane]));
+            store(j, (part[0][r][lane] + part[1][r][lane]) + (part[2][r][lane] + part[3][r][lane]));
         }
     } else {
 #pragma unroll
@@ -198,9 +235,12 @@ __device__ SAR_INLINE inline void few_weights(const DwArgs& a, int accumulate, f
     int64_t lo, hi;
     a.types.span(t, lo, hi);
     float16_t acc = {};
+    using Z = ZTraits<ZR>;
+    using Plain = typename Z::Plain;
     struct Step {
-        float x[U][8], z[U][8];
+        float x[U][8], z[U][8], pre[Z::kFormed ? U : 1][8];
     };
+    float column = 0.f;        // sum of dZ's column f over this lane's rows
     auto load = [&](Step& s, int64_t r0) SAR_INLINE {
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -208,7 +248,8 @@ __device__ SAR_INLINE inline void few_weights(const DwArgs& a, int accumulate, f
             for (int j = 0; j < 8; ++j) {
                 const int64_t r = min(r0 + u * kTurn + h * 8 + j, hi - 1);
                 s.x[u][j] = x_value<XR>(a, r, k);
-                s.z[u][j] = z_value<ZR>(a, r, f);
+                s.z[u][j] = z_value<Plain>(a, r, f);
+                if constexpr (Z::kFormed) s.pre[u][j] = value_of(static_cast<const typename ZR::T*>(a.pre)[r * a.F + f]);
             }
     };
     auto multiply = [&](Step& s, int64_t r0) SAR_INLINE {
@@ -216,10 +257,17 @@ __device__ SAR_INLINE inline void few_weights(const DwArgs& a, int accumulate, f
         for (int u = 0; u < U; ++u) {
             if (r0 + u * kTurn >= hi) break;
             float x[8], z[8];
+            if constexpr (Z::kFormed) {
+                with_act(a.act, [&](auto which) SAR_INLINE {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) s.z[u][j] = act_grad<decltype(which)::value>(s.z[u][j], s.pre[u][j]);
+                });
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const bool in = r0 + u * kTurn + h * 8 + j < hi;
                 x[j] = in ? s.x[u][j] : 0.f, z[j] = in ? s.z[u][j] : 0.f;
+                if constexpr (Z::kSums) column += z[j];
             }
             uint4 p[3], q[3];
             auto whole = [](const float (&v)[8]) SAR_INLINE {        // (bf16 values: not rounded)
@@ -238,6 +286,15 @@ __device__ SAR_INLINE inline void few_weights(const DwArgs& a, int accumulate, f
                 split8(z, q);
             } else {
                 q[0] = whole(z);
+                if constexpr (PZ == 2) {
+                    const uint32_t words[4] = {q[0].x, q[0].y, q[0].z, q[0].w};
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float left = z[j] - __uint_as_float(j % 2 ? words[j / 2] & 0xffff0000u : words[j / 2] << 16);
+                        z[j] = fabsf(left) < __builtin_inff() ? left : 0.f;        // (an infinity has no second piece)
+                    }
+                    q[1] = whole(z);
+                }
             }
             float16_t sum = {};
 #pragma unroll
@@ -248,6 +305,14 @@ __device__ SAR_INLINE inline void few_weights(const DwArgs& a, int accumulate, f
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[r] = fmaf(sum[r], (PX == 3 ? kDown : 1.f) * (PZ == 3 ? kDown : 1.f), acc[r]);
         }
+    };
+    auto whole_z = [&](int64_t r) SAR_INLINE {
+        float v = z_value<Plain>(a, r, f);
+        if constexpr (Z::kFormed) {
+            const float pre = value_of(static_cast<const typename ZR::T*>(a.pre)[r * a.F + f]);
+            with_act(a.act, [&](auto which) { v = act_grad<decltype(which)::value>(v, pre); });
+        }
+        return v;
     };
     const int64_t from = lo + wave * 16;
     constexpr int kNext = U * kTurn;
@@ -266,12 +331,26 @@ __device__ SAR_INLINE inline void few_weights(const DwArgs& a, int accumulate, f
             for (int64_t r0 = from; r0 < hi; r0 += kTurn)
                 for (int64_t r = r0; r < min(r0 + 16, hi); r += 2) {
                     const bool in = r + h < hi;
-                    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(in ? x_value<XR>(a, r + h, k) : 0.f, in ? z_value<ZR>(a, r + h, f) : 0.f, acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(in ? x_value<XR>(a, r + h, k) : 0.f, in ? whole_z(r + h) : 0.f, acc, 0, 0, 0);
                 }
         }
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) part[wave][r][lane] = acc[r];
+    if constexpr (Z::kSums) {
+        if (a.sums && k0 == 0) {           // (the same for all of the workgroup)
+            __shared__ float columns[WAVES][32];
+            column += __shfl_xor(column, 32);
+            if (h == 0) columns[wave][lane] = column;
+            __syncthreads();
+            if (wave == 0 && h == 0 && f0 + lane < a.F) {
+                float v = 0.f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) v += columns[w][lane];
+                a.sums[f] = accumulate ? a.sums[f] + v : v;
+            }
+        }
+    }
     __syncthreads();
     // lane holds column f; register r holds weight row 8*(r/4) + 4*h + r%4: two registers a wavefront
     if (f0 + (lane & 31) >= a.F) return;
@@ -289,11 +368,11 @@ __device__ SAR_INLINE inline void few_weights(const DwArgs& a, int accumulate, f
 
 // ---- launches
 
-template <typename T, bool TRANS, int PARTS, typename E>
-__global__ __launch_bounds__(256, 2) void k_typed_few(TypedRows a, E e)
+template <typename T, bool TRANS, int PARTS, typename E, typename Q>
+__global__ __launch_bounds__(256, 2) void k_typed_few(TypedRows a, E e, Q prologue)
 {
     __shared__ float sums[PARTS == 4 ? 4 * 16 * 64 : 1];
-    few_rows<T, TRANS, PARTS, 4>(a, blockIdx.x, blockIdx.y, sums, e);
+    few_rows<T, TRANS, PARTS, 4>(a, blockIdx.x, blockIdx.y, sums, e, prologue);
 }
 
 template <typename XR, typename ZR, int WAVES>
@@ -304,14 +383,14 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_dw_few(DwArgs a, int ac
 }
 
 // Both: workgroups from `rows_from` on (as many as there are) take dX, the others dW.
-template <typename XR, typename ZR, int WAVES, int PARTS>
+template <typename XR, typename ZR, int WAVES, int PARTS, typename Q>
 __global__ __launch_bounds__(WAVES * 64, 2) void k_typed_few_bwd(DwArgs a, int accumulate, float* dW, TypedRows g, unsigned across, unsigned down, unsigned rows_from,
-                                                                 unsigned rows, unsigned beside)
+                                                                 unsigned rows, unsigned beside, Q prologue)
 {
     __shared__ float sums[WAVES * 16 * 64];
     const unsigned i = blockIdx.x - rows_from;
     if (i < rows) {
-        few_rows<typename ZR::T, true, PARTS, WAVES>(g, i / beside, i % beside, sums);
+        few_rows<typename ZR::T, true, PARTS, WAVES>(g, i / beside, i % beside, sums, NoEpilogue{}, prologue);
     } else {
         const unsigned w = blockIdx.x < rows_from ? blockIdx.x : blockIdx.x - rows;
         few_weights<XR, ZR, WAVES>(a, accumulate, dW, w % across * 32, w / across % down * 32, w / across / down, sums);
@@ -326,17 +405,17 @@ bool shared_blocks(const TypedRows& a) { return a.C > 64 && row_blocks(a.types) 
 // types, 400 x 512, 30.7 and 15.7).
 bool eight_waves(const Types& types) { return types.n > 64 * (int64_t)types.T; }
 
-template <typename T, bool TRANS, typename E = NoEpilogue>
-int product(const TypedRows& a, hipStream_t st, const E& e = {})
+template <typename T, bool TRANS, typename E = NoEpilogue, typename Q = NoPrologue>
+int product(const TypedRows& a, hipStream_t st, const E& e = {}, const Q& q = {})
 {
     const unsigned groups = (unsigned)row_blocks(a.types);
-    if (shared_blocks(a)) k_typed_few<T, TRANS, 4, E><<<dim3(groups, (a.N + 31) / 32), 256, 0, st>>>(a, e);
-    else k_typed_few<T, TRANS, 1, E><<<dim3(groups, (a.N + 127) / 128), 256, 0, st>>>(a, e);
+    if (shared_blocks(a)) k_typed_few<T, TRANS, 4, E, Q><<<dim3(groups, (a.N + 31) / 32), 256, 0, st>>>(a, e, q);
+    else k_typed_few<T, TRANS, 1, E, Q><<<dim3(groups, (a.N + 127) / 128), 256, 0, st>>>(a, e, q);
     SAR_LAUNCH_CHECK();
     return SAR_OK;
 }
 
-DwArgs dw_args(const TypedDw& g) { return {g.X, g.Xq, g.Xe, g.dZ, g.partial, g.types, g.K, g.F, 0}; }
+DwArgs dw_args(const TypedDw& g) { return {g.X, g.Xq, g.Xe, g.dZ, g.partial, g.types, g.K, g.F, 0, g.pre, g.act, g.sums}; }
 
 template <typename XR, typename ZR>
 int weights(const TypedDw& g, hipStream_t st)
@@ -352,26 +431,40 @@ int weights(const TypedDw& g, hipStream_t st)
 // bits, together and apart: 300 x 256 -> 256 of 5 types 6.9 and 10.3 us, 2000 x 256 -> 256 of 8 types 18.1 and 23.3, 8000 x 256 -> 256 of 46 types 53.5 and 50.9, 4735 x 258 -> 400 of 46
 // 80.8 and 62.2).
 constexpr int64_t kBothWaves = 16384;
-template <typename XR, typename ZR, int WAVES, int PARTS>
-int both(const TypedDw& g, const TypedRows& a, hipStream_t st)
+template <typename XR, typename ZR, int WAVES, int PARTS, typename Q>
+int both(const TypedDw& g, const TypedRows& a, hipStream_t st, const Q& q)
 {
     const unsigned across = (g.K + 31) / 32, down = (g.F + 31) / 32, beside = (a.N + 32 * (WAVES / PARTS) - 1) / (32 * (WAVES / PARTS));
     const int64_t dw = (int64_t)across * down * g.types.T, dx = row_blocks(a.types) * beside;
     if ((dw + dx) * WAVES > kBothWaves) {
         SAR_TRY((weights<XR, ZR>(g, st)));
-        return product<typename ZR::T, true>(a, st);
+        return product<typename ZR::T, true>(a, st, NoEpilogue{}, q);
     }
     // the longer contraction first: they need not all fit at once
-    k_typed_few_bwd<XR, ZR, WAVES, PARTS><<<(unsigned)(dw + dx), WAVES * 64, 0, st>>>(dw_args(g), g.accumulate, g.dW, a, across, down,
-                                                                                    g.types.n < g.F ? 0u : (unsigned)dw, (unsigned)dx, beside);
+    k_typed_few_bwd<XR, ZR, WAVES, PARTS, Q><<<(unsigned)(dw + dx), WAVES * 64, 0, st>>>(dw_args(g), g.accumulate, g.dW, a, across, down,
+                                                                                    g.types.n < g.F ? 0u : (unsigned)dw, (unsigned)dx, beside, q);
     SAR_LAUNCH_CHECK();
     return SAR_OK;
 }
-template <typename XR, typename ZR>
-int both(const TypedDw& g, const TypedRows& a, hipStream_t st)
+template <typename XR, typename ZR, typename Q = NoPrologue>
+int both(const TypedDw& g, const TypedRows& a, hipStream_t st, const Q& q = {})
 {
-    if (eight_waves(g.types)) return shared_blocks(a) ? both<XR, ZR, 8, 4>(g, a, st) : both<XR, ZR, 8, 1>(g, a, st);
-    return shared_blocks(a) ? both<XR, ZR, 4, 4>(g, a, st) : both<XR, ZR, 4, 1>(g, a, st);
+    if (eight_waves(g.types)) return shared_blocks(a) ? both<XR, ZR, 8, 4>(g, a, st, q) : both<XR, ZR, 8, 1>(g, a, st, q);
+    return shared_blocks(a) ? both<XR, ZR, 4, 4>(g, a, st, q) : both<XR, ZR, 4, 1>(g, a, st, q);
+}
+
+// The transform's with its activation: dW with db, dX with dA, or one of the two.
+template <typename T, typename XR, typename FORMED, typename SUMS>
+int act_bwd(const TypedDw& g, const TypedRows& a, void* dA, hipStream_t st)
+{
+    const bool weights_too = g.dW != nullptr;
+    if (g.pre) {
+        const ActPrologue q{g.pre, dA, g.act};
+        if (weights_too && a.out) return both<XR, FORMED>(g, a, st, q);
+        return weights_too ? weights<XR, FORMED>(g, st) : product<T, true>(a, st, NoEpilogue{}, q);
+    }
+    if (weights_too && a.out) return both<XR, SUMS>(g, a, st);
+    return weights_too ? weights<XR, SUMS>(g, st) : product<T, true>(a, st);
 }
 
 }  // namespace
@@ -416,6 +509,11 @@ int few_dw_and_dx(int dtype, const TypedDw& g, const TypedRows& a, hipStream_t s
 {
     if (dtype == SAR_F32) return g.Xq ? both<PackedRows, F32Rows>(g, a, st) : both<F32Rows, F32Rows>(g, a, st);
     return g.Xq ? both<PackedRows, Bf16Rows>(g, a, st) : both<Bf16Rows, Bf16Rows>(g, a, st);
+}
+
+int few_act_bwd(int dtype, const TypedDw& g, const TypedRows& a, void* dA, hipStream_t st)
+{
+    return dtype == SAR_F32 ? act_bwd<float, F32Rows, F32Formed, F32Sums>(g, a, dA, st) : act_bwd<bf16_t, Bf16Rows, Bf16Formed, Bf16Sums>(g, a, dA, st);
 }
 
 }  // namespace sar
