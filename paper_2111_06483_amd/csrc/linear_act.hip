@@ -81,17 +81,18 @@ int groups_of(int dtype, int64_t n, int F)
     return (int)std::max<int64_t>(1, std::min<int64_t>((n + rows - 1) / rows, std::max(1, std::min(kActGroups, (1 << 22) / F))));
 }
 
-// Whether a product's operand is kept: rows enough for the copies of it to pay.
-template <typename T, typename P>
+// Whether a product's operand is kept.
+template <typename T>
 bool kept(int64_t n, int C, int N)
 {
-    return n >= 65536 && N >= 64 && (!P::kAny || N <= 32 * kKeptTiles) && fits_kept<T, P>(C);
+    const int64_t blocks = (N + 32 * kKeptTiles - 1) / (32 * kKeptTiles);
+    return n * blocks >= 65536 && N > 64 && fits_kept<T>(C);
 }
 
 template <typename T>
 int forward(const void* X, const float* W, int64_t n, void* Y, int K, int F, void* work, hipStream_t st, const Epilogue& e)
 {
-    if (kept<T, NoPrologue>(n, K, F)) return run_kept<T, false>(X, W, n, Y, K, F, work, st, e, NoPrologue{});
+    if (kept<T>(n, K, F)) return run_kept<T, false>(X, W, n, Y, K, F, work, st, e);
     return rows_product<T, false>(X, W, Types{nullptr, 1, n}, Y, K, F, work, st, e);
 }
 
@@ -159,11 +160,9 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
     if (sums) SAR_TRY(act_sum(partial, n > 0 ? groups_of(dtype, n, F) : 0, F, accumulate, db, st));
     if (dX && n > 0) {
         if (within) {
-            const ActPrologue q{A, rows, act};
-            if (kept<T, ActPrologue>(n, F, K)) SAR_TRY((run_kept<T, true>(dY, W, n, dX, K, F, work, st, NoEpilogue{}, q)));
-            else SAR_TRY((rows_product<T, true>(dY, W, types, dX, K, F, work, st, NoEpilogue{}, q)));
-        } else if (kept<T, NoPrologue>(n, F, K)) {
-            SAR_TRY((run_kept<T, true>(rows, W, n, dX, K, F, work, st, NoEpilogue{}, NoPrologue{})));
+            SAR_TRY((rows_product<T, true>(dY, W, types, dX, K, F, work, st, NoEpilogue{}, ActPrologue{A, rows, act})));
+        } else if (kept<T>(n, F, K)) {
+            SAR_TRY((run_kept<T, true>(rows, W, n, dX, K, F, work, st, NoEpilogue{})));
         } else {
             SAR_TRY((rows_product<T, true>(rows, W, types, dX, K, F, work, st)));
         }

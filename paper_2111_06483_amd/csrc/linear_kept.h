@@ -15,10 +15,9 @@ namespace {
 constexpr int kKeptWaves = 8, kKeptThreads = kKeptWaves * 64;
 constexpr size_t kKeptLds = 160 * 1024;
 
-template <typename E, typename P>
+template <typename E>
 struct KeptArgs {
     RowsArgs<E> rows;
-    P prologue;
     int64_t n;
 };
 
@@ -101,8 +100,8 @@ __device__ SAR_INLINE inline void finish_kept(const E& e, void* out, const Place
 }
 
 // CHUNKS: of the contraction; RES: a residual.
-template <typename T, int NT, int CHUNKS, bool TRANS, bool RES, typename E, typename P>
-__global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E, P> g)
+template <typename T, int NT, int CHUNKS, bool TRANS, bool RES, typename E>
+__global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E> g)
 {
     using Sh = WholeShare<T, NT>;
     const RowsArgs<E>& a = g.rows;
@@ -126,7 +125,7 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E, P> g)
     }
 
     const int tiles = (int)((g.n + 31) / 32), step = groups * kKeptWaves;
-    uint4 raw[CHUNKS][kRaw], pre[P::kAny ? CHUNKS : 1][kRaw];
+    uint4 raw[CHUNKS][kRaw];
     auto fetch = [&](int tile, int chunk) SAR_INLINE {
         int own = lane;
         asm volatile("" : "+v"(own));
@@ -136,50 +135,21 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E, P> g)
 #pragma unroll
         for (int k = 0; k < kRaw; ++k) {
             const uint32_t row = min((uint32_t)(8 * k + (own >> 3)), most) * (uint32_t)a.C;
-            auto piece = [&](const void* p) SAR_INLINE {
-                const T* rows = static_cast<const T*>(p) + r0 * a.C;
-                // (rows of less than a piece: one chunk, value by value)
-                if (CHUNKS > 1 || a.C >= N) return load16(within_tile<const T>(rows, (row + (uint32_t)min(c, a.C - N)) * (uint32_t)sizeof(T)));
-                return Cols<T>::load(rows + row, c, a.C, a.C);
-            };
-            raw[chunk][k] = piece(a.A);
-            if constexpr (P::kAny) pre[chunk][k] = piece(g.prologue.pre);
+            const T* rows = static_cast<const T*>(a.A) + r0 * a.C;
+            // (rows of less than a piece: one chunk, value by value)
+            raw[chunk][k] = CHUNKS > 1 || a.C >= N ? load16(within_tile<const T>(rows, (row + (uint32_t)min(c, a.C - N)) * (uint32_t)sizeof(T)))
+                                                   : Cols<T>::load(rows + row, c, a.C, a.C);
         }
     };
     uint4* const rows = lds + kStages * kFrags * 64 + wave * 256;
     // a chunk, from the lanes that brought it to those that multiply it
-    auto hand_over = [&](int tile, int chunk, uint4 (&x)[kRaw]) SAR_INLINE {
+    auto hand_over = [&](int chunk, uint4 (&x)[kRaw]) SAR_INLINE {
         const int c = chunk * CH + (lane & 7) * N;
         if (chunk == CHUNKS - 1 && c + N > a.C) {
-            auto cut = [&](uint4& v) SAR_INLINE {
-                if (c >= a.C) v = make_uint4(0u, 0u, 0u, 0u);
-                else if (a.C >= N) v = front_of_piece<T>(v, a.C - c);
-            };
 #pragma unroll
             for (int k = 0; k < kRaw; ++k) {
-                cut(raw[chunk][k]);
-                if constexpr (P::kAny) cut(pre[chunk][k]);
-            }
-        }
-        if constexpr (P::kAny) {
-#pragma unroll
-            for (int k = 0; k < kRaw; ++k) form_piece<T>(g.prologue.act, raw[chunk][k], pre[chunk][k]);
-            if (g.prologue.formed && block == 0) {
-                // (of whole tiles without a branch, as the results are stored)
-                T* const to = static_cast<T*>(g.prologue.formed) + (int64_t)tile * 32 * a.C;
-                if ((chunk + 1) * CH <= a.C && (int64_t)tile * 32 + 32 <= g.n) {
-#pragma unroll
-                    for (int k = 0; k < kRaw; ++k)
-                        store16(within_tile<T>(to, ((uint32_t)(8 * k + (lane >> 3)) * (uint32_t)a.C + (uint32_t)c) * (uint32_t)sizeof(T)), raw[chunk][k]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < kRaw; ++k) {
-                        float v[N];
-                        Cols<T>::unpack(raw[chunk][k], v);
-                        if ((int64_t)tile * 32 + 8 * k + (lane >> 3) < g.n) Cols<T>::store(to + (8 * k + (lane >> 3)) * a.C, c, a.C, v);
-                    }
-                    __builtin_amdgcn_s_waitcnt(0);
-                }
+                if (c >= a.C) raw[chunk][k] = make_uint4(0u, 0u, 0u, 0u);
+                else if (a.C >= N) raw[chunk][k] = front_of_piece<T>(raw[chunk][k], a.C - c);
             }
         }
 #pragma unroll
@@ -213,7 +183,7 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E, P> g)
 #pragma unroll
         for (int chunk = 0; chunk < CHUNKS; ++chunk) {
             uint4 p[S / SB][1][SB][kSP], x[kRaw];
-            hand_over(tile, chunk, x);
+            hand_over(chunk, x);
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 if constexpr (PC == 3) {
@@ -245,7 +215,7 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E, P> g)
         bool odd = false;
 #pragma unroll
         for (int i = 0; i < NT; ++i) odd |= not_finite(acc[i]);
-        if (__any(odd)) exact_tiles<T, Sh, TRANS>(a, g.prologue, 0, min(r0 + (lane & 31), g.n - 1), n0, 0, acc);
+        if (__any(odd)) exact_tiles<T, Sh, TRANS>(a, NoPrologue{}, 0, min(r0 + (lane & 31), g.n - 1), n0, 0, acc);
         const Place<Sh> at = place();
         if constexpr (RES) {
 #pragma unroll
@@ -260,21 +230,18 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E, P> g)
     }
 }
 
-// Four column tiles, eight wavefronts' rows: the chunks of a contraction that fit beside them (bf16), or that a lane's registers take (fp32; with what
-// dA is formed of fewer).
-constexpr int kKeptTiles = 4;
-template <typename T, typename P>
-constexpr int kMostKeptChunks = sizeof(T) == 2 || !P::kAny ? 4 : 3;
-template <typename T, typename P>
+// Four column tiles, eight wavefronts' rows: the chunks of a contraction that fit beside them (bf16), or that a lane's registers take (fp32).
+constexpr int kKeptTiles = 4, kMostKeptChunks = 4;
+template <typename T>
 bool fits_kept(int C)
 {
-    static_assert((kMostKeptChunks<T, P> * Mode<T>::kSteps * Mode<T>::kPieces * kKeptTiles + kKeptWaves * 4) * 1024 <= kKeptLds, "LDS of a compute unit");
-    return (C + kChunk<T> - 1) / kChunk<T> <= kMostKeptChunks<T, P>;
+    static_assert((kMostKeptChunks * Mode<T>::kSteps * Mode<T>::kPieces * kKeptTiles + kKeptWaves * 4) * 1024 <= kKeptLds, "LDS of a compute unit");
+    return (C + kChunk<T> - 1) / kChunk<T> <= kMostKeptChunks;
 }
 
-// out [n, N] = (A [n, C], by the prologue) B; TRANS: B = W^T.  work: lay_bytes.
-template <typename T, int CHUNKS, bool TRANS, typename E, typename P>
-int run_kept_chunks(const void* A, const float* W, int64_t n, void* out, int K, int F, void* work, hipStream_t st, const E& e, const P& prologue)
+// out [n, N] = A [n, C] B; TRANS: B = W^T.  work: lay_bytes.
+template <typename T, int CHUNKS, bool TRANS, typename E>
+int run_kept_chunks(const void* A, const float* W, int64_t n, void* out, int K, int F, void* work, hipStream_t st, const E& e)
 {
     constexpr int NT = kKeptTiles;
     const int C = TRANS ? F : K, N = TRANS ? K : F, blocks = (N + 32 * NT - 1) / (32 * NT);
@@ -283,7 +250,7 @@ int run_kept_chunks(const void* A, const float* W, int64_t n, void* out, int K, 
     const LayArgs l{W, pieces, 1, K, F, C, N, CHUNKS, blocks, Types{nullptr, 1, n}, nullptr, 0, (unsigned)lay};
     k_typed_lay<T, NT, TRANS, WholeShare<T, NT>><<<(unsigned)lay, 256, 0, st>>>(l);
     SAR_LAUNCH_CHECK();
-    const KeptArgs<E, P> a{{A, pieces, W, out, nullptr, C, N, CHUNKS, blocks, K, F, e}, prologue, n};
+    const KeptArgs<E> a{{A, pieces, W, out, nullptr, C, N, CHUNKS, blocks, K, F, e}, n};
     constexpr size_t shared = ((size_t)CHUNKS * Mode<T>::kSteps * Mode<T>::kPieces * NT + kKeptWaves * 4) * 1024;
     const int turns = std::max(1, (shared > kKeptLds / 2 ? 32 : 64) / blocks);
     auto launch = [&](auto* fn) {
@@ -293,21 +260,19 @@ int run_kept_chunks(const void* A, const float* W, int64_t n, void* out, int K, 
         return (int)SAR_OK;
     };
     if constexpr (E::kAny) {
-        if (e.res) return launch(k_rows_kept<T, NT, CHUNKS, TRANS, true, E, P>);
+        if (e.res) return launch(k_rows_kept<T, NT, CHUNKS, TRANS, true, E>);
     }
-    return launch(k_rows_kept<T, NT, CHUNKS, TRANS, false, E, P>);
+    return launch(k_rows_kept<T, NT, CHUNKS, TRANS, false, E>);
 }
 
-template <typename T, bool TRANS, typename E, typename P>
-int run_kept(const void* A, const float* W, int64_t n, void* out, int K, int F, void* work, hipStream_t st, const E& e, const P& p)
+template <typename T, bool TRANS, typename E>
+int run_kept(const void* A, const float* W, int64_t n, void* out, int K, int F, void* work, hipStream_t st, const E& e)
 {
     switch (((TRANS ? F : K) + kChunk<T> - 1) / kChunk<T>) {
-    case 1: return run_kept_chunks<T, 1, TRANS>(A, W, n, out, K, F, work, st, e, p);
-    case 2: return run_kept_chunks<T, 2, TRANS>(A, W, n, out, K, F, work, st, e, p);
-    case 3: return run_kept_chunks<T, 3, TRANS>(A, W, n, out, K, F, work, st, e, p);
-    default:
-        if constexpr (kMostKeptChunks<T, P> == 4) return run_kept_chunks<T, 4, TRANS>(A, W, n, out, K, F, work, st, e, p);
-        return fail(SAR_ERR_UNSUPPORTED, "a contraction of %d values is not kept", TRANS ? F : K);
+    case 1: return run_kept_chunks<T, 1, TRANS>(A, W, n, out, K, F, work, st, e);
+    case 2: return run_kept_chunks<T, 2, TRANS>(A, W, n, out, K, F, work, st, e);
+    case 3: return run_kept_chunks<T, 3, TRANS>(A, W, n, out, K, F, work, st, e);
+    default: return run_kept_chunks<T, 4, TRANS>(A, W, n, out, K, F, work, st, e);
     }
 }
 
