@@ -81,12 +81,14 @@ int groups_of(int dtype, int64_t n, int F)
     return (int)std::max<int64_t>(1, std::min<int64_t>((n + rows - 1) / rows, std::max(1, std::min(kActGroups, (1 << 22) / F))));
 }
 
-// Whether a product's operand is kept.
+// Whether a product's operand is kept: from a tile of 32 rows for every wavefront of the chip on (256 -> 256, bf16, by GELU with a residual: 32 thousand
+// rows 25.6 us, by the other kernel 28.4, 65536 rows 38.3 and 46.3, 867187 433 and 576; 64 -> 128 16 thousand rows 14.7 and 7.8, 131072 32.9 and
+// 34.0; 47 -> 64, half of a block empty, 400 thousand rows 108 and 50; 128 -> 70, pairs of neighbours, 135 and 112).
 template <typename T>
 bool kept(int64_t n, int C, int N)
 {
     const int64_t blocks = (N + 32 * kKeptTiles - 1) / (32 * kKeptTiles);
-    return n * blocks >= 65536 && N > 64 && fits_kept<T>(C);
+    return n * blocks >= 256 * kKeptWaves * 32 && fits_kept<T>(C, N);
 }
 
 template <typename T>

@@ -33,29 +33,31 @@ __device__ SAR_INLINE inline void residual_of(const Epilogue& e, const Place<SH>
 }
 
 // A wavefront's results, from the sums to memory.  Loads and stores are waited for in the order in which they were sent, by counting those sent since, and
-// what a branch may have sent does not count: so that the next rows, which are under way, need not be waited for behind these results' stores,
-// whole tiles (FULL) are stored without a branch, and the bias is in registers from the beginning.
-template <typename T, typename SH, bool FULL, bool RES, typename E, int NW, int KNOWN>
+// what a branch may have sent does not count: so that the next rows, which are under way, need not be waited for behind these results' stores, these are
+// sent without a branch, what lies behind the last row or column to a place outside of the tile's buffer, where the memory unit drops it.  (A guard around
+// each where a tile is not whole, and a wait behind them: 400000 x 100 -> 172, bf16, 226 us, so 153; 200 -> 400 514 and 348.)
+template <typename T, typename SH, bool RES, typename E, int NW, int KNOWN>
 __device__ SAR_INLINE inline void finish_kept(const E& e, void* out, const Place<SH>& at, const float (&bias)[NW], float16_t (&acc)[NW],
-                                              Neighbours<T, SH::IL> (&res)[KNOWN][4])
+                                              const Neighbours<T, SH::IL> (&res)[KNOWN][4])
 {
-    constexpr int IL = SH::IL, kSteps = NW / IL * 4;
+    constexpr int IL = SH::IL, kSteps = NW / IL * 4, kWords = IL * (int)sizeof(T) / 4;
     const int64_t tile = at.tile();
     auto store = [&](void* to, int s, const float (&v)[4][IL]) SAR_INLINE {
         const int n = at.column(s / 4);
+        const auto buffer = __builtin_amdgcn_make_buffer_rsrc(static_cast<T*>(to) + tile, 0, 32 * at.N * (int)sizeof(T), 0x00020000);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int i = at.row(4 * (s % 4) + k);
-            T* const p = within_tile<T>(static_cast<T*>(to) + tile, ((uint32_t)i * (uint32_t)at.N + (uint32_t)n) * (uint32_t)sizeof(T));
-            if (FULL || (i < at.rows && n + IL <= at.N)) {
-                Neighbours<T, IL> w;
-                w.set(v[k]);
-                *reinterpret_cast<Neighbours<T, IL>*>(p) = w;
-            } else if (i < at.rows) {
+            const uint32_t place = ((uint32_t)i * (uint32_t)at.N + (uint32_t)n) * (uint32_t)sizeof(T);
+            const int where = i < at.rows && n < at.N ? (int)place : -1;
+            Neighbours<T, IL> w;
+            w.set(v[k]);
+            typedef uint32_t Words __attribute__((ext_vector_type(kWords)));
+            Words x;
 #pragma unroll
-                for (int j = 0; j < IL; ++j)
-                    if (n + j < at.N) p[j] = from_f32<T>(v[k][j]);
-            }
+            for (int j = 0; j < kWords; ++j) x[j] = w.x[j];
+            if constexpr (kWords == 4) __builtin_amdgcn_raw_buffer_store_b128(x, buffer, where, 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b64(x, buffer, where, 0, 0);
         }
     };
 #pragma unroll
@@ -66,7 +68,6 @@ __device__ SAR_INLINE inline void finish_kept(const E& e, void* out, const Place
 #pragma unroll
             for (int j = 0; j < IL; ++j) v[k][j] = acc[s / 4 * IL + j][4 * (s % 4) + k];
         if constexpr (E::kAny) {
-            if constexpr (RES && !FULL) fetch_residual<T, SH>(e, at, s, res[s]);
             auto add_residual = [&]() SAR_INLINE {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
@@ -221,22 +222,18 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E> g)
 #pragma unroll
             for (int s = kEarly; s < kSteps; ++s) residual_of<T, Sh>(a.epilogue, at, s, res[s]);
         }
-        if (at.rows == 32 && n0 + 32 * NT <= a.N) {
-            finish_kept<T, Sh, true, RES>(a.epilogue, a.out, at, bias, acc, res);
-        } else {
-            finish_kept<T, Sh, false, RES>(a.epilogue, a.out, at, bias, acc, res);
-            __builtin_amdgcn_s_waitcnt(0);
-        }
+        finish_kept<T, Sh, RES>(a.epilogue, a.out, at, bias, acc, res);
     }
 }
 
 // Four column tiles, eight wavefronts' rows: the chunks of a contraction that fit beside them (bf16), or that a lane's registers take (fp32).
 constexpr int kKeptTiles = 4, kMostKeptChunks = 4;
+// Whether they do, columns are whole groups of a lane's neighbours, and more than what half a block leaves empty.
 template <typename T>
-bool fits_kept(int C)
+bool fits_kept(int C, int N)
 {
     static_assert((kMostKeptChunks * Mode<T>::kSteps * Mode<T>::kPieces * kKeptTiles + kKeptWaves * 4) * 1024 <= kKeptLds, "LDS of a compute unit");
-    return (C + kChunk<T> - 1) / kChunk<T> <= kMostKeptChunks;
+    return (C + kChunk<T> - 1) / kChunk<T> <= kMostKeptChunks && N % WholeShare<T, kKeptTiles>::IL == 0 && N > 16 * kKeptTiles;
 }
 
 // out [n, N] = A [n, C] B; TRANS: B = W^T.  work: lay_bytes.
