@@ -169,7 +169,7 @@ def moved(t, by):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("by", [1, 3])
-@pytest.mark.parametrize("n,K,F,C", [(301, 33, 47, 47), (66_000, 47, 70, 9), (20, 17, 64, 5001)])
+@pytest.mark.parametrize("n,K,F,C", [(301, 33, 47, 47), (66_000, 47, 70, 9), (66_001, 47, 72, 100), (20, 17, 64, 5001)])
 def test_tensors_at_any_address(n, K, F, C, by, dtype):
     s = Student(n, K, F, C, dtype, seed=7)
     s.step()
