@@ -152,6 +152,7 @@ struct ActDw {
     int64_t n;
     int K, F, accumulate;
     void* work;
+    void* formed;          // receives dA, of an even F; or null
 };
 size_t act_dw_bytes(int64_t n, int K, int F);
 int act_dw(int dtype, const ActDw& g, hipStream_t st);

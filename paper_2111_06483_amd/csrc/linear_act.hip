@@ -145,13 +145,15 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
         const TypedDw g{X, nullptr, nullptr, dY, dW, types, K, F, accumulate, nullptr, formed ? A : nullptr, act, db};
         return few_act_bwd(dtype, g, {dY, W, dX, types, F, K, K, F}, dA, st);
     }
-    // What forms dA: the product for dX of many rows, in bf16 the one for dW too; otherwise a launch of its own.
-    const bool within = formed && dX && n > 0 && !few_dx, again = formed && dW && !few_dw && sizeof(T) == 2;
+    // What forms dA of many rows: in bf16 the product for dW, which writes it for dX, or for who asked for it; without that the product for dX; otherwise a launch
+    // of its own.  (867187 x 256 -> 256, bf16, GELU: both products form it 847 us, dW writes it kWrites.)
+    const bool again = formed && dW && !few_dw && sizeof(T) == 2, writes = again && (dX || dA) && F % 2 == 0 && n > 0;
+    const bool within = formed && dX && n > 0 && !few_dx && !writes;
     const bool reads = (dW && !again) || (dX && !within);
     void* const rows = !formed ? const_cast<void*>(dY) : dA ? dA : reads ? high : nullptr;
     void* const low = formed && dW && few_dw && sizeof(T) == 2 ? high + rounded((size_t)n * F * sizeof(T)) : nullptr;
     const bool sums = db && (!dW || few_dw);       // (otherwise with dW)
-    void* const written = formed ? (within ? nullptr : rows) : dA;
+    void* const written = formed ? (within || writes ? nullptr : rows) : dA;
     if (n > 0 && (written || low || sums)) {
         const int lanes = lanes_of(dtype, F), groups = groups_of(dtype, n, F);
         const ActBwdArgs a{dY, A, written, low, sums ? partial : nullptr, n, F, act, lanes};
@@ -160,20 +162,20 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
         SAR_LAUNCH_CHECK();
     }
     if (sums) SAR_TRY(act_sum(partial, n > 0 ? groups_of(dtype, n, F) : 0, F, accumulate, db, st));
+    auto weights = [&]() -> int {
+        return act_dw(dtype, {X, again ? dY : rows, again ? A : nullptr, act, dW, db, n, K, F, accumulate, work, writes ? rows : nullptr}, st);
+    };
+    if (writes) SAR_TRY(weights());
     if (dX && n > 0) {
-        if (within) {
-            SAR_TRY((rows_product<T, true>(dY, W, types, dX, K, F, work, st, NoEpilogue{}, ActPrologue{A, rows, act})));
-        } else if (kept<T>(n, F, K)) {
-            SAR_TRY((run_kept<T, true>(rows, W, n, dX, K, F, work, st, NoEpilogue{})));
-        } else {
-            SAR_TRY((rows_product<T, true>(rows, W, types, dX, K, F, work, st)));
-        }
+        if (within) SAR_TRY((rows_product<T, true>(dY, W, types, dX, K, F, work, st, NoEpilogue{}, ActPrologue{A, rows, act})));
+        else if (kept<T>(n, F, K)) SAR_TRY((run_kept<T, true>(rows, W, n, dX, K, F, work, st, NoEpilogue{})));
+        else SAR_TRY((rows_product<T, true>(rows, W, types, dX, K, F, work, st)));
     }
     if (dW && few_dw) {
         SAR_TRY(typed_dw(dtype, {X, nullptr, nullptr, rows, dW, types, K, F, accumulate, static_cast<float*>(work)}, st));
         if (low && n > 0) SAR_TRY(typed_dw(dtype, {X, nullptr, nullptr, low, dW, types, K, F, 1, static_cast<float*>(work)}, st));
-    } else if (dW) {
-        SAR_TRY(act_dw(dtype, {X, again ? dY : rows, again ? A : nullptr, act, dW, db, n, K, F, accumulate, work}, st));
+    } else if (dW && !writes) {
+        SAR_TRY(weights());
     }
     return SAR_OK;
 }

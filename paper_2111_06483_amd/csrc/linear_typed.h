@@ -97,8 +97,12 @@ struct Bf16Sums : Bf16Rows {
 struct Bf16Formed {
     using T = bf16_t;
     static constexpr int kPieces = 2, kCols = 2;
-    static constexpr bool kSums = true, kFormed = true;
+    static constexpr bool kSums = true, kFormed = true, kWritten = false;
     using Plain = Bf16Rows;
+};
+// ... and written, rounded, for the other product.
+struct Bf16Written : Bf16Formed {
+    static constexpr bool kWritten = true;
 };
 template <typename ZR, typename = void>
 struct ZTraits {
@@ -124,6 +128,7 @@ struct DwArgs {
     const void* pre = nullptr;
     int act = 0;
     float* sums = nullptr;
+    void* formed = nullptr;
 };
 
 // A value of X as fp32.

@@ -120,8 +120,10 @@ struct FormedUnit {
         Plain::load(w + Plain::kRegs, pre, group, rows, full, c, width);
     }
     // `negate`: of dY's sign, which leaves X as it is (a quarter of the values to turn)
+    // `formed`: WRITTEN: the chunk's rows of dA, which are written as bf16 (what is not there: outside of the buffer).
+    template <bool WRITTEN>
     static __device__ SAR_INLINE inline void put(uint32_t* w, int act, uint4* out, int stride, int group, int rows, bool full, int c, int width, bool negate,
-                                                 float (&sums)[2])
+                                                 float (&sums)[2], bf16_t* formed, bool mine)
     {
         float v[2][8];
         const uint32_t flip = negate ? 0x80008000u : 0u;
@@ -145,6 +147,14 @@ struct FormedUnit {
         if (c == width - 1) {          // the two values end with the row's last
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[0][k] = v[1][k];
+        }
+        if constexpr (WRITTEN) {
+            const auto buffer = __builtin_amdgcn_make_buffer_rsrc(formed, 0, mine ? rows * width * (int)sizeof(bf16_t) : 0, 0x00020000);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int place = ((8 * group + k) * width + c) * (int)sizeof(bf16_t);
+                __builtin_amdgcn_raw_buffer_store_b32(pack2_bf16(v[0][k], v[1][k]) ^ flip, buffer, c < width ? place : -1, 0, 0);
+            }
         }
         uint32_t hi[2][4], lo[2][4];
         float largest = 0.f;
@@ -324,7 +334,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
             if (first >= kZUnits || (kZUnits % 64 && id >= kZUnits)) continue;
             const int g = id / (TF / 2), c = id % (TF / 2) * 2;
             if constexpr (ZTraits<ZR>::kFormed) {
-                FormedUnit::put(raw.z[u], a.act, buf + kXSize + g * TF + place_of(c), kGroups * TF, g, rows, full, f0 + c, a.F, negate, sums[u]);
+                FormedUnit::put<ZR::kWritten>(raw.z[u], a.act, buf + kXSize + g * TF + place_of(c), kGroups * TF, g, rows, full, f0 + c, a.F, negate, sums[u],
+                                              ZR::kWritten ? static_cast<bf16_t*>(a.formed) + r0 * a.F : nullptr, blockIdx.y == 0);
             } else {
                 Unit<Plain>::put(raw.z[u], buf + kXSize + g * TF + place_of(c), kGroups * TF, g, rows, full, f0 + c, a.F, false);
                 if constexpr (ZTraits<ZR>::kSums) {
