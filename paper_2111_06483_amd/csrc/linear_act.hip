@@ -146,7 +146,7 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
         return few_act_bwd(dtype, g, {dY, W, dX, types, F, K, K, F}, dA, st);
     }
     // What forms dA of many rows: in bf16 the product for dW, which writes it for dX, or for who asked for it; without that the product for dX; otherwise a launch
-    // of its own.  (867187 x 256 -> 256, bf16, GELU: both products form it 847 us, dW writes it kWrites.)
+    // of its own.  (867187 x 256 -> 256, bf16, GELU: both products form it 847 us, dW writes it 727.)
     const bool again = formed && dW && !few_dw && sizeof(T) == 2, writes = again && (dX || dA) && F % 2 == 0 && n > 0;
     const bool within = formed && dX && n > 0 && !few_dx && !writes;
     const bool reads = (dW && !again) || (dX && !within);
