@@ -184,11 +184,10 @@ __device__ inline void merge8(uint32_t (&v)[8], const uint32_t (&sorted)[8])
     for (int i = 0; i < 8; ++i) v[i] = max(v[i], sorted[7 - i]);
     settle8(v);
 }
+
 // ---- how rows are laid over threads
 
 // Rows of up to 32 values a lane of a wavefront stay in registers.
-template <typename T>
-constexpr int kMostPieces = 32 / Cols<T>::N;
 constexpr int kMostInLanes = 64 * 32;
 
 struct ClassShape {

@@ -6,8 +6,8 @@
 //
 // One pass over the student's scores each way (class_rows.h).  The teacher's few classes meet the student's scores by gathers that are under way with the row, and in the
 // gradient where the tile still is on the chip, in the list's order, so that a class that is listed twice has the same sum in every run.
-// What bounds it: 1734375 x 172, bf16, eight classes: 144 us, 5.0 TB/s: memory; gradient, 4096 x 50000, bf16, 32 classes: 144 us, 5.7 TB/s; 306250 x 47, fp32, eight: 41 us, 3.4 TB/s, three barriers
-// a tile of 80 rows (by one lane a row 62; tiles of 40 rows no faster).
+// What bounds it: 1734375 x 172, bf16, eight classes: 144 us, 5.0 TB/s: memory; gradient, 4096 x 50000, bf16, 32 classes: 144 us, 5.7 TB/s; 306250 x 47, fp32, eight: 41 us, 3.4 TB/s: short for the
+// chip's memory to come up to its rate (lists by one lane a row 62; tiles of 40 rows, six workgroups a compute unit, a third barrier: the same).
 #include "class_rows.h"
 
 namespace sar {
@@ -133,15 +133,15 @@ __device__ inline RowGrad row_grad(const GradArgs& a, int64_t row, bool is, floa
 }
 __device__ inline float student_part(float x, const RowGrad& r, float by) { return r.g * __builtin_amdgcn_exp2f(fmaf(x, by, -r.lse)); }
 
-// Short rows, several a tile: the student's part goes to LDS, the teacher's is subtracted there, the tile is written as a whole.  Lists are read
-// as they lie, a lane an entry, up to kEntries a thread.
+// Short rows, several a tile: what the teacher takes off goes to LDS, zeros elsewhere, and meets the student's part there.  Lists are read as they lie,
+// a lane an entry, up to kEntries a thread.
 constexpr int kEntries = 4;
 template <typename T>
 __global__ __launch_bounds__(kClassThreads) void k_distill_bwd(GradArgs a)
 {
     constexpr int N = Cols<T>::N, U = kTileValues / (kClassThreads * N);
     __shared__ RowGrad rows[kMostTileRows + 1];
-    __shared__ __attribute__((aligned(16))) float tile[kTileValues];
+    __shared__ __attribute__((aligned(16))) float taught[kTileValues];
     __shared__ uint8_t named[kTileValues];
     const Teacher& q = a.teacher;
     const int j = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes, groups = kClassThreads / a.lanes;
@@ -155,6 +155,10 @@ __global__ __launch_bounds__(kClassThreads) void k_distill_bwd(GradArgs a)
         uint4 raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) raw[u] = Cols<T>::load(X, (u * kClassThreads + (int)threadIdx.x) * N, values, left);
+        if (index != blockIdx.x) __syncthreads();      // (the last tile has been read)
+#pragma unroll
+        for (int u = 0; u < kTileValues / (4 * kClassThreads); ++u)
+            *reinterpret_cast<float4*>(taught + (u * kClassThreads + threadIdx.x) * 4) = make_float4(0.f, 0.f, 0.f, 0.f);
         int place[kEntries];           // of the entry's class in the tile, -1 without one
         float p[kEntries];
 #pragma unroll
@@ -178,20 +182,23 @@ __global__ __launch_bounds__(kClassThreads) void k_distill_bwd(GradArgs a)
 #pragma unroll
         for (int k = 0; k < kEntries; ++k) {
             if (k * groups >= count) continue;
-            if (!__any(place[k] >= 0 && named[place[k]] != j)) continue;
-            float sum = 0.f;
-            bool first = true;
-            for (int l = 0; l < q.k; ++l) {
-                const int from = ((int)threadIdx.x & 63 & ~(a.lanes - 1)) + l, other = __shfl(place[k], from);
-                const float more = __shfl(p[k], from);
-                if (other == place[k]) {
-                    sum += more;
-                    first &= l >= j;
+            if (__any(place[k] >= 0 && named[place[k]] != j)) {
+                float sum = 0.f;
+                bool first = true;
+                for (int l = 0; l < q.k; ++l) {
+                    const int from = ((int)threadIdx.x & 63 & ~(a.lanes - 1)) + l, other = __shfl(place[k], from);
+                    const float more = __shfl(p[k], from);
+                    if (other == place[k]) {
+                        sum += more;
+                        first &= l >= j;
+                    }
                 }
+                p[k] = sum;
+                if (!first) place[k] = -1;
             }
-            p[k] = sum;
-            if (!first) place[k] = -1;
+            if (place[k] >= 0) taught[place[k]] = p[k];
         }
+        __syncthreads();
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int e = (u * kClassThreads + (int)threadIdx.x) * N;
@@ -208,22 +215,9 @@ __global__ __launch_bounds__(kClassThreads) void k_distill_bwd(GradArgs a)
                 for (int i = 0; i < N; ++i) x[i] = student_part(x[i], rows[min(tile_row(a.t, e + i), count - 1)], q.by);
             }
 #pragma unroll
-            for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(tile + e + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kEntries; ++k)
-            if (place[k] >= 0) tile[place[k]] -= p[k];
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int e = (u * kClassThreads + (int)threadIdx.x) * N;
-            if (e >= values) continue;
-            float x[N];
-#pragma unroll
             for (int i = 0; i < N; i += 4) {
-                const float4 v = *reinterpret_cast<const float4*>(tile + e + i);
-                x[i] = v.x, x[i + 1] = v.y, x[i + 2] = v.z, x[i + 3] = v.w;
+                const float4 v = *reinterpret_cast<const float4*>(taught + e + i);
+                x[i] -= v.x, x[i + 1] -= v.y, x[i + 2] -= v.z, x[i + 3] -= v.w;
             }
             Cols<T>::store(dX, e, values, x);
         }

@@ -248,6 +248,17 @@ def test_relu_takes_its_output_as_what_it_was_taken_of():
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,K,F", [(300, 40, 72), (20_000, 40, 47), (66_001, 40, 72), (66_001, 40, 132)])
+def test_the_argument_in_the_place_of_the_residual(n, K, F, dtype):
+    X, W, b, R = inputs(n, K, F, dtype, 5)
+    Y, A, work = torch.empty_like(R), torch.empty_like(R), scratch(n, K, F)[0]
+    sar.sar_linear_act_fwd(X, W, b, R, sar.SAR_ACT_SILU, False, Y, A, work)
+    same, Y2 = R.clone(), torch.empty_like(R)
+    sar.sar_linear_act_fwd(X, W, b, same, sar.SAR_ACT_SILU, False, Y2, same, work)
+    assert torch.equal(Y, Y2) and torch.equal(A, same)
+
+
 def test_no_rows():
     for dtype in DTYPES:
         X, Y, W = torch.empty(0, 8, dtype=dtype, device="cuda"), torch.empty(0, 6, dtype=dtype, device="cuda"), torch.ones(8, 6, device="cuda")
