@@ -140,15 +140,15 @@ def test_errors_of_the_transform(at):
     assert fwd(res=at + 8196) == BAD and says("overlaps")
     assert fwd(res=at + 12288, A=at + 12288, after=1) == BAD and says("overlaps")
     assert fwd(n=0, X=none, W=none, Y=none) == 0
-    bwd = lambda dY=at, A=at + 1024, X=at + 2048, W=at + 3072, act=1, acc=0, dW=at + 4096, db=at + 5120, dX=at + 6144, dA=at + 7168, dtype=0, n=4, K=8, F=6, work=at, \
+    bwd = lambda dY=at, A=at + 800, X=at + 1600, W=at + 2400, act=1, acc=0, dW=at + 3200, db=at + 4000, dX=at + 4800, dA=at + 5600, dtype=0, n=4, K=8, F=6, work=at, \
         wb=much: lib.sar_linear_act_bwd(dY, A, X, W, act, acc, dW, db, dX, dA, dtype, n, K, F, work, wb, none)
     assert bwd(act=7) == UNSUPPORTED and bwd(dtype=3) == UNSUPPORTED and bwd(work=none) == BAD and bwd(wb=8) == BAD
     assert bwd(dY=none) == BAD and bwd(A=none) == BAD and bwd(X=none) == BAD and bwd(W=none) == BAD and says("null")
-    for other in (at, at + 1024, at + 2048, at + 3072, at + 7168):
+    for other in (at, at + 800, at + 1600, at + 2400, at + 5600):
         assert bwd(dX=other) == BAD and says("dX must not alias")
-    for other in (at, at + 1024, at + 2048):
+    for other in (at, at + 800, at + 1600):
         assert bwd(dA=other) == BAD and says("dA must not alias")
-    assert bwd(dW=at + 3072) == BAD and says("dW must not alias")
+    assert bwd(dW=at + 2400) == BAD and says("dW must not alias")
     size = ctypes.c_size_t()
     assert lib.sar_linear_act_workspace_bytes(4, 8, 6, none) == BAD and lib.sar_linear_act_workspace_bytes(-1, 8, 6, ctypes.byref(size)) == BAD
     # the calls that there were before take their own activations alone
