@@ -28,8 +28,14 @@ __device__ inline V over_lanes(V v, Op op)
     if constexpr (L >= 4) v = op(v, other(std::integral_constant<int, 0x4E>{}));       // lane ^ 2
     if constexpr (L >= 8) v = op(v, other(std::integral_constant<int, 0x141>{}));      // the other four of eight
     if constexpr (L >= 16) v = op(v, other(std::integral_constant<int, 0x140>{}));     // the other eight of sixteen
-    if constexpr (L >= 32) v = op(v, (V)__shfl_xor(v, 16));
-    if constexpr (L >= 64) v = op(v, (V)__shfl_xor(v, 32));
+    // (a lane's own value and the one of lane ^ 16, lane ^ 32, in either order)
+    const auto both = [&](auto r) {
+        const uint32_t x = r[0], y = r[1];
+        return op(__builtin_bit_cast(V, x), __builtin_bit_cast(V, y));
+    };
+    const auto word = [&] { return __builtin_bit_cast(uint32_t, v); };
+    if constexpr (L >= 32) v = both(__builtin_amdgcn_permlane16_swap(word(), word(), false, false));
+    if constexpr (L >= 64) v = both(__builtin_amdgcn_permlane32_swap(word(), word(), false, false));
     return v;
 }
 template <int L>
@@ -144,13 +150,28 @@ __device__ inline void offer_top(TopKey& list, TopKey c, TopKey last)
     uint64_t in = __ballot(c > last);
     if (__builtin_popcountll(in) > 8) {                // (a sort and a merge are some eight insertions)
         sort_top(c);
-        merge_top(list, c);
+        if (key_at(list, 0) == 0) list = c;
+        else merge_top(list, c);
         return;
     }
     while (in) {
         const int l = __builtin_ctzll(in);
         in &= in - 1;
         insert_top(list, key_at(c, l));
+    }
+}
+
+// The lists of a workgroup's first `count` wavefronts, which are in `lists` too: the first one's then has all of them.  All wavefronts.
+template <int WAVES>
+__device__ inline void join_lists(TopKey& top, TopKey (*lists)[kMostTop], int wave, int lane, int count)
+{
+#pragma unroll 1
+    for (int half = WAVES / 2; half >= 1; half /= 2) {
+        if (wave < half) {
+            if (wave + half < count) merge_top(top, lists[wave + half][lane]);
+            if (half > 1) lists[wave][lane] = top;
+        }
+        if (half > 1) __syncthreads();
     }
 }
 
@@ -205,13 +226,14 @@ inline ClassShape class_shape(int dtype, int64_t n, int C)
 }
 
 // Longer rows are cut into parts of whole pieces, a workgroup each; several parts a row where there are few rows, and a second launch that joins them.
-constexpr int64_t kWideGroups = 1024;
+constexpr int64_t kWideGroups = 512;
+constexpr int kMostParts = 64;                         // a lane of a wavefront for each
 inline int64_t least_part(int dtype) { return (int64_t)kClassThreads * 4 * (dtype == SAR_F32 ? 4 : 8); }
 inline int parts_of(int dtype, int64_t n, int C)
 {
     if (C <= kMostInLanes) return 1;
     const int64_t want = (kWideGroups + n - 1) / std::max<int64_t>(n, 1), most = (C + least_part(dtype) - 1) / least_part(dtype);
-    return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, 64}));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, kMostParts}));
 }
 // Values of a part, a multiple of eight.
 inline int64_t part_width(int C, int parts) { return ((C + parts - 1) / parts + 7) / 8 * 8; }
@@ -219,7 +241,7 @@ inline int64_t part_width(int C, int parts) { return ((C + parts - 1) / parts + 
 inline int64_t most_parts(int64_t n, int C)
 {
     if (C <= kMostInLanes) return 0;
-    const int64_t most = std::min<int64_t>((C + least_part(SAR_F32) - 1) / least_part(SAR_F32), 64), rows = std::min(n, kWideGroups);
+    const int64_t most = std::min<int64_t>((C + least_part(SAR_F32) - 1) / least_part(SAR_F32), kMostParts), rows = std::min(n, kWideGroups);
     return most > 1 ? std::min(rows * most, rows + kWideGroups) : 0;
 }
 
@@ -306,14 +328,17 @@ __global__ __launch_bounds__(kClassThreads) void k_class_wide(ClassRows a, typen
         const int64_t c0 = part * a.width, c1 = min(c0 + a.width, (int64_t)a.C);
         RowSums sums{-__builtin_inff(), 0.f, 0.f};
         TopKey top = 0;
+        uint4 raw[U], next[U];
+        auto read = [&](int64_t at) {
+#pragma unroll
+            for (int i = 0; i < U; ++i) next[i] = Cols<T>::load(x, (int)min(at + (i * kClassThreads + (int)threadIdx.x) * N, c1), a.C, left);
+        };
+        read(c0);
         for (int64_t at = c0; at < c1; at += kClassThreads * N * U) {
-            uint4 raw[U];
             float v[U][N];
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int64_t c = min(at + (i * kClassThreads + (int)threadIdx.x) * N, (int64_t)a.C);
-                raw[i] = Cols<T>::load(x, (int)c, a.C, left);
-            }
+            for (int i = 0; i < U; ++i) raw[i] = next[i];
+            read(at + kClassThreads * N * U);           // (under way meanwhile)
             float most = -__builtin_inff();
 #pragma unroll
             for (int i = 0; i < U; ++i) {
@@ -373,25 +398,15 @@ __global__ __launch_bounds__(kClassThreads) void k_class_wide(ClassRows a, typen
         if (lane == 0) wave_sums[wave] = sums;
         if constexpr (Job::kTop) wave_top[wave][lane] = top;
         __syncthreads();
-        if (wave != 0) continue;
-        RowSums all = wave_sums[0];
-#pragma unroll
-        for (int w = 1; w < kClassWaves; ++w) all.m = fmaxf(all.m, wave_sums[w].m);
-        const float m = all.m;
-        all = wave_sums[0];
-        move_sums(all, m, a.by, 1.f);
-#pragma unroll
-        for (int w = 1; w < kClassWaves; ++w) {
-            RowSums more = wave_sums[w];
-            move_sums(more, m, a.by, 1.f);
-            all.s += more.s, all.u += more.u;
-        }
         if constexpr (Job::kTop) {
-            if (a.k > 0) {
-#pragma unroll 1
-                for (int w = 1; w < kClassWaves; ++w) merge_top(top, wave_top[w][lane]);
-            }
+            if (a.k > 0) join_lists<kClassWaves>(top, wave_top, wave, lane, kClassWaves);
         }
+        if (wave != 0) continue;
+        RowSums all{-__builtin_inff(), 0.f, 0.f};
+        if (lane < kClassWaves) all = wave_sums[lane];
+        move_sums(all, lanes_largest<64>(all.m), a.by, 1.f);
+        all.s = lanes_sum<64>(all.s);
+        if constexpr (Job::kEntropy) all.u = lanes_sum<64>(all.u);
         if (a.parts == 1) {
             all.u *= a.over;
             Job::template in_wave<T>(a, job, row, all, top);
@@ -404,29 +419,38 @@ __global__ __launch_bounds__(kClassThreads) void k_class_wide(ClassRows a, typen
     }
 }
 
-// The parts of a row, a wavefront each row.
+// The parts of a row, by a workgroup.
+constexpr int kJoinWaves = 8;
 template <typename T, typename Job>
-__global__ __launch_bounds__(kClassThreads) void k_class_join(ClassRows a, typename Job::Args job)
+__global__ __launch_bounds__(kJoinWaves* kWave) void k_class_join(ClassRows a, typename Job::Args job)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * kClassWaves + (threadIdx.x >> 6);
-    if (row >= a.n) return;
+    __shared__ TopKey wave_top[Job::kTop ? kJoinWaves : 1][kMostTop];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row = blockIdx.x;
     RowSums all{-__builtin_inff(), 0.f, 0.f};
-    if (lane < a.parts) all = a.sums[row * a.parts + lane];
+    if (wave == 0 && lane < a.parts) all = a.sums[row * a.parts + lane];
+    TopKey top = 0;
+    if constexpr (Job::kTop) {
+        if (a.k > 0) {
+            TopKey list[kMostParts / kJoinWaves];
+#pragma unroll
+            for (int i = 0; i < kMostParts / kJoinWaves; ++i) {
+                const int p = i * kJoinWaves + wave;
+                list[i] = p < a.parts && lane < a.k ? a.lists[(row * a.parts + p) * a.k + lane] : 0ull;
+            }
+            top = list[0];
+#pragma unroll
+            for (int i = 1; i < kMostParts / kJoinWaves; ++i)
+                if (i * kJoinWaves + wave < a.parts) merge_top(top, list[i]);
+            wave_top[wave][lane] = top;
+            __syncthreads();
+            join_lists<kJoinWaves>(top, wave_top, wave, lane, a.parts);
+        }
+    }
+    if (wave != 0) return;
     move_sums(all, lanes_largest<64>(all.m), a.by, 1.f);
     all.s = lanes_sum<64>(all.s);
     all.u = lanes_sum<64>(all.u) * a.over;
-    TopKey top = 0;
-    if constexpr (Job::kTop) {
-        const int count = a.parts * a.k;
-        const TopKey* lists = a.lists + row * count;
-        for (int i = 0; i < count; i += 64) {
-            TopKey c = i + lane < count ? lists[i + lane] : 0ull;
-            sort_top(c);
-            if (i == 0) top = c;
-            else merge_top(top, c);
-        }
-    }
     Job::template in_wave<T>(a, job, row, all, top);
 }
 
@@ -484,7 +508,7 @@ int run_classes(ClassRows a, const typename Job::Args& job, const char* what, vo
         k_class_wide<T, Job><<<groups, kClassThreads, 0, st>>>(a, job);
         SAR_LAUNCH_CHECK();
         if (a.parts > 1) {
-            k_class_join<T, Job><<<(unsigned)((a.n + kClassWaves - 1) / kClassWaves), kClassThreads, 0, st>>>(a, job);
+            k_class_join<T, Job><<<(unsigned)a.n, kJoinWaves * kWave, 0, st>>>(a, job);
             SAR_LAUNCH_CHECK();
         }
         return SAR_OK;
