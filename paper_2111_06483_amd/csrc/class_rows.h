@@ -260,14 +260,23 @@ struct ClassRows {
 template <typename T, int R>
 constexpr bool ends_in(int r) { return r >= R - (R > 4 ? 2 : 1); }
 
-// A row's pieces of `T` in the lanes t of TPR, -inf behind the row's end.
+// A row's pieces of `T` in the lanes t of TPR, -inf behind the row's end.  inner: none of the workgroup's rows is so near to the tensor's end that a piece passes that.
 template <typename T, int TPR, int R>
-__device__ inline void row_in_lanes(const ClassRows& a, int64_t row, int t, float (&v)[R][Cols<T>::N])
+__device__ inline void row_in_lanes(const ClassRows& a, int64_t row, int t, bool inner, float (&v)[R][Cols<T>::N])
 {
     constexpr int N = Cols<T>::N;
     uint4 raw[R];
+    const T* x = static_cast<const T*>(a.X) + row * a.C;
+    if (inner) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) raw[r] = Cols<T>::load(static_cast<const T*>(a.X) + row * a.C, (t + r * TPR) * N, a.C, (a.n - row) * a.C);
+        for (int r = 0; r < R; ++r) {
+            const int c = (t + r * TPR) * N;
+            raw[r] = load16(x + (ends_in<T, R>(r) && c >= a.C ? 0 : c));
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r) raw[r] = Cols<T>::load(x, (t + r * TPR) * N, a.C, (a.n - row) * a.C);
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         Cols<T>::unpack(raw[r], v[r]);
@@ -290,7 +299,7 @@ __global__ __launch_bounds__(kClassThreads) void k_class_rows(ClassRows a, typen
         const bool there = row < a.n;
         float v[R][N];
         const auto other = Job::template begin<T>(a, job, min(row, a.n - 1), t);       // (what else is read of a row, under way with it)
-        row_in_lanes<T, TPR, R>(a, min(row, a.n - 1), t, v);
+        row_in_lanes<T, TPR, R>(a, min(row, a.n - 1), t, (a.n - base - kRows) * a.C >= N, v);
         RowSums sums{-__builtin_inff(), 0.f, 0.f};
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -329,9 +338,13 @@ __global__ __launch_bounds__(kClassThreads) void k_class_wide(ClassRows a, typen
         RowSums sums{-__builtin_inff(), 0.f, 0.f};
         TopKey top = 0;
         uint4 raw[U], next[U];
+        const bool ends = c1 + N > left;           // whether the part's last piece may pass the tensor's end
         auto read = [&](int64_t at) {
 #pragma unroll
-            for (int i = 0; i < U; ++i) next[i] = Cols<T>::load(x, (int)min(at + (i * kClassThreads + (int)threadIdx.x) * N, c1), a.C, left);
+            for (int i = 0; i < U; ++i) {
+                const int c = (int)min(at + (i * kClassThreads + (int)threadIdx.x) * N, c1);
+                next[i] = ends ? Cols<T>::load(x, c, a.C, left) : load16(x + c);
+            }
         };
         read(c0);
         for (int64_t at = c0; at < c1; at += kClassThreads * N * U) {
