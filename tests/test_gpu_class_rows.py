@@ -76,6 +76,17 @@ def test_top_classes(n, C, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("n,C,k", [(511, 8193, 2), (512, 8193, 2), (300, 9000, 5), (255, 9000, 64), (40, 20_000, 64), (3, 1_000_003, 8), (1, 300_001, 64), (6, 262_144, 0)])
+def test_rows_in_parts(n, C, k, dtype):
+    """A row by one workgroup, by a few, by the most there are; rows whose top classes are in one part, and in every part as many."""
+    X, label = scores(n, C, dtype, 14)
+    for row, x in ((1, torch.linspace(-8, 8, C)), (2, torch.linspace(8, -8, C)), (3, (torch.arange(C) % 4096 == 77) * 4.0)):
+        if row < n:
+            X[row] = x.to(dtype)
+    check_forward(X, label, k)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("C", [6, 47, 172, 1001, 3001, 30_001])
 def test_equal_scores(C, dtype):
     """Of few different values, -0 and 0 among them; rows of one value; rising and falling rows."""
