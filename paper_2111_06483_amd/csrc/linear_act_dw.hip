@@ -55,11 +55,10 @@ int act_dw(int dtype, const ActDw& g, hipStream_t st)
     float* const partial = static_cast<float*>(g.work);
     const DwArgs a{g.X, nullptr, nullptr, g.dY, partial, Types{nullptr, 1, g.n}, g.K, g.F, s.share, g.pre, g.act,
                    g.db ? partial + (s.groups + 1) * g.K * g.F : nullptr, g.formed};
-    SAR_TRY(dtype == SAR_F32 ? (run_all<F32Rows, F32Sums, kChunk32 / 16, 1>(a, s, g.accumulate, g.dW, st))
-            : g.formed       ? (run_all<Bf16Rows, Bf16Written, kChunk16 / 16, 2>(a, s, g.accumulate, g.dW, st))
-            : formed         ? (run_all<Bf16Rows, Bf16Formed, kChunk16 / 16, 2>(a, s, g.accumulate, g.dW, st))
-                             : (run_all<Bf16Rows, Bf16Sums, kChunk16 / 16, 2>(a, s, g.accumulate, g.dW, st)));
-    return g.db ? act_sum(a.sums, (int)s.groups, g.F, g.accumulate, g.db, st) : SAR_OK;
+    return dtype == SAR_F32 ? run_all<F32Rows, F32Sums, kChunk32 / 16, 1>(a, s, g.accumulate, g.dW, st, g.db)
+           : g.formed       ? run_all<Bf16Rows, Bf16Written, kChunk16 / 16, 2>(a, s, g.accumulate, g.dW, st, g.db)
+           : formed         ? run_all<Bf16Rows, Bf16Formed, kChunk16 / 16, 2>(a, s, g.accumulate, g.dW, st, g.db)
+                            : run_all<Bf16Rows, Bf16Sums, kChunk16 / 16, 2>(a, s, g.accumulate, g.dW, st, g.db);
 }
 
 }  // namespace sar

@@ -520,19 +520,52 @@ __device__ float sum_again(const DwArgs& a, int64_t w, int64_t lo, int64_t hi, i
     return v;
 }
 
+// db (+)= the sums of `groups` workgroups, in order: eight columns a workgroup of 256 threads, whose 32 slices take every 32nd, four at a time.
+__device__ inline void sum_columns(const float* sums, int groups, int F, int block, float* part, int accumulate, float* db)
+{
+    const int k = threadIdx.x & 7, slice = threadIdx.x >> 3, c = block * 8 + k;
+    float v = 0.f;
+    if (c < F) {
+        for (int w = slice; w < groups; w += 4 * 32) {
+            float x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[u] = w + u * 32 < groups ? sums[(int64_t)(w + u * 32) * F + c] : 0.f;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) v += x[u];
+        }
+    }
+    part[threadIdx.x] = v;
+    __syncthreads();
+    if (slice == 0 && c < F) {
+        float total = 0.f;
+#pragma unroll
+        for (int s = 0; s < 32; ++s) total += part[s * 8 + k];
+        db[c] = accumulate ? db[c] + total : total;
+    }
+}
+
 // dW[t] (+)= the places of the workgroups that have rows of type t, in order.  32 threads take 32 or, where weights are whole pieces of
 // four, 128 consecutive values; eight such groups of a workgroup take every eighth place, four at a time.
-template <typename XR, typename ZR, int V>
-__global__ __launch_bounds__(256) void k_typed_sum(DwArgs a, int accumulate, float* dW)
+// SUMS: of one type, with db (or null) in the workgroups from `blocks` on.
+template <typename XR, typename ZR, int V, bool SUMS>
+__global__ __launch_bounds__(256) void k_typed_sum(DwArgs a, int accumulate, float* dW, int blocks, float* db)
 {
     __shared__ float part[8][32][V];
+    if constexpr (SUMS) {
+        if ((int)blockIdx.x >= blocks) {
+            const int groups = (int)((a.types.n + a.share - 1) / a.share);
+            sum_columns(a.sums, groups, a.F, (int)blockIdx.x - blocks, &part[0][0][0], accumulate, db);
+            return;
+        }
+    }
+    const int across = SUMS ? blocks : (int)gridDim.x;
     const int e = threadIdx.x & 31, z = threadIdx.x >> 5, t = blockIdx.y;
     const int64_t count = (int64_t)a.K * a.F;
     int64_t lo, hi;
     a.types.span(t, lo, hi);
     const int64_t w0 = lo / a.share, w1 = hi > lo ? (hi - 1) / a.share + 1 : w0;
     struct __attribute__((packed, aligned(4))) Values { float v[V]; };
-    for (int64_t k0 = (int64_t)blockIdx.x * (32 * V); k0 < count; k0 += (int64_t)gridDim.x * (32 * V)) {
+    for (int64_t k0 = (int64_t)blockIdx.x * (32 * V); k0 < count; k0 += (int64_t)across * (32 * V)) {
         const int64_t k = k0 + e * V;
         Values sum = {};
         if (k < count) {
@@ -647,7 +680,7 @@ int run(const DwArgs& a, const Shape& s, hipStream_t st)
 
 // S: products of 16 rows a chunk; W: chunks under way in the wide tiles, whose sums leave fewer registers.
 template <typename XR, typename ZR, int S, int W>
-int run_all(const DwArgs& a, const Shape& s, int accumulate, float* dW, hipStream_t st)
+int run_all(const DwArgs& a, const Shape& s, int accumulate, float* dW, hipStream_t st, float* db = nullptr)
 {
     if (a.types.n > 0) {
         if (s.tk == 256) SAR_TRY((run<XR, ZR, 4, 2, 2, 2, S, W>(a, s, st)));
@@ -662,8 +695,11 @@ int run_all(const DwArgs& a, const Shape& s, int accumulate, float* dW, hipStrea
     const bool single = count % 4 != 0 || count * a.types.T < 512 * 128;
     const int64_t per = single ? 32 : 128, blocks = std::min<int64_t>((count + per - 1) / per, 1 << 20);
     using Plain = typename ZTraits<ZR>::Plain;
-    if (single) k_typed_sum<XR, Plain, 1><<<dim3((unsigned)blocks, a.types.T), 256, 0, st>>>(a, accumulate, dW);
-    else k_typed_sum<XR, Plain, 4><<<dim3((unsigned)blocks, a.types.T), 256, 0, st>>>(a, accumulate, dW);
+    // (columns' sums in a launch of their own: 5 us more)
+    constexpr bool kSums = ZTraits<ZR>::kSums;
+    const dim3 grid((unsigned)(blocks + (db ? (a.F + 7) / 8 : 0)), a.types.T);
+    if (single) k_typed_sum<XR, Plain, 1, kSums><<<grid, 256, 0, st>>>(a, accumulate, dW, (int)blocks, db);
+    else k_typed_sum<XR, Plain, 4, kSums><<<grid, 256, 0, st>>>(a, accumulate, dW, (int)blocks, db);
     SAR_LAUNCH_CHECK();
     return SAR_OK;
 }
