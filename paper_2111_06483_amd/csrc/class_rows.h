@@ -214,10 +214,13 @@ constexpr int kMostInLanes = 64 * 32;
 struct ClassShape {
     int tpr, r;            // lanes a row, pieces a lane
 };
-inline ClassShape class_shape(int dtype, int64_t n, int C)
+inline ClassShape class_shape(int dtype, int64_t n, int C, int k)
 {
     const int vec = dtype == SAR_F32 ? 4 : 8, pieces = (C + vec - 1) / vec, most = 32 / vec;
-    int tpr = 4;
+    // A piece or two are a lane's or two's, of up to three of the k classes each; otherwise four lanes or more.  (1000000 rows, bf16, us by one or two lanes / by four: log
+    // probabilities, four classes without k 7 / 16, k = 3 13 / 29, sixteen classes, k = 3 19 / 29; distillation, C = k = 2 9 / 19, 4 20 / 21, 8 92 / 30.)
+    int tpr = 1;
+    while (tpr < 4 && (pieces > tpr || k > 3 * tpr)) tpr <<= 1;
     while (tpr < 64 && pieces > tpr * most) tpr <<= 1;
     // few rows are spread over more lanes
     while (tpr < 64 && pieces > tpr && n * tpr < 64 * 2048) tpr <<= 1;
@@ -479,8 +482,12 @@ int run_in_lanes(int r, const ClassRows& a, const typename Job::Args& job, hipSt
 {
     constexpr int kRows = kClassThreads / TPR;
     const unsigned groups = (unsigned)std::min<int64_t>((a.n + kRows - 1) / kRows, 1 << 20);
-    switch (r) {
-    case 1: k_class_rows<T, TPR, 1, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
+    if (TPR < 4 || r == 1) {
+        k_class_rows<T, TPR, 1, Job><<<groups, kClassThreads, 0, st>>>(a, job);
+        SAR_LAUNCH_CHECK();
+        return SAR_OK;
+    }
+    if constexpr (TPR >= 4) switch (r) {
     case 2: k_class_rows<T, TPR, 2, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
     case 3: k_class_rows<T, TPR, 3, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
     case 4: k_class_rows<T, TPR, 4, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
@@ -500,8 +507,10 @@ int run_classes(ClassRows a, const typename Job::Args& job, const char* what, vo
 {
     const int dtype = sizeof(T) == 4 ? SAR_F32 : SAR_BF16;
     if (a.C <= kMostInLanes) {
-        const ClassShape s = class_shape(dtype, a.n, a.C);
+        const ClassShape s = class_shape(dtype, a.n, a.C, a.k);
         switch (s.tpr) {
+        case 1: return run_in_lanes<T, Job, 1>(s.r, a, job, st);
+        case 2: return run_in_lanes<T, Job, 2>(s.r, a, job, st);
         case 4: return run_in_lanes<T, Job, 4>(s.r, a, job, st);
         case 8: return run_in_lanes<T, Job, 8>(s.r, a, job, st);
         case 16: return run_in_lanes<T, Job, 16>(s.r, a, job, st);

@@ -3,7 +3,7 @@
 //   m = max x, S = sum exp(x - m), U = sum exp(x - m) (x - m):  lse = m + log S, log p_c = (x_c - m) - log S, H = log S - U / S
 //   dx_c = g ([c = label] - p_c) - h p_c (log p_c + H)
 //
-// One pass over the scores each way (class_rows.h): rows of up to 2048 classes in the registers of 4 to 64 lanes, several rows a wavefront; longer ones by a
+// One pass over the scores each way (class_rows.h): rows of up to 2048 classes in the registers of 1 to 64 lanes, several rows a wavefront; longer ones by a
 // workgroup with the running largest, or, of few rows, by several and a second launch.  Exponentials are taken of differences from the largest, so that 32 bits hold; the
 // entropy's sum is taken with them.  The gradient needs no sums: tiles of whole pieces, whatever the rows' lengths.
 // What bounds it: 1734375 x 172, bf16, eight classes: 223 us, 3.3 TB/s of its 735 MB (a copy: 144): vector instructions, 730 for eight rows of a wavefront, half of them for

@@ -42,6 +42,10 @@ def check_forward(X, label, k):
     n, C = X.shape
     logp, lse, entropy, top = (cr.f64(t) if torch.is_tensor(t) else t for t in forward(X, label, k))
     x, lab = cr.f64(X), label.cpu().numpy()
+    some = ~np.isneginf(x).all(1)
+    assert np.isneginf(lse[~some]).all() and (entropy[~some] == 0).all() and np.isneginf(logp[~some & (lab >= 0) & (lab < C)]).all()
+    assert np.isneginf(cr.f64(top[0])[~some]).all() and (top[1].cpu().numpy()[~some] == -1).all()
+    x, lab, logp, lse, entropy = x[some], lab[some], logp[some], lse[some], entropy[some]
     s = cr.Softmax(x)
     assert (np.abs(lse - s.lse[:, 0]) <= s.off_lse[:, 0]).all()
     assert (np.abs(entropy - s.entropy[:, 0]) <= s.off_entropy[:, 0]).all()
@@ -50,7 +54,7 @@ def check_forward(X, label, k):
     assert (logp[~has] == 0).all()
     want = s.logp[rows, at]
     assert (np.abs(logp[has] - want) <= s.off_log[rows, 0] + 3 * cr.U * (np.abs(s.d[rows, at]) + np.abs(want))).all()
-    value, index = cr.f64(top[0]), top[1].cpu().numpy()
+    value, index = cr.f64(top[0])[some], top[1].cpu().numpy()[some]
     want = cr.top(x, k)
     assert (index == want).all()
     none, at = want < 0, np.where(want < 0, 0, want)
@@ -73,6 +77,18 @@ def test_forward_of_every_width(C, dtype):
 def test_top_classes(n, C, k, dtype):
     X, label = scores(n, C, dtype, 1)
     check_forward(X, label, k)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("k", [0, 1, 3, 4, 6, 7])
+@pytest.mark.parametrize("C", [1, 2, 3, 4, 5, 7, 8, 9, 12, 16])
+def test_few_classes(C, k, dtype):
+    """A row by one lane, two or four; the last rows' pieces pass the tensor's end."""
+    for n in (1, 2, 256, 1025):
+        X, label = scores(n, C, dtype, 15)
+        X[n // 2] = float("-inf")
+        check_forward(X, label, k)
+    check_distill(scores(1025, C, dtype, 16)[0], teacher(1025, C, k, 3), 1.5, dtype)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
