@@ -214,14 +214,20 @@ constexpr int kMostInLanes = 64 * 32;
 struct ClassShape {
     int tpr, r;            // lanes a row, pieces a lane
 };
-inline ClassShape class_shape(int dtype, int64_t n, int C, int k)
+// top: k classes are looked for; otherwise k listed ones are read, a lane each as far as they go.
+inline ClassShape class_shape(int dtype, int64_t n, int C, int k, bool top)
 {
     const int vec = dtype == SAR_F32 ? 4 : 8, pieces = (C + vec - 1) / vec, most = 32 / vec;
     // A piece or two are a lane's or two's, of up to three of the k classes each; otherwise four lanes or more.  (1000000 rows, bf16, us by one or two lanes / by four: log
     // probabilities, four classes without k 7 / 16, k = 3 13 / 29, sixteen classes, k = 3 19 / 29; distillation, C = k = 2 9 / 19, 4 20 / 21, 8 92 / 30.)
     int tpr = 1;
     while (tpr < 4 && (pieces > tpr || k > 3 * tpr)) tpr <<= 1;
-    while (tpr < 64 && pieces > tpr * most) tpr <<= 1;
+    // 32 values a lane; of many bf16 rows 48, for half the lanes to share what is done once a row (172 classes, eight of them, 872093 rows by four lanes 111 us, by eight
+    // 124, 100000 rows 17.4 and 16.9; eight listed ones, two a lane, 91 and 73; 300 classes, 500000 rows, one a lane, 62 and 72).
+    auto holds = [&](int lanes) {
+        return pieces <= lanes * most || (vec == 8 && pieces <= lanes * 6 && n * lanes >= 64 * 16384 && (top || k <= lanes));
+    };
+    while (tpr < 64 && !holds(tpr)) tpr <<= 1;
     // few rows are spread over more lanes
     while (tpr < 64 && pieces > tpr && n * tpr < 64 * 2048) tpr <<= 1;
     const int r = (pieces + tpr - 1) / tpr;
@@ -492,10 +498,8 @@ int run_in_lanes(int r, const ClassRows& a, const typename Job::Args& job, hipSt
     case 3: k_class_rows<T, TPR, 3, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
     case 4: k_class_rows<T, TPR, 4, Job><<<groups, kClassThreads, 0, st>>>(a, job); break;
     default:
-        if constexpr (sizeof(T) == 4) {
-            if (r == 6) k_class_rows<T, TPR, 6, Job><<<groups, kClassThreads, 0, st>>>(a, job);
-            else k_class_rows<T, TPR, 8, Job><<<groups, kClassThreads, 0, st>>>(a, job);
-        }
+        if (sizeof(T) == 2 || r == 6) k_class_rows<T, TPR, 6, Job><<<groups, kClassThreads, 0, st>>>(a, job);
+        else if constexpr (sizeof(T) == 4) k_class_rows<T, TPR, 8, Job><<<groups, kClassThreads, 0, st>>>(a, job);
     }
     SAR_LAUNCH_CHECK();
     return SAR_OK;
@@ -507,7 +511,7 @@ int run_classes(ClassRows a, const typename Job::Args& job, const char* what, vo
 {
     const int dtype = sizeof(T) == 4 ? SAR_F32 : SAR_BF16;
     if (a.C <= kMostInLanes) {
-        const ClassShape s = class_shape(dtype, a.n, a.C, a.k);
+        const ClassShape s = class_shape(dtype, a.n, a.C, a.k, Job::kTop);
         switch (s.tpr) {
         case 1: return run_in_lanes<T, Job, 1>(s.r, a, job, st);
         case 2: return run_in_lanes<T, Job, 2>(s.r, a, job, st);
