@@ -6,8 +6,8 @@
 // One pass over the scores each way (class_rows.h): rows of up to 2048 classes in the registers of 1 to 64 lanes, several rows a wavefront; longer ones by a
 // workgroup with the running largest, or, of few rows, by several and a second launch.  Exponentials are taken of differences from the largest, so that 32 bits hold; the
 // entropy's sum is taken with them.  The gradient needs no sums: tiles of whole pieces, whatever the rows' lengths.
-// What bounds it: 1734375 x 172, bf16, eight classes: 223 us, 3.3 TB/s of its 735 MB (a copy: 144): vector instructions, 730 for eight rows of a wavefront, half of them for
-// the eight classes (without any 137 us, as distill.hip's pass over the same scores); 306250 x 47, fp32, five: 20 us, 3.7 TB/s; 64 x 65536, fp32, eight: 15.1 us, two launches, 12.2
+// What bounds it: 1734375 x 172, bf16, eight classes: 208 us, 3.5 TB/s of its 735 MB (a copy: 144): vector instructions, half of them for the
+// eight classes (without any 137 us, as distill.hip's pass over the same scores); 306250 x 47, fp32, five: 20 us, 3.7 TB/s; 64 x 65536, fp32, eight: 15.1 us, two launches, 12.2
 // and 3.8 under the trace (without classes 8.9).  Gradient, 1734375 x 172, bf16: 241 us, 5.1 TB/s.
 #include "class_rows.h"
 
