@@ -541,8 +541,8 @@ int sar_linear_act_fwd(const void* X, const float* W, const float* bias, const v
 /* With dA = dY act'(A):  dW = X^T dA (fp32 [K,F]), db = sum_i dA_i (fp32 [F]), both added to what is there where accumulate != 0, else
  * overwritten, and summed in a fixed order; dX = dA W^T ([n,K] of `dtype`, OVERWRITTEN); dA ([n,F] of `dtype`, OVERWRITTEN: the gradient of a residual inside
  * the activation; that of one behind it is dY).  Each of the four may be NULL.  A as sar_linear_act_fwd wrote it (not read with SAR_ACT_NONE); X only for
- * dW, W only for dX.  The derivative is taken of A as it is stored, in 32 bits.  Of bf16 rows dW sums products of dA to 16 bits (2^-17 of it), db dA in 32, and dX
- * products of dA rounded to bf16 as dX itself is.  dX and dA must not overlap what is read or each other. */
+ * dW, W only for dX.  The derivative is taken of A as it is stored, in 32 bits (with SAR_ACT_RELU dA = dY where A > 0, else 0).  Of bf16
+ * rows dW and dX sum products of dA to 16 bits (2^-17 of it), db dA in 32.  dX and dA must not overlap what is read or each other. */
 int sar_linear_act_bwd(const void* dY, const void* A, const void* X, const float* W, int act, int accumulate, float* dW, float* db, void* dX, void* dA,
                        int dtype, int64_t n, int K, int F, void* work, size_t work_bytes, void* stream);
 

@@ -96,19 +96,26 @@ __device__ __attribute__((always_inline)) inline void with_act(int act, F&& f)
     }
 }
 
-// What is done to a row's values before they are multiplied: nothing, or dA = dY act'(A) is formed of them.
+// What is done to a row's values before they are multiplied: nothing; dA = dY act'(A) is formed of them; or they are the first pieces of values whose others lie
+// elsewhere.  Of bf16 rows dA is multiplied as two pieces of bf16, 16 bits: of one, a result's terms would have 8 before they are added up and rounded
+// (867187 x 256 -> 256, by GELU: dX is 1.66e-3 off from 64 bits, which is its own rounding; of one piece 2.35e-3).
 struct NoPrologue {
-    static constexpr bool kAny = false;
+    static constexpr bool kAny = false, kForms = false;
 };
 struct ActPrologue {
-    static constexpr bool kAny = true;
+    static constexpr bool kAny = true, kForms = true;
     const void* pre;       // [n, C]: what the activation was taken of
-    void* formed;          // [n, C] or null: the rows as they are multiplied
+    void* formed;          // [n, C] or null: receives dA
     int act;
 };
+struct LowPieces {
+    static constexpr bool kAny = true, kForms = false;
+    const void* low;       // [n, C] of bf16
+};
 
+// dA of a piece of dY, rounded; bf16: what the rounding left, in `low` (beside an infinity nothing).
 template <typename T>
-__device__ __attribute__((always_inline)) inline void form_piece(int act, uint4& d, const uint4& pre)
+__device__ __attribute__((always_inline)) inline void form_piece(int act, uint4& d, const uint4& pre, uint4& low)
 {
     constexpr int N = Cols<T>::N;
     float v[N], a[N];
@@ -119,15 +126,29 @@ __device__ __attribute__((always_inline)) inline void form_piece(int act, uint4&
         for (int j = 0; j < N; ++j) v[j] = act_grad<decltype(which)::value>(v[j], a[j]);
     });
     d = Cols<T>::round(v);
+    if constexpr (sizeof(T) == 2) {
+        Cols<T>::unpack(d, a);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float left = v[j] - a[j];
+            v[j] = fabsf(left) < __builtin_inff() ? left : 0.f;
+        }
+        low = Cols<T>::round(v);
+    }
 }
 
-// ... of one value, at place `at` of the rows.
+// One value, at place `at` of the rows, whole.
 template <typename T>
 __device__ inline float formed_value(const ActPrologue& p, float d, int64_t at)
 {
     const float a = value_of(static_cast<const T*>(p.pre)[at]);
     with_act(p.act, [&](auto which) { d = act_grad<decltype(which)::value>(d, a); });
-    return value_of(from_f32<T>(d));
+    return d;
+}
+template <typename T>
+__device__ inline float formed_value(const LowPieces& p, float d, int64_t at)
+{
+    return d + value_of(static_cast<const T*>(p.low)[at]);
 }
 
 // One value of the product, place `at` of the rows, with its bias and residual.
@@ -153,6 +174,7 @@ struct ActDw {
     int K, F, accumulate;
     void* work;
     void* formed;          // receives dA, of an even F; or null
+    void* low;             // ... what its rounding left; or null
 };
 size_t act_dw_bytes(int64_t n, int K, int F);
 int act_dw(int dtype, const ActDw& g, hipStream_t st);

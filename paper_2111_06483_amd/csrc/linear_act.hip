@@ -6,7 +6,8 @@
 //   - Forward, and dX of rows that are already dA: many rows by linear_kept.h, whose wavefronts keep memory busy while they multiply; operands that do not fit
 //     there by linear_typed_rows.h; few rows in one launch by linear_typed_few.hip.  Activations cost instructions: GELU some 20 a value, 60 us of 867187 x 256 values.
 //   - Backward: dA is formed where a product brings its rows, never in a pass of its own but where no product wants it (k_act_bwd), or few rows' columns are
-//     many.  bf16: the product for dW forms it (linear_act_dw.hip), as two pieces of bf16, and writes it rounded for dX.  fp32: the product for dX forms and
+//     many.  bf16: the product for dW forms it (linear_act_dw.hip), as two pieces of bf16, and writes them for dX, which multiplies them as such: rounded to one, dA
+//     would have dX off by another rounding of its own size.  fp32: the product for dX forms and
 //     writes it, the one for dW reads it.  db leaves with dW.  Few rows: dW, db, dX and dA in one launch.
 // What bounds it: forward, 867187 x 256 -> 256, bf16, GELU, a residual and its argument kept: 428 to 451 us, 4.0 TB/s of its 1.78 GB (their copy: 349), the vector
 // instructions in use 63% of the time, the matrix cores 28%; 306250 x 100 -> 256, fp32, ReLU with a residual 180 us, 4.2 TB/s.  Backward, 867187 x 256 -> 256, bf16, GELU: 727
@@ -106,6 +107,17 @@ int forward(const void* X, const float* W, int64_t n, void* Y, int K, int F, voi
     return rows_product<T, false>(X, W, Types{nullptr, 1, n}, Y, K, F, work, st, e);
 }
 
+// dX of rows of dA that are formed, or (bf16) in two pieces.
+template <typename T, typename Q>
+int product_of(const void* rows, const float* W, int64_t n, void* dX, int K, int F, void* work, hipStream_t st, const Q& q)
+{
+    if constexpr (sizeof(T) == 2) {
+        if (kept<T>(n, F, K)) return run_kept<T, true>(rows, W, n, dX, K, F, work, st, NoEpilogue{}, q);
+    }
+    if constexpr (sizeof(T) == 2 || Q::kForms) return rows_product<T, true>(rows, W, Types{nullptr, 1, n}, dX, K, F, work, st, NoEpilogue{}, q);
+    return fail(SAR_ERR_UNSUPPORTED, "linear with activation: fp32 rows in pieces");
+}
+
 size_t rounded(size_t b) { return (b + 255) / 256 * 256; }
 size_t partial_bytes(int64_t n, int F)
 {
@@ -153,13 +165,16 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
         const TypedDw g{X, nullptr, nullptr, dY, dW, types, K, F, accumulate, nullptr, formed ? A : nullptr, act, db};
         return few_act_bwd(dtype, g, {dY, W, dX, types, F, K, K, F}, dA, st);
     }
-    // What forms dA of many rows: in bf16 the product for dW, which writes it for dX, or for who asked for it; without that the product for dX; otherwise a launch
-    // of its own.  (867187 x 256 -> 256, bf16, GELU: both products form it 847 us, dW writes it 727.)
-    const bool again = formed && dW && !few_dw && sizeof(T) == 2, writes = again && (dX || dA) && F % 2 == 0 && n > 0;
-    const bool within = formed && dX && n > 0 && !few_dx && !writes;
+    // What forms dA of many rows: in bf16 the product for dW, which writes it for dX (two pieces, of which the first may be the caller's dA), or for who asked for it;
+    // without that the product for dX; otherwise a launch of its own.  (867187 x 256 -> 256, bf16, GELU: dW writes it 886 us, of one piece, that dX had fewer bits of, 735;
+    // dX alone, which forms it for either half of its columns, 625.)
+    const bool bf16 = sizeof(T) == 2, again = formed && dW && !few_dw && bf16;
+    const bool writes = again && F % 2 == 0 && n > 0 && (dA || (dX && !few_dx));
+    const bool within = formed && dX && n > 0 && (few_dx ? bf16 : !writes);
     const bool reads = (dW && !again) || (dX && !within);
     void* const rows = !formed ? const_cast<void*>(dY) : dA ? dA : reads ? high : nullptr;
-    void* const low = formed && dW && few_dw && sizeof(T) == 2 ? high + rounded((size_t)n * F * sizeof(T)) : nullptr;
+    char* const second = high + rounded((size_t)n * F * sizeof(bf16_t));       // (bf16)
+    void* const low = formed && dW && few_dw && bf16 ? second : nullptr;
     const bool sums = db && (!dW || few_dw);       // (otherwise with dW)
     void* const written = formed ? (within || writes ? nullptr : rows) : dA;
     if (n > 0 && (written || low || sums)) {
@@ -171,11 +186,14 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
     }
     if (sums) SAR_TRY(act_sum(partial, n > 0 ? groups_of(dtype, n, F) : 0, F, accumulate, db, st));
     auto weights = [&]() -> int {
-        return act_dw(dtype, {X, again ? dY : rows, again ? A : nullptr, act, dW, db, n, K, F, accumulate, work, writes ? rows : nullptr}, st);
+        return act_dw(dtype, {X, again ? dY : rows, again ? A : nullptr, act, dW, db, n, K, F, accumulate, work, writes ? rows : nullptr, writes && dX && !within ? second : nullptr}, st);
     };
     if (writes) SAR_TRY(weights());
     if (dX && n > 0) {
-        if (within) SAR_TRY((rows_product<T, true>(dY, W, types, dX, K, F, work, st, NoEpilogue{}, ActPrologue{A, rows, act})));
+        const TypedDw none{nullptr, nullptr, nullptr, nullptr, nullptr, types, K, F, 0, nullptr, A, act};
+        if (within && few_dx) SAR_TRY(few_act_bwd(dtype, none, {dY, W, dX, types, F, K, K, F}, writes ? nullptr : rows, st));
+        else if (within) SAR_TRY(product_of<T>(dY, W, n, dX, K, F, work, st, ActPrologue{A, rows, act}));
+        else if (writes) SAR_TRY(product_of<T>(rows, W, n, dX, K, F, work, st, LowPieces{second}));
         else if (kept<T>(n, F, K)) SAR_TRY((run_kept<T, true>(rows, W, n, dX, K, F, work, st, NoEpilogue{})));
         else SAR_TRY((rows_product<T, true>(rows, W, types, dX, K, F, work, st)));
     }

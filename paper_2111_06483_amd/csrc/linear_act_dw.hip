@@ -1,8 +1,8 @@
 // Weight and bias gradients of the transform with its activation: dW (+)= X^T dA, db (+)= sum over rows of dA, by the kernels of linear_typed_dw.h with one type.
 //
 // Of bf16 rows dA = dY act'(A) is formed where a workgroup brings the rows and multiplied as two pieces of bf16 (16 bits; one piece would leave dW, an
-// fp32 sum, with 8), and written as one for the product that forms dX.  A workgroup's tile is rather 256 x 128 than 128 x 256: it is dA that costs instructions.
-// 867187 x 256 x 256, bf16, traced: of dY as it is 250 us, by ReLU 427 (two more tensors pass), by SiLU 490, by GELU 560.  What it waits for are vector instructions, some 43
+// fp32 sum, with 8), and written as such for the product that forms dX.  A workgroup's tile is rather 256 x 128 than 128 x 256: it is dA that costs instructions.
+// 867187 x 256 x 256, bf16, traced: of dY as it is 250 us; dA written in one piece by ReLU 427, by SiLU 490, by GELU 560, in both 617.  What it waits for are vector instructions, some 43
 // a value of dA by GELU, which the matrix instructions of the same wavefront do not hide.  (Fewer of them elsewhere, signs and infinities: no gain that shows.)
 #include "linear_typed_dw.h"
 
@@ -54,7 +54,7 @@ int act_dw(int dtype, const ActDw& g, hipStream_t st)
     const Shape s = shape_of(g.n, g.K, g.F, dtype == SAR_F32 ? kChunk32 : kChunk16, formed);
     float* const partial = static_cast<float*>(g.work);
     const DwArgs a{g.X, nullptr, nullptr, g.dY, partial, Types{nullptr, 1, g.n}, g.K, g.F, s.share, g.pre, g.act,
-                   g.db ? partial + (s.groups + 1) * g.K * g.F : nullptr, g.formed};
+                   g.db ? partial + (s.groups + 1) * g.K * g.F : nullptr, g.formed, g.low};
     return dtype == SAR_F32 ? run_all<F32Rows, F32Sums, kChunk32 / 16, 1>(a, s, g.accumulate, g.dW, st, g.db)
            : g.formed       ? run_all<Bf16Rows, Bf16Written, kChunk16 / 16, 2>(a, s, g.accumulate, g.dW, st, g.db)
            : formed         ? run_all<Bf16Rows, Bf16Formed, kChunk16 / 16, 2>(a, s, g.accumulate, g.dW, st, g.db)

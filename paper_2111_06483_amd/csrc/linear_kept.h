@@ -6,7 +6,7 @@
 // Why: with the operand passing through LDS for every 128 rows (linear_typed_rows.h) its copies, which a barrier waits for, take as long as the products, and the
 // rows' own way from memory is waited for at each.  867187 x 256 -> 256, bf16, GELU, residual, argument kept, 1.78 GB: that way 576 us; so, a chunk of rows ahead 564; the next
 // rows and residuals whole, under way without a branch, 433; stores without a branch 428.  (Two passes over the rows for 256 columns: both at about the same time on
-// one XCD, the second from its L2.)
+// one XCD, the second from its L2.)  Bf16 rows of dA in two pieces are a third product and twice the bytes: 256 -> 256, the same rows, traced, 271 us of one, 433 of two.
 #pragma once
 
 #include "linear_typed_rows.h"
@@ -18,10 +18,11 @@ namespace {
 constexpr int kKeptWaves = 8, kKeptThreads = kKeptWaves * 64;
 constexpr size_t kKeptLds = 160 * 1024;
 
-template <typename E>
+template <typename E, typename Q>
 struct KeptArgs {
     RowsArgs<E> rows;
     int64_t n;
+    Q prologue;
 };
 
 // The residuals of step s as fetch_residual has them, without a branch: what lies behind the last column or row is read from them.
@@ -103,10 +104,12 @@ __device__ SAR_INLINE inline void finish_kept(const E& e, void* out, const Place
     }
 }
 
-// CHUNKS: of the contraction; RES: a residual.
-template <typename T, int NT, int CHUNKS, bool TRANS, bool RES, typename E>
-__global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E> g)
+// CHUNKS: of the contraction; RES: a residual; Q: rows as they are, or (bf16) in two pieces, read or formed here, whose second ones meet the operand's first.
+template <typename T, int NT, int CHUNKS, bool TRANS, bool RES, typename E, typename Q>
+__global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E, Q> g)
 {
+    constexpr bool kLow = Q::kAny;
+    static_assert(!kLow || sizeof(T) == 2, "two pieces of bf16");
     using Sh = WholeShare<T, NT>;
     const RowsArgs<E>& a = g.rows;
     constexpr int PC = Mode<T>::kPieces, S = Mode<T>::kSteps, CH = kChunk<T>, N = Cols<T>::N, SB = Mode<T>::kStage, kSP = PC == 3 ? 3 : 1;
@@ -129,8 +132,8 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E> g)
     }
 
     const int tiles = (int)((g.n + 31) / 32), step = groups * kKeptWaves;
-    uint4 raw[CHUNKS][kRaw];
-    auto fetch = [&](int tile, int chunk) SAR_INLINE {
+    uint4 raw[CHUNKS][kRaw], low[kLow ? CHUNKS : 1][kRaw];
+    auto fetch = [&](const void* from, uint4 (&to)[kRaw], int tile, int chunk) SAR_INLINE {
         int own = lane;
         asm volatile("" : "+v"(own));
         const int c = chunk * CH + (own & 7) * N;
@@ -139,25 +142,30 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E> g)
 #pragma unroll
         for (int k = 0; k < kRaw; ++k) {
             const uint32_t row = min((uint32_t)(8 * k + (own >> 3)), most) * (uint32_t)a.C;
-            const T* rows = static_cast<const T*>(a.A) + r0 * a.C;
+            const T* rows = static_cast<const T*>(from) + r0 * a.C;
             // (rows of less than a piece: one chunk, value by value)
-            raw[chunk][k] = CHUNKS > 1 || a.C >= N ? load16(within_tile<const T>(rows, (row + (uint32_t)min(c, a.C - N)) * (uint32_t)sizeof(T)))
+            to[k] = CHUNKS > 1 || a.C >= N ? load16(within_tile<const T>(rows, (row + (uint32_t)min(c, a.C - N)) * (uint32_t)sizeof(T)))
                                                    : Cols<T>::load(rows + row, c, a.C, a.C);
         }
     };
+    auto fetch_chunk = [&](int tile, int chunk) SAR_INLINE {
+        fetch(a.A, raw[chunk], tile, chunk);
+        if constexpr (Q::kForms) fetch(g.prologue.pre, low[chunk], tile, chunk);
+        else if constexpr (kLow) fetch(g.prologue.low, low[chunk], tile, chunk);
+    };
     uint4* const rows = lds + kStages * kFrags * 64 + wave * 256;
     // a chunk, from the lanes that brought it to those that multiply it
-    auto hand_over = [&](int chunk, uint4 (&x)[kRaw]) SAR_INLINE {
+    auto hand_over = [&](int chunk, uint4 (&v)[kRaw], uint4 (&x)[kRaw]) SAR_INLINE {
         const int c = chunk * CH + (lane & 7) * N;
         if (chunk == CHUNKS - 1 && c + N > a.C) {
 #pragma unroll
             for (int k = 0; k < kRaw; ++k) {
-                if (c >= a.C) raw[chunk][k] = make_uint4(0u, 0u, 0u, 0u);
-                else if (a.C >= N) raw[chunk][k] = front_of_piece<T>(raw[chunk][k], a.C - c);
+                if (c >= a.C) v[k] = make_uint4(0u, 0u, 0u, 0u);
+                else if (a.C >= N) v[k] = front_of_piece<T>(v[k], a.C - c);
             }
         }
 #pragma unroll
-        for (int k = 0; k < kRaw; ++k) rows[(8 * k + (lane >> 3)) * 8 + ((lane & 7) ^ (lane >> 3))] = raw[chunk][k];
+        for (int k = 0; k < kRaw; ++k) rows[(8 * k + (lane >> 3)) * 8 + ((lane & 7) ^ (lane >> 3))] = v[k];
 #pragma unroll
         for (int k = 0; k < kRaw; ++k) x[k] = rows[(lane & 31) * 8 + ((h * kRaw + k) ^ (lane & 7))];
     };
@@ -165,7 +173,7 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E> g)
     int tile = group * kKeptWaves + wave;
     if (tile < tiles) {
 #pragma unroll
-        for (int chunk = 0; chunk < CHUNKS; ++chunk) fetch(tile, chunk);
+        for (int chunk = 0; chunk < CHUNKS; ++chunk) fetch_chunk(tile, chunk);
     }
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
@@ -186,8 +194,24 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E> g)
         float sign = kDown * kDown;
 #pragma unroll
         for (int chunk = 0; chunk < CHUNKS; ++chunk) {
-            uint4 p[S / SB][1][SB][kSP], x[kRaw];
-            hand_over(chunk, x);
+            uint4 p[S / SB][1][SB][kSP], x[kRaw], y[kRaw];
+            if constexpr (Q::kForms) {
+#pragma unroll
+                for (int k = 0; k < kRaw; ++k) form_piece<T>(g.prologue.act, raw[chunk][k], low[chunk][k], low[chunk][k]);
+            }
+            hand_over(chunk, raw[chunk], x);
+            if constexpr (kLow) hand_over(chunk, low[chunk], y);
+            if constexpr (Q::kForms) {
+                if (g.prologue.formed && block == 0) {
+#pragma unroll
+                    for (int k = 0; k < kRaw; ++k) {
+                        const int64_t i = r0 + 8 * k + (lane >> 3);
+                        float v[N];
+                        Cols<T>::unpack(raw[chunk][k], v);
+                        if (i < g.n) Cols<T>::store(static_cast<T*>(g.prologue.formed) + i * a.C, chunk * CH + (lane & 7) * N, a.C, v);
+                    }
+                }
+            }
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 if constexpr (PC == 3) {
@@ -208,18 +232,34 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E> g)
                     for (int s = 0; s < kEarly; ++s) residual_of<T, Sh>(a.epilogue, at, s, res[s]);
                 }
             }
-            fetch(min(tile + step, tiles - 1), chunk);         // (the last one's are not looked at)
+            fetch_chunk(min(tile + step, tiles - 1), chunk);         // (the last one's are not looked at)
 #pragma unroll
             for (int part = 0; part < S / SB; ++part) {
+                const uint4* const b = lds + (chunk * (S / SB) + part) * (kFrags * 64) + lane;
                 float16_t(&sums)[1][NT] = reinterpret_cast<float16_t(&)[1][NT]>(acc);
-                multiply_stage<T, NT, 1, NT>(lds + (chunk * (S / SB) + part) * (kFrags * 64) + lane, p[part], sign, sums);
+                if constexpr (kLow) {
+                    auto add = [&](int i, const uint4& v, const uint4& w) SAR_INLINE {
+                        acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v), __builtin_bit_cast(bf16x8_t, w), acc[i], 0, 0, 0);
+                    };
+#pragma unroll
+                    for (int s = 0; s < SB; ++s)
+#pragma unroll
+                        for (int i = 0; i < NT; ++i) {
+                            const uint4 w0 = b[s * PC * NT * 64 + i * 64], w1 = b[(s * PC + 1) * NT * 64 + i * 64];
+                            add(i, x[part * SB + s], w1);
+                            add(i, y[part * SB + s], w0);
+                            add(i, x[part * SB + s], w0);
+                        }
+                } else {
+                    multiply_stage<T, NT, 1, NT>(b, p[part], sign, sums);
+                }
             }
             sign = -sign;
         }
         bool odd = false;
 #pragma unroll
         for (int i = 0; i < NT; ++i) odd |= not_finite(acc[i]);
-        if (__any(odd)) exact_tiles<T, Sh, TRANS>(a, NoPrologue{}, 0, min(r0 + (lane & 31), g.n - 1), n0, 0, acc);
+        if (__any(odd)) exact_tiles<T, Sh, TRANS>(a, g.prologue, 0, min(r0 + (lane & 31), g.n - 1), n0, 0, acc);
         const Place<Sh> at = place();
         if constexpr (RES) {
 #pragma unroll
@@ -240,8 +280,8 @@ bool fits_kept(int C, int N)
 }
 
 // out [n, N] = A [n, C] B; TRANS: B = W^T.  work: lay_bytes.
-template <typename T, int CHUNKS, bool TRANS, typename E>
-int run_kept_chunks(const void* A, const float* W, int64_t n, void* out, int K, int F, void* work, hipStream_t st, const E& e)
+template <typename T, int CHUNKS, bool TRANS, typename E, typename Q>
+int run_kept_chunks(const void* A, const float* W, int64_t n, void* out, int K, int F, void* work, hipStream_t st, const E& e, const Q& q)
 {
     constexpr int NT = kKeptTiles;
     const int C = TRANS ? F : K, N = TRANS ? K : F, blocks = (N + 32 * NT - 1) / (32 * NT);
@@ -250,7 +290,7 @@ int run_kept_chunks(const void* A, const float* W, int64_t n, void* out, int K, 
     const LayArgs l{W, pieces, 1, K, F, C, N, CHUNKS, blocks, Types{nullptr, 1, n}, nullptr, 0, (unsigned)lay};
     k_typed_lay<T, NT, TRANS, WholeShare<T, NT>><<<(unsigned)lay, 256, 0, st>>>(l);
     SAR_LAUNCH_CHECK();
-    const KeptArgs<E> a{{A, pieces, W, out, nullptr, C, N, CHUNKS, blocks, K, F, e}, n};
+    const KeptArgs<E, Q> a{{A, pieces, W, out, nullptr, C, N, CHUNKS, blocks, K, F, e}, n, q};
     constexpr size_t shared = ((size_t)CHUNKS * Mode<T>::kSteps * Mode<T>::kPieces * NT + kKeptWaves * 4) * 1024;
     const int turns = std::max(1, (shared > kKeptLds / 2 ? 32 : 64) / blocks);
     auto launch = [&](auto* fn) {
@@ -260,19 +300,19 @@ int run_kept_chunks(const void* A, const float* W, int64_t n, void* out, int K, 
         return (int)SAR_OK;
     };
     if constexpr (E::kAny) {
-        if (e.res) return launch(k_rows_kept<T, NT, CHUNKS, TRANS, true, E>);
+        if (e.res) return launch(k_rows_kept<T, NT, CHUNKS, TRANS, true, E, Q>);
     }
-    return launch(k_rows_kept<T, NT, CHUNKS, TRANS, false, E>);
+    return launch(k_rows_kept<T, NT, CHUNKS, TRANS, false, E, Q>);
 }
 
-template <typename T, bool TRANS, typename E>
-int run_kept(const void* A, const float* W, int64_t n, void* out, int K, int F, void* work, hipStream_t st, const E& e)
+template <typename T, bool TRANS, typename E, typename Q = NoPrologue>
+int run_kept(const void* A, const float* W, int64_t n, void* out, int K, int F, void* work, hipStream_t st, const E& e, const Q& q = {})
 {
     switch (((TRANS ? F : K) + kChunk<T> - 1) / kChunk<T>) {
-    case 1: return run_kept_chunks<T, 1, TRANS>(A, W, n, out, K, F, work, st, e);
-    case 2: return run_kept_chunks<T, 2, TRANS>(A, W, n, out, K, F, work, st, e);
-    case 3: return run_kept_chunks<T, 3, TRANS>(A, W, n, out, K, F, work, st, e);
-    default: return run_kept_chunks<T, 4, TRANS>(A, W, n, out, K, F, work, st, e);
+    case 1: return run_kept_chunks<T, 1, TRANS>(A, W, n, out, K, F, work, st, e, q);
+    case 2: return run_kept_chunks<T, 2, TRANS>(A, W, n, out, K, F, work, st, e, q);
+    case 3: return run_kept_chunks<T, 3, TRANS>(A, W, n, out, K, F, work, st, e, q);
+    default: return run_kept_chunks<T, 4, TRANS>(A, W, n, out, K, F, work, st, e, q);
     }
 }
 

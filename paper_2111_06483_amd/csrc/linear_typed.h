@@ -100,7 +100,7 @@ struct Bf16Formed {
     static constexpr bool kSums = true, kFormed = true, kWritten = false;
     using Plain = Bf16Rows;
 };
-// ... and written, rounded, for the other product.
+// ... and written, rounded, and what the rounding left, for the other product.
 struct Bf16Written : Bf16Formed {
     static constexpr bool kWritten = true;
 };
@@ -129,6 +129,7 @@ struct DwArgs {
     int act = 0;
     float* sums = nullptr;
     void* formed = nullptr;
+    void* low = nullptr;
 };
 
 // A value of X as fp32.

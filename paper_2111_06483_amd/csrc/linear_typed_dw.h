@@ -120,10 +120,10 @@ struct FormedUnit {
         Plain::load(w + Plain::kRegs, pre, group, rows, full, c, width);
     }
     // `negate`: of dY's sign, which leaves X as it is (a quarter of the values to turn)
-    // `formed`: WRITTEN: the chunk's rows of dA, which are written as bf16 (what is not there: outside of the buffer).
+    // `formed`, `low`: WRITTEN: the chunk's rows of dA, which are written as bf16, and of what that leaves, or null (what is not there: outside of the buffer).
     template <bool WRITTEN>
     static __device__ SAR_INLINE inline void put(uint32_t* w, int act, uint4* out, int stride, int group, int rows, bool full, int c, int width, bool negate,
-                                                 float (&sums)[2], bf16_t* formed, bool mine)
+                                                 float (&sums)[2], bf16_t* formed, bf16_t* low, bool mine)
     {
         float v[2][8];
         const uint32_t flip = negate ? 0x80008000u : 0u;
@@ -148,14 +148,6 @@ struct FormedUnit {
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[0][k] = v[1][k];
         }
-        if constexpr (WRITTEN) {
-            const auto buffer = __builtin_amdgcn_make_buffer_rsrc(formed, 0, mine ? rows * width * (int)sizeof(bf16_t) : 0, 0x00020000);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int place = ((8 * group + k) * width + c) * (int)sizeof(bf16_t);
-                __builtin_amdgcn_raw_buffer_store_b32(pack2_bf16(v[0][k], v[1][k]) ^ flip, buffer, c < width ? place : -1, 0, 0);
-            }
-        }
         uint32_t hi[2][4], lo[2][4];
         float largest = 0.f;
 #pragma unroll
@@ -179,6 +171,17 @@ struct FormedUnit {
                     if ((hi[j][k] & 0x7fffu) == 0x7f80u) lo[j][k] &= 0xffff0000u;
                     if ((hi[j][k] & 0x7fff0000u) == 0x7f800000u) lo[j][k] &= 0xffffu;
                 }
+        }
+        if constexpr (WRITTEN) {
+            const int bytes = mine ? rows * width * (int)sizeof(bf16_t) : 0;
+            const auto first = __builtin_amdgcn_make_buffer_rsrc(formed, 0, bytes, 0x00020000), second = __builtin_amdgcn_make_buffer_rsrc(low, 0, low ? bytes : 0, 0x00020000);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int place = c < width ? ((8 * group + k) * width + c) * (int)sizeof(bf16_t) : -1;
+                const uint32_t which = k % 2 ? 0x07060302u : 0x05040100u;
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(hi[1][k / 2], hi[0][k / 2], which) ^ flip, first, place, 0, 0);
+                __builtin_amdgcn_raw_buffer_store_b32(__builtin_amdgcn_perm(lo[1][k / 2], lo[0][k / 2], which) ^ flip, second, place, 0, 0);
+            }
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -335,7 +338,8 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
             const int g = id / (TF / 2), c = id % (TF / 2) * 2;
             if constexpr (ZTraits<ZR>::kFormed) {
                 FormedUnit::put<ZR::kWritten>(raw.z[u], a.act, buf + kXSize + g * TF + place_of(c), kGroups * TF, g, rows, full, f0 + c, a.F, negate, sums[u],
-                                              ZR::kWritten ? static_cast<bf16_t*>(a.formed) + r0 * a.F : nullptr, blockIdx.y == 0);
+                                              ZR::kWritten ? static_cast<bf16_t*>(a.formed) + r0 * a.F : nullptr,
+                                              ZR::kWritten && a.low ? static_cast<bf16_t*>(a.low) + r0 * a.F : nullptr, blockIdx.y == 0);
             } else {
                 Unit<Plain>::put(raw.z[u], buf + kXSize + g * TF + place_of(c), kGroups * TF, g, rows, full, f0 + c, a.F, false);
                 if constexpr (ZTraits<ZR>::kSums) {

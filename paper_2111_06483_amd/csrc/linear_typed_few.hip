@@ -113,6 +113,7 @@ __device__ SAR_INLINE inline void few_rows(const TypedRows& a, int64_t row_block
         for (int u = 0; u < U; ++u) {
             const int c = k0 + u * 16 + h * 8;
             if (k0 + u * 16 >= a.C) break;
+            uint4 low = make_uint4(0u, 0u, 0u, 0u);        // (bf16: a piece is the product's eight values)
             if constexpr (Q::kAny) {
 #pragma unroll
                 for (int p = 0; p < kRaw; ++p) {
@@ -120,7 +121,7 @@ __device__ SAR_INLINE inline void few_rows(const TypedRows& a, int64_t row_block
                     auto cut = [&](uint4& v) SAR_INLINE { v = make_uint4(v.x & m.x, v.y & m.y, v.z & m.z, v.w & m.w); };
                     cut(g.x[u][p]);
                     cut(g.pre[u][p]);
-                    form_piece<T>(prologue.act, g.x[u][p], g.pre[u][p]);
+                    form_piece<T>(prologue.act, g.x[u][p], g.pre[u][p], low);
                     if (prologue.formed && n0 == 0 && first + (lane & 31) < end) {
                         float v[N];
                         Cols<T>::unpack(g.x[u][p], v);
@@ -153,6 +154,8 @@ __device__ SAR_INLINE inline void few_rows(const TypedRows& a, int64_t row_block
                     big[j] = pack2_bf16(w[2 * j], w[2 * j + 1]);
                     small[j] = pack2_bf16(w[2 * j] - __uint_as_float(big[j] << 16), w[2 * j + 1] - __uint_as_float(big[j] & 0xffff0000u));
                 }
+                if constexpr (Q::kAny)
+                    acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, low), __builtin_bit_cast(bf16x8_t, make_uint4(big[0], big[1], big[2], big[3])), acc[0], 0, 0, 0);
                 acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p), __builtin_bit_cast(bf16x8_t, make_uint4(small[0], small[1], small[2], small[3])), acc[0], 0, 0, 0);
                 acc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, p), __builtin_bit_cast(bf16x8_t, make_uint4(big[0], big[1], big[2], big[3])), acc[0], 0, 0, 0);
             }

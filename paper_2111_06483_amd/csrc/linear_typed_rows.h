@@ -450,6 +450,10 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a
     constexpr int kRaw = 64 / 16;                        // 16-byte pieces of a row that a lane holds of a chunk
     constexpr int kFrags = kStageFrags<T, NT>, kSP = P == 3 ? 3 : 1;
     static_assert(S / SB == 2, "a barrier between taking a chunk's rows and handing over the next one's");
+    // Bf16 rows in two pieces are multiplied in two turns a chunk, by their first pieces and by their second ones, which wait in registers that hold the next
+    // chunk's rows afterwards.
+    constexpr int kTurns = Q::kAny && sizeof(T) == 2 ? 2 : 1;
+    static_assert(!Q::kAny || Q::kForms || sizeof(T) == 2, "two pieces of bf16");
     extern __shared__ __attribute__((aligned(16))) uint4 lds[];      // [2][kFrags][64] of B, [4][32][8] of rows
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5, wr = wave / Sh::WC, wc = wave % Sh::WC;
 
@@ -489,9 +493,15 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a
     uint4 pre[Q::kAny ? kRaw : 1];
     auto fetch_a = [&](const Tile& w, int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
         fetch_from(a.A, w, chunk, v);
-        if constexpr (Q::kAny) fetch_from(prologue.pre, w, chunk, pre);
+        if constexpr (Q::kForms) fetch_from(prologue.pre, w, chunk, pre);
+        else if constexpr (Q::kAny) fetch_from(prologue.low, w, chunk, pre);
     };
     uint4* const rows = lds + 2 * kFrags * 64;
+    uint4 later[kTurns > 1 ? kRaw : 1];
+    auto to_lds = [&](const uint4 (&v)[kRaw]) SAR_INLINE {
+#pragma unroll
+        for (int p = 0; p < kRaw; ++p) rows[wave * 256 + (8 * p + (lane >> 3)) * 8 + ((lane & 7) ^ (lane >> 3))] = v[p];
+    };
     auto hand_over = [&](const Tile& w, int chunk, uint4 (&v)[kRaw]) SAR_INLINE {
         const int c = chunk * CH + (lane & 7) * N;
         if ((chunk + 1) * CH > a.C && c + N > a.C) {
@@ -505,9 +515,9 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a
                 if constexpr (Q::kAny) cut(pre[p]);
             }
         }
-        if constexpr (Q::kAny) {
+        if constexpr (Q::kForms) {
 #pragma unroll
-            for (int p = 0; p < kRaw; ++p) form_piece<T>(prologue.act, v[p], pre[p]);
+            for (int p = 0; p < kRaw; ++p) form_piece<T>(prologue.act, v[p], pre[p], later[kTurns > 1 ? p : 0]);
             if (prologue.formed && blockIdx.y == 0) {
 #pragma unroll
                 for (int p = 0; p < kRaw; ++p) {
@@ -517,9 +527,11 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a
                     if (i < w.end) Cols<T>::store(static_cast<T*>(prologue.formed) + i * a.C, c, a.C, u);
                 }
             }
-        }
+        } else if constexpr (Q::kAny) {
 #pragma unroll
-        for (int p = 0; p < kRaw; ++p) rows[wave * 256 + (8 * p + (lane >> 3)) * 8 + ((lane & 7) ^ (lane >> 3))] = v[p];
+            for (int p = 0; p < kRaw; ++p) later[p] = pre[p];
+        }
+        to_lds(v);
     };
     auto take = [&](int m, uint4 (&v)[kRaw]) SAR_INLINE {
 #pragma unroll
@@ -547,8 +559,10 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a
 #pragma unroll
             for (int i = 0; i < NW; ++i) acc[m][i] = float16_t{};
         float sign = kDown * kDown;        // (fp32 products: rows' and weights' 2^24)
-        for (int chunk = 0; chunk < a.chunks; ++chunk) {
-            const bool more = chunk + 1 < a.chunks, coming = more ? here : there;
+        for (int turn = 0; turn < a.chunks * kTurns; ++turn) {
+            const int chunk = turn / kTurns;
+            const bool second = kTurns > 1 && turn % kTurns == 0;         // the next turn is that of this chunk's second pieces
+            const bool more = chunk + 1 < a.chunks, coming = !second && (more ? here : there);
             uint4 p[S / SB][MR][SB][kSP];
             if (works) {
 #pragma unroll
@@ -573,12 +587,16 @@ __global__ __launch_bounds__(kTileWaves * 64, 2) void k_typed_rows(RowsArgs<E> a
 #pragma unroll
             for (int part = 0; part < S / SB; ++part) {
                 const int stage = chunk * (S / SB) + part;
-                const uint4* from = stage + 1 < stages ? pieces_of(tile, stage + 1) : another ? pieces_of(after, 0) : nullptr;
+                const bool again = second && part == S / SB - 1;
+                const uint4* from = again ? pieces_of(tile, chunk * (S / SB)) : stage + 1 < stages ? pieces_of(tile, stage + 1) : another ? pieces_of(after, 0) : nullptr;
                 stage_products<T, NT>(lds + (buffer ^ 1) * kFrags * 64, from, lds + (buffer * kFrags + wc * NW) * 64 + lane, p[part], sign, works,
                                       acc, [&]() SAR_INLINE {
                                           if (part == 0 && coming) fetch_a(more ? tile : after, more ? chunk + 1 : 0, raw);
                                       });
                 if (part == S / SB - 1 && coming) hand_over(more ? tile : after, more ? chunk + 1 : 0, raw);
+                if constexpr (kTurns > 1) {
+                    if (again && here) to_lds(later);
+                }
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
                 buffer ^= 1;
@@ -635,7 +653,8 @@ size_t list_bytes(int64_t n, int T) { return (size_t)(most_tiles(n, T) + 1) * si
 template <typename T, bool TRANS, typename E = NoEpilogue, typename Q = NoPrologue>
 int rows_product(const void* A, const float* W, const Types& types, void* out, int K, int F, void* work, hipStream_t st, const E& e = {}, const Q& q = {})
 {
-    const int C = TRANS ? F : K, N = TRANS ? K : F, NT = tiles_of(types.n, N);
+    // (formed bf16 rows, whose pieces take registers: four column tiles at most; 867187 x 256 -> 256, by GELU, 803 us, by eight, which spill 57, 951)
+    const int C = TRANS ? F : K, N = TRANS ? K : F, NT = std::min(tiles_of(types.n, N), Q::kForms && sizeof(T) == 2 ? 4 : 8);
     if (!Q::kAny && few_blocks(types, N)) return few_product(sizeof(T) == 4 ? SAR_F32 : SAR_BF16, TRANS, {A, W, out, types, C, N, K, F}, e, st);
     const int chunks = (C + kChunk<T> - 1) / kChunk<T>, blocks = (N + 32 * NT - 1) / (32 * NT);
     const int64_t most = most_tiles(types.n, types.T);
@@ -643,7 +662,10 @@ int rows_product(const void* A, const float* W, const Types& types, void* out, i
     uint4* const pieces = static_cast<uint4*>(work) + (most + 1);
     const RowsArgs<E> a{A, pieces, W, out, list, C, N, chunks, blocks, K, F, e};
     const LayArgs l{W, pieces, types.T, K, F, C, N, chunks, blocks, types, list, most, 0};
-    return NT == 2 ? run_rows<T, 2, TRANS>(a, q, l, st) : NT == 4 ? run_rows<T, 4, TRANS>(a, q, l, st) : run_rows<T, 8, TRANS>(a, q, l, st);
+    if constexpr (!(Q::kForms && sizeof(T) == 2)) {
+        if (NT == 8) return run_rows<T, 8, TRANS>(a, q, l, st);
+    }
+    return NT == 2 ? run_rows<T, 2, TRANS>(a, q, l, st) : run_rows<T, 4, TRANS>(a, q, l, st);
 }
 
 }  // namespace
