@@ -1,6 +1,7 @@
 // What is done to a row of X W before it is stored: bias, residual, activation (linear_act.hip); the activations and their derivatives.
 #pragma once
 
+#include "linear_typed.h"
 #include "packed.h"
 #include "sar_internal.h"
 
@@ -160,6 +161,18 @@ __device__ inline float finish_value(const Epilogue& e, float v, float bias, flo
     if (e.pre) static_cast<T*>(e.pre)[at] = from_f32<T>(v);
     with_act(e.act, [&](auto act) { v = act_of<decltype(act)::value>(v); });
     return e.after ? v + res : v;
+}
+
+// A value of dZ, formed where ZR's rows are.
+template <typename ZR>
+__device__ __attribute__((always_inline)) inline float whole_z(const DwArgs& a, int64_t r, int f)
+{
+    float v = z_value<typename ZTraits<ZR>::Plain>(a, r, f);
+    if constexpr (ZTraits<ZR>::kFormed) {
+        const float pre = value_of(static_cast<const typename ZR::T*>(a.pre)[r * a.F + f]);
+        with_act(a.act, [&](auto which) { v = act_grad<decltype(which)::value>(v, pre); });
+    }
+    return v;
 }
 
 // dW (+)= X^T dA and db (+)= the sums of dA's columns, dA = dY act'(A) formed where it is read (bf16), or dY as it is (act 0, pre null); db may be

@@ -513,14 +513,14 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
     }
 }
 
-// What a workgroup's place w + t should hold where it holds no finite number: three pieces of bf16 are no infinity, no NaN and none of the
-// numbers that are too large to be scaled up (kUp).  Summed again from the operands, by multiply-adds.
+// What a workgroup's place w + t should hold where it holds no finite number: pieces of bf16 are no infinity and no NaN, three of them none of the
+// numbers that are too large to be scaled up (kUp), and an infinity of X times a second piece of zero is NaN.  Summed again from the operands, by multiply-adds.
 template <typename XR, typename ZR>
 __device__ float sum_again(const DwArgs& a, int64_t w, int64_t lo, int64_t hi, int64_t element)
 {
     const int k = (int)(element / a.F), f = (int)(element % a.F);
     float v = 0.f;
-    for (int64_t r = max(lo, w * a.share); r < min(hi, (w + 1) * a.share); ++r) v = fmaf(x_value<XR>(a, r, k), z_value<ZR>(a, r, f), v);
+    for (int64_t r = max(lo, w * a.share); r < min(hi, (w + 1) * a.share); ++r) v = fmaf(x_value<XR>(a, r, k), whole_z<ZR>(a, r, f), v);
     return v;
 }
 
@@ -581,7 +581,7 @@ __global__ __launch_bounds__(256) void k_typed_sum(DwArgs a, int accumulate, flo
                     x[u] = Values{};
                     if (w + u * 8 < w1) x[u] = *reinterpret_cast<const Values*>(p + (w + u * 8) * count);
                 }
-                if constexpr (ZR::kPieces == 3) {
+                if constexpr (ZR::kPieces > 1) {
                     float zero = 0.f;
 #pragma unroll
                     for (int u = 0; u < 4 * V; ++u) zero = fmaf(x[u / V].v[u % V], 0.f, zero);
@@ -698,12 +698,12 @@ int run_all(const DwArgs& a, const Shape& s, int accumulate, float* dW, hipStrea
     const int64_t count = (int64_t)a.K * a.F;
     const bool single = count % 4 != 0 || count * a.types.T < 512 * 128;
     const int64_t per = single ? 32 : 128, blocks = std::min<int64_t>((count + per - 1) / per, 1 << 20);
-    using Plain = typename ZTraits<ZR>::Plain;
+    using Rows = std::conditional_t<ZTraits<ZR>::kFormed, Bf16Formed, typename ZTraits<ZR>::Plain>;
     // (columns' sums in a launch of their own: 5 us more)
     constexpr bool kSums = ZTraits<ZR>::kSums;
     const dim3 grid((unsigned)(blocks + (db ? (a.F + 7) / 8 : 0)), a.types.T);
-    if (single) k_typed_sum<XR, Plain, 1, kSums><<<grid, 256, 0, st>>>(a, accumulate, dW, (int)blocks, db);
-    else k_typed_sum<XR, Plain, 4, kSums><<<grid, 256, 0, st>>>(a, accumulate, dW, (int)blocks, db);
+    if (single) k_typed_sum<XR, Rows, 1, kSums><<<grid, 256, 0, st>>>(a, accumulate, dW, (int)blocks, db);
+    else k_typed_sum<XR, Rows, 4, kSums><<<grid, 256, 0, st>>>(a, accumulate, dW, (int)blocks, db);
     SAR_LAUNCH_CHECK();
     return SAR_OK;
 }

@@ -309,14 +309,6 @@ __device__ SAR_INLINE inline void few_weights(const DwArgs& a, int accumulate, f
             for (int r = 0; r < 16; ++r) acc[r] = fmaf(sum[r], (PX == 3 ? kDown : 1.f) * (PZ == 3 ? kDown : 1.f), acc[r]);
         }
     };
-    auto whole_z = [&](int64_t r) SAR_INLINE {
-        float v = z_value<Plain>(a, r, f);
-        if constexpr (Z::kFormed) {
-            const float pre = value_of(static_cast<const typename ZR::T*>(a.pre)[r * a.F + f]);
-            with_act(a.act, [&](auto which) { v = act_grad<decltype(which)::value>(v, pre); });
-        }
-        return v;
-    };
     const int64_t from = lo + wave * 16;
     constexpr int kNext = U * kTurn;
     if (from < hi) {
@@ -329,12 +321,12 @@ __device__ SAR_INLINE inline void few_weights(const DwArgs& a, int accumulate, f
             if (r0 + 2 * kNext < hi) load(s[0], r0 + 2 * kNext);
             multiply(s[1], r0 + kNext);
         }
-        if (PZ == 3 && __any(not_finite(acc))) {
+        if (PZ > 1 && __any(not_finite(acc))) {        // (an infinity times a second piece of nothing is NaN)
             acc = float16_t{};
             for (int64_t r0 = from; r0 < hi; r0 += kTurn)
                 for (int64_t r = r0; r < min(r0 + 16, hi); r += 2) {
                     const bool in = r + h < hi;
-                    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(in ? x_value<XR>(a, r + h, k) : 0.f, in ? whole_z(r + h) : 0.f, acc, 0, 0, 0);
+                    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(in ? x_value<XR>(a, r + h, k) : 0.f, in ? whole_z<ZR>(a, r + h, f) : 0.f, acc, 0, 0, 0);
                 }
         }
     }
