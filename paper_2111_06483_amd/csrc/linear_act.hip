@@ -5,10 +5,11 @@
 // Bias, residual and activation meet the sums in registers, in 32 bits, and are rounded once; the products are formed as in linear_typed.hip (one type).
 //   - Forward, and dX of rows that are already dA: many rows by linear_kept.h, whose wavefronts keep memory busy while they multiply; operands that do not fit
 //     there by linear_typed_rows.h; few rows in one launch by linear_typed_few.hip.  Activations cost instructions: GELU some 20 a value, 60 us of 867187 x 256 values.
-//   - Backward: dA is formed where a product brings its rows, never in a pass of its own but where no product wants it (k_act_bwd), or few rows' columns are
-//     many.  bf16: the product for dW forms it (linear_act_dw.hip), as two pieces of bf16, and writes them for dX, which multiplies them as such: rounded to one, dA
+//   - Backward: dA is formed where a product brings its rows, never in a pass of its own but where no product wants it (k_act_bwd).
+//     bf16: the product for dW forms it (linear_act_dw.hip), as two pieces of bf16, and writes them for dX, which multiplies them as such: rounded to one, dA
 //     would have dX off by another rounding of its own size.  fp32: the product for dX forms and
-//     writes it, the one for dW reads it.  db leaves with dW.  Few rows: dW, db, dX and dA in one launch.
+//     writes it, the one for dW reads it.  db leaves with dW.  Few rows: dW, db, dX and dA in one launch, or one
+//     each where dX has many columns.
 // What bounds it: forward, 867187 x 256 -> 256, bf16, GELU, a residual and its argument kept: 428 to 451 us, 4.0 TB/s of its 1.78 GB (their copy: 349), the vector
 // instructions in use 63% of the time, the matrix cores 28%; 306250 x 100 -> 256, fp32, ReLU with a residual 180 us, 4.2 TB/s.  Backward, 867187 x 256 -> 256, bf16, GELU: 727
 // to 767 us, of it dW 450 (2.2 GB with the dA that it writes; vector instructions 70%), dX 270; 306250 x 256 -> 256, fp32, ELU 605 to 640 us, 128 TFLOP/s of products (a large
@@ -27,7 +28,6 @@ struct ActBwdArgs {
     const void* dY;
     const void* A;
     void* dA;              // [n, F] of dtype, or null
-    void* low;             // bf16: what dA's rounding left, in bf16; or null
     float* partial;        // [gridDim.x, F], or null
     int64_t n;
     int F, act, lanes;     // lanes: of a row, a power of two
@@ -56,13 +56,6 @@ __global__ __launch_bounds__(kActThreads) void k_act_bwd(ActBwdArgs a)
 #pragma unroll
         for (int j = 0; j < N; ++j) total[j] += d[j];
         if (a.dA) Cols<T>::store(static_cast<T*>(a.dA) + at, c, a.F, d);
-        if (a.low) {
-            float high[N];
-            Cols<T>::unpack(Cols<T>::round(d), high);
-#pragma unroll
-            for (int j = 0; j < N; ++j) d[j] -= high[j];
-            Cols<T>::store(static_cast<T*>(a.low) + at, c, a.F, d);
-        }
     }
     if (!a.partial) return;
 #pragma unroll
@@ -168,18 +161,18 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
     // What forms dA of many rows: in bf16 the product for dW, which writes it for dX (two pieces, of which the first may be the caller's dA), or for who asked for it;
     // without that the product for dX; otherwise a launch of its own.  (867187 x 256 -> 256, bf16, GELU: dW writes it 886 us, of one piece, that dX had fewer bits of, 735;
     // dX alone, which forms it for either half of its columns, 625.)
-    const bool bf16 = sizeof(T) == 2, again = formed && dW && !few_dw && bf16;
+    // (Few rows' dW forms it in either type, with db.)
+    const bool bf16 = sizeof(T) == 2, few = dW && few_dw && n > 0, again = formed && dW && !few_dw && bf16;
     const bool writes = again && F % 2 == 0 && n > 0 && (dA || (dX && !few_dx));
     const bool within = formed && dX && n > 0 && (few_dx ? bf16 : !writes);
-    const bool reads = (dW && !again) || (dX && !within);
+    const bool reads = (dW && !few && !again) || (dX && !within);
     void* const rows = !formed ? const_cast<void*>(dY) : dA ? dA : reads ? high : nullptr;
     char* const second = high + rounded((size_t)n * F * sizeof(bf16_t));       // (bf16)
-    void* const low = formed && dW && few_dw && bf16 ? second : nullptr;
-    const bool sums = db && (!dW || few_dw);       // (otherwise with dW)
+    const bool sums = db && !dW;       // (otherwise with dW)
     void* const written = formed ? (within || writes ? nullptr : rows) : dA;
-    if (n > 0 && (written || low || sums)) {
+    if (n > 0 && (written || sums)) {
         const int lanes = lanes_of(dtype, F), groups = groups_of(dtype, n, F);
-        const ActBwdArgs a{dY, A, written, low, sums ? partial : nullptr, n, F, act, lanes};
+        const ActBwdArgs a{dY, A, written, sums ? partial : nullptr, n, F, act, lanes};
         const int across = (F + lanes * Cols<T>::N - 1) / (lanes * Cols<T>::N);
         k_act_bwd<T><<<dim3(groups, across), kActThreads, 0, st>>>(a);
         SAR_LAUNCH_CHECK();
@@ -197,12 +190,8 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
         else if (kept<T>(n, F, K)) SAR_TRY((run_kept<T, true>(rows, W, n, dX, K, F, work, st, NoEpilogue{})));
         else SAR_TRY((rows_product<T, true>(rows, W, types, dX, K, F, work, st)));
     }
-    if (dW && few_dw) {
-        SAR_TRY(typed_dw(dtype, {X, nullptr, nullptr, rows, dW, types, K, F, accumulate, static_cast<float*>(work)}, st));
-        if (low && n > 0) SAR_TRY(typed_dw(dtype, {X, nullptr, nullptr, low, dW, types, K, F, 1, static_cast<float*>(work)}, st));
-    } else if (dW && !writes) {
-        SAR_TRY(weights());
-    }
+    if (few) return few_act_bwd(dtype, {X, nullptr, nullptr, dY, dW, types, K, F, accumulate, nullptr, formed ? A : nullptr, act, db}, {}, nullptr, st);
+    if (dW && !writes) return weights();
     return SAR_OK;
 }
 

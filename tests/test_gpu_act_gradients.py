@@ -4,7 +4,7 @@ import torch
 
 from paper_2111_06483_amd import sar
 from tests import nodewise as nw
-from tests.test_gpu_linear_act import ACTS, act, f64, inputs, scratch, stored
+from tests.test_gpu_linear_act import ACTS, act, check_bwd, f64, inputs, scratch, stored
 from tests.test_gpu_linear_typed import rows_off
 
 pytestmark = pytest.mark.gpu
@@ -49,3 +49,13 @@ def test_dx_rounds_once(n, K, F, want):
         assert ((f64(out["dX"]) - exact).abs() <= stored(BF16, tol, exact)).all(), name
         if "dA" in want:
             assert ((f64(out["dA"]) - d).abs() <= stored(BF16, off, d)).all(), name
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("want", [("dW", "dA"), ("db", "dA"), ("dW", "db", "dA"), ("db", "dX", "dA"), ("dW", "db", "dX")])
+# few rows; few of which dX has many columns; dX's blocks few and dW's rows not; many
+@pytest.mark.parametrize("n,K,F", [(1, 7, 9), (300, 40, 72), (100, 40_000, 32), (2000, 64, 128), (9001, 47, 71), (66_000, 80, 72)])
+def test_more_forms(n, K, F, want, dtype):
+    for name in ("none", "gelu"):
+        check_bwd(n, K, F, dtype, name, want=want, seed=3)
+        check_bwd(n, K, F, dtype, name, accumulate=True, want=want, seed=4)

@@ -56,10 +56,19 @@ def check(n, K, F, dtype, name, want, in_X, in_dY):
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("name", ["none", "relu", "silu"])
-# few rows, many, kept operands, more than what is kept
-@pytest.mark.parametrize("n,K,F", [(300, 40, 72), (2000, 64, 128), (3000, 40, 71), (20_000, 300, 260), (65_600, 80, 72), (65_600, 80, 255)])
+# few rows, few rows of which dX has many columns, many, kept operands, more than what is kept
+@pytest.mark.parametrize("n,K,F", [(300, 40, 72), (100, 40_000, 32), (2000, 64, 128), (3000, 40, 71), (20_000, 300, 260), (65_600, 80, 72), (65_600, 80, 255)])
 def test_they_reach_the_gradients_that_have_them(n, K, F, name, dtype):
     for in_X, in_dY in ((True, False), (False, True), (True, True)):
         check(n, K, F, dtype, name, ALL, in_X, in_dY)
         check(n, K, F, dtype, name, ("dW", "db"), in_X, in_dY)
         check(n, K, F, dtype, name, ("dW", "dX"), in_X, in_dY)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("name", ["none", "relu", "silu"])
+@pytest.mark.parametrize("n,K,F", [(300, 40, 72), (100, 40_000, 32), (3000, 40, 71), (65_600, 80, 72)])
+def test_without_the_rows_gradient(n, K, F, name, dtype):
+    for in_X, in_dY in ((False, False), (True, False), (False, True)):
+        check(n, K, F, dtype, name, ("dW", "dA"), in_X, in_dY)
+        check(n, K, F, dtype, name, ("dW", "db", "dA"), in_X, in_dY)
