@@ -160,10 +160,12 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
     }
     // What forms dA of many rows: in bf16 the product for dW, which writes it for dX (two pieces, of which the first may be the caller's dA), or for who asked for it;
     // without that the product for dX; otherwise a launch of its own.  (867187 x 256 -> 256, bf16, GELU: dW writes it 886 us, of one piece, that dX had fewer bits of, 735;
-    // dX alone, which forms it for either half of its columns, 625.)
+    // dX alone, which forms it for either half of its columns, 625.)  One block of columns of dX that is kept forms it again for fewer bytes: 400000 rows, written / formed twice,
+    // 128 -> 256 by SiLU 459 / 386, 128 -> 128 by ReLU 214 / 187, by GELU 230 / 224, with dA wanted 230 / 243; 100 -> 256 by GELU 448 / 423.
     // (Few rows' dW forms it in either type, with db.)
     const bool bf16 = sizeof(T) == 2, few = dW && few_dw && n > 0, again = formed && dW && !few_dw && bf16;
-    const bool writes = again && F % 2 == 0 && n > 0 && (dA || (dX && !few_dx));
+    const bool twice = bf16 && K <= 32 * kKeptTiles && kept<T>(n, F, K);
+    const bool writes = again && F % 2 == 0 && n > 0 && (dA || (dX && !few_dx && !twice));
     const bool within = formed && dX && n > 0 && (few_dx ? bf16 : !writes);
     const bool reads = (dW && !few && !again) || (dX && !within);
     void* const rows = !formed ? const_cast<void*>(dY) : dA ? dA : reads ? high : nullptr;
