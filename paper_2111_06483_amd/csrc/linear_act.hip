@@ -239,7 +239,8 @@ extern "C" int sar_linear_act_bwd(const void* dY, const void* A, const void* X, 
         SAR_CHECK_ARG(!dX || W, "null pointer (W)");
         SAR_CHECK_ARG(!dX || (apart(dX, in, dY, out) && apart(dX, in, A, out) && apart(dX, in, X, in) && apart(dX, in, W, w) && apart(dX, in, dA, out)),
                       "linear with activation: dX must not alias dY, A, X, W or dA");
-        SAR_CHECK_ARG(!dA || (apart(dA, out, dY, out) && apart(dA, out, A, out) && apart(dA, out, X, in)), "linear with activation: dA must not alias dY, A or X");
+        SAR_CHECK_ARG(!dA || (apart(dA, out, dY, out) && apart(dA, out, A, out) && apart(dA, out, X, in) && (!dX || apart(dA, out, W, w))),
+                      "linear with activation: dA must not alias dY, A, X or W");
         SAR_CHECK_ARG(!dW || !W || apart(dW, w, W, w), "linear with activation: dW must not alias W");
     }
     return dtype == SAR_F32 ? act_bwd<float>(dY, A, X, W, act, accumulate, dW, db, dX, dA, n, K, F, work, as_stream(stream))

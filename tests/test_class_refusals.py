@@ -201,3 +201,11 @@ def test_scratch_of_more_rows_serves_fewer(C, k):
 def test_scratch_of_the_transform_grows_with_the_rows(K, F):
     sizes = [sar.sar_linear_act_workspace_bytes(n, K, F) for n in counts()]
     assert sizes == sorted(sizes)
+
+
+def test_the_gradient_in_the_place_of_the_weights(at):
+    lib = sar.lib()
+    bwd = lambda dA, W=at + 2400, dX=at + 4800: lib.sar_linear_act_bwd(at, at + 800, at + 1600, W, 1, 0, at + 3200, at + 4000, dX, dA, 0, 4, 8, 6, at, 1 << 40, None)
+    # (W: 192 bytes, dA: 96)
+    for dA in (at + 2400, at + 2308, at + 2588):
+        assert bwd(dA) == BAD and says("dA must not alias")
