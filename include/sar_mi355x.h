@@ -573,7 +573,7 @@ int sar_logprob_workspace_bytes(int64_t n, int C, int k, size_t* bytes);
  * added to a row's changes nothing), as sar_logprob_fwd lists them.  q = softmax of a row's top_value / T, s = softmax(x / T):
  *   loss[i] = sum_j q_j (log q_j - log s_{top_index_j}),  lse[i] = log sum_c exp(x_c / T)   (fp32 [n], either may be NULL)
  * An index outside 0..C-1 is no entry, nor is a value of -inf; a class listed twice counts twice; a row without entries has loss 0.  0 <= k <= 64;
- * T > 0. */
+ * T > 0, finite, and so that log2(e) / T is. */
 int sar_distill_fwd(const void* X, int k, const float* top_value, const int32_t* top_index, float temperature, float* loss, float* lse, int dtype, int64_t n,
                     int C, void* work, size_t work_bytes, void* stream);
 

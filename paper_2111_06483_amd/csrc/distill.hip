@@ -275,7 +275,7 @@ __global__ __launch_bounds__(kClassThreads) void k_distill_bwd_wide(GradArgs a)
 
 int check_temperature(float T)
 {
-    SAR_CHECK_ARG(T > 0.f && std::isfinite(T) && std::isfinite(1.f / T), "distillation: temperature %g", (double)T);
+    SAR_CHECK_ARG(T > 0.f && std::isfinite(T) && std::isfinite(kLog2e / T), "distillation: temperature %g", (double)T);       // (the larger of its factors)
     return SAR_OK;
 }
 

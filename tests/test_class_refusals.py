@@ -209,3 +209,11 @@ def test_the_gradient_in_the_place_of_the_weights(at):
     # (W: 192 bytes, dA: 96)
     for dA in (at + 2400, at + 2308, at + 2588):
         assert bwd(dA) == BAD and says("dA must not alias")
+
+
+@pytest.mark.parametrize("T", [3.0e-39, 3.5e-39, 4.2e-39])
+def test_temperatures_whose_exponents_have_no_factor(at, T):
+    """1 / T is a number of 32 bits, log2(e) / T is none."""
+    lib, none = sar.lib(), None
+    assert lib.sar_distill_fwd(at, 2, at, at, T, at, at, 0, 4, 8, none, 0, none) == BAD and says("temperature")
+    assert lib.sar_distill_bwd(at, 2, at, at, T, at, at, at, 0, 4, 8, none) == BAD and says("temperature")
