@@ -561,7 +561,7 @@ int sar_linear_act_workspace_bytes(int64_t n, int K, int F, size_t* bytes);
 int sar_logprob_fwd(const void* X, const int32_t* label, float* logp, float* lse, float* entropy, int k, float* top_value, int32_t* top_index, int dtype,
                     int64_t n, int C, void* work, size_t work_bytes, void* stream);
 
-/* dX[i,c] = dlogp[i] ([c = label] - p_c) - dentropy[i] p_c (log p_c + entropy[i])  (OVERWRITTEN, `dtype`, may be X), with p_c = exp(x_c - lse[i]); rows
+/* dX[i,c] = dlogp[i] ([c = label] - p_c) - dentropy[i] p_c (log p_c + entropy[i])  (OVERWRITTEN, `dtype`; X itself or apart from it), with p_c = exp(x_c - lse[i]); rows
  * whose label is no class have no part of dlogp.  lse, entropy from sar_logprob_fwd; dlogp, dentropy fp32 [n], either may be NULL (0); label only for
  * dlogp, entropy only for dentropy. */
 int sar_logprob_bwd(const void* X, const int32_t* label, const float* lse, const float* entropy, const float* dlogp, const float* dentropy, void* dX, int dtype,
@@ -577,7 +577,7 @@ int sar_logprob_workspace_bytes(int64_t n, int C, int k, size_t* bytes);
 int sar_distill_fwd(const void* X, int k, const float* top_value, const int32_t* top_index, float temperature, float* loss, float* lse, int dtype, int64_t n,
                     int C, void* work, size_t work_bytes, void* stream);
 
-/* dX[i,c] = dloss[i] / T (s_c - sum of the q_j whose class is c)  (OVERWRITTEN, `dtype`, may be X; 0 in a row without entries); lse from sar_distill_fwd at the
+/* dX[i,c] = dloss[i] / T (s_c - sum of the q_j whose class is c)  (OVERWRITTEN, `dtype`; X itself or apart from it; 0 in a row without entries); lse from sar_distill_fwd at the
  * same T, dloss fp32 [n]. */
 int sar_distill_bwd(const void* X, int k, const float* top_value, const int32_t* top_index, float temperature, const float* lse, const float* dloss, void* dX,
                     int dtype, int64_t n, int C, void* stream);

@@ -567,6 +567,14 @@ inline ClassTiles class_tiles(int64_t n, int C, int values = kTileValues, int mo
 }
 __device__ inline int tile_row(const ClassTiles& t, int place) { return t.C > 1 ? (int)__umulhi((uint32_t)place, t.magic) : place; }
 
+// Refuses a gradient that lies across the scores: in their place (a workgroup reads its scores before it writes) or beside them.
+inline int check_gradient(const char* what, int dtype, int64_t n, int C, const void* X, const void* dX)
+{
+    const size_t bytes = (size_t)n * C * (dtype == SAR_F32 ? 4 : 2);
+    SAR_CHECK_ARG(dX == X || apart(dX, bytes, X, bytes), "%s: dX overlaps X, and is not X", what);
+    return SAR_OK;
+}
+
 // Refuses what no call takes.
 inline int check_classes(const char* what, int dtype, int64_t n, int C, int k)
 {

@@ -314,6 +314,7 @@ extern "C" int sar_distill_bwd(const void* X, int k, const float* top_value, con
     SAR_TRY(check_temperature(temperature));
     if (n == 0) return SAR_OK;
     SAR_CHECK_ARG(X && lse && dloss && dX && (k == 0 || (top_value && top_index)), "null pointer (X, top_value, top_index, lse, dloss, dX)");
+    SAR_TRY(check_gradient("distillation", dtype, n, C, X, dX));
     int lanes = 1;
     while (lanes < k) lanes <<= 1;
     const bool wide = C > kTileValues / 2;

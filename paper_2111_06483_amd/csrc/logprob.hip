@@ -289,6 +289,7 @@ extern "C" int sar_logprob_bwd(const void* X, const int32_t* label, const float*
     SAR_CHECK_ARG(X && lse && dX, "null pointer (X, lse, dX)");
     SAR_CHECK_ARG(!dlogp || label, "null pointer (label)");
     SAR_CHECK_ARG(!dentropy || entropy, "null pointer (entropy)");
+    SAR_TRY(check_gradient("log probabilities", dtype, n, C, X, dX));
     const GradArgs a{class_tiles(n, C), X, label, lse, entropy, dlogp, dentropy, dX};
     return dtype == SAR_F32 ? logprob_bwd<float>(a, as_stream(stream)) : logprob_bwd<bf16_t>(a, as_stream(stream));
 }

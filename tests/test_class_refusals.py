@@ -217,3 +217,13 @@ def test_temperatures_whose_exponents_have_no_factor(at, T):
     lib, none = sar.lib(), None
     assert lib.sar_distill_fwd(at, 2, at, at, T, at, at, 0, 4, 8, none, 0, none) == BAD and says("temperature")
     assert lib.sar_distill_bwd(at, 2, at, at, T, at, at, at, 0, 4, 8, none) == BAD and says("temperature")
+
+
+@pytest.mark.parametrize("dtype,size", [(0, 4), (1, 2)])
+def test_gradients_that_lie_across_the_scores(at, dtype, size):
+    """In the scores' place or beside them, not shifted: other rows' scores would be read after they are overwritten."""
+    lib, none, n, C = sar.lib(), None, 4, 8
+    X, far = at + 4096, at + 16384
+    for by in (-n * C * size + size, -C * size, -size, size, C * size, n * C * size - size):
+        assert lib.sar_logprob_bwd(X, far, far, far, far, far, X + by, dtype, n, C, none) == BAD and says("overlaps")
+        assert lib.sar_distill_bwd(X, 2, far, far, 1.0, far, far, X + by, dtype, n, C, none) == BAD and says("overlaps")
