@@ -154,7 +154,12 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E, Q> g)
         else if constexpr (kLow) fetch(g.prologue.low, low[chunk], tile, chunk);
     };
     uint4* const rows = lds + kStages * kFrags * 64 + wave * 256;
-    // a chunk, from the lanes that brought it to those that multiply it
+    // A chunk, from the lanes that brought it to those that multiply it.  The lanes meet before what others wrote is read, and before it is written again: no
+    // instruction, but without it lanes that a branch parts from the others (a row's last piece) may be sent through all of this ahead of them.
+    auto meet = []() SAR_INLINE {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
     auto hand_over = [&](int chunk, uint4 (&v)[kRaw], uint4 (&x)[kRaw]) SAR_INLINE {
         const int c = chunk * CH + (lane & 7) * N;
         if (chunk == CHUNKS - 1 && c + N > a.C) {
@@ -166,8 +171,10 @@ __global__ __launch_bounds__(kKeptThreads, 2) void k_rows_kept(KeptArgs<E, Q> g)
         }
 #pragma unroll
         for (int k = 0; k < kRaw; ++k) rows[(8 * k + (lane >> 3)) * 8 + ((lane & 7) ^ (lane >> 3))] = v[k];
+        meet();
 #pragma unroll
         for (int k = 0; k < kRaw; ++k) x[k] = rows[(lane & 31) * 8 + ((h * kRaw + k) ^ (lane & 7))];
+        meet();
     };
 
     int tile = group * kKeptWaves + wave;

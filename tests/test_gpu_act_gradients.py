@@ -34,7 +34,7 @@ def run(X, W, dY, A, name, want, accumulate=False):
 # few rows in one launch; few blocks of dX alone; kept operands, whole and ragged; contractions that are not kept; few columns
 @pytest.mark.parametrize("want", [("dX",), ("dX", "dA"), ("db", "dX"), ("dW", "dX"), ("dW", "db", "dX", "dA")])
 @pytest.mark.parametrize("n,K,F", [(1, 5, 3), (37, 33, 47), (300, 100, 256), (900, 400, 31), (2000, 64, 128), (9001, 200, 400), (30_011, 172, 47), (66_000, 256, 256),
-                                   (66_001, 100, 72), (65_999, 128, 127), (66_000, 40, 72), (66_000, 256, 400), (66_000, 129, 260)])
+                                   (66_001, 100, 72), (66_005, 72, 47), (66_000, 100, 46), (65_999, 128, 63), (65_999, 128, 127), (66_000, 40, 72), (66_000, 256, 400), (66_000, 129, 260)])
 def test_dx_rounds_once(n, K, F, want):
     """bf16: dX = dA W^T from dA = dY act'(A) to 16 bits (two pieces of 8: 2^-17 of it), and what a product of both operands' second pieces is (2^-16
     of a term), rounded once when it is stored; twice as many products are added up."""
