@@ -534,7 +534,8 @@ int sar_linear_bwd_packed(const int8_t* Xq, const uint8_t* Xe, const void* dZ, c
  * ([n,F] of `dtype`, or NULL) receives a, which the backward pass reads; of ReLU with no residual behind it Y serves there as
  * well.  Sums and activation in 32 bits, rounded once when stored; the products as precise as those of sar_linear_typed_fwd.  Y may be res (A too, of a
  * residual inside), and must not overlap X, W or A.  n < 2^31 - 256; K, F <= 65536.  act: any sar_act.
- * work: scratch of at least sar_linear_act_workspace_bytes, 16-byte aligned; that of n rows serves fewer as well. */
+ * work: scratch of at least sar_linear_act_workspace_bytes, 16-byte aligned; that of n rows serves fewer as well.  The forward pass alone needs no more than
+ * sar_linear_typed_workspace_bytes of one type: the rest is dA's, for the backward pass. */
 int sar_linear_act_fwd(const void* X, const float* W, const float* bias, const void* res, int act, int res_after, void* Y, void* A, int dtype, int64_t n,
                        int K, int F, void* work, size_t work_bytes, void* stream);
 

@@ -131,11 +131,12 @@ int check_act(int act)
     return SAR_OK;
 }
 
-int check_work(int dtype, int64_t n, int K, int F, const void* work, size_t work_bytes)
+// forward: the operand's pieces and the row blocks' list are all that it lays out.
+int check_work(int dtype, int64_t n, int K, int F, bool forward, const void* work, size_t work_bytes)
 {
     if (dtype != SAR_F32 && dtype != SAR_BF16) return fail(SAR_ERR_UNSUPPORTED, "dtype %d is neither SAR_F32 nor SAR_BF16", dtype);
     size_t need = 0;
-    SAR_TRY(sar_linear_act_workspace_bytes(n, K, F, &need));
+    SAR_TRY(forward ? sar_linear_typed_workspace_bytes(n, K, F, 1, &need) : sar_linear_act_workspace_bytes(n, K, F, &need));
     SAR_CHECK_ARG(work && work_bytes >= need, "linear with activation: work has %zu bytes, needs %zu", work ? work_bytes : 0, need);
     SAR_CHECK_ARG((reinterpret_cast<uintptr_t>(work) & 15) == 0, "linear with activation: work must be 16-byte aligned");
     return SAR_OK;
@@ -215,7 +216,7 @@ extern "C" int sar_linear_act_fwd(const void* X, const float* W, const float* bi
                                   int64_t n, int K, int F, void* work, size_t work_bytes, void* stream)
 {
     SAR_TRY(check_act(act));
-    SAR_TRY(check_work(dtype, n, K, F, work, work_bytes));
+    SAR_TRY(check_work(dtype, n, K, F, true, work, work_bytes));
     if (n == 0) return SAR_OK;
     SAR_CHECK_ARG(X && W && Y, "null pointer (X, W, Y)");
     const size_t b = dtype == SAR_F32 ? 4 : 2, in = (size_t)n * K * b, out = (size_t)n * F * b;
@@ -231,7 +232,7 @@ extern "C" int sar_linear_act_bwd(const void* dY, const void* A, const void* X, 
                                   void* dA, int dtype, int64_t n, int K, int F, void* work, size_t work_bytes, void* stream)
 {
     SAR_TRY(check_act(act));
-    SAR_TRY(check_work(dtype, n, K, F, work, work_bytes));
+    SAR_TRY(check_work(dtype, n, K, F, false, work, work_bytes));
     if (n > 0) {
         const size_t b = dtype == SAR_F32 ? 4 : 2, in = (size_t)n * K * b, out = (size_t)n * F * b, w = (size_t)K * F * 4;
         SAR_CHECK_ARG(dY && (act == SAR_ACT_NONE || A), "null pointer (dY, A)");

@@ -550,7 +550,8 @@ def sar_linear_bwd_packed(packed, dZ: torch.Tensor, W: torch.Tensor, accumulate:
 
 def sar_linear_act_fwd(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor], res: Optional[torch.Tensor], act: int, res_after: bool,
                        Y: torch.Tensor, A: Optional[torch.Tensor], work: torch.Tensor) -> None:
-    """Y = act(X W + bias + res), or, with res_after, act(X W + bias) + res; A receives what the activation was taken of."""
+    """Y = act(X W + bias + res), or, with res_after, act(X W + bias) + res; A receives what the activation was taken of.  Of
+    `work` this pass needs sar_linear_typed_workspace_bytes(n, K, F, 1) alone."""
     native().linear_act_fwd(X, W, bias, res, act, res_after, Y, A, work)
 
 

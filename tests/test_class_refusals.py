@@ -227,3 +227,10 @@ def test_gradients_that_lie_across_the_scores(at, dtype, size):
     for by in (-n * C * size + size, -C * size, -size, size, C * size, n * C * size - size):
         assert lib.sar_logprob_bwd(X, far, far, far, far, far, X + by, dtype, n, C, none) == BAD and says("overlaps")
         assert lib.sar_distill_bwd(X, 2, far, far, 1.0, far, far, X + by, dtype, n, C, none) == BAD and says("overlaps")
+
+
+@pytest.mark.parametrize("n,K,F", [(4, 8, 6), (1 << 20, 256, 256)])
+def test_scratch_that_the_forward_pass_needs(at, n, K, F):
+    lib, none = sar.lib(), None
+    size = sar.sar_linear_typed_workspace_bytes(n, K, F, 1)
+    assert lib.sar_linear_act_fwd(at, at, none, none, 1, 0, at, none, 0, n, K, F, at, size - 1, none) == BAD and says(f"needs {size}")
