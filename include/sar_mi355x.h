@@ -553,7 +553,7 @@ int sar_linear_act_workspace_bytes(int64_t n, int K, int F, size_t* bytes);
  * X [n,C] of `dtype`: a row's scores, by which p = softmax(x) (at a temperature T: softmax(x / T)).  C <= 2^30.  A class with a score of -inf is out: it has
  * no probability, and no gradient but what it has as a label.  A row of -inf alone has lse = -inf, entropy 0, log probability -inf, no top class, a distillation loss of
  * +inf and no gradient.  A NaN or +inf makes a row's results and gradient NaN (but for classes out of -inf, 0 or NaN; its top classes
- * are then any of the row's).  Sums in 32 bits.
+ * are then any of the row's, or -1).  Sums in 32 bits.
  * work: scratch of at least the call's ..._workspace_bytes, 16-byte aligned (NULL where that is 0); that of n rows serves fewer as well. */
 
 /* lse[i] = log sum_c exp(x_c), logp[i] = x_label - lse (0 for a label that is no class: one outside 0..C-1, such as -1), entropy[i] = -sum_c p_c log p_c

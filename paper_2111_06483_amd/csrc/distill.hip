@@ -6,8 +6,9 @@
 //
 // One pass over the student's scores each way (class_rows.h).  The teacher's few classes meet the student's scores by gathers that are under way with the row, and in the
 // gradient where the tile still is on the chip, in the list's order, so that a class that is listed twice has the same sum in every run.
-// What bounds it: 1734375 x 172, bf16, eight classes: 137 us, 5.3 TB/s: memory; gradient, 4096 x 50000, bf16, 32 classes: 144 us, 5.7 TB/s; 306250 x 47, fp32, eight: 41 us, 3.4 TB/s: short for the
-// chip's memory to come up to its rate (lists by one lane a row 62; tiles of 40 rows, six workgroups a compute unit, a third barrier: the same).
+// What bounds it: 1734375 x 172, bf16, eight classes: 137 us, 5.3 TB/s: memory; gradient, 4096 x 50000, bf16, 32 classes: 144 us, 5.7 TB/s; 306250 x 47, fp32, eight: 41 us, 3.4 TB/s (a
+// copy of as many bytes 27.5, the gradient of log probabilities, whose workgroups have no lists and more of them fit, 28): a workgroup's reads, lists and two barriers stand one behind the
+// other, with nothing of a next tile under way (lists by one lane a row 62; tiles of 40 rows, six workgroups a compute unit, a third barrier: the same).
 #include "class_rows.h"
 
 namespace sar {

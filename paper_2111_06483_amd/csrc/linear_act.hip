@@ -11,9 +11,9 @@
 //     writes it, the one for dW reads it.  db leaves with dW.  Few rows: dW, db, dX and dA in one launch, or one
 //     each where dX has many columns.
 // What bounds it: forward, 867187 x 256 -> 256, bf16, GELU, a residual and its argument kept: 428 to 451 us, 4.0 TB/s of its 1.78 GB (their copy: 349), the vector
-// instructions in use 63% of the time, the matrix cores 28%; 306250 x 100 -> 256, fp32, ReLU with a residual 180 us, 4.2 TB/s.  Backward, 867187 x 256 -> 256, bf16, GELU: 727
-// to 767 us, of it dW 450 (2.2 GB with the dA that it writes; vector instructions 70%), dX 270; 306250 x 256 -> 256, fp32, ELU 605 to 640 us, 128 TFLOP/s of products (a large
-// library product: 150).
+// instructions in use 63% of the time, the matrix cores 28%; 306250 x 100 -> 256, fp32, ReLU with a residual 180 us, 4.2 TB/s.  Backward, 867187 x 256 -> 256, bf16, GELU: 886
+// to 925 us, of it (traced) dW 575 (2.7 GB with the two pieces of dA that it writes; vector instructions 68%), dX 394 (three products, matrix cores 59%; 2.2 GB); 306250 x 256 ->
+// 256, fp32, ELU 605 to 640 us, 128 TFLOP/s of products (a large library product: 150).
 #include "linear_kept.h"
 
 namespace sar {
@@ -83,9 +83,11 @@ int groups_of(int dtype, int64_t n, int F)
     return (int)std::max<int64_t>(1, std::min<int64_t>((n + rows - 1) / rows, std::max(1, std::min(kActGroups, (1 << 22) / F))));
 }
 
-// Whether a product's operand is kept: from a tile of 32 rows for every wavefront of the chip on (256 -> 256, bf16, by GELU with a residual: 32 thousand
-// rows 25.6 us, by the other kernel 28.4, 65536 rows 38.3 and 46.3, 867187 433 and 576; 64 -> 128 16 thousand rows 14.7 and 7.8, 131072 32.9 and
-// 34.0; 47 -> 64, half of a block empty, 400 thousand rows 108 and 50; 128 -> 70, pairs of neighbours, 135 and 112).
+// Whether a product's operand is kept: from a tile of 32 rows for every wavefront of the chip on, 65536 rows where there is one block of columns, about where the two are
+// level (us kept / by the other kernel, by GELU with a residual, 16, 32, 64, 96 and 128 thousand rows: 64 -> 128 bf16 15.6 / 8.6, 17.4 / 16.1, 20.2 / 22.5, 29.0 / 29.4, 30.8 / 34.9;
+// 256 -> 128 bf16 22.4 / 15.0, 24.0 / 20.9, 28.1 / 27.6, 42.8 / 43.3, 46.2 / 50.4; 128 -> 128 fp32 25.3 / 17.7, 27.2 / 22.5, 35.5 / 36.8, 52.2 / 52.2, 57.6 / 62.8; two blocks, 128 -> 256
+// bf16, 19.3 / 18.6, 21.5 / 23.7, 32.4 / 45.4).  256 -> 256, bf16, 867187 rows 433 / 576; 47 -> 64, half of a block empty, 400 thousand rows 108 / 50; 128 -> 70, pairs of
+// neighbours, 135 / 112.
 template <typename T>
 bool kept(int64_t n, int C, int N)
 {

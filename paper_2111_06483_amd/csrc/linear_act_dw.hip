@@ -2,7 +2,7 @@
 //
 // Of bf16 rows dA = dY act'(A) is formed where a workgroup brings the rows and multiplied as two pieces of bf16 (16 bits; one piece would leave dW, an
 // fp32 sum, with 8), and written as such for the product that forms dX.  A workgroup's tile is rather 256 x 128 than 128 x 256: it is dA that costs instructions.
-// 867187 x 256 x 256, bf16, traced: of dY as it is 250 us; dA written in one piece by ReLU 427, by SiLU 490, by GELU 560, in both 617.  What it waits for are vector instructions, some 43
+// 867187 x 256 x 256, bf16, traced: of dY as it is 249 us, by ReLU 466 (four more tensors pass), by SiLU 528, by GELU 575.  What it waits for are vector instructions, some 44
 // a value of dA by GELU, which the matrix instructions of the same wavefront do not hide.  (Fewer of them elsewhere, signs and infinities: no gain that shows.)
 #include "linear_typed_dw.h"
 

@@ -6,7 +6,7 @@
 // Why: with the operand passing through LDS for every 128 rows (linear_typed_rows.h) its copies, which a barrier waits for, take as long as the products, and the
 // rows' own way from memory is waited for at each.  867187 x 256 -> 256, bf16, GELU, residual, argument kept, 1.78 GB: that way 576 us; so, a chunk of rows ahead 564; the next
 // rows and residuals whole, under way without a branch, 433; stores without a branch 428.  (Two passes over the rows for 256 columns: both at about the same time on
-// one XCD, the second from its L2.)  Bf16 rows of dA in two pieces are a third product and twice the bytes: 256 -> 256, the same rows, traced, 271 us of one, 433 of two.
+// one XCD, the second from its L2.)  Bf16 rows of dA in two pieces are a third product and twice the bytes: 256 -> 256, the same rows, traced, 287 us of one, 394 of two.
 #pragma once
 
 #include "linear_typed_rows.h"

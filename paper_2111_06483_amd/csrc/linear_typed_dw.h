@@ -447,7 +447,6 @@ __global__ __launch_bounds__(kThreads, 2) void k_typed_dw(DwArgs a)
             int64_t r0 = first;
             // As long as the chunks to come are full ones: loads without a branch, which would have all of them waited for (their number is not known behind it;
             // 306250 x 256 -> 256 fp32, both products, 597 us for 617, 867187 bf16 835 for 850).
-            //
             if (ZTraits<ZR>::kSums && a.K >= 2 && a.F >= 2) {
                 constexpr std::integral_constant<bool, true> whole{};
                 for (; r0 + (2 * AHEAD + 1) * 16 * S <= end; r0 += AHEAD * 16 * S) {

@@ -8,7 +8,7 @@
 // entropy's sum is taken with them.  The gradient needs no sums: tiles of whole pieces, whatever the rows' lengths.
 // What bounds it: 1734375 x 172, bf16, eight classes: 208 us, 3.5 TB/s of its 735 MB (a copy: 144): vector instructions, half of them for the
 // eight classes (without any 137 us, as distill.hip's pass over the same scores); 306250 x 47, fp32, five: 20 us, 3.7 TB/s; 64 x 65536, fp32, eight: 15.1 us, two launches, 12.2
-// and 3.8 under the trace (without classes 8.9).  Gradient, 1734375 x 172, bf16: 241 us, 5.1 TB/s.
+// and 3.8 under the trace (without classes 8.9).  More than eight of a bf16 row, and any of an fp32 one, are a search over the row for each: 1734375 x 172, bf16, nine 297 us, 16 421, 40 986.  Gradient, 1734375 x 172, bf16: 241 us, 5.1 TB/s.
 #include "class_rows.h"
 
 namespace sar {
