@@ -109,8 +109,7 @@ int product_of(const void* rows, const float* W, int64_t n, void* dX, int K, int
     if constexpr (sizeof(T) == 2) {
         if (kept<T>(n, F, K)) return run_kept<T, true>(rows, W, n, dX, K, F, work, st, NoEpilogue{}, q);
     }
-    if constexpr (sizeof(T) == 2 || Q::kForms) return rows_product<T, true>(rows, W, Types{nullptr, 1, n}, dX, K, F, work, st, NoEpilogue{}, q);
-    return fail(SAR_ERR_UNSUPPORTED, "linear with activation: fp32 rows in pieces");
+    return rows_product<T, true>(rows, W, Types{nullptr, 1, n}, dX, K, F, work, st, NoEpilogue{}, q);
 }
 
 size_t rounded(size_t b) { return (b + 255) / 256 * 256; }
@@ -166,7 +165,8 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
     // dX alone, which forms it for either half of its columns, 625.)  One block of columns of dX that is kept forms it again for fewer bytes: 400000 rows, written / formed twice,
     // 128 -> 256 by SiLU 459 / 386, 128 -> 128 by ReLU 214 / 187, by GELU 230 / 224, with dA wanted 230 / 243; 100 -> 256 by GELU 448 / 423.
     // (Few rows' dW forms it in either type, with db.)
-    const bool bf16 = sizeof(T) == 2, few = dW && few_dw && n > 0, again = formed && dW && !few_dw && bf16;
+    constexpr bool bf16 = sizeof(T) == 2;
+    const bool few = dW && few_dw && n > 0, again = formed && dW && !few_dw && bf16;
     const bool twice = bf16 && K <= 32 * kKeptTiles && kept<T>(n, F, K);
     const bool writes = again && F % 2 == 0 && n > 0 && (dA || (dX && !few_dx && !twice));
     const bool within = formed && dX && n > 0 && (few_dx ? bf16 : !writes);
@@ -189,11 +189,17 @@ int act_bwd(const void* dY, const void* A, const void* X, const float* W, int ac
     if (writes) SAR_TRY(weights());
     if (dX && n > 0) {
         const TypedDw none{nullptr, nullptr, nullptr, nullptr, nullptr, types, K, F, 0, nullptr, A, act};
-        if (within && few_dx) SAR_TRY(few_act_bwd(dtype, none, {dY, W, dX, types, F, K, K, F}, writes ? nullptr : rows, st));
-        else if (within) SAR_TRY(product_of<T>(dY, W, n, dX, K, F, work, st, ActPrologue{A, rows, act}));
-        else if (writes) SAR_TRY(product_of<T>(rows, W, n, dX, K, F, work, st, LowPieces{second}));
-        else if (kept<T>(n, F, K)) SAR_TRY((run_kept<T, true>(rows, W, n, dX, K, F, work, st, NoEpilogue{})));
-        else SAR_TRY((rows_product<T, true>(rows, W, types, dX, K, F, work, st)));
+        if (within && few_dx) {
+            SAR_TRY(few_act_bwd(dtype, none, {dY, W, dX, types, F, K, K, F}, writes ? nullptr : rows, st));
+        } else if (within) {
+            SAR_TRY(product_of<T>(dY, W, n, dX, K, F, work, st, ActPrologue{A, rows, act}));
+        } else if (writes) {
+            if constexpr (bf16) SAR_TRY(product_of<T>(rows, W, n, dX, K, F, work, st, LowPieces{second}));
+        } else if (kept<T>(n, F, K)) {
+            SAR_TRY((run_kept<T, true>(rows, W, n, dX, K, F, work, st, NoEpilogue{})));
+        } else {
+            SAR_TRY((rows_product<T, true>(rows, W, types, dX, K, F, work, st)));
+        }
     }
     if (few) return few_act_bwd(dtype, {X, nullptr, nullptr, dY, dW, types, K, F, accumulate, nullptr, formed ? A : nullptr, act, db}, {}, nullptr, st);
     if (dW && !writes) return weights();
